@@ -42,7 +42,7 @@
 extern "C" {
 #endif
 
-#define KDTOPK_ABI_VERSION 3
+#define KDTOPK_ABI_VERSION 4
 
 typedef enum kd_status {
   KD_OK = 0,
@@ -352,6 +352,188 @@ kd_status kd_scale_grads(const float* grad_loss,
                          void* grad_W_out,
                          int64_t n_W,
                          void* hip_stream);
+
+/*
+ * ---- Operators around the loss ------------------------------------------
+ * The conventions above hold for them too (device pointers, the caller's
+ * buffers, checks before anything is enqueued, one stream, the same bits from
+ * the same inputs). They allocate nothing and never synchronise, so they may be
+ * captured into a HIP graph; calls that overlap in time need workspaces of their
+ * own. kd_profile_enable times the loss's kernels only.
+ *
+ * Logits rows are [N, ld] with V <= ld columns used (the rest is never read),
+ * and may start at any element boundary. A logit that is not a number counts
+ * as -inf everywhere below; +inf is the largest value.
+ */
+
+/* Rows of logits of which the K largest are wanted. */
+typedef struct kd_rows {
+  int64_t N;           /* rows; 0 <= N < 2^31                                */
+  int64_t V;           /* vocabulary size; 1 <= V <= 1048576                 */
+  int64_t ld;          /* elements between rows; V <= ld <= 2^31             */
+  int32_t K;           /* 1 <= K <= V, K <= 4096                             */
+  int32_t dtype;       /* kd_dtype of the logits                             */
+  int32_t flags;       /* 0 or KD_FLAG_TEACHER_LOGPROBS                      */
+} kd_rows;
+
+/*
+ * Bytes of device workspace kd_topk_entries and kd_teacher_cache_write need: at
+ * most 64 MiB (or one row's, up to 72 KiB) and small terms. Pure host function.
+ */
+kd_status kd_topk_entries_workspace_size(const kd_rows* p, size_t* bytes);
+
+/*
+ * The K largest logits of each row, as the loss takes them: the target of a
+ * teacher that runs beside the student, or the proposal of a drafting student.
+ *
+ *   logits   [N, ld] dtype
+ *   idx      [N, K] int32  out: vocabulary indices, largest logit first, of
+ *                          equal ones the lowest index first
+ *   value    [N, K] fp32   out: the logits; with KD_FLAG_TEACHER_LOGPROBS the
+ *                          log-probabilities over the whole vocabulary
+ *                          (z - log sum exp z; -inf in a row of -inf only)
+ *   workspace, workspace_bytes   at least kd_topk_entries_workspace_size bytes,
+ *                          16-byte aligned
+ *
+ * A row with fewer than K logits above -inf has its list filled with -inf at
+ * the lowest indices of such columns. Errors: KD_ERR_NULL_PTR, KD_ERR_BAD_SHAPE,
+ * KD_ERR_BAD_ARG (flags), KD_ERR_UNSUPPORTED (dtype, a pointer that is not
+ * aligned to its elements, workspace not to 16 bytes),
+ * KD_ERR_WORKSPACE_TOO_SMALL, KD_ERR_DEVICE.
+ */
+kd_status kd_topk_entries(const kd_rows* p, const void* logits, int32_t* idx, float* value,
+                          void* workspace, size_t workspace_bytes, void* hip_stream);
+
+/*
+ * The same selection written to a teacher cache at half the bytes: an entry is
+ * index << 12 | code, and a row has a scale (top, step):
+ *   value of an entry = top - code * step, code 0..4094; code 4095 = no entry.
+ * step = (largest - least kept logit) / 4094 in fp32, so a kept value is off by
+ * at most step / 2. Entries that are -inf or more than 1024 below the row's
+ * largest (whose probability is 0 at every temperature up to 9) are not
+ * kept: their code is 4095. top is the largest logit, or its log-probability
+ * with KD_FLAG_TEACHER_LOGPROBS; -inf marks a row that keeps nothing. Infinite
+ * logits are stored as the largest finite number.
+ *
+ *   entries  [N, K] uint32   out
+ *   scale    [N, 2] fp32     out
+ *
+ * Arguments and errors as for kd_topk_entries. A part of a larger cache is
+ * written through pointers to its first row.
+ */
+kd_status kd_teacher_cache_write(const kd_rows* p, const void* logits, uint32_t* entries,
+                                 float* scale, void* workspace, size_t workspace_bytes,
+                                 void* hip_stream);
+
+/*
+ * Rows of a teacher cache as the loss takes them.
+ *
+ *   entries [N, K] uint32, scale [N, 2] fp32   the cache (N K may pass 2^32)
+ *   rows          [M] int64 or NULL   the cache row of each token; NULL: row m
+ *                                     (then M <= N). A row may be named twice
+ *   teacher_idx   [M, K] int32        out: indices
+ *   teacher_logit [M, K] fp32         out: top - code * step, rounded once;
+ *                                     -inf for an entry that was not kept
+ *   ignore        [M] uint8 or NULL   out: 1 for a token without a target (a
+ *                                     cache row that keeps nothing, or a row
+ *                                     number outside [0, N)), else 0. Such a
+ *                                     token's indices are -1 and its logits 0
+ *
+ * The three outputs are the loss's arguments of these names (a token without a
+ * target has to be ignored there). Errors: KD_ERR_NULL_PTR, KD_ERR_BAD_SHAPE
+ * (N or M < 0, M >= 2^31, K outside 1..4096, M > N without rows),
+ * KD_ERR_UNSUPPORTED (alignment to the elements), KD_ERR_DEVICE.
+ */
+kd_status kd_teacher_cache_read(int64_t N, int32_t K, const uint32_t* entries, const float* scale,
+                                const int64_t* rows, int64_t M, int32_t* teacher_idx,
+                                float* teacher_logit, uint8_t* ignore, void* hip_stream);
+
+/*
+ * Hidden states in 8 bits, held from a forward to its backward: 1.03 bytes an
+ * element instead of 2 or 4. Each block of 32 consecutive columns has one byte s
+ * as scale 2^(s - 127) and its elements as e4m3 codes, rounded to nearest even:
+ * 4 significant bits, off by at most 2^-4 of the element, or by 2^-10 of the
+ * scale where the element is below 2^-6 of it. The scale is the least power of
+ * two, at least 2^-127, that leaves the block's largest magnitude at 448 or
+ * below. (The last 1/32 of the types' range, which would round to 2^128, is held
+ * as 1.875 2^127.) A block with an element that is infinite or not a number has s = 255
+ * and reads back as not a number.
+ *
+ *   hidden   [N, D] dtype; D a multiple of 32, 32 <= D <= 65536
+ *   codes    [N, D] uint8, scales [N, D / 32] uint8
+ *
+ * kd_checkpoint_read gives the values back in either dtype (exact in both above
+ * 2^-133). hidden and codes 16-byte aligned. Errors: KD_ERR_NULL_PTR,
+ * KD_ERR_BAD_SHAPE, KD_ERR_UNSUPPORTED (dtype, D % 32, alignment),
+ * KD_ERR_DEVICE.
+ */
+kd_status kd_checkpoint_write(int64_t N, int64_t D, int32_t dtype, const void* hidden,
+                              uint8_t* codes, uint8_t* scales, void* hip_stream);
+kd_status kd_checkpoint_read(int64_t N, int64_t D, int32_t dtype, const uint8_t* codes,
+                             const uint8_t* scales, void* hidden, void* hip_stream);
+
+/* Sequences with drafted tokens. */
+typedef struct kd_draft {
+  int64_t B;           /* sequences; 0 <= B <= 2^20                          */
+  int64_t T;           /* drafted tokens of a sequence at most; 0..1024      */
+  int64_t V;           /* vocabulary size; 1 <= V <= 1048576                 */
+  int64_t ld_target;   /* elements between the target's rows; >= V           */
+  int64_t ld_draft;    /* between the draft's rows (dense draft only); >= V  */
+  int32_t K;           /* entries of the draft's distribution, 1..4096 and
+                          <= V; 0 = the draft's logits are dense             */
+  int32_t dtype;       /* kd_dtype of the target's and a dense draft's logits */
+  double temperature;  /* tau of both distributions; finite and > 0 (64 bits,
+                          as what it divides is)                             */
+  int32_t flags;       /* 0                                                  */
+} kd_draft;
+
+kd_status kd_verify_draft_workspace_size(const kd_draft* p, size_t* bytes);
+
+/*
+ * Verification of drafted tokens (speculative sampling) with a distilled
+ * student as draft: the tokens that come out are distributed as the target's
+ * own. Per sequence, with p_t = softmax(target logits / tau) and q_t the
+ * draft's distribution at place t, the drafted tokens d_0, d_1, ... are kept
+ * while u_t q_t(d_t) < p_t(d_t); the next token behind the r kept ones is the
+ * first v at which the running sum of x passes u_T sum(x), where x = max(p_r -
+ * q_r, 0) if d_r was rejected and p_r if all were kept (x = p_r too where
+ * p_r - q_r is nowhere above 0). Probabilities, sums and comparisons are in 64
+ * bits.
+ *
+ *   target_logits [B, T + 1, ld_target] dtype   row t: behind t drafted tokens
+ *   draft_tokens  [B, T] int32     a token outside [0, V) is rejected
+ *   draft_idx     [B, T, K] int32, draft_logit [B, T, K] fp32   K > 0: the
+ *                                  draft's distribution is the softmax of the
+ *                                  K logits at tau, 0 elsewhere (kd_topk_entries
+ *                                  of the draft's logits). An index outside
+ *                                  [0, V) belongs to no token; one that repeats
+ *                                  counts with the sum
+ *   draft_logits  [B, T, ld_draft] dtype        K = 0: dense
+ *   uniform       [B, T + 1] fp32  random numbers in [0, 1): T for the
+ *                                  comparisons, the last for the next token
+ *   lengths       [B] int32 or NULL   drafted tokens of each sequence (values
+ *                                  outside 0..T count as the nearer end); NULL =
+ *                                  T. Rows behind a sequence's end are not read
+ *   tokens        [B, T + 1] int32 out: kept tokens, the next token, then -1.
+ *                                  The next token is -1 where the target's row
+ *                                  is -inf throughout
+ *   accepted      [B] int32        out: r
+ *   accept_prob   [B, T] fp32 or NULL   out: min(1, p_t(d_t) / q_t(d_t)) of each
+ *                                  drafted token (1 where only q is 0, 0 where
+ *                                  both are), 0 behind the sequence's end
+ *
+ * The draft's arrays are not used with T = 0 (a draw from the target alone). A
+ * small tau gives the greedy check. B (2 T + 1) times the 2048-column segments
+ * of a row may be at most 2^25. Errors: KD_ERR_NULL_PTR, KD_ERR_BAD_SHAPE,
+ * KD_ERR_BAD_ARG (temperature, flags), KD_ERR_UNSUPPORTED (dtype, alignment),
+ * KD_ERR_WORKSPACE_TOO_SMALL, KD_ERR_DEVICE.
+ */
+kd_status kd_verify_draft(const kd_draft* p, const void* target_logits,
+                          const int32_t* draft_tokens, const int32_t* draft_idx,
+                          const float* draft_logit, const void* draft_logits,
+                          const float* uniform, const int32_t* lengths, int32_t* tokens,
+                          int32_t* accepted, float* accept_prob, void* workspace,
+                          size_t workspace_bytes, void* hip_stream);
 
 /*
  * Instrumentation, not part of the method: per-kernel timing with HIP events.

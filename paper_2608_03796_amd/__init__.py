@@ -27,7 +27,10 @@ STATUS = {
 EXPORTED = ("kd_topk_kl_workspace_size", "kd_topk_kl_fwd_bwd", "kd_topk_kl_fwd_bwd_noalloc",
             "kd_topk_kl_fwd",
             "kd_topk_kl_bwd", "kd_topk_kl_check_indices", "kd_scale_grads", "kd_status_string",
-            "kd_abi_version", "kd_profile_enable", "kd_profile_read")
+            "kd_abi_version", "kd_profile_enable", "kd_profile_read",
+            "kd_topk_entries_workspace_size", "kd_topk_entries", "kd_teacher_cache_write",
+            "kd_teacher_cache_read", "kd_checkpoint_write", "kd_checkpoint_read",
+            "kd_verify_draft_workspace_size", "kd_verify_draft")
 
 
 class KdError(RuntimeError):
@@ -45,6 +48,18 @@ class KdProblem(ctypes.Structure):
 class KdKernelTime(ctypes.Structure):
     _fields_ = [("name", ctypes.c_char * 32), ("launches", ctypes.c_int64),
                 ("total_ms", ctypes.c_double), ("flops", ctypes.c_double)]
+
+
+class KdRows(ctypes.Structure):
+    _fields_ = [("N", ctypes.c_int64), ("V", ctypes.c_int64), ("ld", ctypes.c_int64),
+                ("K", ctypes.c_int32), ("dtype", ctypes.c_int32), ("flags", ctypes.c_int32)]
+
+
+class KdDraft(ctypes.Structure):
+    _fields_ = [("B", ctypes.c_int64), ("T", ctypes.c_int64), ("V", ctypes.c_int64),
+                ("ld_target", ctypes.c_int64), ("ld_draft", ctypes.c_int64),
+                ("K", ctypes.c_int32), ("dtype", ctypes.c_int32),
+                ("temperature", ctypes.c_double), ("flags", ctypes.c_int32)]
 
 
 _lib = None
@@ -87,6 +102,19 @@ def load_library(path: Optional[str] = None) -> ctypes.CDLL:
     lib.kd_profile_enable.restype = ctypes.c_int
     lib.kd_profile_read.argtypes = [ctypes.POINTER(KdKernelTime), ctypes.c_int]
     lib.kd_profile_read.restype = ctypes.c_int
+    i32 = ctypes.c_int32
+    rows, draft = ctypes.POINTER(KdRows), ctypes.POINTER(KdDraft)
+    for name, argtypes in (
+            ("kd_topk_entries_workspace_size", [rows, ctypes.POINTER(sz)]),
+            ("kd_topk_entries", [rows, vp, vp, vp, vp, sz, vp]),
+            ("kd_teacher_cache_write", [rows, vp, vp, vp, vp, sz, vp]),
+            ("kd_teacher_cache_read", [i64, i32, vp, vp, vp, i64, vp, vp, vp, vp]),
+            ("kd_checkpoint_write", [i64, i64, i32, vp, vp, vp, vp]),
+            ("kd_checkpoint_read", [i64, i64, i32, vp, vp, vp, vp]),
+            ("kd_verify_draft_workspace_size", [draft, ctypes.POINTER(sz)]),
+            ("kd_verify_draft", [draft] + [vp] * 11 + [sz, vp])):
+        getattr(lib, name).argtypes = argtypes
+        getattr(lib, name).restype = ctypes.c_int
     if path is None:
         _lib = lib
     return lib
@@ -542,6 +570,258 @@ def check_indices(teacher_idx, V, chunk=4096, D=64, tau=1.0, dtype=KD_BF16, work
     if rc != 0:
         raise KdError(rc, "kd_topk_kl_check_indices")
     return True
+
+
+def _logits_rows(name, logits, dim):
+    """dtype code and element stride of the rows of logits[..., V]: the last
+    dimension contiguous, the rows evenly spaced."""
+    if logits.device.type != "cuda":
+        raise ValueError(f"{name} must be on a GPU")
+    if logits.dim() != dim:
+        raise ValueError(f"{name} must have {dim} dimensions")
+    code = _dtype_code(logits.dtype)
+    V = logits.shape[-1]
+    ld = V
+    # (a dimension of one row may have any stride)
+    if dim == 2 and logits.shape[0] > 1:
+        ld = logits.stride(0)
+    elif dim == 3:
+        if logits.shape[1] > 1:
+            ld = logits.stride(1)
+        elif logits.shape[0] > 1:
+            ld = logits.stride(0)
+        if logits.shape[0] > 1 and logits.shape[1] > 0 \
+                and logits.stride(0) != logits.shape[1] * ld:
+            raise ValueError(f"the rows of {name} must be evenly spaced")
+    if (V > 1 and logits.stride(-1) != 1) or ld < V:
+        raise ValueError(f"the rows of {name} must be contiguous and must not overlap")
+    return code, ld
+
+
+def _topk_rows(logits, K, logprobs, workspace):
+    """The problem and workspace of a selection, with its checks."""
+    import torch
+    lib = load_library()
+    code, ld = _logits_rows("logits", logits, 2)
+    N, V = logits.shape
+    pr = KdRows(N, V, ld, int(K), code, KD_FLAG_TEACHER_LOGPROBS if logprobs else 0)
+    if workspace is None:
+        n = ctypes.c_size_t(0)
+        rc = lib.kd_topk_entries_workspace_size(ctypes.byref(pr), ctypes.byref(n))
+        if rc != 0:
+            raise KdError(rc, "kd_topk_entries_workspace_size")
+        workspace = torch.empty(n.value, dtype=torch.uint8, device=logits.device)
+    _check_workspace(workspace, logits.device)
+    return lib, pr, workspace
+
+
+def _out_tensors(out, want, device):
+    """The outputs of `want` (name -> (shape, dtype)): from `out`, checked, or new."""
+    import torch
+    out = dict(out or {})
+    res = {}
+    for name, (shape, dtype) in want.items():
+        t = out.get(name)
+        if t is None:
+            t = torch.empty(shape, dtype=dtype, device=device)
+        _check_tensor(name, t, shape, dtype, device)
+        res[name] = t
+    return res
+
+
+def topk_entries(logits, K, logprobs: bool = False, out=None, workspace=None):
+    """kd_topk_entries on the current stream: the K largest logits of each row
+    of logits [N, V] (bf16 or fp32, rows evenly spaced), as the loss takes them.
+    Returns {'teacher_idx' [N, K] int32, 'teacher_logit' [N, K] fp32}, largest
+    first, of equal ones the lowest index first; log-probabilities over the
+    whole vocabulary with logprobs (for teacher_logprobs=True). `out` may carry
+    the outputs, `workspace` a uint8 tensor of topk_workspace_size bytes."""
+    import torch
+    lib, pr, workspace = _topk_rows(logits, K, logprobs, workspace)
+    dev = logits.device
+    res = _out_tensors(out, {"teacher_idx": ((pr.N, pr.K), torch.int32),
+                             "teacher_logit": ((pr.N, pr.K), torch.float32)}, dev)
+    with torch.cuda.device(dev):
+        rc = lib.kd_topk_entries(ctypes.byref(pr), _ptr(logits), _ptr(res["teacher_idx"]),
+                                 _ptr(res["teacher_logit"]), _ptr(workspace),
+                                 ctypes.c_size_t(workspace.numel()), _stream_handle(dev))
+    if rc != 0:
+        raise KdError(rc, "kd_topk_entries")
+    return res
+
+
+def topk_workspace_size(N, V, K, dtype=KD_BF16) -> int:
+    """Bytes of workspace of topk_entries and teacher_cache_write."""
+    n = ctypes.c_size_t(0)
+    pr = KdRows(int(N), int(V), int(V), int(K), int(dtype), 0)
+    rc = load_library().kd_topk_entries_workspace_size(ctypes.byref(pr), ctypes.byref(n))
+    if rc != 0:
+        raise KdError(rc, "kd_topk_entries_workspace_size")
+    return int(n.value)
+
+
+def teacher_cache_write(logits, K, logprobs: bool = False, out=None, workspace=None):
+    """kd_teacher_cache_write on the current stream: the K largest logits of
+    each row as a teacher cache of 4 bytes an entry. Returns {'entries' [N, K]
+    int32 (index << 12 | code), 'scale' [N, 2] fp32 (top, step)}; `out` may
+    carry them, e.g. as rows of a larger cache."""
+    import torch
+    lib, pr, workspace = _topk_rows(logits, K, logprobs, workspace)
+    dev = logits.device
+    res = _out_tensors(out, {"entries": ((pr.N, pr.K), torch.int32),
+                             "scale": ((pr.N, 2), torch.float32)}, dev)
+    with torch.cuda.device(dev):
+        rc = lib.kd_teacher_cache_write(ctypes.byref(pr), _ptr(logits), _ptr(res["entries"]),
+                                        _ptr(res["scale"]), _ptr(workspace),
+                                        ctypes.c_size_t(workspace.numel()), _stream_handle(dev))
+    if rc != 0:
+        raise KdError(rc, "kd_teacher_cache_write")
+    return res
+
+
+def teacher_cache_read(entries, scale, rows=None, out=None):
+    """kd_teacher_cache_read on the current stream: cache rows [N, K] (all of
+    them, or those that `rows` [M] int64 names) as the loss's arguments
+    {'teacher_idx' [M, K], 'teacher_logit' [M, K], 'ignore' [M] uint8}; ignore is
+    1 for a token without a target."""
+    import torch
+    lib = load_library()
+    if entries.device.type != "cuda":
+        raise ValueError("tensors must be on a GPU")
+    if entries.dim() != 2:
+        raise ValueError("entries must be [N, K]")
+    dev = entries.device
+    N, K = entries.shape
+    _check_tensor("entries", entries, (N, K), torch.int32, dev)
+    _check_tensor("scale", scale, (N, 2), torch.float32, dev)
+    M = N
+    if rows is not None:
+        if rows.dim() != 1:
+            raise ValueError("rows must be [M]")
+        M = rows.shape[0]
+        _check_tensor("rows", rows, (M,), torch.int64, dev)
+    res = _out_tensors(out, {"teacher_idx": ((M, K), torch.int32),
+                             "teacher_logit": ((M, K), torch.float32),
+                             "ignore": ((M,), torch.uint8)}, dev)
+    with torch.cuda.device(dev):
+        rc = lib.kd_teacher_cache_read(N, K, _ptr(entries), _ptr(scale), _ptr(rows), M,
+                                       _ptr(res["teacher_idx"]), _ptr(res["teacher_logit"]),
+                                       _ptr(res["ignore"]), _stream_handle(dev))
+    if rc != 0:
+        raise KdError(rc, "kd_teacher_cache_read")
+    return res
+
+
+def checkpoint_write(hidden, out=None):
+    """kd_checkpoint_write on the current stream: hidden [N, D] (bf16 or fp32,
+    D a multiple of 32) in 8 bits, {'codes' [N, D] uint8 (e4m3), 'scales'
+    [N, D / 32] uint8 (power of two, biased by 127)}."""
+    import torch
+    lib = load_library()
+    if hidden.device.type != "cuda":
+        raise ValueError("tensors must be on a GPU")
+    if hidden.dim() != 2 or not hidden.is_contiguous():
+        raise ValueError("hidden must be a contiguous [N, D]")
+    dev, code = hidden.device, _dtype_code(hidden.dtype)
+    N, D = hidden.shape
+    res = _out_tensors(out, {"codes": ((N, D), torch.uint8),
+                             "scales": ((N, D // 32), torch.uint8)}, dev)
+    with torch.cuda.device(dev):
+        rc = lib.kd_checkpoint_write(N, D, code, _ptr(hidden), _ptr(res["codes"]),
+                                     _ptr(res["scales"]), _stream_handle(dev))
+    if rc != 0:
+        raise KdError(rc, "kd_checkpoint_write")
+    return res
+
+
+def _check_checkpoint(codes, scales):
+    import torch
+    if codes.device.type != "cuda":
+        raise ValueError("tensors must be on a GPU")
+    if codes.dim() != 2:
+        raise ValueError("codes must be [N, D]")
+    N, D = codes.shape
+    _check_tensor("codes", codes, (N, D), torch.uint8, codes.device)
+    _check_tensor("scales", scales, (N, D // 32), torch.uint8, codes.device)
+    return N, D, codes.device
+
+
+def checkpoint_read(codes, scales, dtype, out=None):
+    """kd_checkpoint_read on the current stream: the hidden states [N, D] that a
+    checkpoint holds, in dtype (torch.bfloat16 or torch.float32)."""
+    import torch
+    lib = load_library()
+    N, D, dev = _check_checkpoint(codes, scales)
+    code = _dtype_code(dtype)
+    hidden = torch.empty(N, D, dtype=dtype, device=dev) if out is None else out
+    _check_tensor("out", hidden, (N, D), dtype, dev)
+    with torch.cuda.device(dev):
+        rc = lib.kd_checkpoint_read(N, D, code, _ptr(codes), _ptr(scales), _ptr(hidden),
+                                    _stream_handle(dev))
+    if rc != 0:
+        raise KdError(rc, "kd_checkpoint_read")
+    return hidden
+
+
+def verify_draft(target_logits, draft_tokens, uniform, draft_idx=None, draft_logit=None,
+                 draft_logits=None, lengths=None, tau: float = 1.0, accept_prob: bool = False,
+                 out=None, workspace=None):
+    """kd_verify_draft on the current stream: which drafted tokens the target
+    keeps, and the token behind them.
+
+    target_logits [B, T + 1, V] (bf16 or fp32), draft_tokens [B, T] int32,
+    uniform [B, T + 1] fp32 in [0, 1); the draft's distribution as draft_idx and
+    draft_logit [B, T, K] (topk_entries of its logits) or as draft_logits
+    [B, T, V] in the target's dtype; lengths [B] int32 or None. Returns
+    {'tokens' [B, T + 1] int32 (kept, next, then -1), 'accepted' [B] int32} and,
+    when requested, 'accept_prob' [B, T] fp32."""
+    import torch
+    lib = load_library()
+    code, ld = _logits_rows("target_logits", target_logits, 3)
+    dev = target_logits.device
+    B, T, V = target_logits.shape[0], target_logits.shape[1] - 1, target_logits.shape[2]
+    if T < 0:
+        raise ValueError("target_logits must be [B, T + 1, V]")
+    _check_tensor("draft_tokens", draft_tokens, (B, T), torch.int32, dev)
+    _check_tensor("uniform", uniform, (B, T + 1), torch.float32, dev)
+    if (draft_idx is None) != (draft_logit is None):
+        raise ValueError("draft_idx and draft_logit go together")
+    if T > 0 and (draft_idx is None) == (draft_logits is None):
+        raise ValueError("the draft is either draft_idx and draft_logit, or draft_logits")
+    K, ld_draft = 0, V
+    if draft_idx is not None:
+        if draft_idx.dim() != 3 or draft_idx.shape[2] < 1:
+            raise ValueError("draft_idx must be [B, T, K]")
+        K = draft_idx.shape[2]
+        _check_tensor("draft_idx", draft_idx, (B, T, K), torch.int32, dev)
+        _check_tensor("draft_logit", draft_logit, (B, T, K), torch.float32, dev)
+    elif draft_logits is not None:
+        dcode, ld_draft = _logits_rows("draft_logits", draft_logits, 3)
+        if dcode != code or tuple(draft_logits.shape) != (B, T, V) or draft_logits.device != dev:
+            raise ValueError("draft_logits must be [B, T, V] in the target's dtype and device")
+    if lengths is not None:
+        _check_tensor("lengths", lengths, (B,), torch.int32, dev)
+    want = {"tokens": ((B, T + 1), torch.int32), "accepted": ((B,), torch.int32)}
+    if accept_prob:
+        want["accept_prob"] = ((B, T), torch.float32)
+    res = _out_tensors(out, want, dev)
+    pr = KdDraft(B, T, V, ld, ld_draft, K, code, float(tau), 0)
+    if workspace is None:
+        n = ctypes.c_size_t(0)
+        rc = lib.kd_verify_draft_workspace_size(ctypes.byref(pr), ctypes.byref(n))
+        if rc != 0:
+            raise KdError(rc, "kd_verify_draft_workspace_size")
+        workspace = torch.empty(n.value, dtype=torch.uint8, device=dev)
+    _check_workspace(workspace, dev)
+    with torch.cuda.device(dev):
+        rc = lib.kd_verify_draft(
+            ctypes.byref(pr), _ptr(target_logits), _ptr(draft_tokens), _ptr(draft_idx),
+            _ptr(draft_logit), _ptr(draft_logits), _ptr(uniform), _ptr(lengths),
+            _ptr(res["tokens"]), _ptr(res["accepted"]), _ptr(res.get("accept_prob")),
+            _ptr(workspace), ctypes.c_size_t(workspace.numel()), _stream_handle(dev))
+    if rc != 0:
+        raise KdError(rc, "kd_verify_draft")
+    return res
 
 
 def profile_enable(on: bool = True, contractions_only: bool = False):

@@ -1,0 +1,1187 @@
+// HIP kernels (gfx950) around the loss and their launchers:
+//   top-K rows       row_groups -> row_select   the K largest logits of each row, as
+//                    (index, value) or as entries of the teacher cache
+//   teacher cache    cache_read                 entries back to (index, value)
+//   checkpoints      ckpt_write, ckpt_read      hidden states in 8 bits
+//   verification     seg_sums -> accept (-> rest_sums -> pick)
+//                    drafted tokens against the target's probabilities
+#include "kd_ckpt.h"
+#include "kd_device.h"
+#include "kd_ops.h"
+
+namespace kd {
+
+// --------------------------------------------------------------- row reads --
+// A logits row is read in 16-byte vectors at 16-byte boundaries wherever the row
+// starts: column v of the row has the place e = v + shift, shift = the elements
+// between the boundary at or before the row and the row. Vectors that reach
+// past either end of the row are read element by element; what is not of the
+// row reads as -inf.
+template <typename T>
+struct Row {
+  static constexpr int VPT = 16 / (int)sizeof(T);      // elements of a vector
+  static constexpr int U = kSegCols / (64 * VPT);      // vectors of a lane in a segment
+  static constexpr int GL = kGroupCols / VPT;          // lanes of a group
+  const T* p;
+  int V, shift;
+  __device__ __forceinline__ Row(const void* base, int64_t offset, int V_)
+      : p(static_cast<const T*>(base) + offset),
+        V(V_),
+        shift((int)((reinterpret_cast<uintptr_t>(p) & 15u) / sizeof(T))) {}
+
+  // the vector at place e (a multiple of VPT)
+  __device__ __forceinline__ u32x4_t at(int e) const {
+    const int v = e - shift;
+    if (v >= 0 && v + VPT <= V) return *reinterpret_cast<const u32x4_t*>(p + v);
+    uint32_t w[4];
+    if constexpr (sizeof(T) == 2) {
+      uint16_t h[8];
+#pragma unroll
+      for (int i = 0; i < 8; ++i)
+        h[i] = (unsigned)(v + i) < (unsigned)V ? reinterpret_cast<const uint16_t*>(p)[v + i] : 0xff80;
+#pragma unroll
+      for (int i = 0; i < 4; ++i) w[i] = h[2 * i] | (uint32_t)h[2 * i + 1] << 16;
+    } else {
+#pragma unroll
+      for (int i = 0; i < 4; ++i)
+        w[i] = (unsigned)(v + i) < (unsigned)V ? reinterpret_cast<const uint32_t*>(p)[v + i]
+                                               : 0xff800000u;
+    }
+    return u32x4_t{w[0], w[1], w[2], w[3]};
+  }
+  // the calling wave's share of a segment: lane l holds U vectors, 64 apart
+  __device__ __forceinline__ void segment(int seg, u32x4_t* x) const {
+    const int lane = threadIdx.x & 63, e0 = seg * kSegCols;
+    if (e0 >= shift && e0 + kSegCols - shift <= V) {
+      const u32x4_t* q = reinterpret_cast<const u32x4_t*>(p + (e0 - shift)) + lane;
+#pragma unroll
+      for (int u = 0; u < U; ++u) x[u] = q[64 * u];
+    } else {
+#pragma unroll
+      for (int u = 0; u < U; ++u) x[u] = at(e0 + (64 * u + lane) * VPT);
+    }
+  }
+  // element i of a vector; what is not a number counts as -inf
+  static __device__ __forceinline__ float elt(u32x4_t x, int i) {
+    uint32_t b;
+    if constexpr (sizeof(T) == 2) b = i & 1 ? x[i / 2] & 0xffff0000u : x[i / 2] << 16;
+    else b = x[i];
+    return fmaxf(__builtin_bit_cast(float, b), -INFINITY);
+  }
+  __device__ __forceinline__ float one(int v) const {
+    return fmaxf((float)p[v], -INFINITY);
+  }
+};
+
+// values as unsigned numbers of the same order (-0 as +0)
+__device__ __forceinline__ uint32_t order_key(float z) {
+  const uint32_t b = __builtin_bit_cast(uint32_t, z + 0.f);
+  return b & 0x80000000u ? ~b : b | 0x80000000u;
+}
+__device__ __forceinline__ float key_value(uint32_t k) {
+  return __builtin_bit_cast(float, k & 0x80000000u ? k & 0x7fffffffu : ~k);
+}
+constexpr uint32_t kKeyNegInf = 0x007fffffu;
+
+// 2^(log2(e) (z - m)) with m the largest of several z: 0 where z = -inf, and at
+// m = +inf 1 for each z = m
+__device__ __forceinline__ float exp_below(float z, float m) {
+  return z == m ? 1.f : fast_exp2((z - m) * kLog2e);
+}
+
+// ------------------------------------------------------------- top-K rows ----
+// First pass, the one that reads the logits: the largest value of each group of
+// 64 columns, and with LSE the segment's maximum and sum of exp below it. A wave
+// per segment, no LDS and no barrier: bound by the read (the exponentials and
+// maxima take about half of the issue slots that go by at the memory's rate).
+template <typename T, bool LSE>
+__global__ __launch_bounds__(256) void k_row_groups(const T* __restrict__ logits, int64_t ld, int V,
+                                                    int nseg, int waves, float* __restrict__ gmax,
+                                                    float* __restrict__ pm,
+                                                    float* __restrict__ ps) {
+  const int w = blockIdx.x * 4 + wave_id();
+  if (w >= waves) return;
+  const int r = w / nseg, seg = w - r * nseg;
+  const Row<T> row(logits, (int64_t)r * ld, V);
+  constexpr int U = Row<T>::U, VPT = Row<T>::VPT, GL = Row<T>::GL;
+  u32x4_t x[U];
+  row.segment(seg, x);
+  const int lane = threadIdx.x & 63;
+  float mine = -INFINITY, top = -INFINITY;
+#pragma unroll
+  for (int u = 0; u < U; ++u) {
+    float m = Row<T>::elt(x[u], 0);
+#pragma unroll
+    for (int i = 1; i < VPT; ++i) m = fmaxf(m, Row<T>::elt(x[u], i));
+#pragma unroll
+    for (int c = 0; c < (GL == 8 ? 3 : 4); ++c) m = fmaxf(m, dpp_f(m, c));
+    if ((lane & (GL - 1)) == u) mine = m;  // (U <= GL)
+    top = fmaxf(top, m);
+  }
+  static_assert(U <= GL, "a lane of each group keeps each vector's maximum");
+  if ((lane & (GL - 1)) < U)
+    gmax[(int64_t)w * kSegGroups + (lane & (GL - 1)) * (64 / GL) + lane / GL] = mine;
+  if constexpr (LSE) {
+    top = wave_max(top);
+    float s = 0.f;
+    if (top != -INFINITY) {
+#pragma unroll
+      for (int u = 0; u < U; ++u)
+#pragma unroll
+        for (int i = 0; i < VPT; ++i) s += exp_below(Row<T>::elt(x[u], i), top);
+    }
+    s = wave_sum(s);
+    if (lane == 0) {
+      pm[w] = top;
+      ps[w] = s;
+    }
+  }
+}
+
+// Second pass, a workgroup per row. At least K groups have a maximum of at least
+// the K-th largest group maximum, so the K largest elements are among those that
+// reach it, and these lie in the groups whose maximum does: about K groups of
+// 64 columns are read again instead of the row. The bound is searched in the 16
+// leading bits of the maxima (bf16's precision, no higher than the K-th): for
+// V = 131072 and K = 100 there are about 105 such elements. They are sorted by
+// (value, lowest index first), the order of the result, so which thread collected
+// which does not matter. Where more elements reach the bound than fit (many equal
+// values, or V below about 64 K), the K-th largest is found exactly by counting
+// digits over those groups.
+constexpr int kSelThreads = 256;
+constexpr int kSelWaves = kSelThreads / 64;
+constexpr int kHistBins = 2048;
+
+__host__ __device__ constexpr int select_cap(int K) {
+  int c = 1024;
+  while (c < 2 * K) c *= 2;
+  return c;
+}
+// bytes of LDS: the groups' keys, later the candidates or the digit counts; the
+// list of groups
+__host__ __device__ constexpr int select_lds_keys(int G, int K) {
+  const int a = 4 * G, b = 8 * select_cap(K);
+  return (a > b ? a : b) + 15 & ~15;
+}
+__host__ __device__ constexpr int select_lds(int G, int K) {
+  return select_lds_keys(G, K) + 2 * G;
+}
+
+struct SelectShared {
+  int count[2][kSelWaves];
+  int scan[kSelWaves];
+  int found, before;
+  int n, nlist;
+  uint32_t lo, hi;
+  float top, logs;
+  uint32_t wlo[kSelWaves], whi[kSelWaves];
+};
+
+// The bin of `want` (1 = the first) in the bins' order (descending or ascending),
+// and the count of the bins before it; hist holds nb = 2048 or 1024 bins.
+__device__ __forceinline__ void find_bin(SelectShared& s, const int* hist, int nb, bool descending,
+                                         int want, int& bin, int& before) {
+  const int per = nb / kSelThreads, tid = threadIdx.x;
+  int sum = 0;
+  for (int i = 0; i < per; ++i) {
+    const int b = tid * per + i;
+    sum += hist[descending ? nb - 1 - b : b];
+  }
+  int incl = wave_incl_scan(sum);
+  if ((tid & 63) == 63) s.scan[tid >> 6] = incl;
+  __syncthreads();
+  for (int w = 0; w < (tid >> 6); ++w) incl += s.scan[w];
+  int at = incl - sum;
+  if (at < want && want <= incl) {
+    for (int i = 0; i < per; ++i) {
+      const int b = descending ? nb - 1 - (tid * per + i) : tid * per + i;
+      if (at + hist[b] >= want) {
+        s.found = b;
+        s.before = at;
+        break;
+      }
+      at += hist[b];
+    }
+  }
+  __syncthreads();
+  bin = s.found;
+  before = s.before;
+  __syncthreads();
+}
+
+// f(key, v) for every element of the listed groups; all lanes call it, `in` tells
+// whether there is an element
+template <typename T, typename F>
+__device__ __forceinline__ void listed_elements(const Row<T>& row, const uint16_t* list, int n,
+                                                F&& f) {
+  constexpr int GL = Row<T>::GL, VPT = Row<T>::VPT, GPW = 64 / GL;
+  const int lane = threadIdx.x & 63, wave = wave_id();
+  for (int l0 = wave * GPW; l0 < n; l0 += kSelWaves * GPW) {
+    const int l = l0 + lane / GL;
+    const bool have = l < n;
+    const int e = have ? (int)list[l] * kGroupCols + (lane & (GL - 1)) * VPT : 0;
+    const u32x4_t x = row.at(e);
+#pragma unroll
+    for (int i = 0; i < VPT; ++i) {
+      const int v = e + i - row.shift;
+      f(have && (unsigned)v < (unsigned)row.V, order_key(Row<T>::elt(x, i)), v);
+    }
+  }
+}
+
+struct SelectArgs {
+  const void* logits;
+  int64_t ld;
+  int V, K, G, nseg, logprobs;
+  const float *gmax, *pm, *ps;
+  int32_t* idx;
+  float* value;
+  uint32_t* entries;
+  float* scale;
+};
+
+template <typename T>
+__global__ __launch_bounds__(kSelThreads) void k_row_select(SelectArgs a) {
+  extern __shared__ __align__(16) char lds[];
+  __shared__ SelectShared s;
+  const int tid = threadIdx.x, lane = tid & 63, wave = wave_id();
+  const int K = a.K, G = a.G, cap = select_cap(K);
+  const int64_t r = blockIdx.x;
+  const Row<T> row(a.logits, r * a.ld, a.V);
+  uint32_t* keys = reinterpret_cast<uint32_t*>(lds);
+  uint64_t* cand = reinterpret_cast<uint64_t*>(lds);
+  int* hist = reinterpret_cast<int*>(lds);
+  uint16_t* list = reinterpret_cast<uint16_t*>(lds + select_lds_keys(G, K));
+
+  // group maxima, their range, and log of the row's sum of exp
+  uint32_t lo = 0xffffffffu, hi = 0;
+  const float* gm = a.gmax + r * G;
+  for (int i = tid; i < G; i += kSelThreads) {
+    const uint32_t k = order_key(gm[i]);
+    keys[i] = k;
+    lo = min(lo, k);
+    hi = max(hi, k);
+  }
+#pragma unroll
+  for (int o = 32; o >= 1; o >>= 1) {
+    lo = min(lo, (uint32_t)__shfl_xor((int)lo, o));
+    hi = max(hi, (uint32_t)__shfl_xor((int)hi, o));
+  }
+  if (lane == 0) {
+    s.wlo[wave] = lo;
+    s.whi[wave] = hi;
+  }
+  if (tid == 0) s.n = s.nlist = 0;
+  if (a.logprobs && wave == kSelWaves - 1) {
+    const float *pm = a.pm + r * a.nseg, *ps = a.ps + r * a.nseg;
+    float m = -INFINITY, t = 0.f;
+    for (int i = lane; i < a.nseg; i += 64) m = fmaxf(m, pm[i]);
+    m = wave_max(m);
+    if (m != -INFINITY)
+      for (int i = lane; i < a.nseg; i += 64) t += ps[i] * exp_below(pm[i], m);
+    t = wave_sum(t);
+    if (lane == 0) s.logs = m != -INFINITY ? logf(t) : 0.f;
+  }
+  __syncthreads();
+  lo = min(min(s.wlo[0], s.wlo[1]), min(s.wlo[2], s.wlo[3])) >> 16;
+  hi = (max(max(s.whi[0], s.whi[1]), max(s.whi[2], s.whi[3])) >> 16) + 1;
+  // the largest 16-bit prefix that K group maxima reach (0 with fewer groups)
+  if (K > G) lo = hi = 0;
+  for (int it = 0; hi - lo > 1; ++it) {
+    const uint32_t mid = (lo + hi) / 2;
+    int c = 0;
+    for (int i0 = 0; i0 < G; i0 += kSelThreads) {
+      const int i = i0 + tid;
+      c += __popcll(__builtin_amdgcn_ballot_w64(i < G && keys[i < G ? i : 0] >> 16 >= mid));
+    }
+    if (lane == 0) s.count[it & 1][wave] = c;
+    __syncthreads();
+    c = (s.count[it & 1][0] + s.count[it & 1][1]) + (s.count[it & 1][2] + s.count[it & 1][3]);
+    if (c >= K) lo = mid;
+    else hi = mid;
+  }
+  const uint32_t t = lo << 16;
+  for (int i0 = 0; i0 < G; i0 += kSelThreads) {
+    const int i = i0 + tid;
+    const bool q = i < G && keys[i < G ? i : 0] >= t;
+    const uint64_t b = __builtin_amdgcn_ballot_w64(q);
+    if (b == 0) continue;
+    int at = 0;
+    if (lane == 0) at = atomicAdd(&s.nlist, __popcll(b));
+    at = __builtin_amdgcn_readfirstlane(at);
+    if (q) list[at + __builtin_amdgcn_mbcnt_hi((uint32_t)(b >> 32),
+                                               __builtin_amdgcn_mbcnt_lo((uint32_t)b, 0))] =
+        (uint16_t)i;
+  }
+  __syncthreads();
+  const int nlist = s.nlist;
+
+  // elements with key > kth, or = kth and an index up to vcut, as candidates
+  auto gather = [&](uint32_t kth, int vcut) {
+    listed_elements<T>(row, list, nlist, [&](bool in, uint32_t k, int v) {
+      const bool q = in && (k > kth || (k == kth && v <= vcut));
+      const uint64_t b = __builtin_amdgcn_ballot_w64(q);
+      if (b == 0) return;
+      int at = 0;
+      if (lane == 0) at = atomicAdd(&s.n, __popcll(b));
+      at = __builtin_amdgcn_readfirstlane(at) +
+           __builtin_amdgcn_mbcnt_hi((uint32_t)(b >> 32),
+                                     __builtin_amdgcn_mbcnt_lo((uint32_t)b, 0));
+      if (q && at < cap) cand[at] = (uint64_t)k << 32 | (0xffffffffu - (uint32_t)v);
+    });
+    __syncthreads();
+  };
+  gather(t, 0x7fffffff);
+  int n = s.n;
+  if (n > cap) {
+    // the K-th largest exactly: its key in digits of 11, 11 and 10 bits, then,
+    // where not all elements of that key are wanted, the index of the last one
+    uint32_t kth = 0;
+    int want = K;
+    const int shifts[3] = {21, 10, 0};
+#pragma unroll
+    for (int d = 0; d < 3; ++d) {
+      const int sh = shifts[d], nb = d == 2 ? 1024 : kHistBins;
+      const uint32_t mask = d == 0 ? 0u : d == 1 ? 0xffe00000u : 0xfffffc00u;
+      for (int i = tid; i < nb; i += kSelThreads) hist[i] = 0;
+      __syncthreads();
+      listed_elements<T>(row, list, nlist, [&](bool in, uint32_t k, int) {
+        if (in && (k & mask) == kth) atomicAdd(&hist[(k >> sh) & (nb - 1)], 1);
+      });
+      __syncthreads();
+      int bin, before;
+      find_bin(s, hist, nb, true, want, bin, before);
+      kth |= (uint32_t)bin << sh;
+      want -= before;
+    }
+    int vcut = 0;
+#pragma unroll
+    for (int d = 0; d < 2; ++d) {
+      for (int i = tid; i < 1024; i += kSelThreads) hist[i] = 0;
+      __syncthreads();
+      const int first = vcut;
+      listed_elements<T>(row, list, nlist, [&](bool in, uint32_t k, int v) {
+        if (in && k == kth && (d == 0 || v >> 10 == first >> 10))
+          atomicAdd(&hist[d == 0 ? v >> 10 : v & 1023], 1);
+      });
+      __syncthreads();
+      int bin, before;
+      find_bin(s, hist, 1024, false, want, bin, before);
+      vcut |= d == 0 ? bin << 10 : bin;
+      want -= before;
+    }
+    if (tid == 0) s.n = 0;
+    __syncthreads();
+    gather(kth, vcut);
+    n = s.n;
+  }
+  // sorted, largest first
+  if (n <= kSelThreads) {
+    const uint64_t c = tid < n ? cand[tid] : 0;
+    int rank = 0;
+    for (int i = 0; i < n; ++i) rank += cand[i] > c;
+    __syncthreads();
+    if (tid < n) cand[rank] = c;
+  } else {
+    int P = 2 * kSelThreads;
+    while (P < n) P *= 2;
+    for (int i = n + tid; i < P; i += kSelThreads) cand[i] = 0;
+    for (int size = 2; size <= P; size *= 2)
+      for (int st = size / 2; st > 0; st /= 2) {
+        __syncthreads();
+        for (int i = tid; i < P / 2; i += kSelThreads) {
+          const int x = 2 * i - (i & (st - 1)), y = x + st;
+          const uint64_t p = cand[x], q = cand[y];
+          if ((p < q) == ((x & size) == 0)) {
+            cand[x] = q;
+            cand[y] = p;
+          }
+        }
+      }
+  }
+  __syncthreads();
+
+  const float z0 = key_value((uint32_t)(cand[0] >> 32));
+  const float logs = a.logprobs ? s.logs : 0.f;
+  if (a.value != nullptr) {
+    for (int k = tid; k < K; k += kSelThreads) {
+      const uint64_t c = cand[k];
+      const float z = key_value((uint32_t)(c >> 32));
+      const int64_t o = r * K + k;
+      a.idx[o] = (int32_t)(0xffffffffu - (uint32_t)c);
+      a.value[o] = !a.logprobs ? z : z == -INFINITY ? z : (z == z0 ? 0.f : z - z0) - logs;
+    }
+    return;
+  }
+  // cache entries: the kept ones come first; the steps between the first and the
+  // last of them are computed in 64 bits (infinities as the largest finite value)
+  const bool empty = z0 == -INFINITY;
+  const float top = fminf(z0, 3.402823466e38f);
+  if (wave == 0) {
+    int kept = 0;
+    for (int k0 = 0; k0 < K; k0 += 64) {
+      const int k = k0 + lane;
+      const float z = fminf(key_value((uint32_t)(cand[k < K ? k : 0] >> 32)), 3.402823466e38f);
+      kept += __popcll(__builtin_amdgcn_ballot_w64(!empty && k < K && z >= top - kCacheReach));
+    }
+    if (lane == 0) s.n = kept;
+  }
+  __syncthreads();
+  const int kept = s.n;
+  const double dtop = top;
+  float step = 0.f;
+  if (kept > 0) {
+    const float low = fminf(key_value((uint32_t)(cand[kept - 1] >> 32)), 3.402823466e38f);
+    step = (float)((dtop - (double)low) / kCacheCodeMax);
+  }
+  for (int k = tid; k < K; k += kSelThreads) {
+    const uint64_t c = cand[k];
+    const uint32_t v = 0xffffffffu - (uint32_t)c;
+    uint32_t code = kCacheNone;
+    if (k < kept) {
+      const float z = fminf(key_value((uint32_t)(c >> 32)), 3.402823466e38f);
+      const double q = step > 0.f ? __builtin_rint((dtop - (double)z) / (double)step) : 0.0;
+      code = q < (double)kCacheCodeMax ? (uint32_t)q : (uint32_t)kCacheCodeMax;
+    }
+    a.entries[r * K + k] = v << kCacheCodeBits | code;
+  }
+  if (tid == 0) {
+    a.scale[2 * r] = empty ? -INFINITY : a.logprobs ? -logs : top;
+    a.scale[2 * r + 1] = step;
+  }
+}
+
+// ------------------------------------------------------------ teacher cache --
+// Entries back to (index, value): value = top - code * step, rounded once (the
+// product is exact in the fused operation). V4: four entries a thread.
+template <bool V4>
+__global__ __launch_bounds__(256) void k_cache_read(const uint32_t* __restrict__ entries,
+                                                    const float* __restrict__ scale,
+                                                    const int64_t* __restrict__ rows, int64_t N,
+                                                    int64_t M, int K, int rows_per_block,
+                                                    int32_t* __restrict__ idx,
+                                                    float* __restrict__ value,
+                                                    uint8_t* __restrict__ ignore) {
+  constexpr int VPT = V4 ? 4 : 1;
+  const int per = K / VPT;
+  const int64_t stride = (int64_t)gridDim.x * rows_per_block;
+  for (int64_t m0 = (int64_t)blockIdx.x * rows_per_block; m0 < M; m0 += stride) {
+    const int nrow = (int)(M - m0 < rows_per_block ? M - m0 : rows_per_block);
+    for (int i = threadIdx.x; i < nrow * per; i += 256) {
+      const int j = i / per, q = i - j * per;
+      const int64_t m = m0 + j, src = rows != nullptr ? rows[m] : m;
+      const bool have = src >= 0 && src < N;
+      float top = -INFINITY, step = 0.f;
+      uint32_t e[VPT];
+#pragma unroll
+      for (int x = 0; x < VPT; ++x) e[x] = kCacheNone;
+      if (have) {
+        top = scale[2 * src];
+        step = scale[2 * src + 1];
+        const uint32_t* p = entries + src * K + q * VPT;
+        if constexpr (V4) {
+          const u32x4_t w = *reinterpret_cast<const u32x4_t*>(p);
+#pragma unroll
+          for (int x = 0; x < 4; ++x) e[x] = w[x];
+        } else {
+          e[0] = *p;
+        }
+      }
+      const bool empty = top == -INFINITY;
+      int32_t iv[VPT];
+      float zv[VPT];
+#pragma unroll
+      for (int x = 0; x < VPT; ++x) {
+        const int code = (int)(e[x] & ((1u << kCacheCodeBits) - 1));
+        iv[x] = empty ? -1 : (int32_t)(e[x] >> kCacheCodeBits);
+        zv[x] = empty ? 0.f : code == kCacheNone ? -INFINITY : fmaf(-(float)code, step, top);
+      }
+      const int64_t o = m * K + q * VPT;
+      if constexpr (V4) {
+        typedef __attribute__((__vector_size__(16))) int32_t s32x4_t;
+        *reinterpret_cast<s32x4_t*>(idx + o) = s32x4_t{iv[0], iv[1], iv[2], iv[3]};
+        *reinterpret_cast<f32x4_t*>(value + o) = f32x4_t{zv[0], zv[1], zv[2], zv[3]};
+      } else {
+        idx[o] = iv[0];
+        value[o] = zv[0];
+      }
+      if (q == 0 && ignore != nullptr) ignore[m] = empty ? 1 : 0;
+    }
+  }
+}
+
+// -------------------------------------------------------------- checkpoints --
+// Eight elements a thread, four threads a block of 32 (kd_ckpt.h).
+template <typename T>
+__global__ __launch_bounds__(256) void k_ckpt_write(const T* __restrict__ h, int64_t n8,
+                                                    uint8_t* __restrict__ codes,
+                                                    uint8_t* __restrict__ scales) {
+  const int64_t stride = (int64_t)gridDim.x * 256;
+  // (n8 is a multiple of 4: the four threads of a block run or stop together)
+  for (int64_t i = (int64_t)blockIdx.x * 256 + threadIdx.x; i < n8; i += stride) {
+    float v[8];
+    if constexpr (sizeof(T) == 2) {
+      const u32x4_t x = reinterpret_cast<const u32x4_t*>(h)[i];
+#pragma unroll
+      for (int j = 0; j < 4; ++j) {
+        v[2 * j] = __builtin_bit_cast(float, x[j] << 16);
+        v[2 * j + 1] = __builtin_bit_cast(float, x[j] & 0xffff0000u);
+      }
+    } else {
+      const f32x4_t x = reinterpret_cast<const f32x4_t*>(h)[2 * i];
+      const f32x4_t y = reinterpret_cast<const f32x4_t*>(h)[2 * i + 1];
+#pragma unroll
+      for (int j = 0; j < 4; ++j) {
+        v[j] = x[j];
+        v[4 + j] = y[j];
+      }
+    }
+    // magnitudes as bit patterns: their order has infinities and what is not a
+    // number at the end, so neither is lost in the maximum
+    uint32_t m = 0;
+#pragma unroll
+    for (int j = 0; j < 8; ++j) m = max(m, __builtin_bit_cast(uint32_t, v[j]) & 0x7fffffffu);
+    m = max(m, (uint32_t)__builtin_amdgcn_mov_dpp((int)m, 0xB1, 0xF, 0xF, false));
+    m = max(m, (uint32_t)__builtin_amdgcn_mov_dpp((int)m, 0x4E, 0xF, 0xF, false));
+    const int s = ckpt_scale(m);
+    reinterpret_cast<u32x2_t*>(codes)[i] =
+        u32x2_t{ckpt_pack4(v[0], v[1], v[2], v[3], s), ckpt_pack4(v[4], v[5], v[6], v[7], s)};
+    if ((threadIdx.x & 3) == 0) scales[i / 4] = (uint8_t)s;
+  }
+}
+
+template <typename T>
+__global__ __launch_bounds__(256) void k_ckpt_read(const uint8_t* __restrict__ codes,
+                                                   const uint8_t* __restrict__ scales, int64_t n16,
+                                                   T* __restrict__ h) {
+  constexpr int VPT = 16 / (int)sizeof(T);
+  const int64_t stride = (int64_t)gridDim.x * 256;
+  for (int64_t i = (int64_t)blockIdx.x * 256 + threadIdx.x; i < n16; i += stride)
+    reinterpret_cast<u32x4_t*>(h)[i] = ckpt_load16<T>(codes + i * VPT, scales + i * VPT / kCkptBlock, 0, 0, 0);
+}
+
+// ------------------------------------------------------------- verification --
+// A drafted token d at place t is kept while u_t q(d) < p(d), p the target's and
+// q the draft's softmax; the token behind the r kept ones is drawn by the last
+// uniform number u from x = max(p - q, 0) at place r, or from p behind the last
+// drafted one: the first v whose cumulative x exceeds u times the sum of x. A
+// step of that sum is as small as a token's probability, and 2^17 of them stand
+// side by side, so weights, sums and comparisons are in 64 bits (fp64 runs at
+// the rate of unpacked fp32 here).
+
+// 2^y for y <= 0: 2^n times the exponential series of ln(2) f, |f| <= 1/2 (to
+// degree 11: the next term is below 2^-47 of the result)
+__device__ __forceinline__ double exp2_64(double y) {
+  y = fmax(y, -1100.0);
+  const double n = __builtin_rint(y), g = (y - n) * 0.69314718055994530942;
+  double p = 1.0 / 39916800;
+  p = fma(p, g, 1.0 / 3628800);
+  p = fma(p, g, 1.0 / 362880);
+  p = fma(p, g, 1.0 / 40320);
+  p = fma(p, g, 1.0 / 5040);
+  p = fma(p, g, 1.0 / 720);
+  p = fma(p, g, 1.0 / 120);
+  p = fma(p, g, 1.0 / 24);
+  p = fma(p, g, 1.0 / 6);
+  p = fma(p, g, 0.5);
+  p = fma(p, g, 1.0);
+  p = fma(p, g, 1.0);
+  return __builtin_amdgcn_ldexp(p, (int)n);
+}
+// weight of z below the largest m: 2^(c (z - m)); with m = +inf, 1 for z = m; 0
+// where m = -inf (nothing is left)
+__device__ __forceinline__ double weight(float z, float m, double c) {
+  if (z == m) return m == -INFINITY ? 0.0 : 1.0;
+  return exp2_64(((double)z - (double)m) * c);
+}
+__device__ __forceinline__ double wave_sum64(double x) {
+#pragma unroll
+  for (int o = 32; o >= 1; o >>= 1) x += __shfl_xor(x, o);
+  return x;
+}
+__device__ __forceinline__ double wave_incl_scan64(double x) {
+  const int lane = threadIdx.x & 63;
+#pragma unroll
+  for (int o = 1; o < 64; o <<= 1) {
+    const double y = __shfl_up(x, o);
+    if (lane >= o) x += y;
+  }
+  return x;
+}
+
+struct VerifyArgs {
+  const void *target, *draft;
+  int64_t ld_t, ld_d;
+  int B, T, V, K, nseg;
+  const int32_t *tokens, *didx;
+  const float *dlogit, *uniform;
+  const int32_t* lengths;
+  double c;
+  int32_t *out_tokens, *accepted;
+  float* prob;
+  float* segm;
+  double *segs, *segr, *norm;
+};
+__device__ __forceinline__ int drafted(const VerifyArgs& a, int b) {
+  if (a.lengths == nullptr) return a.T;
+  const int n = a.lengths[b];
+  return n < 0 ? 0 : n > a.T ? a.T : n;
+}
+__device__ __forceinline__ int64_t target_row(const VerifyArgs& a, int b, int t) {
+  return (int64_t)b * (a.T + 1) + t;
+}
+__device__ __forceinline__ int64_t draft_row(const VerifyArgs& a, int b, int t) {
+  return (int64_t)b * a.T + t;
+}
+
+// Largest logit and sum of weights of each segment of the rows in question (the
+// target's, then the draft's): the pass that reads the logits. About 20 fp64
+// operations an element: at bf16 these take nearly as long as the read.
+template <typename T>
+__global__ __launch_bounds__(256) void k_seg_sums(VerifyArgs a, int waves) {
+  const int w = blockIdx.x * 4 + wave_id();
+  if (w >= waves) return;
+  const int r = w / a.nseg, seg = w - r * a.nseg;
+  const int nt = a.B * (a.T + 1);
+  const bool tgt = r < nt;
+  const int b = tgt ? r / (a.T + 1) : (r - nt) / a.T;
+  const int t = tgt ? r - b * (a.T + 1) : r - nt - b * a.T;
+  const int n = drafted(a, b);
+  if (tgt ? t > n : t >= n) return;  // no one asks for this row
+  const Row<T> row(tgt ? a.target : a.draft, tgt ? r * a.ld_t : (int64_t)(r - nt) * a.ld_d, a.V);
+  constexpr int U = Row<T>::U, VPT = Row<T>::VPT;
+  u32x4_t x[U];
+  row.segment(seg, x);
+  float m = -INFINITY;
+#pragma unroll
+  for (int u = 0; u < U; ++u)
+#pragma unroll
+    for (int i = 0; i < VPT; ++i) m = fmaxf(m, Row<T>::elt(x[u], i));
+  m = wave_max(m);
+  double s = 0.0;
+  if (m != -INFINITY) {
+#pragma unroll
+    for (int u = 0; u < U; ++u) {
+#pragma unroll
+      for (int i = 0; i < VPT; ++i) s += weight(Row<T>::elt(x[u], i), m, a.c);
+    }
+  }
+  s = wave_sum64(s);
+  if ((threadIdx.x & 63) == 0) {
+    a.segm[w] = m;
+    a.segs[w] = s;
+  }
+}
+
+constexpr int kVerThreads = 512;
+constexpr int kVerWaves = kVerThreads / 64;
+constexpr int kVerMaxSegs = 513;   // of 2^20 columns
+struct VerifyShared {
+  double seg[kVerMaxSegs];         // mass of each segment
+  double x[kSegCols];              // the segment the token is drawn from
+  double scan[kVerWaves];
+  double S, total, goal, before;
+  float M;
+  int first, at;
+};
+
+// (M, S) of a row from its segments, by the calling wave
+__device__ __forceinline__ void merge_row(const VerifyArgs& a, int64_t r, float& M, double& S) {
+  const float* pm = a.segm + r * a.nseg;
+  const double* ps = a.segs + r * a.nseg;
+  const int lane = threadIdx.x & 63;
+  float m = -INFINITY;
+  for (int i = lane; i < a.nseg; i += 64) m = fmaxf(m, pm[i]);
+  M = wave_max(m);
+  double s = 0.0;
+  if (M != -INFINITY)
+    for (int i = lane; i < a.nseg; i += 64) s += ps[i] * weight(pm[i], M, a.c);
+  S = wave_sum64(s);
+}
+
+// The segment, and in it the place, that the goal falls in: sh.seg holds the
+// mass of each segment. fill(seg) writes the mass of each of its places to sh.x
+// (all threads). Returns the place (or -1 if no place has mass), to all threads.
+template <typename F>
+__device__ __forceinline__ int pick_place(VerifyShared& sh, int nseg, double u, F&& fill) {
+  const int tid = threadIdx.x, lane = tid & 63;
+  // segments: a wave, a run of them per lane
+  if (tid < 64) {
+    const int per = (nseg + 63) / 64, i0 = lane * per;
+    double sum = 0.0;
+    for (int i = i0; i < i0 + per && i < nseg; ++i) sum += sh.seg[i];
+    const double incl = wave_incl_scan64(sum);
+    const double total = __shfl(incl, 63);
+    const double goal = u * total;
+    double at = incl - sum;
+    int first = nseg;
+    double before = 0.0;
+    for (int i = i0; i < i0 + per && i < nseg; ++i) {
+      if (first == nseg && at + sh.seg[i] > goal) {
+        first = i;
+        before = at;
+      }
+      at += sh.seg[i];
+    }
+    // the first lane's find; the last segment with mass if rounding left none
+    const uint64_t found = __builtin_amdgcn_ballot_w64(first < nseg);
+    int last = -1;
+    for (int i = i0; i < i0 + per && i < nseg; ++i)
+      if (sh.seg[i] > 0.0) last = i;
+    const uint64_t some = __builtin_amdgcn_ballot_w64(last >= 0);
+    if (found != 0) {
+      const int l = __builtin_ctzll(found);
+      first = __shfl(first, l);
+      before = __shfl(before, l);
+    } else if (some != 0) {
+      first = __shfl(last, 63 - __builtin_clzll(some));
+      before = 0.0;
+    }
+    if (lane == 0) {
+      sh.total = total;
+      sh.goal = found != 0 ? goal - before : INFINITY;
+      sh.first = total > 0.0 ? first : nseg;
+    }
+  }
+  __syncthreads();
+  const int first = sh.first;
+  if (first >= nseg) return -1;
+  // within the segment the first place past the goal, else its last with mass;
+  // where the segment has none after all, the next ones', then the ones' before
+  for (int i = 0; i < nseg; ++i) {
+    const int seg = first + i < nseg ? first + i : nseg - 1 - i;
+    fill(seg);
+    if (tid == 0) sh.at = kSegCols;
+    __syncthreads();
+    constexpr int per = kSegCols / kVerThreads;
+    double v[per], sum = 0.0;
+    int last = -1;
+#pragma unroll
+    for (int j = 0; j < per; ++j) {
+      v[j] = sh.x[tid * per + j];
+      sum += v[j];
+      if (v[j] > 0.0) last = tid * per + j;
+    }
+    double incl = wave_incl_scan64(sum);
+    if (lane == 63) sh.scan[tid >> 6] = incl;
+    __syncthreads();
+    for (int w = 0; w < (tid >> 6); ++w) incl += sh.scan[w];
+    double at = incl - sum;
+    const double goal = i == 0 ? sh.goal : first + i < nseg ? 0.0 : INFINITY;
+#pragma unroll
+    for (int j = per - 1; j >= 0; --j) {
+      // (from the end: the first one stays; sums as in the forward order)
+      double c = at;
+      for (int k = 0; k <= j; ++k) c += v[k];
+      if (c > goal && v[j] > 0.0) atomicMin(&sh.at, tid * per + j);
+    }
+    __syncthreads();
+    int place = sh.at;
+    __syncthreads();
+    if (place == kSegCols) {
+      if (tid == 0) sh.at = -1;
+      __syncthreads();
+      if (last >= 0) atomicMax(&sh.at, last);
+      __syncthreads();
+      place = sh.at;
+      __syncthreads();
+    }
+    if (place >= 0) return seg * kSegCols + place;
+  }
+  return -1;
+}
+
+// place -> token, and the tokens behind it
+__device__ __forceinline__ void write_tokens(const VerifyArgs& a, int b, int r, int next) {
+  int32_t* out = a.out_tokens + (int64_t)b * (a.T + 1);
+  for (int t = threadIdx.x; t <= a.T; t += kVerThreads)
+    out[t] = t < r ? a.tokens[(int64_t)b * a.T + t] : t == r ? next : -1;
+  if (threadIdx.x == 0) a.accepted[b] = r;
+}
+
+// the segment's masses of the target's row: p times S, places outside 0
+template <typename T>
+__device__ __forceinline__ void fill_target(VerifyShared& sh, const Row<T>& row, int seg, float M,
+                                            double c) {
+  constexpr int VPT = Row<T>::VPT;
+  for (int j = threadIdx.x; j < kSegCols / VPT; j += kVerThreads) {
+    const u32x4_t x = row.at(seg * kSegCols + j * VPT);
+#pragma unroll
+    for (int i = 0; i < VPT; ++i) sh.x[j * VPT + i] = weight(Row<T>::elt(x, i), M, c);
+  }
+}
+
+// A workgroup per sequence: the places' probabilities of their tokens (a wave per
+// place), the first rejected place, and with a draft of K entries the draw. The
+// draft's K entries take their part of a segment's mass out of its sum: no pass
+// over the vocabulary but the one segment's.
+template <typename T, bool DENSE>
+__global__ __launch_bounds__(kVerThreads) void k_accept(VerifyArgs a) {
+  extern __shared__ __align__(16) char lds[];
+  __shared__ VerifyShared sh;
+  const int b = blockIdx.x, tid = threadIdx.x, lane = tid & 63, wave = wave_id();
+  const int n = drafted(a, b);
+  if (tid == 0) sh.first = n;
+  __syncthreads();
+  if (a.prob != nullptr)
+    for (int t = n + tid; t < a.T; t += kVerThreads) a.prob[draft_row(a, b, t)] = 0.f;
+  for (int t = wave; t < n; t += kVerWaves) {
+    const int64_t rt = target_row(a, b, t), rd = draft_row(a, b, t);
+    const int d = a.tokens[rd];
+    const bool known = (unsigned)d < (unsigned)a.V;
+    float M;
+    double S;
+    merge_row(a, rt, M, S);
+    const Row<T> row(a.target, rt * a.ld_t, a.V);
+    const double p = known && S > 0.0 ? weight(row.one(d), M, a.c) / S : 0.0;
+    double q = 0.0;
+    if constexpr (DENSE) {
+      merge_row(a, (int64_t)a.B * (a.T + 1) + rd, M, S);
+      const Row<T> dr(a.draft, rd * a.ld_d, a.V);
+      q = known && S > 0.0 ? weight(dr.one(d), M, a.c) / S : 0.0;
+    } else {
+      const float* l = a.dlogit + rd * a.K;
+      const int32_t* ix = a.didx + rd * a.K;
+      float m = -INFINITY;
+      for (int k = lane; k < a.K; k += 64) m = fmaxf(m, l[k]);
+      m = wave_max(m);
+      double s = 0.0, w = 0.0;
+      for (int k = lane; k < a.K; k += 64) {
+        const double e = weight(fmaxf(l[k], -INFINITY), m, a.c);
+        s += e;
+        if (ix[k] == d) w += e;
+      }
+      s = wave_sum64(s);
+      w = wave_sum64(w);
+      q = known && s > 0.0 ? w / s : 0.0;
+    }
+    if (lane == 0) {
+      const double u = a.uniform[target_row(a, b, t)];
+      if (!(u * q < p)) atomicMin(&sh.first, t);
+      if (a.prob != nullptr)
+        a.prob[rd] = q > 0.0 ? (float)fmin(p / q, 1.0) : p > 0.0 ? 1.f : 0.f;
+    }
+  }
+  __syncthreads();
+  const int r = sh.first;
+  __syncthreads();
+  const int64_t rt = target_row(a, b, r);
+  if (wave == 0) {
+    float M;
+    double S;
+    merge_row(a, rt, M, S);
+    if (lane == 0) {
+      sh.M = M;
+      sh.S = S;
+    }
+  }
+  if constexpr (DENSE) {
+    if (wave == 1 && r < n) {
+      float M;
+      double S;
+      merge_row(a, (int64_t)a.B * (a.T + 1) + draft_row(a, b, r), M, S);
+      if (lane == 0) {
+        a.norm[4 * b + 2] = M;
+        a.norm[4 * b + 3] = S;
+      }
+    }
+    __syncthreads();
+    if (tid == 0) {
+      a.norm[4 * b] = sh.M;
+      a.norm[4 * b + 1] = sh.S;
+      a.accepted[b] = r;
+    }
+    return;
+  }
+  __syncthreads();
+  const float M = sh.M;
+  const double S = sh.S;
+  const Row<T> row(a.target, rt * a.ld_t, a.V);
+  const float* pm = a.segm + rt * a.nseg;
+  const double* ps = a.segs + rt * a.nseg;
+  // entries of the draft at the rejected place: min(p, q) times S at the first
+  // of each index (an index that repeats counts once, with the sum), else 0
+  double* em = reinterpret_cast<double*>(lds);
+  int* ei = reinterpret_cast<int*>(em + a.K);
+  const bool rest = r < n && S > 0.0;
+  if (rest) {
+    const float* l = a.dlogit + draft_row(a, b, r) * a.K;
+    const int32_t* ix = a.didx + draft_row(a, b, r) * a.K;
+    float m = -INFINITY;
+    for (int k = lane; k < a.K; k += 64) m = fmaxf(m, l[k]);  // (each wave for itself)
+    m = wave_max(m);
+    double s = 0.0;
+    for (int k = lane; k < a.K; k += 64) s += weight(fmaxf(l[k], -INFINITY), m, a.c);
+    s = wave_sum64(s);
+    for (int k = tid; k < a.K; k += kVerThreads) {
+      em[k] = s > 0.0 ? weight(fmaxf(l[k], -INFINITY), m, a.c) / s : 0.0;
+      ei[k] = ix[k];
+    }
+    __syncthreads();
+    for (int k0 = 0; k0 < a.K; k0 += kVerThreads) {
+      const int k = k0 + tid;
+      double q = 0.0;
+      int v = -1;
+      if (k < a.K) {
+        v = ei[k];
+        bool again = (unsigned)v >= (unsigned)a.V;
+        for (int j = 0; j < a.K; ++j)
+          if (ei[j] == v) {
+            q += em[j];
+            if (j < k) again = true;
+          }
+        if (again) v = -1;
+        if (v >= 0) q = fmin(q * S, weight(row.one(v), M, a.c));
+      }
+      // (the sums of this round's threads read em of all entries: written after)
+      __syncthreads();
+      if (k < a.K) reinterpret_cast<double*>(ei + ((a.K + 1) & ~1))[k] = v >= 0 ? q : 0.0;
+    }
+    em = reinterpret_cast<double*>(ei + ((a.K + 1) & ~1));
+    __syncthreads();
+  }
+  for (int i = tid; i < a.nseg; i += kVerThreads) {
+    double x = M == -INFINITY ? 0.0 : ps[i] * weight(pm[i], M, a.c);
+    if (rest) {
+      double take = 0.0;
+      for (int k = 0; k < a.K; ++k)
+        if ((unsigned)ei[k] < (unsigned)a.V && (ei[k] + row.shift) / kSegCols == i) take += em[k];
+      x = fmax(x - take, 0.0);
+    }
+    sh.seg[i] = x;
+  }
+  __syncthreads();
+  const double u = a.uniform[target_row(a, b, a.T)];
+  int place = pick_place(sh, a.nseg, u, [&](int seg) {
+    fill_target<T>(sh, row, seg, M, a.c);
+    __syncthreads();
+    if (rest)
+      for (int k = tid; k < a.K; k += kVerThreads) {
+        const int e = ei[k] + row.shift - seg * kSegCols;
+        if (em[k] > 0.0 && (unsigned)e < (unsigned)kSegCols) sh.x[e] -= em[k];
+      }
+    __syncthreads();
+  });
+  if (place < 0 && rest) {
+    // p does not exceed q anywhere: from p
+    for (int i = tid; i < a.nseg; i += kVerThreads) sh.seg[i] = ps[i] * weight(pm[i], M, a.c);
+    __syncthreads();
+    place = pick_place(sh, a.nseg, u, [&](int seg) {
+      fill_target<T>(sh, row, seg, M, a.c);
+      __syncthreads();
+    });
+  }
+  write_tokens(a, b, r, place < 0 ? -1 : place - row.shift);
+}
+
+// the masses of a dense draft's rejected row: max(p - q, 0), p where nothing was
+// rejected; places count from the target row's boundary
+struct RestRow {
+  float Mt, Md;
+  double St, Sd;
+  bool rest;
+  __device__ __forceinline__ RestRow(const VerifyArgs& a, int b, bool rest_) : rest(rest_) {
+    Mt = (float)a.norm[4 * b];
+    St = a.norm[4 * b + 1];
+    Md = rest ? (float)a.norm[4 * b + 2] : 0.f;
+    Sd = rest ? a.norm[4 * b + 3] : 0.0;
+  }
+  __device__ __forceinline__ double mass(float zt, float zd, double c) const {
+    const double p = St > 0.0 ? weight(zt, Mt, c) / St : 0.0;
+    if (!rest) return p;
+    const double q = Sd > 0.0 ? weight(zd, Md, c) / Sd : 0.0;
+    return fmax(p - q, 0.0);
+  }
+};
+// vector of the draft's row at the target's place e (its own boundary may differ)
+template <typename T>
+__device__ __forceinline__ u32x4_t draft_at(const Row<T>& d, int e, int shift) {
+  if (d.shift == shift) return d.at(e);
+  constexpr int VPT = Row<T>::VPT;
+  uint32_t w[4];
+  const int v = e - shift;
+  if constexpr (sizeof(T) == 2) {
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+      const uint16_t* h = reinterpret_cast<const uint16_t*>(d.p);
+      const uint32_t x = (unsigned)(v + 2 * i) < (unsigned)d.V ? h[v + 2 * i] : 0xff80u;
+      const uint32_t y = (unsigned)(v + 2 * i + 1) < (unsigned)d.V ? h[v + 2 * i + 1] : 0xff80u;
+      w[i] = x | y << 16;
+    }
+  } else {
+#pragma unroll
+    for (int i = 0; i < VPT; ++i)
+      w[i] = (unsigned)(v + i) < (unsigned)d.V ? reinterpret_cast<const uint32_t*>(d.p)[v + i]
+                                               : 0xff800000u;
+  }
+  return u32x4_t{w[0], w[1], w[2], w[3]};
+}
+
+// Dense draft: the mass of each segment at the place where the sequence ended,
+// a wave per segment.
+template <typename T>
+__global__ __launch_bounds__(256) void k_rest_sums(VerifyArgs a, int waves) {
+  const int w = blockIdx.x * 4 + wave_id();
+  if (w >= waves) return;
+  const int b = w / a.nseg, seg = w - b * a.nseg;
+  const int r = a.accepted[b];
+  const bool rest = r < drafted(a, b);
+  const RestRow m(a, b, rest);
+  const Row<T> row(a.target, target_row(a, b, r) * a.ld_t, a.V);
+  const Row<T> dr(a.draft, draft_row(a, b, rest ? r : 0) * a.ld_d, a.V);
+  constexpr int VPT = Row<T>::VPT, U = Row<T>::U;
+  const int lane = threadIdx.x & 63;
+  double s = 0.0;
+#pragma unroll 2
+  for (int u = 0; u < U; ++u) {
+    const int e = seg * kSegCols + (64 * u + lane) * VPT;
+    const u32x4_t x = row.at(e);
+    const u32x4_t y = rest ? draft_at<T>(dr, e, row.shift) : x;
+#pragma unroll
+    for (int i = 0; i < VPT; ++i) s += m.mass(Row<T>::elt(x, i), Row<T>::elt(y, i), a.c);
+  }
+  s = wave_sum64(s);
+  if (lane == 0) a.segr[w] = s;
+}
+
+template <typename T>
+__global__ __launch_bounds__(kVerThreads) void k_pick(VerifyArgs a) {
+  __shared__ VerifyShared sh;
+  const int b = blockIdx.x, tid = threadIdx.x;
+  const int r = a.accepted[b];
+  const bool rest = r < drafted(a, b);
+  const int64_t rt = target_row(a, b, r);
+  const Row<T> row(a.target, rt * a.ld_t, a.V);
+  const Row<T> dr(a.draft, draft_row(a, b, rest ? r : 0) * a.ld_d, a.V);
+  const RestRow m(a, b, rest);
+  for (int i = tid; i < a.nseg; i += kVerThreads) sh.seg[i] = a.segr[(int64_t)b * a.nseg + i];
+  __syncthreads();
+  const double u = a.uniform[target_row(a, b, a.T)];
+  constexpr int VPT = Row<T>::VPT;
+  int place = pick_place(sh, a.nseg, u, [&](int seg) {
+    for (int j = tid; j < kSegCols / VPT; j += kVerThreads) {
+      const int e = seg * kSegCols + j * VPT;
+      const u32x4_t x = row.at(e);
+      const u32x4_t y = rest ? draft_at<T>(dr, e, row.shift) : x;
+#pragma unroll
+      for (int i = 0; i < VPT; ++i)
+        sh.x[j * VPT + i] = m.mass(Row<T>::elt(x, i), Row<T>::elt(y, i), a.c);
+    }
+    __syncthreads();
+  });
+  if (place < 0 && rest && m.St > 0.0) {
+    const float* pm = a.segm + rt * a.nseg;
+    const double* ps = a.segs + rt * a.nseg;
+    for (int i = tid; i < a.nseg; i += kVerThreads) sh.seg[i] = ps[i] * weight(pm[i], m.Mt, a.c);
+    __syncthreads();
+    place = pick_place(sh, a.nseg, u, [&](int seg) {
+      fill_target<T>(sh, row, seg, m.Mt, a.c);
+      __syncthreads();
+    });
+  }
+  write_tokens(a, b, r, place < 0 ? -1 : place - row.shift);
+}
+
+}  // namespace kd
+
+// ================================================================ launchers ==
+using namespace kd;
+
+template <typename T>
+static int launch_topk(const KdTopkArgs& a, hipStream_t s) {
+  const int64_t waves = a.rows * a.nseg;
+  const dim3 grid((unsigned)((waves + 3) / 4));
+  const T* x = static_cast<const T*>(a.logits);
+  if (a.logprobs)
+    hipLaunchKernelGGL((k_row_groups<T, true>), grid, dim3(256), 0, s, x, a.ld, a.V, a.nseg,
+                       (int)waves, a.gmax, a.pm, a.ps);
+  else
+    hipLaunchKernelGGL((k_row_groups<T, false>), grid, dim3(256), 0, s, x, a.ld, a.V, a.nseg,
+                       (int)waves, a.gmax, (float*)nullptr, (float*)nullptr);
+  const int G = a.nseg * kSegGroups;
+  const SelectArgs q{a.logits, a.ld, a.V, a.K, G, a.nseg, a.logprobs, a.gmax, a.pm, a.ps,
+                     a.idx, a.value, a.entries, a.scale};
+  hipLaunchKernelGGL(k_row_select<T>, dim3((unsigned)a.rows), dim3(kSelThreads),
+                     (size_t)select_lds(G, a.K), s, q);
+  return (int)hipGetLastError();
+}
+
+extern "C" int kd_launch_topk(const KdTopkArgs* a, void* stream) {
+  hipStream_t s = static_cast<hipStream_t>(stream);
+  return a->dtype == 1 ? launch_topk<__bf16>(*a, s) : launch_topk<float>(*a, s);
+}
+
+extern "C" int kd_launch_cache_read(const KdCacheReadArgs* a, void* stream) {
+  hipStream_t s = static_cast<hipStream_t>(stream);
+  const bool v4 = a->K % 4 == 0 && (((uintptr_t)a->entries | (uintptr_t)a->idx |
+                                     (uintptr_t)a->value) & 15u) == 0;
+  // rows of a block: about 1024 pieces, at most 64 rows
+  const int per = v4 ? a->K / 4 : a->K;
+  const int rpb = per >= 1024 ? 1 : 1024 / per > 64 ? 64 : 1024 / per;
+  const int64_t blocks = (a->M + rpb - 1) / rpb;
+  const dim3 grid((unsigned)(blocks < (1 << 20) ? blocks : 1 << 20));
+  if (v4)
+    hipLaunchKernelGGL(k_cache_read<true>, grid, dim3(256), 0, s, a->entries, a->scale, a->rows,
+                       a->N, a->M, a->K, rpb, a->idx, a->value, a->ignore);
+  else
+    hipLaunchKernelGGL(k_cache_read<false>, grid, dim3(256), 0, s, a->entries, a->scale, a->rows,
+                       a->N, a->M, a->K, rpb, a->idx, a->value, a->ignore);
+  return (int)hipGetLastError();
+}
+
+static unsigned stream_blocks(int64_t threads) {
+  const int64_t b = (threads + 255) / 256;
+  return (unsigned)(b < 16384 ? b : 16384);
+}
+
+extern "C" int kd_launch_ckpt_write(const void* hidden, int dtype, int64_t n, uint8_t* codes,
+                                    uint8_t* scales, void* stream) {
+  hipStream_t s = static_cast<hipStream_t>(stream);
+  const dim3 grid(stream_blocks(n / 8));
+  if (dtype == 1)
+    hipLaunchKernelGGL(k_ckpt_write<__bf16>, grid, dim3(256), 0, s,
+                       static_cast<const __bf16*>(hidden), n / 8, codes, scales);
+  else
+    hipLaunchKernelGGL(k_ckpt_write<float>, grid, dim3(256), 0, s,
+                       static_cast<const float*>(hidden), n / 8, codes, scales);
+  return (int)hipGetLastError();
+}
+
+extern "C" int kd_launch_ckpt_read(const uint8_t* codes, const uint8_t* scales, int dtype,
+                                   int64_t n, void* hidden, void* stream) {
+  hipStream_t s = static_cast<hipStream_t>(stream);
+  if (dtype == 1)
+    hipLaunchKernelGGL(k_ckpt_read<__bf16>, dim3(stream_blocks(n / 8)), dim3(256), 0, s, codes,
+                       scales, n / 8, static_cast<__bf16*>(hidden));
+  else
+    hipLaunchKernelGGL(k_ckpt_read<float>, dim3(stream_blocks(n / 4)), dim3(256), 0, s, codes,
+                       scales, n / 4, static_cast<float*>(hidden));
+  return (int)hipGetLastError();
+}
+
+template <typename T>
+static int launch_verify(const KdVerifyArgs& q, hipStream_t s) {
+  const VerifyArgs a{q.target, q.draft, q.ld_t, q.ld_d, q.B, q.T, q.V, q.K, q.nseg,
+                     q.tokens, q.didx, q.dlogit, q.uniform, q.lengths, q.c, q.out_tokens,
+                     q.accepted, q.prob, q.segm, q.segs, q.segr, q.norm};
+  const bool dense = q.draft != nullptr;
+  const int64_t waves = ((int64_t)q.B * (q.T + 1) + (dense ? (int64_t)q.B * q.T : 0)) * q.nseg;
+  hipLaunchKernelGGL(k_seg_sums<T>, dim3((unsigned)((waves + 3) / 4)), dim3(256), 0, s, a,
+                     (int)waves);
+  if (!dense) {
+    // q of the entries, their indices, and the mass they take
+    const size_t lds = (size_t)q.K * 16 + (size_t)((q.K + 1) & ~1) * 4;
+    hipLaunchKernelGGL((k_accept<T, false>), dim3(q.B), dim3(kVerThreads), lds, s, a);
+    return (int)hipGetLastError();
+  }
+  hipLaunchKernelGGL((k_accept<T, true>), dim3(q.B), dim3(kVerThreads), 0, s, a);
+  const int64_t w2 = (int64_t)q.B * q.nseg;
+  hipLaunchKernelGGL(k_rest_sums<T>, dim3((unsigned)((w2 + 3) / 4)), dim3(256), 0, s, a, (int)w2);
+  hipLaunchKernelGGL(k_pick<T>, dim3(q.B), dim3(kVerThreads), 0, s, a);
+  return (int)hipGetLastError();
+}
+
+extern "C" int kd_launch_verify(const KdVerifyArgs* a, void* stream) {
+  hipStream_t s = static_cast<hipStream_t>(stream);
+  return a->dtype == 1 ? launch_verify<__bf16>(*a, s) : launch_verify<float>(*a, s);
+}

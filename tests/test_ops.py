@@ -1,0 +1,446 @@
+"""The operators around the loss on the GPU against the fp64 oracle: top-K
+entries, the teacher cache, 8-bit checkpoints, draft verification."""
+import numpy as np
+import pytest
+import torch
+
+import kd_inputs as ki
+from oracle import ops_oracle as oo
+from tests.helpers import to64
+
+pytestmark = pytest.mark.gpu
+
+DT = {"bf16": torch.bfloat16, "f32": torch.float32}
+E32 = 2.0 ** -24  # half a step of fp32, relative
+
+
+def _gen(seed):
+    g = torch.Generator(device="cuda")
+    g.manual_seed(seed)
+    return g
+
+
+def _logits(N, V, dtype, seed, ld=None, offset=0, std=5.0):
+    """[N, V] view with rows `ld` apart that starts `offset` elements into its storage."""
+    ld = V if ld is None else ld
+    flat = torch.full((offset + N * ld,), float("nan"), dtype=DT[dtype], device="cuda")
+    x = flat[offset:].view(N, ld)[:, :V]
+    x.copy_(torch.randn(N, V, generator=_gen(seed), device="cuda") * std)
+    return x
+
+
+SPECIALS = ("plain", "ties", "constant", "masked", "lowest", "nan", "inf", "ascending")
+
+
+def _special(x, kind):
+    """Rows with the values that a selection can go wrong at, in place."""
+    N, V = x.shape
+    low = torch.finfo(x.dtype).min
+    if kind == "ties":
+        x.copy_((x / 4).round() * 4)
+    elif kind == "constant":
+        x.fill_(-1.5)
+    elif kind == "masked":           # three columns left, in the last row none
+        keep = x[:, [0, V // 2, V - 1]].clone()
+        x.fill_(float("-inf"))
+        x[:, [0, V // 2, V - 1]] = keep
+        x[-1] = float("-inf")
+    elif kind == "lowest":           # the same by the type's lowest value
+        keep = x[:, [0, V // 2, V - 1]].clone()
+        x.fill_(low)
+        x[:, [0, V // 2, V - 1]] = keep
+        x[-1] = low
+    elif kind == "nan":
+        x[:, ::3] = float("nan")
+        x[-1] = float("nan")
+    elif kind == "inf":
+        x[0, V // 3] = float("inf")
+        x[-1, [0, V - 1]] = float("inf")
+        x[:, 1] = float("-inf")
+    elif kind == "ascending":
+        x.copy_(torch.arange(V, device=x.device).to(x.dtype) * 0.5)
+    return x
+
+
+def _check_topk(kd, x, K):
+    a = x.float().cpu().numpy().astype(np.float64)
+    got = kd.topk_entries(x, K)
+    lp = kd.topk_entries(x, K, logprobs=True)
+    torch.cuda.synchronize()
+    idx, val = oo.topk_entries(a, K)
+    assert np.array_equal(to64(got["teacher_idx"]), idx)
+    assert np.array_equal(to64(got["teacher_logit"]), val)
+    idx, val = oo.topk_entries(a, K, True)
+    assert np.array_equal(to64(lp["teacher_idx"]), idx)
+    g = to64(lp["teacher_logit"])
+    fin = np.isfinite(val)
+    assert np.array_equal(fin, np.isfinite(g)) and np.array_equal(g[~fin], val[~fin])
+    # log of the sum: each exp off by up to 4 half steps (difference, product and
+    # 2^x), the sum of positive terms by one for each of the additions on its
+    # longest path (32 in a lane, 6 in a wave, 9 + 6 over the segments); then the
+    # logarithm, the difference and the value's own roundings
+    assert np.all(np.abs(g[fin] - val[fin]) <= 64 * E32 + 3 * E32 * np.abs(val[fin]))
+
+
+@pytest.mark.parametrize("kind", SPECIALS)
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+@pytest.mark.parametrize("N,V,K,ld,offset", [
+    (3, 1, 1, None, 0), (4, 7, 7, 9, 1), (5, 64, 3, None, 3), (3, 300, 300, 301, 5),
+    (2, 2049, 100, 2051, 7), (3, 6500, 100, None, 0), (2, 32003, 257, 32005, 2)])
+def test_topk_entries(gpu_lib, N, V, K, ld, offset, dtype, kind):
+    print(f"[topk] {N} {V} {K} ld={ld} +{offset} {dtype} {kind}", flush=True)
+    x = _logits(N, V, dtype, 11, ld, offset)
+    if V >= 3:
+        _special(x, kind)
+    _check_topk(gpu_lib, x, K)
+
+
+@pytest.mark.parametrize("dtype,N,V,K", [
+    ("bf16", 2, 131072, 100), ("f32", 1, 131072, 100), ("bf16", 2, 1 << 20, 4096),
+    ("f32", 1, (1 << 20) - 3, 1000), ("bf16", 2, 50257, 4096), ("f32", 2, 5000, 4096)])
+def test_topk_entries_large(gpu_lib, dtype, N, V, K):
+    print(f"[topk] {dtype} {N} {V} {K}", flush=True)
+    _check_topk(gpu_lib, _logits(N, V, dtype, 12), K)
+
+
+def test_topk_many_rows_in_batches(gpu_lib):
+    """More rows than the workspace holds at a time."""
+    kd, N, V, K = gpu_lib, 500000, 9, 2
+    assert kd.topk_workspace_size(N, V, K) < 70 << 20
+    x = _logits(N, V, "bf16", 13)
+    got = kd.topk_entries(x, K)
+    idx, val = oo.topk_entries(x.float().cpu().numpy(), K)
+    assert np.array_equal(to64(got["teacher_idx"]), idx)
+    assert np.array_equal(to64(got["teacher_logit"]), val)
+
+
+@pytest.mark.parametrize("kind", SPECIALS)
+@pytest.mark.parametrize("logprobs", [False, True])
+@pytest.mark.parametrize("dtype,N,V,K", [("bf16", 3, 300, 8), ("f32", 4, 5003, 100),
+                                          ("bf16", 3, 40000, 129), ("f32", 2, 70, 70)])
+def test_teacher_cache(gpu_lib, dtype, N, V, K, logprobs, kind):
+    kd = gpu_lib
+    print(f"[cache] {dtype} {N} {V} {K} {logprobs} {kind}", flush=True)
+    x = _special(_logits(N, V, dtype, 21), kind)
+    # written into the middle of a larger cache
+    entries = torch.full((N + 2, K), 7, dtype=torch.int32, device="cuda")
+    scale = torch.full((N + 2, 2), 7.0, device="cuda")
+    kd.teacher_cache_write(x, K, logprobs=logprobs,
+                           out={"entries": entries[1:-1], "scale": scale[1:-1]})
+    e, top, step = oo.cache_write(x.float().cpu().numpy(), K, logprobs)
+    got_e = to64(entries).astype(np.int64) & 0xffffffff
+    assert np.array_equal(got_e[1:-1], e)
+    assert (got_e[[0, -1]] == 7).all() and bool((scale[[0, -1]] == 7.0).all())
+    sc = to64(scale[1:-1])
+    assert np.array_equal(sc[:, 1], step.astype(np.float64))
+    fin = np.isfinite(top)
+    assert np.array_equal(fin, np.isfinite(sc[:, 0]))
+    # top as in _check_topk; exact without log-probabilities
+    tol = 64 * E32 + 3 * E32 * np.abs(top[fin]) if logprobs else 0.0
+    assert np.all(np.abs(sc[fin, 0] - top[fin]) <= tol)
+    # read back: all rows, and rows by number (twice the same, outside the cache)
+    for rows in (None, [N, 0, N + 1, -1, 1, 1, N + 2, 1 << 40, -(1 << 40)]):
+        r = None if rows is None else torch.tensor(rows, device="cuda")
+        t = kd.teacher_cache_read(entries, scale, rows=r)
+        idx, logit, ignore = oo.cache_read(to64(entries), to64(scale), rows)
+        assert np.array_equal(to64(t["teacher_idx"]), idx)
+        assert np.array_equal(to64(t["ignore"]), ignore)
+        g = to64(t["teacher_logit"])
+        assert np.array_equal(np.isfinite(g), np.isfinite(logit))
+        f = np.isfinite(logit)
+        assert np.array_equal(g[f], logit[f].astype(np.float32).astype(np.float64))
+
+
+def test_teacher_cache_far_rows(gpu_lib):
+    """Entries past 2^32 elements of a cache (17 GB)."""
+    kd, K = gpu_lib, 4096
+    N = (1 << 20) + 5
+    entries = torch.empty(N, K, dtype=torch.int32, device="cuda")
+    scale = torch.empty(N, 2, device="cuda")
+    rows = torch.tensor([N - 1, 0, 1 << 19, N - 3], device="cuda")
+    for i, r in enumerate(rows.tolist()):
+        entries[r] = torch.arange(K, device="cuda", dtype=torch.int32) * 4096 + i
+        scale[r] = torch.tensor([10.0 * i, 0.5], device="cuda")
+    t = kd.teacher_cache_read(entries, scale, rows=rows)
+    for i in range(4):
+        assert torch.equal(t["teacher_idx"][i], torch.arange(K, device="cuda", dtype=torch.int32))
+        assert bool((t["teacher_logit"][i] == 10.0 * i - 0.5 * i).all())
+    assert not bool(t["ignore"].any())
+
+
+# -------------------------------------------------------------- checkpoints --
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+@pytest.mark.parametrize("N,D", [(1, 32), (3, 64), (77, 768), (5, 96)])
+def test_checkpoint_round_trip(gpu_lib, N, D, dtype):
+    kd = gpu_lib
+    x = torch.randn(N, D, generator=_gen(31), device="cuda")
+    # magnitudes from far below to far above 1, block by block and inside blocks
+    x *= torch.exp2(torch.randint(-40, 41, (N, D // 32, 1), generator=_gen(32), device="cuda")
+                    .expand(N, D // 32, 32).reshape(N, D).float())
+    x *= torch.exp2(-torch.randint(0, 24, (N, D), generator=_gen(33), device="cuda").float())
+    x = x.to(DT[dtype])
+    if N > 2:
+        x[0, :32] = 0.0
+        x[1, 3] = float("inf")
+        x[2, 40] = float("nan")
+        x[2, :32] = torch.finfo(DT[dtype]).max * (1 - 2 * (torch.arange(32, device="cuda") % 2))
+    c = kd.checkpoint_write(x)
+    want, s = oo.checkpoint(to64(x))
+    assert np.array_equal(to64(c["scales"]), s)
+    for out in (torch.bfloat16, torch.float32):
+        got = to64(kd.checkpoint_read(c["codes"], c["scales"], out))
+        assert np.array_equal(got, want, equal_nan=True)
+
+
+def test_checkpoint_every_code(gpu_lib):
+    """Every e4m3 code at several scales, and every bf16 magnitude's rounding."""
+    kd = gpu_lib
+    codes = torch.arange(256, dtype=torch.uint8, device="cuda").view(1, 256).repeat(5, 1)
+    scales = torch.tensor([0, 1, 127, 200, 240], dtype=torch.uint8, device="cuda")
+    got = kd.checkpoint_read(codes, scales[:, None].repeat(1, 8).contiguous(), torch.float32)
+    one = np.empty(256)
+    for c in range(256):
+        e, m = c >> 3 & 15, c & 7
+        v = m * 2.0 ** -9 if e == 0 else (8 + m) * 2.0 ** (e - 10)
+        one[c] = np.nan if c & 127 == 127 else -v if c & 128 else v
+    for i, s in enumerate(scales.tolist()):
+        assert np.array_equal(to64(got[i]), one * 2.0 ** (s - 127), equal_nan=True)
+    bits = torch.arange(0, 0x7f80, device="cuda").to(torch.int16)
+    bits = torch.cat([bits, bits[:0x80]])  # (a whole number of blocks)
+    x = bits.view(torch.bfloat16).view(-1, 32)
+    for top in (0, 1):  # alone, and below a large value of the block
+        y = x.clone()
+        if top:
+            y[:, 0] = 2.0 ** 14
+        c = kd.checkpoint_write(y)
+        want, s = oo.checkpoint(to64(y))
+        assert np.array_equal(to64(c["scales"]), s)
+        assert np.array_equal(to64(kd.checkpoint_read(c["codes"], c["scales"], torch.float32)), want)
+
+
+# ------------------------------------------------------------- verification --
+def _draft(B, T, V, K, dtype, seed, ld=0, masked=0.0, err=0.7):
+    g = _gen(seed)
+    target = _logits(B * (T + 1), V, dtype, seed, V + ld)
+    if masked:
+        target[:, torch.rand(V, generator=g, device="cuda") < masked] = float("-inf")
+    target = target.unflatten(0, (B, T + 1))
+    t = target[:, :T].float()
+    d = (t + err * torch.randn(B, T, V, generator=g, device="cuda")).to(DT[dtype])
+    # (a tenth of the tokens are any: unlikely ones are rejected)
+    tokens = d.float().add(-torch.log(-torch.log(
+        torch.rand(B, T, V, generator=g, device="cuda").clamp(1e-9, 1 - 1e-7)))).argmax(2)
+    tokens = torch.where(torch.rand(B, T, generator=g, device="cuda") < 0.1,
+                         torch.randint(0, V, (B, T), generator=g, device="cuda"), tokens).int()
+    u = torch.rand(B, T + 1, generator=g, device="cuda")
+    if K:
+        e = d.float().topk(K, dim=2)
+        return target, tokens, u, dict(draft_idx=e.indices.int().contiguous(),
+                                       draft_logit=e.values.contiguous())
+    return target, tokens, u, dict(draft_logits=d)
+
+
+def _dense_q(draft, V, tau):
+    if "draft_logits" in draft:
+        d = to64(draft["draft_logits"])
+        return np.stack([[oo.softmax(r, tau) for r in s] for s in d]).reshape(*d.shape)
+    i, l = to64(draft["draft_idx"]), to64(draft["draft_logit"])
+    return np.stack([[oo.draft_distribution(i[b, t], l[b, t], V, tau) for t in range(i.shape[1])]
+                     for b in range(i.shape[0])]).reshape(i.shape[0], i.shape[1], V)
+
+
+def _check_verify(kd, target, tokens, u, draft, tau=1.0, lengths=None):
+    V = target.shape[2]
+    out = kd.verify_draft(target, tokens, u, lengths=lengths, tau=tau, accept_prob=True, **draft)
+    torch.cuda.synchronize()
+    q = _dense_q(draft, V, tau) if tokens.shape[1] else np.zeros((target.shape[0], 0, V))
+    want = oo.verify_draft(to64(target), to64(tokens), to64(u), q,
+                           None if lengths is None else to64(lengths), tau)
+    assert np.array_equal(to64(out["accepted"]), want[1])
+    assert np.array_equal(to64(out["tokens"]), want[0])
+    # computed in 64 bits, rounded once
+    assert np.all(np.abs(to64(out["accept_prob"]) - want[2]) <= E32 * want[2] + 1e-300)
+    return want
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+@pytest.mark.parametrize("B,T,V,K,ld,tau,masked", [
+    (1, 1, 2, 1, 0, 1.0, 0.0), (5, 3, 50, 50, 3, 1.0, 0.0), (7, 4, 2049, 20, 1, 0.7, 0.3),
+    (3, 5, 30011, 100, 5, 1.3, 0.0), (9, 2, 5000, 513, 0, 2.0, 0.9), (2, 2, 9000, 4096, 0, 1.0, 0.0),
+    (5, 3, 50, 0, 3, 1.0, 0.0), (7, 4, 2049, 0, 1, 0.7, 0.3), (3, 5, 30011, 0, 5, 1.3, 0.0),
+    (4, 20, 700, 0, 0, 1.0, 0.5)])
+def test_verify_draft(gpu_lib, B, T, V, K, ld, tau, masked, dtype):
+    print(f"[verify] {B} {T} {V} {K} ld+{ld} tau={tau} {masked} {dtype}", flush=True)
+    accepted = set()
+    for seed in (41, 42):
+        target, tokens, u, draft = _draft(B, T, V, K, dtype, seed, ld, masked)
+        accepted |= set(_check_verify(gpu_lib, target, tokens, u, draft, tau)[1].tolist())
+        n = torch.randint(-1, T + 3, (B,), generator=_gen(seed), device="cuda", dtype=torch.int32)
+        _check_verify(gpu_lib, target, tokens, u, draft, tau, n)
+    if B * T > 8:
+        assert len(accepted) > 1
+
+
+@pytest.mark.parametrize("K", [0, 30])
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+def test_verify_draft_edges(gpu_lib, dtype, K):
+    """Equal distributions, all or nothing masked, infinities and what is not a
+    number, tokens and indices outside the vocabulary, repeated indices, uniform
+    numbers at the ends."""
+    B, T, V = 8, 3, 3001
+    target, tokens, u, draft = _draft(B, T, V, K, dtype, 51, ld=7)
+    z = target.clone()
+    z[0] = float("-inf")                       # nothing left
+    z[1, 1] = torch.finfo(DT[dtype]).min       # all at the type's lowest value: uniform
+    z[2, 0, 5] = float("inf")
+    z[2, 1, [3, 9]] = float("inf")
+    z[3, :, ::2] = float("nan")
+    u[4] = 0.0
+    u[5] = 1.0 - 2.0 ** -24
+    tokens[6, 0] = V
+    tokens[7, 1] = -5
+    if K:
+        draft["draft_idx"][3, :, 4] = V + 3
+        draft["draft_idx"][4, :, 7] = draft["draft_idx"][4, :, 2]
+        draft["draft_idx"][5, :, :] = draft["draft_idx"][5, :, :1]
+        draft["draft_idx"][6, 1, 1] = -1
+        draft["draft_logit"][7] = float("-inf")
+        draft["draft_logit"][1, 2, 3] = float("nan")
+        draft["draft_logit"][1, 1, 3] = float("inf")
+    else:
+        draft["draft_logits"][7] = float("-inf")
+        draft["draft_logits"][5, 1] = z[5, 1]   # the draft is the target there
+        draft["draft_logits"][3, :, ::3] = float("nan")
+        draft["draft_logits"][1, 1, 3] = float("inf")
+    _check_verify(gpu_lib, z, tokens, u, draft)
+    _check_verify(gpu_lib, z, tokens, u, draft, tau=1e-30)  # greedy
+    # rejected although p = q everywhere (a uniform number of 1): from p
+    u[:] = 1.0
+    u[:, T] = 0.5
+    if not K:
+        draft["draft_logits"] = z[:, :T].contiguous()
+    out = gpu_lib.verify_draft(z, tokens, u, **draft)
+    assert int(out["accepted"][3]) == 0
+    assert 0 <= int(out["tokens"][3, 0]) < V
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+def test_verify_without_draft(gpu_lib, dtype):
+    """T = 0: a draw from the target alone; and B = 0."""
+    target, tokens, u, _ = _draft(6, 0, 4099, 0, dtype, 61, ld=1)
+    _check_verify(gpu_lib, target, tokens, u, {})
+    out = gpu_lib.verify_draft(target[:0], tokens[:0], u[:0])
+    assert out["tokens"].shape == (0, 1)
+
+
+def test_verify_draft_large_vocabulary(gpu_lib):
+    for K in (0, 100):
+        target, tokens, u, draft = _draft(2, 2, 1 << 20, K, "bf16", 71)
+        _check_verify(gpu_lib, target, tokens, u, draft)
+
+
+def test_verify_draft_follows_the_target(gpu_lib):
+    """Over many uniform numbers the token that comes out has the target's
+    probabilities, whatever the draft: counts within 6 standard deviations."""
+    kd, V, B = gpu_lib, 12, 200000
+    g = _gen(81)
+    z = torch.randn(1, 2, V, generator=g, device="cuda")
+    d = torch.randn(1, 1, V, generator=g, device="cuda")
+    p, q = torch.softmax(z[0, 0].double(), 0), torch.softmax(d[0, 0].double(), 0)
+    tokens = torch.multinomial(q.expand(1, V), B, replacement=True, generator=g).view(B, 1).int()
+    u = torch.rand(B, 2, generator=g, device="cuda")
+    for draft in (dict(draft_logits=d.expand(B, 1, V).contiguous()),
+                  dict(draft_idx=torch.arange(V, device="cuda").int().expand(B, 1, V).contiguous(),
+                       draft_logit=d.expand(B, 1, V).contiguous())):
+        out = kd.verify_draft(z.expand(B, 2, V).contiguous(), tokens, u, **draft)
+        n = torch.bincount(out["tokens"][:, 0].long(), minlength=V).double()
+        assert bool(((n - B * p).abs() <= 6 * (B * p * (1 - p)).sqrt()).all())
+
+
+# ------------------------------------------------------- streams and graphs --
+def test_graph_replays_and_streams(gpu_lib):
+    """Captured calls replay to the eager results between eager work, and a call on
+    another stream gives the same bits."""
+    kd, B, T, V, K = gpu_lib, 6, 3, 9001, 40
+    target, tokens, u, draft = _draft(B, T, V, K, "bf16", 91)
+    dense = _draft(B, T, V, 0, "bf16", 91)[3]
+    rows = target[:, 0].contiguous()
+    h = ki.make_hidden(33, 128, torch.bfloat16, "cuda", seed=5)
+
+    def calls():
+        c = kd.teacher_cache_write(rows, K, logprobs=True)
+        k = kd.checkpoint_write(h)
+        res = dict(kd.topk_entries(rows, K), **c)
+        res.update({"r_" + n: t for n, t in kd.teacher_cache_read(c["entries"], c["scale"]).items()})
+        res.update(k, back=kd.checkpoint_read(k["codes"], k["scales"], h.dtype))
+        res.update(kd.verify_draft(target, tokens, u, accept_prob=True, **draft))
+        res.update({"d_" + n: t for n, t in
+                    kd.verify_draft(target, tokens, u, accept_prob=True, **dense).items()})
+        return res
+    eager = calls()
+    torch.cuda.synchronize()
+    s = torch.cuda.Stream()
+    with torch.cuda.stream(s):
+        other = calls()
+    s.synchronize()
+    for n in eager:
+        assert torch.equal(other[n], eager[n]), n
+    g = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(g):
+        captured = calls()
+    for rep in range(3):
+        for t in captured.values():
+            t.zero_()
+        kd.topk_entries(rows * 0.5, K)
+        torch.cuda.synchronize()
+        g.replay()
+        torch.cuda.synchronize()
+        for n in eager:
+            assert torch.equal(captured[n], eager[n]), (rep, n)
+
+
+def test_bindings_refuse(gpu_lib):
+    """Shapes, dtypes, layouts and devices that the library could not check."""
+    kd = gpu_lib
+    x = _logits(4, 100, "bf16", 1)
+    bad = [lambda: kd.topk_entries(x.cpu(), 3), lambda: kd.topk_entries(x[0], 3),
+           lambda: kd.topk_entries(x.t(), 3), lambda: kd.topk_entries(x[:, ::2], 3),
+           lambda: kd.topk_entries(x[:1].expand(4, 100), 3),
+           lambda: kd.topk_entries(x, 3, out={"teacher_idx": torch.empty(4, 4, dtype=torch.int32,
+                                                                         device="cuda")}),
+           lambda: kd.topk_entries(x, 3, workspace=torch.empty(10, device="cuda")),
+           lambda: kd.teacher_cache_write(x, 3, out={"scale": torch.empty(4, 1, device="cuda")})]
+    c = kd.teacher_cache_write(x, 3)
+    bad += [lambda: kd.teacher_cache_read(c["entries"], c["scale"][:3]),
+            lambda: kd.teacher_cache_read(c["entries"].long(), c["scale"]),
+            lambda: kd.teacher_cache_read(c["entries"], c["scale"],
+                                          rows=torch.zeros(2, dtype=torch.int32, device="cuda")),
+            lambda: kd.teacher_cache_read(c["entries"], c["scale"], rows=torch.zeros(2, dtype=torch.int64)),
+            lambda: kd.teacher_cache_read(c["entries"][:, :2], c["scale"])]
+    h = torch.zeros(4, 64, device="cuda")
+    k = kd.checkpoint_write(h)
+    bad += [lambda: kd.checkpoint_write(h.t()), lambda: kd.checkpoint_write(h.cpu()),
+            lambda: kd.checkpoint_read(k["codes"], k["scales"][:, :1], torch.float32),
+            lambda: kd.checkpoint_read(k["codes"], k["scales"], torch.float32, out=h.bfloat16())]
+    target, tokens, u, draft = _draft(2, 3, 50, 5, "bf16", 2)
+    dense = _draft(2, 3, 50, 0, "bf16", 2)[3]
+    bad += [lambda: kd.verify_draft(target, tokens, u),
+            lambda: kd.verify_draft(target, tokens, u, **draft, **dense),
+            lambda: kd.verify_draft(target, tokens, u, draft_idx=draft["draft_idx"]),
+            lambda: kd.verify_draft(target, tokens, u[:, :3], **draft),
+            lambda: kd.verify_draft(target[:, :0], tokens[:, :0], u[:, :0], **draft),
+            lambda: kd.verify_draft(target[0], tokens, u, **draft),
+            lambda: kd.verify_draft(target.transpose(0, 1), tokens, u, **draft),
+            lambda: kd.verify_draft(target, tokens.long(), u, **draft),
+            lambda: kd.verify_draft(target, tokens, u, draft_logits=dense["draft_logits"].float()),
+            lambda: kd.verify_draft(target, tokens, u, lengths=torch.zeros(2, device="cuda"), **draft)]
+    for i, f in enumerate(bad):
+        with pytest.raises(ValueError):
+            f()
+            pytest.fail(f"call {i} was not refused")
+    with pytest.raises(TypeError):
+        kd.topk_entries(x.half(), 3)
+    with pytest.raises(kd.KdError):
+        kd.topk_entries(x, 101)
+    with pytest.raises(kd.KdError):
+        kd.verify_draft(target, tokens, u, tau=0.0, **draft)
