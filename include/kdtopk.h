@@ -472,6 +472,37 @@ kd_status kd_checkpoint_write(int64_t N, int64_t D, int32_t dtype, const void* h
 kd_status kd_checkpoint_read(int64_t N, int64_t D, int32_t dtype, const uint8_t* codes,
                              const uint8_t* scales, void* hidden, void* hip_stream);
 
+/*
+ * The loss's backward from such a checkpoint: kd_topk_kl_bwd with the hidden rows
+ * h^ that the codes stand for. The gradient is the loss's own at h^: log Z is
+ * formed again from h^ (a log Z of the exact rows would leave the
+ * probabilities of a confident token summing to something other than 1, and a
+ * gradient where there is none), in the same projection as the gradient, so the
+ * three contractions of kd_topk_kl_fwd_bwd run and no saved log Z is needed. With
+ * grad_loss = NULL and no per-token gradients the results are bitwise those of
+ * kd_topk_kl_fwd_bwd on the rows of kd_checkpoint_read.
+ *
+ *   codes, scales     [N, D], [N, D / 32] uint8   kd_checkpoint_write's; the
+ *                                     problem's dtype is that of W, grad_hidden and
+ *                                     the decoded rows. codes 16-byte aligned
+ *   the other arguments, the workspace and the errors as for kd_topk_kl_bwd
+ */
+kd_status kd_topk_kl_bwd_checkpoint(const kd_problem* p,
+                                    const uint8_t* codes,
+                                    const uint8_t* scales,
+                                    const void* W,
+                                    const int32_t* teacher_idx,
+                                    const float* teacher_logit,
+                                    const uint8_t* ignore,
+                                    const float* grad_loss,
+                                    const float* grad_loss_per_token,
+                                    void* grad_hidden,
+                                    float* grad_W,
+                                    int accumulate_grad_W,
+                                    void* workspace,
+                                    size_t workspace_bytes,
+                                    void* hip_stream);
+
 /* Sequences with drafted tokens. */
 typedef struct kd_draft {
   int64_t B;           /* sequences; 0 <= B <= 2^20                          */

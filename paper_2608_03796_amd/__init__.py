@@ -30,6 +30,7 @@ EXPORTED = ("kd_topk_kl_workspace_size", "kd_topk_kl_fwd_bwd", "kd_topk_kl_fwd_b
             "kd_abi_version", "kd_profile_enable", "kd_profile_read",
             "kd_topk_entries_workspace_size", "kd_topk_entries", "kd_teacher_cache_write",
             "kd_teacher_cache_read", "kd_checkpoint_write", "kd_checkpoint_read",
+            "kd_topk_kl_bwd_checkpoint",
             "kd_verify_draft_workspace_size", "kd_verify_draft")
 
 
@@ -102,6 +103,9 @@ def load_library(path: Optional[str] = None) -> ctypes.CDLL:
     lib.kd_profile_enable.restype = ctypes.c_int
     lib.kd_profile_read.argtypes = [ctypes.POINTER(KdKernelTime), ctypes.c_int]
     lib.kd_profile_read.restype = ctypes.c_int
+    lib.kd_topk_kl_bwd_checkpoint.argtypes = [ctypes.POINTER(KdProblem), vp, vp, vp, vp, vp, vp,
+                                              vp, vp, vp, vp, ctypes.c_int, vp, sz, vp]
+    lib.kd_topk_kl_bwd_checkpoint.restype = ctypes.c_int
     i32 = ctypes.c_int32
     rows, draft = ctypes.POINTER(KdRows), ctypes.POINTER(KdDraft)
     for name, argtypes in (
@@ -163,15 +167,16 @@ def alloc_workspace(N, D, V, K, chunk, tau, dtype, device):
     return torch.empty(n, dtype=torch.uint8, device=device)
 
 
-def _check_inputs(hidden, W, teacher_idx, teacher_logit, ignore):
+def _check_inputs(hidden, W, teacher_idx, teacher_logit, ignore, checkpoint=False):
     """Dtypes, shapes, devices and layouts of the inputs. The library takes
-    plain pointers, so every size it will index with is checked here."""
+    plain pointers, so every size it will index with is checked here. With
+    checkpoint, hidden is a checkpoint's codes and W gives the dtype."""
     import torch
     if hidden.device.type != "cuda":
         raise ValueError("tensors must be on a GPU")
     if hidden.dim() != 2 or W.dim() != 2:
         raise ValueError("hidden must be [N, D] and W [V, D]")
-    if W.dtype != hidden.dtype:
+    if W.dtype != hidden.dtype and not checkpoint:
         raise TypeError("hidden and W must share a dtype")
     for name, t, want in (("teacher_idx", teacher_idx, torch.int32),
                           ("teacher_logit", teacher_logit, torch.float32)):
@@ -195,7 +200,7 @@ def _check_inputs(hidden, W, teacher_idx, teacher_logit, ignore):
             raise ValueError("inputs must be contiguous")
         if t.device != hidden.device:
             raise ValueError("inputs must be on one device")
-    return N, D, W.shape[0], K, _dtype_code(hidden.dtype)
+    return N, D, W.shape[0], K, _dtype_code(W.dtype)
 
 
 def _check_tensor(name, t, shape, dtype, device):
@@ -504,7 +509,44 @@ def _autograd_functions():
             scale_grads(g, grad_hidden=gh, grad_hidden_out=gh_out, grad_W=gW, grad_W_out=gW_out)
             return gh_out, gW_out, None, None, None, None, None, None, None
 
-    return {"recompute": TopKKLLoss, "fused": TopKKLLossFused}
+    class TopKKLLossCheckpoint(torch.autograd.Function):
+        """Mean top-K KL loss as an autograd function that keeps its hidden
+        states in 8 bits: forward computes the loss from the exact ones and
+        writes their checkpoint; backward runs kd_topk_kl_bwd_checkpoint with the
+        upstream gradient."""
+
+        @staticmethod
+        def forward(ctx, hidden, W, teacher_idx, teacher_logit, tau, ignore, chunk,
+                    teacher_logprobs, workspace):
+            loss = fwd_bwd(hidden, W, teacher_idx, teacher_logit, tau=tau, ignore=ignore,
+                           chunk=chunk, grad_hidden=False, grad_W=False,
+                           teacher_logprobs=teacher_logprobs, workspace=workspace)["loss"]
+            if ctx.needs_input_grad[0] or ctx.needs_input_grad[1]:
+                c = checkpoint_write(hidden)
+                ctx.save_for_backward(c["codes"], c["scales"], W, teacher_idx, teacher_logit,
+                                      *([ignore] if ignore is not None else []))
+            ctx.cfg = (tau, chunk, teacher_logprobs, ignore is not None)
+            ctx.workspace = workspace
+            return loss
+
+        @staticmethod
+        def backward(ctx, grad_out):
+            tau, chunk, logprobs, has_ignore = ctx.cfg
+            saved = ctx.saved_tensors
+            codes, scales, W, idx, tl = saved[:5]
+            g = grad_out.detach().to(torch.float32).contiguous()
+            res = bwd_checkpoint(codes, scales, W, idx, tl, tau=tau,
+                                 ignore=saved[5] if has_ignore else None, chunk=chunk, grad_loss=g,
+                                 grad_hidden=ctx.needs_input_grad[0],
+                                 grad_W=ctx.needs_input_grad[1], teacher_logprobs=logprobs,
+                                 workspace=ctx.workspace)
+            gW = res.get("grad_W")
+            if gW is not None and gW.dtype != W.dtype:
+                gW = gW.to(W.dtype)
+            return res.get("grad_hidden"), gW, None, None, None, None, None, None, None
+
+    return {"recompute": TopKKLLoss, "fused": TopKKLLossFused,
+            "checkpoint": TopKKLLossCheckpoint}
 
 
 _TOPK_KL = None
@@ -512,7 +554,7 @@ _TOPK_KL = None
 
 def topk_kl_loss(hidden, W, teacher_idx, teacher_logit, tau: float = 1.0, ignore=None,
                  chunk: int = 4096, teacher_logprobs: bool = False, schedule: str = "fused",
-                 workspace=None):
+                 workspace=None, checkpoint: bool = False):
     """Differentiable mean top-K KL loss.
 
     schedule="fused": when hidden or W needs a gradient, the forward computes
@@ -530,12 +572,20 @@ def topk_kl_loss(hidden, W, teacher_idx, teacher_logit, tau: float = 1.0, ignore
     kd_topk_kl_fwd alone and which saves only log Z.
     schedule="recompute": Algorithm 1's schedule through the split entry
     points (forward saves log Z; backward recomputes the logits).
+    checkpoint=True (schedule="recompute" only): the hidden states are kept from
+    forward to backward in 8 bits (checkpoint_write: 1.03 bytes an element
+    instead of 2 or 4; the caller's own tensor may be freed), and the gradients
+    are those of the loss at the values held (bwd_checkpoint). The loss itself is
+    computed from the exact ones.
     workspace: a uint8 device tensor of at least workspace_size(...) bytes to
     reuse across calls (allocated per call when None)."""
     import torch
     global _TOPK_KL
     if schedule not in ("fused", "recompute"):
         raise ValueError("schedule must be 'fused' or 'recompute'")
+    if checkpoint and schedule != "recompute":
+        raise ValueError("checkpoint=True goes with schedule='recompute' (the fused schedule keeps "
+                         "gradients, not hidden states)")
     if not torch.is_grad_enabled():
         # no graph will be built: the loss alone (no gradient work; ignored
         # tokens left out)
@@ -544,7 +594,7 @@ def topk_kl_loss(hidden, W, teacher_idx, teacher_logit, tau: float = 1.0, ignore
                        teacher_logprobs=teacher_logprobs, workspace=workspace)["loss"]
     if _TOPK_KL is None:
         _TOPK_KL = _autograd_functions()
-    return _TOPK_KL[schedule].apply(hidden, W, teacher_idx, teacher_logit, float(tau), ignore,
+    return _TOPK_KL["checkpoint" if checkpoint else schedule].apply(hidden, W, teacher_idx, teacher_logit, float(tau), ignore,
                                     int(chunk), bool(teacher_logprobs), workspace)
 
 
@@ -761,6 +811,48 @@ def checkpoint_read(codes, scales, dtype, out=None):
     if rc != 0:
         raise KdError(rc, "kd_checkpoint_read")
     return hidden
+
+
+def bwd_checkpoint(codes, scales, W, teacher_idx, teacher_logit, tau: float = 1.0, ignore=None,
+                   chunk: int = 4096, grad_loss=None, grad_loss_per_token=None,
+                   grad_hidden: bool = True, grad_W: bool = True, grad_W_out=None,
+                   accumulate_grad_W: bool = False, workspace=None,
+                   teacher_logprobs: bool = False, grad_hidden_f32: bool = False):
+    """kd_topk_kl_bwd_checkpoint: gradients of the loss at the hidden states that
+    a checkpoint holds (checkpoint_write's codes and scales), in W's dtype. The
+    other arguments as for bwd, without a saved log-normaliser. Returns a dict
+    with 'grad_hidden' and 'grad_W' as requested."""
+    import torch
+    lib = load_library()
+    N, D, dev = _check_checkpoint(codes, scales)
+    _, _, V, K, dt = _check_inputs(codes, W, teacher_idx, teacher_logit, ignore, checkpoint=True)
+    if grad_loss is not None and grad_loss.numel() == 1:
+        _check_tensor("grad_loss", grad_loss, tuple(grad_loss.shape), torch.float32, dev)
+    elif grad_loss is not None:
+        raise ValueError("grad_loss must hold one value (the upstream gradient of the mean)")
+    if grad_loss_per_token is not None:
+        _check_tensor("grad_loss_per_token", grad_loss_per_token, (N,), torch.float32, dev)
+    res = {}
+    if grad_hidden:
+        res["grad_hidden"] = torch.empty(N, D, device=dev,
+                                         dtype=torch.float32 if grad_hidden_f32 else W.dtype)
+    if grad_W:
+        res["grad_W"] = grad_W_out if grad_W_out is not None else torch.empty(
+            V, D, dtype=torch.float32, device=dev)
+        _check_tensor("grad_W", res["grad_W"], (V, D), torch.float32, dev)
+    pr = problem(N, D, V, K, chunk, tau, dt, _flags(teacher_logprobs, grad_hidden_f32))
+    if workspace is None:
+        workspace = alloc_workspace(N, D, V, K, chunk, tau, dt, dev)
+    _check_workspace(workspace, dev)
+    with torch.cuda.device(dev):
+        rc = lib.kd_topk_kl_bwd_checkpoint(
+            ctypes.byref(pr), _ptr(codes), _ptr(scales), _ptr(W), _ptr(teacher_idx),
+            _ptr(teacher_logit), _ptr(ignore), _ptr(grad_loss), _ptr(grad_loss_per_token),
+            _ptr(res.get("grad_hidden")), _ptr(res.get("grad_W")), int(bool(accumulate_grad_W)),
+            _ptr(workspace), ctypes.c_size_t(workspace.numel()), _stream_handle(dev))
+    if rc != 0:
+        raise KdError(rc, "kd_topk_kl_bwd_checkpoint")
+    return res
 
 
 def verify_draft(target_logits, draft_tokens, uniform, draft_idx=None, draft_logit=None,

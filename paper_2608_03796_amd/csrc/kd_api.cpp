@@ -392,17 +392,20 @@ struct Call {
   void* ws;
   size_t ws_bytes;
   void* stream;
+  // the hidden rows as 8-bit checkpoints instead (hidden null)
+  const uint8_t *codes, *scales;
 };
 
 // Common checks: problem, pointers every mode needs, alignment, workspace
 // (unless the workspace is the library's own scratch).
 kd_status validate(const kd_problem* p, const Call& c, const Plan& pl, bool own_ws = false) {
   if (!own_ws && c.ws == nullptr) return KD_ERR_NULL_PTR;
-  if (p->N > 0 && (c.hidden == nullptr || c.W == nullptr || c.idx == nullptr ||
+  if (p->N > 0 && ((c.codes == nullptr ? c.hidden == nullptr : c.scales == nullptr) ||
+                   c.W == nullptr || c.idx == nullptr ||
                    c.tlogit == nullptr))
     return KD_ERR_NULL_PTR;
   if (c.accumulate != 0 && c.accumulate != 1) return KD_ERR_BAD_ARG;
-  if (!aligned16(c.hidden) || !aligned16(c.W) || !aligned16(c.grad_hidden) ||
+  if (!aligned16(c.hidden) || !aligned16(c.codes) || !aligned16(c.W) || !aligned16(c.grad_hidden) ||
       !aligned16(c.grad_W) || !aligned16(c.ws))
     return KD_ERR_UNSUPPORTED;
   if (!own_ws && c.ws_bytes < pl.total) return KD_ERR_WORKSPACE_TOO_SMALL;
@@ -463,9 +466,12 @@ kd_status enqueue(const kd_problem* p, const Plan& pl, const Call& c) {
     a.rows = rcount;
     a.inv_tau = 1.0f / p->temperature;
     a.W = c.W;
-    a.Hc = compact ? hcomp + g * pl.D * pl.eb
-                   : static_cast<const char*>(c.hidden) + row0 * pl.D * pl.eb;
+    a.Hc = compact || c.codes != nullptr
+               ? hcomp + g * pl.D * pl.eb
+               : static_cast<const char*>(c.hidden) + row0 * pl.D * pl.eb;
     a.hidden = c.hidden;
+    a.codes = c.codes;
+    a.scales = c.scales;
     a.tidx_in = c.idx;
     a.tidx = reinterpret_cast<int32_t*>(ws + pl.off_tidx) + o * pl.K;
     a.tlogit = c.tlogit;
@@ -568,7 +574,13 @@ kd_status enqueue(const kd_problem* p, const Plan& pl, const Call& c) {
     const int64_t row_first = row0 + rcount - group_tokens;
     if (want_dh && pl.dh_per_group && !dh(row_first, group_tokens, 0)) return KD_ERR_DEVICE;
     if (want_dw) {
-      tail.Hg = compact ? c.hidden : static_cast<const char*>(c.hidden) + row_first * pl.D * pl.eb;
+      const int64_t first = compact ? 0 : row_first * pl.D;
+      if (c.codes != nullptr) {
+        tail.codes = c.codes + first;
+        tail.scales = c.scales + first / 32;
+      } else {
+        tail.Hg = static_cast<const char*>(c.hidden) + first * pl.eb;
+      }
       tail.tokens = group_tokens;
       tail.Ht = ws + pl.off_ht;
       tail.rowscale = scaled ? fac : nullptr;
@@ -665,6 +677,32 @@ kd_status kd_topk_kl_bwd(const kd_problem* p, const void* hidden, const void* W,
   const Plan pl = make_plan(p);
   st = validate(p, c, pl);
   if (st != KD_OK) return st;
+  if (debug_index_check() && p->N > 0) {
+    st = kd_topk_kl_check_indices(p, teacher_idx, workspace, workspace_bytes, hip_stream);
+    if (st != KD_OK) return st;
+  }
+  return enqueue(p, pl, c);
+}
+
+kd_status kd_topk_kl_bwd_checkpoint(const kd_problem* p, const uint8_t* codes,
+                                    const uint8_t* scales, const void* W,
+                                    const int32_t* teacher_idx, const float* teacher_logit,
+                                    const uint8_t* ignore, const float* grad_loss,
+                                    const float* grad_loss_per_token, void* grad_hidden,
+                                    float* grad_W, int accumulate_grad_W, void* workspace,
+                                    size_t workspace_bytes, void* hip_stream) {
+  kd_status st = check_problem(p);
+  if (st != KD_OK) return st;
+  if (p->N > 0 && codes == nullptr) return KD_ERR_NULL_PTR;
+  // the schedule of the fused call (log Z of the decoded rows comes from the
+  // projection that gives the gradient), without its loss
+  const Call c{KD_MODE_FWD_BWD, nullptr, W, teacher_idx, teacher_logit, ignore, nullptr, nullptr,
+               nullptr, nullptr, grad_loss, grad_loss_per_token, grad_hidden, grad_W,
+               accumulate_grad_W, workspace, workspace_bytes, hip_stream, codes, scales};
+  const Plan pl = make_plan(p);
+  st = validate(p, c, pl);
+  if (st != KD_OK) return st;
+  if (grad_hidden == nullptr && grad_W == nullptr) return KD_OK;
   if (debug_index_check() && p->N > 0) {
     st = kd_topk_kl_check_indices(p, teacher_idx, workspace, workspace_bytes, hip_stream);
     if (st != KD_OK) return st;

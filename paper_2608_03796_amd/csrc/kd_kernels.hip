@@ -30,6 +30,7 @@
 // group is 6 launches, which were 11, and one more each with a mask, for K > 128
 // (prologue and buckets apart), where the projection's last tiles run as small ones
 // and where dW's last round is split (fixup).
+#include "kd_ckpt.h"
 #include "kd_device.h"
 #include "kd_f32.h"
 #include <type_traits>
@@ -78,6 +79,9 @@ __global__ void k_fill_f32(float* p, int64_t n, float v) {
 // exceeds 2^kRefGap falls back to its own max. The row's fallback flag is
 // cleared.
 //
+// With codes (8-bit checkpoints), the row's hidden values are decoded to
+// hcomp's row r, with a rowmap or without, and read there.
+//
 // LDS hash set of the row's valid indices (power-of-two slots, at least K):
 // size in ints for K entries
 __host__ __device__ constexpr int prologue_hash_slots(int K) {
@@ -117,7 +121,8 @@ struct PrologueArgs {
   float k2;
   float* rowR;
   int* rowFlag;
-  // with a rowmap
+  const uint8_t *codes, *scales;
+  // with a rowmap, hcomp also with codes
   char* hcomp;
   char* gH;
   int64_t gh_row_bytes;
@@ -176,7 +181,14 @@ __device__ __forceinline__ void prologue_row(const PrologueArgs& a, int r, char*
   }
   constexpr int VPT = 16 / (int)sizeof(T);  // elements per 16-byte piece
   const T* hrow = static_cast<const T*>(a.hidden) + t * a.D;
-  if (a.rowmap != nullptr) {
+  if (a.codes != nullptr) {
+    // (each lane reads back the pieces that it writes here)
+    T* dst = reinterpret_cast<T*>(a.hcomp) + (int64_t)r * a.D;
+#pragma unroll 4
+    for (int q = lane; q < a.D / VPT; q += 64)
+      reinterpret_cast<u32x4_t*>(dst)[q] = ckpt_load16<T>(a.codes, a.scales, t, a.D, q * VPT);
+    hrow = dst;
+  } else if (a.rowmap != nullptr) {
     const u32x4_t* src = reinterpret_cast<const u32x4_t*>(hrow);
     u32x4_t* dst = reinterpret_cast<u32x4_t*>(a.hcomp + (int64_t)r * a.D * sizeof(T));
 #pragma unroll 4
@@ -1585,9 +1597,12 @@ __device__ __forceinline__ void dh_reduce(int block, int blocks, const DhArgs& a
 // for tokens <= t < ldt (ldt a multiple of 64), so that the dW contraction
 // reads them with the tokens (its K dimension) contiguous. One 64 x 64 block
 // per workgroup, 16-byte loads and stores on both sides. With a rowmap,
-// column t is hidden row rowmap[t] (-1: zeros).
+// column t is hidden row rowmap[t] (-1: zeros). With codes, the rows are decoded
+// from 8-bit checkpoints.
 template <typename T>
-__device__ __forceinline__ void transpose_rows(int bt, int bd, const T* __restrict__ H, int tokens,
+__device__ __forceinline__ void transpose_rows(int bt, int bd, const T* __restrict__ H,
+                                               const uint8_t* __restrict__ codes,
+                                               const uint8_t* __restrict__ scales, int tokens,
                                                int D, T* __restrict__ Ht, int ldt,
                                                const float* __restrict__ rowscale,
                                                const int* __restrict__ rowmap) {
@@ -1602,7 +1617,9 @@ __device__ __forceinline__ void transpose_rows(int bt, int bd, const T* __restri
     const int row = q / (64 / VPT), c = (q % (64 / VPT)) * VPT;
     u32x4_t v = u32x4_t{0u, 0u, 0u, 0u};
     const int64_t src = t0 + row >= tokens ? -1 : rowmap != nullptr ? rowmap[t0 + row] : t0 + row;
-    if (src >= 0) v = *reinterpret_cast<const u32x4_t*>(H + src * D + d0 + c);
+    if (src >= 0)
+      v = codes != nullptr ? ckpt_load16<T>(codes, scales, src, D, d0 + c)
+                           : *reinterpret_cast<const u32x4_t*>(H + src * D + d0 + c);
     T e[VPT];
     __builtin_memcpy(e, &v, 16);
     // a per-token factor of the gradient rows is applied to the hidden rows
@@ -1632,6 +1649,7 @@ struct TailArgs {
   int nt, nr;
   // transpose
   const void* H;
+  const uint8_t *codes, *scales;
   int tokens, D;
   void* Ht;
   int ldt;
@@ -1650,8 +1668,8 @@ __global__ __launch_bounds__(256) void k_tail(TailArgs a) {
   const int b = blockIdx.x;
   if (b < a.nt) {
     const int td = a.D / 64;
-    transpose_rows<T>(b / td, b % td, static_cast<const T*>(a.H), a.tokens, a.D,
-                      static_cast<T*>(a.Ht), a.ldt, a.rowscale, a.rowmap);
+    transpose_rows<T>(b / td, b % td, static_cast<const T*>(a.H), a.codes, a.scales, a.tokens,
+                      a.D, static_cast<T*>(a.Ht), a.ldt, a.rowscale, a.rowmap);
   } else if (b < a.nt + a.nr) {
     dh_reduce<T, DTS>(b - a.nt, a.nr, a.dh);
   } else {
@@ -2143,6 +2161,8 @@ static int launch_chunk_impl(const KdChunkArgs& a, hipStream_t s) {
       p.rowCoefM = a.rowCoefM;
       p.rowL2 = a.rowL2;
       p.hidden = a.hidden;
+      p.codes = a.codes;
+      p.scales = a.scales;
       p.W = a.W;
       p.k2 = k2;
       p.rowR = a.one_projection ? a.rowR : nullptr;
@@ -2300,6 +2320,8 @@ static int launch_tail_impl(const KdTailArgs& a, hipStream_t s) {
   TailArgs t{};
   if (a.Ht != nullptr) {
     t.H = a.Hg;
+    t.codes = a.codes;
+    t.scales = a.scales;
     t.tokens = (int)a.tokens;
     t.Ht = a.Ht;
     t.ldt = (int)(((a.tokens + 63) / 64) * 64);

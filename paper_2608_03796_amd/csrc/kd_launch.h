@@ -45,6 +45,10 @@ struct KdChunkArgs {
   const void* Hc;           // the projection's token rows (hidden + row0 * D, or the
                             // workspace's copy of the rows' hidden rows with a rowmap)
   const void* hidden;       // full [N, D] (the reference logits read rows by token)
+  // hidden states as 8-bit checkpoints [N, D], [N, D / 32], or null: the prologue
+  // writes each prepared row's values to Hc (the workspace's rows) and reads
+  // them there; hidden is then not used
+  const uint8_t *codes, *scales;
   const int32_t* tidx_in;   // full [N, K] (the caller's)
   int32_t* tidx;            // [rows, K] the prologue's copy (repeats -1), read by the rest
   const float* tlogit;      // full [N, K] (prologue indexes with row0)
@@ -221,6 +225,7 @@ struct KdTailArgs {
   int dtype;
   int64_t D;
   const void* Hg;           // the group's hidden rows [tokens, D] (full with a rowmap)
+  const uint8_t *codes, *scales;  // or the same rows of 8-bit checkpoints
   int64_t tokens;
   void* Ht;                 // [D, tokens rounded up to 64], or null
   const float* rowscale;    // [tokens] factor of each dZ row (applied to the

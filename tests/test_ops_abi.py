@@ -144,3 +144,29 @@ def test_verify_pointers_rejected(lib):
     # no sequences: nothing launched
     assert _verify(lib, _draft(B=0), target=None, tokens=None, uniform=None, out=None,
                    accepted=None) == 0
+
+
+def test_bwd_checkpoint_rejected(lib):
+    def call(pr, codes=FAKE, scales=FAKE, W=FAKE, idx=FAKE, tl=FAKE, gh=FAKE, gw=FAKE, acc=0,
+             ws=FAKE, n=BIG):
+        return lib.kd_topk_kl_bwd_checkpoint(
+            None if pr is None else ctypes.byref(pr), _v(codes), _v(scales), _v(W), _v(idx), _v(tl),
+            None, None, None, _v(gh), _v(gw), acc, _v(ws), ctypes.c_size_t(n), None)
+    pr = kd.problem(256, 256, 4096, 16, 64, 1.0, kd.KD_BF16)
+    assert call(None) == 1
+    for kw in (dict(codes=None), dict(scales=None), dict(W=None), dict(idx=None), dict(tl=None),
+               dict(ws=None)):
+        assert call(pr, **kw) == 1
+    for kw in (dict(codes=FAKE + 8), dict(W=FAKE + 8), dict(gh=FAKE + 8), dict(gw=FAKE + 8),
+               dict(ws=FAKE + 8)):
+        assert call(pr, **kw) == 4
+    assert call(pr, acc=2) == 3
+    need = ctypes.c_size_t(0)
+    assert lib.kd_topk_kl_workspace_size(ctypes.byref(pr), ctypes.byref(need)) == 0
+    assert call(pr, n=need.value - 1) == 5
+    for kw, code in ((dict(tau=0.0), 3), (dict(chunk=0), 3), (dict(D=96), 4), (dict(K=0), 2)):
+        a = dict(N=256, D=256, V=4096, K=16, chunk=64, tau=1.0, dtype=kd.KD_BF16)
+        a.update(kw)
+        assert call(kd.problem(**a)) == code
+    # no gradient asked for: nothing launched
+    assert call(pr, gh=None, gw=None) == 0
