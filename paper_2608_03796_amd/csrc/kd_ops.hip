@@ -61,13 +61,15 @@ struct Row {
       for (int u = 0; u < U; ++u) x[u] = at(e0 + (64 * u + lane) * VPT);
     }
   }
-  // element i of a vector; what is not a number counts as -inf
-  static __device__ __forceinline__ float elt(u32x4_t x, int i) {
+  // element i of a vector
+  static __device__ __forceinline__ float raw(u32x4_t x, int i) {
     uint32_t b;
     if constexpr (sizeof(T) == 2) b = i & 1 ? x[i / 2] & 0xffff0000u : x[i / 2] << 16;
     else b = x[i];
-    return fmaxf(__builtin_bit_cast(float, b), -INFINITY);
+    return __builtin_bit_cast(float, b);
   }
+  // the same; what is not a number counts as -inf
+  static __device__ __forceinline__ float elt(u32x4_t x, int i) { return fmaxf(raw(x, i), -INFINITY); }
   __device__ __forceinline__ float one(int v) const {
     return fmaxf((float)p[v], -INFINITY);
   }
@@ -138,19 +140,22 @@ __global__ __launch_bounds__(256) void k_row_groups(const T* __restrict__ logits
   }
 }
 
-// Second pass, a workgroup per row. At least K groups have a maximum of at least
-// the K-th largest group maximum, so the K largest elements are among those that
-// reach it, and these lie in the groups whose maximum does: about K groups of
-// 64 columns are read again instead of the row. The bound is searched in the 16
-// leading bits of the maxima (bf16's precision, no higher than the K-th): for
-// V = 131072 and K = 100 there are about 105 such elements. They are sorted by
-// (value, lowest index first), the order of the result, so which thread collected
-// which does not matter. Where more elements reach the bound than fit (many equal
-// values, or V below about 64 K), the K-th largest is found exactly by counting
-// digits over those groups.
-constexpr int kSelThreads = 256;
-constexpr int kSelWaves = kSelThreads / 64;
+// Second pass, a workgroup of NT threads per row. At least K groups have a maximum
+// of at least the K-th largest group maximum, so the K largest elements are among
+// those that reach it, and these lie in the groups whose maximum does: about K
+// groups of 64 columns are read again instead of the row. The bound is searched in
+// the 16 leading bits of the maxima (bf16's precision, no higher than the K-th),
+// four of them a thread (each the largest of several groups where the row has
+// more than 4 NT): for V = 131072 and K = 100 there are about 105 elements
+// that reach it. They are sorted by (value, lowest index first), the order of the
+// result, so which thread collected which does not matter. Where more elements
+// reach the bound than fit (many equal values, or V below about 64 K), the
+// K-th largest is found exactly by counting digits over those groups.
+//
+// The pass is latency-bound (a few dependent reads and barriers per row), so what
+// counts is rows in flight, and for few rows the time of one.
 constexpr int kHistBins = 2048;
+constexpr int kBoundKeys = 4;
 
 __host__ __device__ constexpr int select_cap(int K) {
   int c = 1024;
@@ -161,27 +166,28 @@ __host__ __device__ constexpr int select_cap(int K) {
 // list of groups
 __host__ __device__ constexpr int select_lds_keys(int G, int K) {
   const int a = 4 * G, b = 8 * select_cap(K);
-  return (a > b ? a : b) + 15 & ~15;
+  return ((a > b ? a : b) + 15) & ~15;
 }
 __host__ __device__ constexpr int select_lds(int G, int K) {
   return select_lds_keys(G, K) + 2 * G;
 }
 
+template <int NT>
 struct SelectShared {
-  int count[2][kSelWaves];
-  int scan[kSelWaves];
+  int reach[10][4];  // groups that reach each bound of a step of the search
+  int scan[NT / 64];
   int found, before;
   int n, nlist;
-  uint32_t lo, hi;
-  float top, logs;
-  uint32_t wlo[kSelWaves], whi[kSelWaves];
+  float logs;
+  uint32_t wlo[NT / 64], whi[NT / 64];
 };
 
 // The bin of `want` (1 = the first) in the bins' order (descending or ascending),
 // and the count of the bins before it; hist holds nb = 2048 or 1024 bins.
-__device__ __forceinline__ void find_bin(SelectShared& s, const int* hist, int nb, bool descending,
-                                         int want, int& bin, int& before) {
-  const int per = nb / kSelThreads, tid = threadIdx.x;
+template <int NT>
+__device__ __forceinline__ void find_bin(SelectShared<NT>& s, const int* hist, int nb,
+                                         bool descending, int want, int& bin, int& before) {
+  const int per = nb / NT, tid = threadIdx.x;
   int sum = 0;
   for (int i = 0; i < per; ++i) {
     const int b = tid * per + i;
@@ -209,23 +215,31 @@ __device__ __forceinline__ void find_bin(SelectShared& s, const int* hist, int n
   __syncthreads();
 }
 
-// f(key, v) for every element of the listed groups; all lanes call it, `in` tells
-// whether there is an element
-template <typename T, typename F>
-__device__ __forceinline__ void listed_elements(const Row<T>& row, const uint16_t* list, int n,
-                                                F&& f) {
+// lanes of the wave below this one whose bit is set
+__device__ __forceinline__ int lanes_below(uint64_t b) {
+  return __builtin_amdgcn_mbcnt_hi((uint32_t)(b >> 32), __builtin_amdgcn_mbcnt_lo((uint32_t)b, 0));
+}
+
+// f(in, key, v) for the VPT elements of a vector of each listed group, by all
+// lanes; `in` tells whether there is an element
+template <typename T, int NT, typename F>
+__device__ __forceinline__ void listed_vectors(const Row<T>& row, const uint16_t* list, int n,
+                                               F&& f) {
   constexpr int GL = Row<T>::GL, VPT = Row<T>::VPT, GPW = 64 / GL;
   const int lane = threadIdx.x & 63, wave = wave_id();
-  for (int l0 = wave * GPW; l0 < n; l0 += kSelWaves * GPW) {
+  for (int l0 = wave * GPW; l0 < n; l0 += NT / 64 * GPW) {
     const int l = l0 + lane / GL;
     const bool have = l < n;
     const int e = have ? (int)list[l] * kGroupCols + (lane & (GL - 1)) * VPT : 0;
     const u32x4_t x = row.at(e);
+    bool in[VPT];
+    uint32_t k[VPT];
 #pragma unroll
     for (int i = 0; i < VPT; ++i) {
-      const int v = e + i - row.shift;
-      f(have && (unsigned)v < (unsigned)row.V, order_key(Row<T>::elt(x, i)), v);
+      in[i] = have && (unsigned)(e + i - row.shift) < (unsigned)row.V;
+      k[i] = order_key(Row<T>::elt(x, i));
     }
+    f(in, k, e - row.shift);
   }
 }
 
@@ -240,10 +254,11 @@ struct SelectArgs {
   float* scale;
 };
 
-template <typename T>
-__global__ __launch_bounds__(kSelThreads) void k_row_select(SelectArgs a) {
+template <typename T, int NT>
+__global__ __launch_bounds__(NT) void k_row_select(SelectArgs a) {
   extern __shared__ __align__(16) char lds[];
-  __shared__ SelectShared s;
+  __shared__ SelectShared<NT> s;
+  constexpr int VPT = Row<T>::VPT;
   const int tid = threadIdx.x, lane = tid & 63, wave = wave_id();
   const int K = a.K, G = a.G, cap = select_cap(K);
   const int64_t r = blockIdx.x;
@@ -254,14 +269,23 @@ __global__ __launch_bounds__(kSelThreads) void k_row_select(SelectArgs a) {
   uint16_t* list = reinterpret_cast<uint16_t*>(lds + select_lds_keys(G, K));
 
   // group maxima, their range, and log of the row's sum of exp
+  uint32_t key[kBoundKeys] = {};  // 0: below every value's
   uint32_t lo = 0xffffffffu, hi = 0;
   const float* gm = a.gmax + r * G;
-  for (int i = tid; i < G; i += kSelThreads) {
-    const uint32_t k = order_key(gm[i]);
-    keys[i] = k;
-    lo = min(lo, k);
-    hi = max(hi, k);
+  for (int i0 = tid; i0 < G; i0 += kBoundKeys * NT) {
+#pragma unroll
+    for (int j = 0; j < kBoundKeys; ++j) {
+      const int i = i0 + j * NT;
+      if (i < G) {
+        const uint32_t k = order_key(gm[i]);
+        keys[i] = k;
+        key[j] = max(key[j], k);
+        lo = min(lo, k);
+      }
+    }
   }
+#pragma unroll
+  for (int j = 0; j < kBoundKeys; ++j) hi = max(hi, key[j]);
 #pragma unroll
   for (int o = 32; o >= 1; o >>= 1) {
     lo = min(lo, (uint32_t)__shfl_xor((int)lo, o));
@@ -272,7 +296,8 @@ __global__ __launch_bounds__(kSelThreads) void k_row_select(SelectArgs a) {
     s.whi[wave] = hi;
   }
   if (tid == 0) s.n = s.nlist = 0;
-  if (a.logprobs && wave == kSelWaves - 1) {
+  if (tid < 40) s.reach[tid / 4][tid & 3] = 0;
+  if (a.logprobs && wave == NT / 64 - 1) {
     const float *pm = a.pm + r * a.nseg, *ps = a.ps + r * a.nseg;
     float m = -INFINITY, t = 0.f;
     for (int i = lane; i < a.nseg; i += 64) m = fmaxf(m, pm[i]);
@@ -283,51 +308,82 @@ __global__ __launch_bounds__(kSelThreads) void k_row_select(SelectArgs a) {
     if (lane == 0) s.logs = m != -INFINITY ? logf(t) : 0.f;
   }
   __syncthreads();
-  lo = min(min(s.wlo[0], s.wlo[1]), min(s.wlo[2], s.wlo[3])) >> 16;
-  hi = (max(max(s.whi[0], s.whi[1]), max(s.whi[2], s.whi[3])) >> 16) + 1;
-  // the largest 16-bit prefix that K group maxima reach (0 with fewer groups)
-  if (K > G) lo = hi = 0;
+  lo = s.wlo[lane % (NT / 64)];
+  hi = s.whi[lane % (NT / 64)];
+#pragma unroll
+  for (int o = NT / 128; o >= 1; o >>= 1) {
+    lo = min(lo, (uint32_t)__shfl_xor((int)lo, o));
+    hi = max(hi, (uint32_t)__shfl_xor((int)hi, o));
+  }
+  lo = (uint32_t)__builtin_amdgcn_readfirstlane((int)lo) >> 16;
+  hi = ((uint32_t)__builtin_amdgcn_readfirstlane((int)hi) >> 16) + 1;
+  // the largest 16-bit prefix that K of the maxima reach, or 0 where there are
+  // fewer of them; lo always is reached by K, hi never. A step tries three bounds
+  // and leaves a quarter of the range: at most 9 steps
+  if (K > min(G, kBoundKeys * NT)) lo = hi = 0;
   for (int it = 0; hi - lo > 1; ++it) {
-    const uint32_t mid = (lo + hi) / 2;
-    int c = 0;
-    for (int i0 = 0; i0 < G; i0 += kSelThreads) {
-      const int i = i0 + tid;
-      c += __popcll(__builtin_amdgcn_ballot_w64(i < G && keys[i < G ? i : 0] >> 16 >= mid));
+    const uint32_t d = hi - lo;
+    const uint32_t m1 = lo + (d + 3) / 4, m2 = lo + (d + 1) / 2, m3 = lo + (3 * d + 3) / 4;
+    int c1 = 0, c2 = 0, c3 = 0;
+#pragma unroll
+    for (int j = 0; j < kBoundKeys; ++j) {
+      const uint32_t k = key[j] >> 16;
+      c1 += __popcll(__builtin_amdgcn_ballot_w64(k >= m1));
+      c2 += __popcll(__builtin_amdgcn_ballot_w64(k >= m2));
+      c3 += __popcll(__builtin_amdgcn_ballot_w64(k >= m3));
     }
-    if (lane == 0) s.count[it & 1][wave] = c;
+    if (lane < 3) atomicAdd(&s.reach[it][lane], lane == 0 ? c1 : lane == 1 ? c2 : c3);
     __syncthreads();
-    c = (s.count[it & 1][0] + s.count[it & 1][1]) + (s.count[it & 1][2] + s.count[it & 1][3]);
-    if (c >= K) lo = mid;
-    else hi = mid;
+    c1 = s.reach[it][0];
+    c2 = s.reach[it][1];
+    c3 = s.reach[it][2];
+    // (bounds at hi or above are reached by fewer than K)
+    if (m3 < hi && c3 >= K) lo = m3;
+    else if (c2 >= K) lo = m2, hi = min(hi, m3);
+    else if (c1 >= K) lo = m1, hi = m2;
+    else hi = m1;
   }
   const uint32_t t = lo << 16;
-  for (int i0 = 0; i0 < G; i0 += kSelThreads) {
+  // the groups that reach the bound, one reservation per wave
+  int mine = 0;
+  for (int i0 = 0; i0 < G; i0 += NT) {
+    const int i = i0 + tid;
+    mine += __popcll(__builtin_amdgcn_ballot_w64(i < G && keys[i < G ? i : 0] >= t));
+  }
+  int at = 0;
+  if (lane == 0 && mine > 0) at = atomicAdd(&s.nlist, mine);
+  at = __builtin_amdgcn_readfirstlane(at);
+  for (int i0 = 0; i0 < G; i0 += NT) {
     const int i = i0 + tid;
     const bool q = i < G && keys[i < G ? i : 0] >= t;
     const uint64_t b = __builtin_amdgcn_ballot_w64(q);
-    if (b == 0) continue;
-    int at = 0;
-    if (lane == 0) at = atomicAdd(&s.nlist, __popcll(b));
-    at = __builtin_amdgcn_readfirstlane(at);
-    if (q) list[at + __builtin_amdgcn_mbcnt_hi((uint32_t)(b >> 32),
-                                               __builtin_amdgcn_mbcnt_lo((uint32_t)b, 0))] =
-        (uint16_t)i;
+    if (q) list[at + lanes_below(b)] = (uint16_t)i;
+    at += __popcll(b);
   }
   __syncthreads();
   const int nlist = s.nlist;
 
   // elements with key > kth, or = kth and an index up to vcut, as candidates
   auto gather = [&](uint32_t kth, int vcut) {
-    listed_elements<T>(row, list, nlist, [&](bool in, uint32_t k, int v) {
-      const bool q = in && (k > kth || (k == kth && v <= vcut));
-      const uint64_t b = __builtin_amdgcn_ballot_w64(q);
-      if (b == 0) return;
-      int at = 0;
-      if (lane == 0) at = atomicAdd(&s.n, __popcll(b));
-      at = __builtin_amdgcn_readfirstlane(at) +
-           __builtin_amdgcn_mbcnt_hi((uint32_t)(b >> 32),
-                                     __builtin_amdgcn_mbcnt_lo((uint32_t)b, 0));
-      if (q && at < cap) cand[at] = (uint64_t)k << 32 | (0xffffffffu - (uint32_t)v);
+    listed_vectors<T, NT>(row, list, nlist, [&](const bool* in, const uint32_t* k, int v) {
+      uint64_t b[VPT];
+      int total = 0;
+#pragma unroll
+      for (int i = 0; i < VPT; ++i) {
+        b[i] = __builtin_amdgcn_ballot_w64(in[i] && (k[i] > kth || (k[i] == kth && v + i <= vcut)));
+        total += __popcll(b[i]);
+      }
+      if (total == 0) return;
+      int to = 0;
+      if (lane == 0) to = atomicAdd(&s.n, total);
+      to = __builtin_amdgcn_readfirstlane(to);
+#pragma unroll
+      for (int i = 0; i < VPT; ++i) {
+        const int o = to + lanes_below(b[i]);
+        if ((b[i] >> lane & 1) != 0 && o < cap)
+          cand[o] = (uint64_t)k[i] << 32 | (0xffffffffu - (uint32_t)(v + i));
+        to += __popcll(b[i]);
+      }
     });
     __syncthreads();
   };
@@ -343,30 +399,34 @@ __global__ __launch_bounds__(kSelThreads) void k_row_select(SelectArgs a) {
     for (int d = 0; d < 3; ++d) {
       const int sh = shifts[d], nb = d == 2 ? 1024 : kHistBins;
       const uint32_t mask = d == 0 ? 0u : d == 1 ? 0xffe00000u : 0xfffffc00u;
-      for (int i = tid; i < nb; i += kSelThreads) hist[i] = 0;
+      for (int i = tid; i < nb; i += NT) hist[i] = 0;
       __syncthreads();
-      listed_elements<T>(row, list, nlist, [&](bool in, uint32_t k, int) {
-        if (in && (k & mask) == kth) atomicAdd(&hist[(k >> sh) & (nb - 1)], 1);
+      listed_vectors<T, NT>(row, list, nlist, [&](const bool* in, const uint32_t* k, int) {
+#pragma unroll
+        for (int i = 0; i < VPT; ++i)
+          if (in[i] && (k[i] & mask) == kth) atomicAdd(&hist[(k[i] >> sh) & (nb - 1)], 1);
       });
       __syncthreads();
       int bin, before;
-      find_bin(s, hist, nb, true, want, bin, before);
+      find_bin<NT>(s, hist, nb, true, want, bin, before);
       kth |= (uint32_t)bin << sh;
       want -= before;
     }
     int vcut = 0;
 #pragma unroll
     for (int d = 0; d < 2; ++d) {
-      for (int i = tid; i < 1024; i += kSelThreads) hist[i] = 0;
+      for (int i = tid; i < 1024; i += NT) hist[i] = 0;
       __syncthreads();
       const int first = vcut;
-      listed_elements<T>(row, list, nlist, [&](bool in, uint32_t k, int v) {
-        if (in && k == kth && (d == 0 || v >> 10 == first >> 10))
-          atomicAdd(&hist[d == 0 ? v >> 10 : v & 1023], 1);
+      listed_vectors<T, NT>(row, list, nlist, [&](const bool* in, const uint32_t* k, int v) {
+#pragma unroll
+        for (int i = 0; i < VPT; ++i)
+          if (in[i] && k[i] == kth && (d == 0 || (v + i) >> 10 == first >> 10))
+            atomicAdd(&hist[d == 0 ? (v + i) >> 10 : (v + i) & 1023], 1);
       });
       __syncthreads();
       int bin, before;
-      find_bin(s, hist, 1024, false, want, bin, before);
+      find_bin<NT>(s, hist, 1024, false, want, bin, before);
       vcut |= d == 0 ? bin << 10 : bin;
       want -= before;
     }
@@ -375,21 +435,27 @@ __global__ __launch_bounds__(kSelThreads) void k_row_select(SelectArgs a) {
     gather(kth, vcut);
     n = s.n;
   }
-  // sorted, largest first
-  if (n <= kSelThreads) {
-    const uint64_t c = tid < n ? cand[tid] : 0;
+  // sorted, largest first: each candidate's rank among all of them, by as many
+  // lanes as there are for it; or, when there are more than threads, bitonic
+  if (n <= NT) {
+    int per = NT, each = 1;  // places of candidates, lanes of each
+    while (per / 2 >= n && each < 64) per /= 2, each *= 2;
+    const int j = tid / each, sub = tid & (each - 1);
+    const uint64_t c = j < n ? cand[j] : 0;
     int rank = 0;
-    for (int i = 0; i < n; ++i) rank += cand[i] > c;
+#pragma unroll 4
+    for (int i = sub; i < n; i += each) rank += cand[i] > c;
+    for (int o = each / 2; o >= 1; o >>= 1) rank += __shfl_xor(rank, o);
     __syncthreads();
-    if (tid < n) cand[rank] = c;
+    if (j < n && sub == 0) cand[rank] = c;
   } else {
-    int P = 2 * kSelThreads;
+    int P = 2 * NT;
     while (P < n) P *= 2;
-    for (int i = n + tid; i < P; i += kSelThreads) cand[i] = 0;
+    for (int i = n + tid; i < P; i += NT) cand[i] = 0;
     for (int size = 2; size <= P; size *= 2)
       for (int st = size / 2; st > 0; st /= 2) {
         __syncthreads();
-        for (int i = tid; i < P / 2; i += kSelThreads) {
+        for (int i = tid; i < P / 2; i += NT) {
           const int x = 2 * i - (i & (st - 1)), y = x + st;
           const uint64_t p = cand[x], q = cand[y];
           if ((p < q) == ((x & size) == 0)) {
@@ -404,7 +470,7 @@ __global__ __launch_bounds__(kSelThreads) void k_row_select(SelectArgs a) {
   const float z0 = key_value((uint32_t)(cand[0] >> 32));
   const float logs = a.logprobs ? s.logs : 0.f;
   if (a.value != nullptr) {
-    for (int k = tid; k < K; k += kSelThreads) {
+    for (int k = tid; k < K; k += NT) {
       const uint64_t c = cand[k];
       const float z = key_value((uint32_t)(c >> 32));
       const int64_t o = r * K + k;
@@ -434,7 +500,7 @@ __global__ __launch_bounds__(kSelThreads) void k_row_select(SelectArgs a) {
     const float low = fminf(key_value((uint32_t)(cand[kept - 1] >> 32)), 3.402823466e38f);
     step = (float)((dtop - (double)low) / kCacheCodeMax);
   }
-  for (int k = tid; k < K; k += kSelThreads) {
+  for (int k = tid; k < K; k += NT) {
     const uint64_t c = cand[k];
     const uint32_t v = 0xffffffffu - (uint32_t)c;
     uint32_t code = kCacheNone;
@@ -594,6 +660,49 @@ __device__ __forceinline__ double weight(float z, float m, double c) {
   if (z == m) return m == -INFINITY ? 0.0 : 1.0;
   return exp2_64(((double)z - (double)m) * c);
 }
+// Weights below one m, for passes over whole rows: 2^(y / 16) with y = 16 c (z - m)
+// by a table of 2^(i / 16) in LDS and the series of degree 5 for the rest of up to
+// half a sixteenth (the next term is below 2^-42 of the result). 11 fp64 operations
+// where exp2_64 with its difference, comparison and sum takes 23. z is held above
+// m - 990 / c, where weights no longer count (2^-990; -inf and what is not a number
+// end there too), which fp32 can tell from m where `fast`; elsewhere (infinities,
+// extreme tau) weight() serves.
+struct Weights {
+  double c, c16, mc16;
+  float m, floor;
+  bool fast;
+  const double* tab;
+  __device__ __forceinline__ Weights(float m_, double c_, const double* t) : c(c_), m(m_), tab(t) {
+    const double reach = 990.0 / c, big = fabs((double)m);
+    fast = reach > big * (1.0 / 65536) && reach < 1e37 && big < 1e37;
+    floor = (float)((double)m - reach);
+    c16 = 16.0 * c;
+    mc16 = -(double)m * c16;
+  }
+  __device__ __forceinline__ double quick(float z) const {
+    const double y = fma((double)fmaxf(z, floor), c16, mc16);
+    const double t = y + 0x1.8p52;  // the nearest whole number in the low bits
+    const double g = y - (t - 0x1.8p52);
+    const int n = (int)(uint32_t)__builtin_bit_cast(uint64_t, t);
+    // (ln 2 / 16)^k / k!
+    double p = fma(g, 1.271587195055813162e-9, 1.467610032291942926e-7);
+    p = fma(p, g, 1.355080777949745605e-5);
+    p = fma(p, g, 9.383847928089871575e-4);
+    p = fma(p, g, 4.332169878499658184e-2);
+    p = fma(p, g, 1.0);
+    const uint64_t e = __builtin_bit_cast(uint64_t, tab[n & 15]) +
+                       ((uint64_t)(uint32_t)((n >> 4) << 20) << 32);
+    return p * __builtin_bit_cast(double, e);
+  }
+  __device__ __forceinline__ double exact(float z) const { return weight(z, m, c); }
+};
+constexpr int kTab = 16;
+__device__ const double kRoots[kTab] = {
+    1.0, 1.0442737824274138403, 1.0905077326652576592, 1.1387886347566916537,
+    1.1892071150027210667, 1.2418578120734840486, 1.2968395546510096659, 1.3542555469368927283,
+    1.4142135623730950488, 1.4768261459394993114, 1.5422108254079408236, 1.6104903319492543082,
+    1.6817928305074290861, 1.7562521603732994831, 1.8340080864093424635, 1.9152065613971472939};
+
 __device__ __forceinline__ double wave_sum64(double x) {
 #pragma unroll
   for (int o = 32; o >= 1; o >>= 1) x += __shfl_xor(x, o);
@@ -635,10 +744,12 @@ __device__ __forceinline__ int64_t draft_row(const VerifyArgs& a, int b, int t) 
 }
 
 // Largest logit and sum of weights of each segment of the rows in question (the
-// target's, then the draft's): the pass that reads the logits. About 20 fp64
-// operations an element: at bf16 these take nearly as long as the read.
+// target's, then the draft's): the pass that reads the logits.
 template <typename T>
 __global__ __launch_bounds__(256) void k_seg_sums(VerifyArgs a, int waves) {
+  __shared__ double tab[kTab];
+  if (threadIdx.x < kTab) tab[threadIdx.x] = kRoots[threadIdx.x];
+  __syncthreads();
   const int w = blockIdx.x * 4 + wave_id();
   if (w >= waves) return;
   const int r = w / a.nseg, seg = w - r * a.nseg;
@@ -660,10 +771,22 @@ __global__ __launch_bounds__(256) void k_seg_sums(VerifyArgs a, int waves) {
   m = wave_max(m);
   double s = 0.0;
   if (m != -INFINITY) {
+    const Weights q(m, a.c, tab);
+    if (q.fast) {
+      double h = 0.0;
 #pragma unroll
-    for (int u = 0; u < U; ++u) {
+      for (int u = 0; u < U; ++u) {
 #pragma unroll
-      for (int i = 0; i < VPT; ++i) s += weight(Row<T>::elt(x[u], i), m, a.c);
+        for (int i = 0; i < VPT; i += 2) {
+          s += q.quick(Row<T>::raw(x[u], i));
+          h += q.quick(Row<T>::raw(x[u], i + 1));
+        }
+      }
+      s += h;
+    } else {
+#pragma unroll
+      for (int u = 0; u < U; ++u)
+        for (int i = 0; i < VPT; ++i) s += q.exact(Row<T>::elt(x[u], i));
     }
   }
   s = wave_sum64(s);
@@ -821,17 +944,26 @@ __global__ __launch_bounds__(kVerThreads) void k_accept(VerifyArgs a) {
   __shared__ VerifyShared sh;
   const int b = blockIdx.x, tid = threadIdx.x, lane = tid & 63, wave = wave_id();
   const int n = drafted(a, b);
+  // (S, M) of the target's row at each place; the entries' arrays behind them
+  double* rowS = reinterpret_cast<double*>(lds);
+  double *em = rowS + a.T + 1, *eq = em + a.K;
+  float* rowM = reinterpret_cast<float*>(eq + a.K);
   if (tid == 0) sh.first = n;
   __syncthreads();
   if (a.prob != nullptr)
     for (int t = n + tid; t < a.T; t += kVerThreads) a.prob[draft_row(a, b, t)] = 0.f;
-  for (int t = wave; t < n; t += kVerWaves) {
+  for (int t = wave; t <= n; t += kVerWaves) {
     const int64_t rt = target_row(a, b, t), rd = draft_row(a, b, t);
-    const int d = a.tokens[rd];
-    const bool known = (unsigned)d < (unsigned)a.V;
     float M;
     double S;
     merge_row(a, rt, M, S);
+    if (lane == 0) {
+      rowM[t] = M;
+      rowS[t] = S;
+    }
+    if (t == n) break;
+    const int d = a.tokens[rd];
+    const bool known = (unsigned)d < (unsigned)a.V;
     const Row<T> row(a.target, rt * a.ld_t, a.V);
     const double p = known && S > 0.0 ? weight(row.one(d), M, a.c) / S : 0.0;
     double q = 0.0;
@@ -866,44 +998,38 @@ __global__ __launch_bounds__(kVerThreads) void k_accept(VerifyArgs a) {
   const int r = sh.first;
   __syncthreads();
   const int64_t rt = target_row(a, b, r);
-  if (wave == 0) {
-    float M;
-    double S;
-    merge_row(a, rt, M, S);
-    if (lane == 0) {
-      sh.M = M;
-      sh.S = S;
-    }
-  }
+  const float M = rowM[r];
+  const double S = rowS[r];
   if constexpr (DENSE) {
-    if (wave == 1 && r < n) {
-      float M;
-      double S;
-      merge_row(a, (int64_t)a.B * (a.T + 1) + draft_row(a, b, r), M, S);
+    if (wave == 0 && r < n) {
+      float Md;
+      double Sd;
+      merge_row(a, (int64_t)a.B * (a.T + 1) + draft_row(a, b, r), Md, Sd);
       if (lane == 0) {
-        a.norm[4 * b + 2] = M;
-        a.norm[4 * b + 3] = S;
+        a.norm[4 * b + 2] = Md;
+        a.norm[4 * b + 3] = Sd;
       }
     }
-    __syncthreads();
     if (tid == 0) {
-      a.norm[4 * b] = sh.M;
-      a.norm[4 * b + 1] = sh.S;
+      a.norm[4 * b] = M;
+      a.norm[4 * b + 1] = S;
       a.accepted[b] = r;
     }
     return;
   }
-  __syncthreads();
-  const float M = sh.M;
-  const double S = sh.S;
   const Row<T> row(a.target, rt * a.ld_t, a.V);
   const float* pm = a.segm + rt * a.nseg;
   const double* ps = a.segs + rt * a.nseg;
-  // entries of the draft at the rejected place: min(p, q) times S at the first
-  // of each index (an index that repeats counts once, with the sum), else 0
-  double* em = reinterpret_cast<double*>(lds);
-  int* ei = reinterpret_cast<int*>(em + a.K);
+  // entries of the draft at the rejected place: their q, and min(p, q) times S at
+  // the first of each index (one that repeats counts once, with the sum), else 0
+  int* ei = reinterpret_cast<int*>(rowM + a.T + 1);
   const bool rest = r < n && S > 0.0;
+  // lanes of each of `count` sums, over a workgroup: powers of two up to a wave
+  auto lanes_each = [](int count) {
+    int each = 1;
+    while (each < 64 && count * each * 2 <= kVerThreads) each *= 2;
+    return each;
+  };
   if (rest) {
     const float* l = a.dlogit + draft_row(a, b, r) * a.K;
     const int32_t* ix = a.didx + draft_row(a, b, r) * a.K;
@@ -918,37 +1044,43 @@ __global__ __launch_bounds__(kVerThreads) void k_accept(VerifyArgs a) {
       ei[k] = ix[k];
     }
     __syncthreads();
-    for (int k0 = 0; k0 < a.K; k0 += kVerThreads) {
-      const int k = k0 + tid;
+    const int each = lanes_each(a.K), sub = tid & (each - 1);
+    for (int k0 = 0; k0 < a.K; k0 += kVerThreads / each) {
+      const int k = k0 + tid / each;
       double q = 0.0;
-      int v = -1;
+      int again = 0;
+      const int v = k < a.K ? ei[k] : -1;
       if (k < a.K) {
-        v = ei[k];
-        bool again = (unsigned)v >= (unsigned)a.V;
-        for (int j = 0; j < a.K; ++j)
+        for (int j = sub; j < a.K; j += each)
           if (ei[j] == v) {
             q += em[j];
-            if (j < k) again = true;
+            again |= j < k;
           }
-        if (again) v = -1;
-        if (v >= 0) q = fmin(q * S, weight(row.one(v), M, a.c));
       }
-      // (the sums of this round's threads read em of all entries: written after)
-      __syncthreads();
-      if (k < a.K) reinterpret_cast<double*>(ei + ((a.K + 1) & ~1))[k] = v >= 0 ? q : 0.0;
+      for (int o = each / 2; o >= 1; o >>= 1) {
+        q += __shfl_xor(q, o);
+        again |= __shfl_xor(again, o);
+      }
+      if (k < a.K && sub == 0) {
+        const bool counts = (unsigned)v < (unsigned)a.V && again == 0;
+        q = counts ? fmin(q * S, weight(row.one(v), M, a.c)) : 0.0;
+        eq[k] = q;
+      }
     }
-    em = reinterpret_cast<double*>(ei + ((a.K + 1) & ~1));
     __syncthreads();
   }
-  for (int i = tid; i < a.nseg; i += kVerThreads) {
-    double x = M == -INFINITY ? 0.0 : ps[i] * weight(pm[i], M, a.c);
-    if (rest) {
+  {
+    const int each = lanes_each(a.nseg), sub = tid & (each - 1);
+    for (int i0 = 0; i0 < a.nseg; i0 += kVerThreads / each) {
+      const int i = i0 + tid / each;
       double take = 0.0;
-      for (int k = 0; k < a.K; ++k)
-        if ((unsigned)ei[k] < (unsigned)a.V && (ei[k] + row.shift) / kSegCols == i) take += em[k];
-      x = fmax(x - take, 0.0);
+      if (rest && i < a.nseg)
+        for (int k = sub; k < a.K; k += each)
+          if ((unsigned)ei[k] < (unsigned)a.V && (ei[k] + row.shift) / kSegCols == i) take += eq[k];
+      for (int o = each / 2; o >= 1; o >>= 1) take += __shfl_xor(take, o);
+      if (sub == 0 && i < a.nseg)
+        sh.seg[i] = M == -INFINITY ? 0.0 : fmax(ps[i] * weight(pm[i], M, a.c) - take, 0.0);
     }
-    sh.seg[i] = x;
   }
   __syncthreads();
   const double u = a.uniform[target_row(a, b, a.T)];
@@ -958,7 +1090,7 @@ __global__ __launch_bounds__(kVerThreads) void k_accept(VerifyArgs a) {
     if (rest)
       for (int k = tid; k < a.K; k += kVerThreads) {
         const int e = ei[k] + row.shift - seg * kSegCols;
-        if (em[k] > 0.0 && (unsigned)e < (unsigned)kSegCols) sh.x[e] -= em[k];
+        if (eq[k] > 0.0 && (unsigned)e < (unsigned)kSegCols) sh.x[e] -= eq[k];
       }
     __syncthreads();
   });
@@ -977,20 +1109,22 @@ __global__ __launch_bounds__(kVerThreads) void k_accept(VerifyArgs a) {
 // the masses of a dense draft's rejected row: max(p - q, 0), p where nothing was
 // rejected; places count from the target row's boundary
 struct RestRow {
-  float Mt, Md;
-  double St, Sd;
+  Weights t, d;
+  double it, id;  // 1 / S
   bool rest;
-  __device__ __forceinline__ RestRow(const VerifyArgs& a, int b, bool rest_) : rest(rest_) {
-    Mt = (float)a.norm[4 * b];
-    St = a.norm[4 * b + 1];
-    Md = rest ? (float)a.norm[4 * b + 2] : 0.f;
-    Sd = rest ? a.norm[4 * b + 3] : 0.0;
+  __device__ __forceinline__ RestRow(const VerifyArgs& a, int b, bool rest_, const double* tab)
+      : t((float)a.norm[4 * b], a.c, tab),
+        d(rest_ ? (float)a.norm[4 * b + 2] : 0.f, a.c, tab),
+        it(a.norm[4 * b + 1] > 0.0 ? 1.0 / a.norm[4 * b + 1] : 0.0),
+        id(rest_ && a.norm[4 * b + 3] > 0.0 ? 1.0 / a.norm[4 * b + 3] : 0.0),
+        rest(rest_) {}
+  __device__ __forceinline__ bool fast() const { return t.fast && d.fast; }
+  __device__ __forceinline__ double quick(float zt, float zd) const {
+    return fmax(t.quick(zt) * it - d.quick(zd) * id, 0.0);
   }
-  __device__ __forceinline__ double mass(float zt, float zd, double c) const {
-    const double p = St > 0.0 ? weight(zt, Mt, c) / St : 0.0;
-    if (!rest) return p;
-    const double q = Sd > 0.0 ? weight(zd, Md, c) / Sd : 0.0;
-    return fmax(p - q, 0.0);
+  __device__ __forceinline__ double exact(float zt, float zd) const {
+    const double p = t.exact(zt) * it;
+    return rest ? fmax(p - d.exact(zd) * id, 0.0) : p;
   }
 };
 // vector of the draft's row at the target's place e (its own boundary may differ)
@@ -1017,31 +1151,37 @@ __device__ __forceinline__ u32x4_t draft_at(const Row<T>& d, int e, int shift) {
   return u32x4_t{w[0], w[1], w[2], w[3]};
 }
 
-// Dense draft: the mass of each segment at the place where the sequence ended,
-// a wave per segment.
+// Dense draft: the mass of each segment at the place where the sequence ended, a
+// workgroup per segment (two rows with an exponential each: the few segments of a
+// small batch are spread over more of the chip). Nothing rejected: the target's
+// own sums serve.
 template <typename T>
-__global__ __launch_bounds__(256) void k_rest_sums(VerifyArgs a, int waves) {
-  const int w = blockIdx.x * 4 + wave_id();
-  if (w >= waves) return;
-  const int b = w / a.nseg, seg = w - b * a.nseg;
+__global__ __launch_bounds__(256) void k_rest_sums(VerifyArgs a) {
+  __shared__ double tab[kTab], part[4];
+  if (threadIdx.x < kTab) tab[threadIdx.x] = kRoots[threadIdx.x];
+  __syncthreads();
+  const int b = blockIdx.x / a.nseg, seg = blockIdx.x - b * a.nseg;
   const int r = a.accepted[b];
-  const bool rest = r < drafted(a, b);
-  const RestRow m(a, b, rest);
+  if (r >= drafted(a, b)) return;
+  const RestRow m(a, b, true, tab);
   const Row<T> row(a.target, target_row(a, b, r) * a.ld_t, a.V);
-  const Row<T> dr(a.draft, draft_row(a, b, rest ? r : 0) * a.ld_d, a.V);
-  constexpr int VPT = Row<T>::VPT, U = Row<T>::U;
-  const int lane = threadIdx.x & 63;
+  const Row<T> dr(a.draft, draft_row(a, b, r) * a.ld_d, a.V);
+  constexpr int VPT = Row<T>::VPT;
   double s = 0.0;
-#pragma unroll 2
-  for (int u = 0; u < U; ++u) {
-    const int e = seg * kSegCols + (64 * u + lane) * VPT;
-    const u32x4_t x = row.at(e);
-    const u32x4_t y = rest ? draft_at<T>(dr, e, row.shift) : x;
+  for (int e = threadIdx.x * VPT; e < kSegCols; e += 256 * VPT) {
+    const u32x4_t x = row.at(seg * kSegCols + e);
+    const u32x4_t y = draft_at<T>(dr, seg * kSegCols + e, row.shift);
+    if (m.fast()) {
 #pragma unroll
-    for (int i = 0; i < VPT; ++i) s += m.mass(Row<T>::elt(x, i), Row<T>::elt(y, i), a.c);
+      for (int i = 0; i < VPT; ++i) s += m.quick(Row<T>::raw(x, i), Row<T>::raw(y, i));
+    } else {
+      for (int i = 0; i < VPT; ++i) s += m.exact(Row<T>::elt(x, i), Row<T>::elt(y, i));
+    }
   }
   s = wave_sum64(s);
-  if (lane == 0) a.segr[w] = s;
+  if ((threadIdx.x & 63) == 0) part[threadIdx.x >> 6] = s;
+  __syncthreads();
+  if (threadIdx.x == 0) a.segr[blockIdx.x] = (part[0] + part[1]) + (part[2] + part[3]);
 }
 
 template <typename T>
@@ -1053,8 +1193,13 @@ __global__ __launch_bounds__(kVerThreads) void k_pick(VerifyArgs a) {
   const int64_t rt = target_row(a, b, r);
   const Row<T> row(a.target, rt * a.ld_t, a.V);
   const Row<T> dr(a.draft, draft_row(a, b, rest ? r : 0) * a.ld_d, a.V);
-  const RestRow m(a, b, rest);
-  for (int i = tid; i < a.nseg; i += kVerThreads) sh.seg[i] = a.segr[(int64_t)b * a.nseg + i];
+  const RestRow m(a, b, rest, nullptr);
+  const float* pm = a.segm + rt * a.nseg;
+  const double* ps = a.segs + rt * a.nseg;
+  for (int i = tid; i < a.nseg; i += kVerThreads)
+    sh.seg[i] = rest        ? a.segr[(int64_t)b * a.nseg + i]
+                : m.it > 0.0 ? ps[i] * m.t.exact(pm[i]) * m.it
+                             : 0.0;
   __syncthreads();
   const double u = a.uniform[target_row(a, b, a.T)];
   constexpr int VPT = Row<T>::VPT;
@@ -1065,17 +1210,15 @@ __global__ __launch_bounds__(kVerThreads) void k_pick(VerifyArgs a) {
       const u32x4_t y = rest ? draft_at<T>(dr, e, row.shift) : x;
 #pragma unroll
       for (int i = 0; i < VPT; ++i)
-        sh.x[j * VPT + i] = m.mass(Row<T>::elt(x, i), Row<T>::elt(y, i), a.c);
+        sh.x[j * VPT + i] = m.exact(Row<T>::elt(x, i), Row<T>::elt(y, i));
     }
     __syncthreads();
   });
-  if (place < 0 && rest && m.St > 0.0) {
-    const float* pm = a.segm + rt * a.nseg;
-    const double* ps = a.segs + rt * a.nseg;
-    for (int i = tid; i < a.nseg; i += kVerThreads) sh.seg[i] = ps[i] * weight(pm[i], m.Mt, a.c);
+  if (place < 0 && rest && m.it > 0.0) {
+    for (int i = tid; i < a.nseg; i += kVerThreads) sh.seg[i] = ps[i] * m.t.exact(pm[i]);
     __syncthreads();
     place = pick_place(sh, a.nseg, u, [&](int seg) {
-      fill_target<T>(sh, row, seg, m.Mt, a.c);
+      fill_target<T>(sh, row, seg, m.t.m, a.c);
       __syncthreads();
     });
   }
@@ -1086,6 +1229,9 @@ __global__ __launch_bounds__(kVerThreads) void k_pick(VerifyArgs a) {
 
 // ================================================================ launchers ==
 using namespace kd;
+
+constexpr int64_t kSelectFewRows = 512;
+constexpr int kSelectManyEntries = 512;
 
 template <typename T>
 static int launch_topk(const KdTopkArgs& a, hipStream_t s) {
@@ -1101,8 +1247,11 @@ static int launch_topk(const KdTopkArgs& a, hipStream_t s) {
   const int G = a.nseg * kSegGroups;
   const SelectArgs q{a.logits, a.ld, a.V, a.K, G, a.nseg, a.logprobs, a.gmax, a.pm, a.ps,
                      a.idx, a.value, a.entries, a.scale};
-  hipLaunchKernelGGL(k_row_select<T>, dim3((unsigned)a.rows), dim3(kSelThreads),
-                     (size_t)select_lds(G, a.K), s, q);
+  const size_t lds = select_lds(G, a.K);
+  if (a.rows <= kSelectFewRows || a.K > kSelectManyEntries)
+    hipLaunchKernelGGL((k_row_select<T, 1024>), dim3((unsigned)a.rows), dim3(1024), lds, s, q);
+  else
+    hipLaunchKernelGGL((k_row_select<T, 256>), dim3((unsigned)a.rows), dim3(256), lds, s, q);
   return (int)hipGetLastError();
 }
 
@@ -1169,14 +1318,13 @@ static int launch_verify(const KdVerifyArgs& q, hipStream_t s) {
   hipLaunchKernelGGL(k_seg_sums<T>, dim3((unsigned)((waves + 3) / 4)), dim3(256), 0, s, a,
                      (int)waves);
   if (!dense) {
-    // q of the entries, their indices, and the mass they take
-    const size_t lds = (size_t)q.K * 16 + (size_t)((q.K + 1) & ~1) * 4;
+    const size_t lds = (size_t)q.K * 20 + (size_t)(q.T + 1) * 12;
     hipLaunchKernelGGL((k_accept<T, false>), dim3(q.B), dim3(kVerThreads), lds, s, a);
     return (int)hipGetLastError();
   }
-  hipLaunchKernelGGL((k_accept<T, true>), dim3(q.B), dim3(kVerThreads), 0, s, a);
-  const int64_t w2 = (int64_t)q.B * q.nseg;
-  hipLaunchKernelGGL(k_rest_sums<T>, dim3((unsigned)((w2 + 3) / 4)), dim3(256), 0, s, a, (int)w2);
+  hipLaunchKernelGGL((k_accept<T, true>), dim3(q.B), dim3(kVerThreads), (size_t)(q.T + 1) * 12, s,
+                     a);
+  hipLaunchKernelGGL(k_rest_sums<T>, dim3((unsigned)(q.B * q.nseg)), dim3(256), 0, s, a);
   hipLaunchKernelGGL(k_pick<T>, dim3(q.B), dim3(kVerThreads), 0, s, a);
   return (int)hipGetLastError();
 }
