@@ -143,11 +143,10 @@ __global__ __launch_bounds__(256) void k_row_groups(const T* __restrict__ logits
 // Second pass, a workgroup of NT threads per row. At least K groups have a maximum
 // of at least the K-th largest group maximum, so the K largest elements are among
 // those that reach it, and these lie in the groups whose maximum does: about K
-// groups of 64 columns are read again instead of the row. The bound is searched in
+// groups of 64 columns are read again instead of the row. The bound is found in
 // the 16 leading bits of the maxima (bf16's precision, no higher than the K-th),
-// four of them a thread (each the largest of several groups where the row has
-// more than 4 NT): for V = 131072 and K = 100 there are about 105 elements
-// that reach it. They are sorted by (value, lowest index first), the order of the
+// by counting them per value from the largest down: for V = 131072 and K = 100 there
+// are about 105 elements that reach it. They are sorted by (value, lowest index first), the order of the
 // result, so which thread collected which does not matter. Where more elements
 // reach the bound than fit (many equal values, or V below about 64 K), the
 // K-th largest is found exactly by counting digits over those groups.
@@ -155,7 +154,8 @@ __global__ __launch_bounds__(256) void k_row_groups(const T* __restrict__ logits
 // The pass is latency-bound (a few dependent reads and barriers per row), so what
 // counts is rows in flight, and for few rows the time of one.
 constexpr int kHistBins = 2048;
-constexpr int kBoundKeys = 4;
+constexpr int kBoundBins = 1024;
+constexpr int kUnroll = 4;  // reads in flight
 
 __host__ __device__ constexpr int select_cap(int K) {
   int c = 1024;
@@ -174,12 +174,12 @@ __host__ __device__ constexpr int select_lds(int G, int K) {
 
 template <int NT>
 struct SelectShared {
-  int reach[10][4];  // groups that reach each bound of a step of the search
+  int bound[kBoundBins];  // maxima by their distance from the largest
   int scan[NT / 64];
   int found, before;
   int n, nlist;
   float logs;
-  uint32_t wlo[NT / 64], whi[NT / 64];
+  uint32_t whi[NT / 64];
 };
 
 // The bin of `want` (1 = the first) in the bins' order (descending or ascending),
@@ -268,35 +268,25 @@ __global__ __launch_bounds__(NT) void k_row_select(SelectArgs a) {
   int* hist = reinterpret_cast<int*>(lds);
   uint16_t* list = reinterpret_cast<uint16_t*>(lds + select_lds_keys(G, K));
 
-  // group maxima, their range, and log of the row's sum of exp
-  uint32_t key[kBoundKeys] = {};  // 0: below every value's
-  uint32_t lo = 0xffffffffu, hi = 0;
+  // group maxima, the largest of them, and log of the row's sum of exp
+  uint32_t hi = 0;
   const float* gm = a.gmax + r * G;
-  for (int i0 = tid; i0 < G; i0 += kBoundKeys * NT) {
+  for (int i0 = tid; i0 < G; i0 += kUnroll * NT) {
+    float g[kUnroll];
 #pragma unroll
-    for (int j = 0; j < kBoundKeys; ++j) {
-      const int i = i0 + j * NT;
-      if (i < G) {
-        const uint32_t k = order_key(gm[i]);
-        keys[i] = k;
-        key[j] = max(key[j], k);
-        lo = min(lo, k);
-      }
+    for (int j = 0; j < kUnroll; ++j) g[j] = i0 + j * NT < G ? gm[i0 + j * NT] : -INFINITY;
+#pragma unroll
+    for (int j = 0; j < kUnroll; ++j) {
+      const uint32_t k = order_key(g[j]);
+      if (i0 + j * NT < G) keys[i0 + j * NT] = k;
+      hi = max(hi, k);
     }
   }
 #pragma unroll
-  for (int j = 0; j < kBoundKeys; ++j) hi = max(hi, key[j]);
-#pragma unroll
-  for (int o = 32; o >= 1; o >>= 1) {
-    lo = min(lo, (uint32_t)__shfl_xor((int)lo, o));
-    hi = max(hi, (uint32_t)__shfl_xor((int)hi, o));
-  }
-  if (lane == 0) {
-    s.wlo[wave] = lo;
-    s.whi[wave] = hi;
-  }
+  for (int o = 32; o >= 1; o >>= 1) hi = max(hi, (uint32_t)__shfl_xor((int)hi, o));
+  if (lane == 0) s.whi[wave] = hi;
   if (tid == 0) s.n = s.nlist = 0;
-  if (tid < 40) s.reach[tid / 4][tid & 3] = 0;
+  for (int i = tid; i < kBoundBins; i += NT) s.bound[i] = 0;
   if (a.logprobs && wave == NT / 64 - 1) {
     const float *pm = a.pm + r * a.nseg, *ps = a.ps + r * a.nseg;
     float m = -INFINITY, t = 0.f;
@@ -308,57 +298,69 @@ __global__ __launch_bounds__(NT) void k_row_select(SelectArgs a) {
     if (lane == 0) s.logs = m != -INFINITY ? logf(t) : 0.f;
   }
   __syncthreads();
-  lo = s.wlo[lane % (NT / 64)];
   hi = s.whi[lane % (NT / 64)];
 #pragma unroll
-  for (int o = NT / 128; o >= 1; o >>= 1) {
-    lo = min(lo, (uint32_t)__shfl_xor((int)lo, o));
-    hi = max(hi, (uint32_t)__shfl_xor((int)hi, o));
-  }
-  lo = (uint32_t)__builtin_amdgcn_readfirstlane((int)lo) >> 16;
-  hi = ((uint32_t)__builtin_amdgcn_readfirstlane((int)hi) >> 16) + 1;
-  // the largest 16-bit prefix that K of the maxima reach, or 0 where there are
-  // fewer of them; lo always is reached by K, hi never. A step tries three bounds
-  // and leaves a quarter of the range: at most 9 steps
-  if (K > min(G, kBoundKeys * NT)) lo = hi = 0;
-  for (int it = 0; hi - lo > 1; ++it) {
-    const uint32_t d = hi - lo;
-    const uint32_t m1 = lo + (d + 3) / 4, m2 = lo + (d + 1) / 2, m3 = lo + (3 * d + 3) / 4;
-    int c1 = 0, c2 = 0, c3 = 0;
+  for (int o = NT / 128; o >= 1; o >>= 1) hi = max(hi, (uint32_t)__shfl_xor((int)hi, o));
+  hi = (uint32_t)__builtin_amdgcn_readfirstlane((int)hi) >> 16;
+  // the largest 16-bit prefix that K maxima reach: by counts where it lies within
+  // 1022 of the largest (eight factors of two), else by halving; 0 where K groups
+  // do not exist
+  uint32_t t = 0;
+  if (K <= G) {
+    for (int i0 = tid; i0 < G; i0 += kUnroll * NT)
 #pragma unroll
-    for (int j = 0; j < kBoundKeys; ++j) {
-      const uint32_t k = key[j] >> 16;
-      c1 += __popcll(__builtin_amdgcn_ballot_w64(k >= m1));
-      c2 += __popcll(__builtin_amdgcn_ballot_w64(k >= m2));
-      c3 += __popcll(__builtin_amdgcn_ballot_w64(k >= m3));
-    }
-    if (lane < 3) atomicAdd(&s.reach[it][lane], lane == 0 ? c1 : lane == 1 ? c2 : c3);
+      for (int j = 0; j < kUnroll; ++j)
+        if (i0 + j * NT < G)
+          atomicAdd(&s.bound[min(hi - (keys[i0 + j * NT] >> 16), (uint32_t)kBoundBins - 1)], 1);
     __syncthreads();
-    c1 = s.reach[it][0];
-    c2 = s.reach[it][1];
-    c3 = s.reach[it][2];
-    // (bounds at hi or above are reached by fewer than K)
-    if (m3 < hi && c3 >= K) lo = m3;
-    else if (c2 >= K) lo = m2, hi = min(hi, m3);
-    else if (c1 >= K) lo = m1, hi = m2;
-    else hi = m1;
+    int bin, before;
+    find_bin<NT>(s, s.bound, kBoundBins, false, K, bin, before);
+    if (bin < kBoundBins - 1) {
+      t = hi - bin;
+    } else {
+      uint32_t top = hi - (kBoundBins - 2);  // reached by fewer than K; 0 by all
+      while (top - t > 1) {
+        const uint32_t mid = (t + top) / 2;
+        int c = 0;
+        for (int i = tid; i < G; i += NT) c += keys[i] >> 16 >= mid;
+#pragma unroll
+        for (int o = 32; o >= 1; o >>= 1) c += __shfl_xor(c, o);
+        if (lane == 0) s.scan[wave] = c;
+        __syncthreads();
+        c = 0;
+        for (int w = 0; w < NT / 64; ++w) c += s.scan[w];
+        if (c >= K) t = mid;
+        else top = mid;
+        __syncthreads();
+      }
+    }
+    t <<= 16;
   }
-  const uint32_t t = lo << 16;
-  // the groups that reach the bound, one reservation per wave
+  // the groups that reach it, one reservation per wave
   int mine = 0;
-  for (int i0 = 0; i0 < G; i0 += NT) {
-    const int i = i0 + tid;
-    mine += __popcll(__builtin_amdgcn_ballot_w64(i < G && keys[i < G ? i : 0] >= t));
+  for (int i0 = tid; i0 - lane < G; i0 += kUnroll * NT) {
+#pragma unroll
+    for (int j = 0; j < kUnroll; ++j) {
+      const int i = i0 + j * NT;
+      mine += __popcll(__builtin_amdgcn_ballot_w64(i < G && keys[min(i, G - 1)] >= t));
+    }
   }
   int at = 0;
   if (lane == 0 && mine > 0) at = atomicAdd(&s.nlist, mine);
   at = __builtin_amdgcn_readfirstlane(at);
-  for (int i0 = 0; i0 < G; i0 += NT) {
-    const int i = i0 + tid;
-    const bool q = i < G && keys[i < G ? i : 0] >= t;
-    const uint64_t b = __builtin_amdgcn_ballot_w64(q);
-    if (q) list[at + lanes_below(b)] = (uint16_t)i;
-    at += __popcll(b);
+  for (int i0 = tid; i0 - lane < G; i0 += kUnroll * NT) {
+    bool q[kUnroll];
+#pragma unroll
+    for (int j = 0; j < kUnroll; ++j) {
+      const int i = i0 + j * NT;
+      q[j] = i < G && keys[min(i, G - 1)] >= t;
+    }
+#pragma unroll
+    for (int j = 0; j < kUnroll; ++j) {
+      const uint64_t b = __builtin_amdgcn_ballot_w64(q[j]);
+      if (q[j]) list[at + lanes_below(b)] = (uint16_t)(i0 + j * NT);
+      at += __popcll(b);
+    }
   }
   __syncthreads();
   const int nlist = s.nlist;
@@ -443,7 +445,7 @@ __global__ __launch_bounds__(NT) void k_row_select(SelectArgs a) {
     const int j = tid / each, sub = tid & (each - 1);
     const uint64_t c = j < n ? cand[j] : 0;
     int rank = 0;
-#pragma unroll 4
+#pragma unroll 8
     for (int i = sub; i < n; i += each) rank += cand[i] > c;
     for (int o = each / 2; o >= 1; o >>= 1) rank += __shfl_xor(rank, o);
     __syncthreads();
@@ -891,20 +893,23 @@ __device__ __forceinline__ int pick_place(VerifyShared& sh, int nseg, double u, 
     for (int w = 0; w < (tid >> 6); ++w) incl += sh.scan[w];
     double at = incl - sum;
     const double goal = i == 0 ? sh.goal : first + i < nseg ? 0.0 : INFINITY;
+    int hit = kSegCols;
 #pragma unroll
-    for (int j = per - 1; j >= 0; --j) {
-      // (from the end: the first one stays; sums as in the forward order)
-      double c = at;
-      for (int k = 0; k <= j; ++k) c += v[k];
-      if (c > goal && v[j] > 0.0) atomicMin(&sh.at, tid * per + j);
+    for (int j = 0; j < per; ++j) {
+      at += v[j];
+      if (hit == kSegCols && at > goal && v[j] > 0.0) hit = tid * per + j;
     }
+    // the first lane's find is the wave's (places ascend with the lanes)
+    const uint64_t any = __builtin_amdgcn_ballot_w64(hit < kSegCols);
+    if (any != 0 && lane == __builtin_ctzll(any)) atomicMin(&sh.at, hit);
     __syncthreads();
     int place = sh.at;
     __syncthreads();
     if (place == kSegCols) {
       if (tid == 0) sh.at = -1;
       __syncthreads();
-      if (last >= 0) atomicMax(&sh.at, last);
+      const uint64_t some = __builtin_amdgcn_ballot_w64(last >= 0);
+      if (some != 0 && lane == 63 - __builtin_clzll(some)) atomicMax(&sh.at, last);
       __syncthreads();
       place = sh.at;
       __syncthreads();
@@ -946,8 +951,10 @@ __global__ __launch_bounds__(kVerThreads) void k_accept(VerifyArgs a) {
   const int n = drafted(a, b);
   // (S, M) of the target's row at each place; the entries' arrays behind them
   double* rowS = reinterpret_cast<double*>(lds);
-  double *em = rowS + a.T + 1, *eq = em + a.K;
-  float* rowM = reinterpret_cast<float*>(eq + a.K);
+  const int Kp = (a.K + 3) & ~3;
+  double *em = rowS + ((a.T + 2) & ~1), *eq = em + Kp;
+  int* ei = reinterpret_cast<int*>(eq + Kp);
+  float* rowM = reinterpret_cast<float*>(ei + Kp);
   if (tid == 0) sh.first = n;
   __syncthreads();
   if (a.prob != nullptr)
@@ -1022,7 +1029,6 @@ __global__ __launch_bounds__(kVerThreads) void k_accept(VerifyArgs a) {
   const double* ps = a.segs + rt * a.nseg;
   // entries of the draft at the rejected place: their q, and min(p, q) times S at
   // the first of each index (one that repeats counts once, with the sum), else 0
-  int* ei = reinterpret_cast<int*>(rowM + a.T + 1);
   const bool rest = r < n && S > 0.0;
   // lanes of each of `count` sums, over a workgroup: powers of two up to a wave
   auto lanes_each = [](int count) {
@@ -1039,44 +1045,59 @@ __global__ __launch_bounds__(kVerThreads) void k_accept(VerifyArgs a) {
     double s = 0.0;
     for (int k = lane; k < a.K; k += 64) s += weight(fmaxf(l[k], -INFINITY), m, a.c);
     s = wave_sum64(s);
-    for (int k = tid; k < a.K; k += kVerThreads) {
-      em[k] = s > 0.0 ? weight(fmaxf(l[k], -INFINITY), m, a.c) / s : 0.0;
-      ei[k] = ix[k];
+    for (int k = tid; k < Kp; k += kVerThreads) {
+      const bool entry = k < a.K;
+      em[k] = entry && s > 0.0 ? weight(fmaxf(l[k], -INFINITY), m, a.c) / s : 0.0;
+      const int v = entry ? ix[k] : -1;
+      ei[k] = (unsigned)v < (unsigned)a.V ? v : -1;
+      eq[k] = 0.0;
     }
     __syncthreads();
+    // (each lane sums over every each-th four of the entries)
+    typedef __attribute__((__vector_size__(16))) int s32x4_t;
     const int each = lanes_each(a.K), sub = tid & (each - 1);
     for (int k0 = 0; k0 < a.K; k0 += kVerThreads / each) {
       const int k = k0 + tid / each;
       double q = 0.0;
       int again = 0;
       const int v = k < a.K ? ei[k] : -1;
-      if (k < a.K) {
-        for (int j = sub; j < a.K; j += each)
-          if (ei[j] == v) {
-            q += em[j];
-            again |= j < k;
-          }
+      if (v >= 0) {
+#pragma unroll 4
+        for (int j = 4 * sub; j < Kp; j += 4 * each) {
+          const s32x4_t w = *reinterpret_cast<const s32x4_t*>(ei + j);
+#pragma unroll
+          for (int x = 0; x < 4; ++x)
+            if (w[x] == v) {
+              q += em[j + x];
+              again |= j + x < k;
+            }
+        }
       }
       for (int o = each / 2; o >= 1; o >>= 1) {
         q += __shfl_xor(q, o);
         again |= __shfl_xor(again, o);
       }
-      if (k < a.K && sub == 0) {
-        const bool counts = (unsigned)v < (unsigned)a.V && again == 0;
-        q = counts ? fmin(q * S, weight(row.one(v), M, a.c)) : 0.0;
-        eq[k] = q;
-      }
+      if (v >= 0 && sub == 0 && again == 0) eq[k] = fmin(q * S, weight(row.one(v), M, a.c));
     }
     __syncthreads();
   }
   {
+    typedef __attribute__((__vector_size__(16))) int s32x4_t;
     const int each = lanes_each(a.nseg), sub = tid & (each - 1);
     for (int i0 = 0; i0 < a.nseg; i0 += kVerThreads / each) {
       const int i = i0 + tid / each;
       double take = 0.0;
-      if (rest && i < a.nseg)
-        for (int k = sub; k < a.K; k += each)
-          if ((unsigned)ei[k] < (unsigned)a.V && (ei[k] + row.shift) / kSegCols == i) take += eq[k];
+      if (rest && i < a.nseg) {
+        // columns of segment i, -1 being of none
+        const int v0 = max(i * kSegCols - row.shift, 0), v1 = (i + 1) * kSegCols - row.shift;
+#pragma unroll 4
+        for (int k = 4 * sub; k < Kp; k += 4 * each) {
+          const s32x4_t w = *reinterpret_cast<const s32x4_t*>(ei + k);
+#pragma unroll
+          for (int x = 0; x < 4; ++x)
+            if (w[x] >= v0 && w[x] < v1) take += eq[k + x];
+        }
+      }
       for (int o = each / 2; o >= 1; o >>= 1) take += __shfl_xor(take, o);
       if (sub == 0 && i < a.nseg)
         sh.seg[i] = M == -INFINITY ? 0.0 : fmax(ps[i] * weight(pm[i], M, a.c) - take, 0.0);
@@ -1318,11 +1339,11 @@ static int launch_verify(const KdVerifyArgs& q, hipStream_t s) {
   hipLaunchKernelGGL(k_seg_sums<T>, dim3((unsigned)((waves + 3) / 4)), dim3(256), 0, s, a,
                      (int)waves);
   if (!dense) {
-    const size_t lds = (size_t)q.K * 20 + (size_t)(q.T + 1) * 12;
+    const size_t lds = (size_t)((q.K + 3) & ~3) * 20 + (size_t)(q.T + 2) * 12;
     hipLaunchKernelGGL((k_accept<T, false>), dim3(q.B), dim3(kVerThreads), lds, s, a);
     return (int)hipGetLastError();
   }
-  hipLaunchKernelGGL((k_accept<T, true>), dim3(q.B), dim3(kVerThreads), (size_t)(q.T + 1) * 12, s,
+  hipLaunchKernelGGL((k_accept<T, true>), dim3(q.B), dim3(kVerThreads), (size_t)(q.T + 2) * 12, s,
                      a);
   hipLaunchKernelGGL(k_rest_sums<T>, dim3((unsigned)(q.B * q.nseg)), dim3(256), 0, s, a);
   hipLaunchKernelGGL(k_pick<T>, dim3(q.B), dim3(kVerThreads), 0, s, a);

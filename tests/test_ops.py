@@ -29,7 +29,8 @@ def _logits(N, V, dtype, seed, ld=None, offset=0, std=5.0):
     return x
 
 
-SPECIALS = ("plain", "ties", "constant", "masked", "lowest", "nan", "inf", "ascending")
+SPECIALS = ("plain", "ties", "constant", "masked", "lowest", "nan", "inf", "ascending", "wide",
+            "logprobs")
 
 
 def _special(x, kind):
@@ -57,6 +58,11 @@ def _special(x, kind):
         x[0, V // 3] = float("inf")
         x[-1, [0, V - 1]] = float("inf")
         x[:, 1] = float("-inf")
+    elif kind == "wide":             # magnitudes over the whole range, either sign
+        e = torch.randint(-120, 121, (N, V), generator=_gen(3), device=x.device).float()
+        x.copy_(x.sign() * torch.exp2(e))
+    elif kind == "logprobs":         # one column near 0, the others far below
+        x.copy_(torch.log_softmax(x.float() * 3, 1) - 1e-5)
     elif kind == "ascending":
         x.copy_(torch.arange(V, device=x.device).to(x.dtype) * 0.5)
     return x
