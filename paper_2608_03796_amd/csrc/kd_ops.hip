@@ -662,48 +662,60 @@ __device__ __forceinline__ double weight(float z, float m, double c) {
   if (z == m) return m == -INFINITY ? 0.0 : 1.0;
   return exp2_64(((double)z - (double)m) * c);
 }
-// Weights below one m, for passes over whole rows: 2^(y / 16) with y = 16 c (z - m)
-// by a table of 2^(i / 16) in LDS and the series of degree 5 for the rest of up to
-// half a sixteenth (the next term is below 2^-42 of the result). 11 fp64 operations
-// where exp2_64 with its difference, comparison and sum takes 23. z is held above
-// m - 990 / c, where weights no longer count (2^-990; -inf and what is not a number
-// end there too), which fp32 can tell from m where `fast`; elsewhere (infinities,
-// extreme tau) weight() serves.
+// Weights below one m, for passes over whole rows: 2^(y / 256) with y = 256 c (z - m)
+// by a table of 2^(i / 256) in LDS and the series of degree 3 for the rest of up to
+// half a step (the next term is below 2^-42 of the result). 9 fp64 operations and 6
+// others where exp2_64 with its difference, comparisons and sum takes 23 and 4. z is
+// held above m - 990 / c, where weights no longer count (2^-990; -inf and what is not
+// a number end there too), which fp32 can tell from m where `fast`; elsewhere
+// (infinities, extreme tau) weight() serves.
+constexpr int kTabBits = 8, kTab = 1 << kTabBits;
+// 2^(i / 256) less i << 12 in its high word: adding n << 12 for n = i + 256 j gives
+// 2^(n / 256)
+struct Roots {
+  uint64_t v[kTab];
+  constexpr Roots() : v() {
+    for (int i = 0; i < kTab; ++i) {
+      const double x = i * (0.69314718055994530942 / kTab);
+      double s = 1.0;
+      for (int k = 24; k >= 1; --k) s = 1.0 + s * x / k;
+      v[i] = __builtin_bit_cast(uint64_t, s) - ((uint64_t)i << (52 - kTabBits));
+    }
+  }
+};
+__device__ constexpr Roots kRoots{};
+__device__ __forceinline__ void load_roots(uint64_t* tab) {
+  for (int i = threadIdx.x; i < kTab; i += blockDim.x) tab[i] = kRoots.v[i];
+  __syncthreads();
+}
 struct Weights {
-  double c, c16, mc16;
+  double c, cs, ms;
   float m, floor;
   bool fast;
-  const double* tab;
-  __device__ __forceinline__ Weights(float m_, double c_, const double* t) : c(c_), m(m_), tab(t) {
+  const uint64_t* tab;
+  __device__ __forceinline__ Weights(float m_, double c_, const uint64_t* t)
+      : c(c_), m(m_), tab(t) {
     const double reach = 990.0 / c, big = fabs((double)m);
     fast = reach > big * (1.0 / 65536) && reach < 1e37 && big < 1e37;
     floor = (float)((double)m - reach);
-    c16 = 16.0 * c;
-    mc16 = -(double)m * c16;
+    cs = (double)kTab * c;
+    ms = -(double)m * cs;
   }
   __device__ __forceinline__ double quick(float z) const {
-    const double y = fma((double)fmaxf(z, floor), c16, mc16);
+    const double y = fma((double)fmaxf(z, floor), cs, ms);
     const double t = y + 0x1.8p52;  // the nearest whole number in the low bits
     const double g = y - (t - 0x1.8p52);
-    const int n = (int)(uint32_t)__builtin_bit_cast(uint64_t, t);
-    // (ln 2 / 16)^k / k!
-    double p = fma(g, 1.271587195055813162e-9, 1.467610032291942926e-7);
-    p = fma(p, g, 1.355080777949745605e-5);
-    p = fma(p, g, 9.383847928089871575e-4);
-    p = fma(p, g, 4.332169878499658184e-2);
+    const uint32_t n = (uint32_t)__builtin_bit_cast(uint64_t, t);
+    // (ln 2 / 256)^k / k!
+    double p = fma(g, 3.30830268054137110e-9, 3.66556559691010608e-6);
+    p = fma(p, g, 2.70760617406228633e-3);
     p = fma(p, g, 1.0);
-    const uint64_t e = __builtin_bit_cast(uint64_t, tab[n & 15]) +
-                       ((uint64_t)(uint32_t)((n >> 4) << 20) << 32);
-    return p * __builtin_bit_cast(double, e);
+    const uint64_t e = tab[n & (kTab - 1)];
+    const uint32_t high = (uint32_t)(e >> 32) + (n << (20 - kTabBits));
+    return p * __builtin_bit_cast(double, (uint64_t)high << 32 | (uint32_t)e);
   }
   __device__ __forceinline__ double exact(float z) const { return weight(z, m, c); }
 };
-constexpr int kTab = 16;
-__device__ const double kRoots[kTab] = {
-    1.0, 1.0442737824274138403, 1.0905077326652576592, 1.1387886347566916537,
-    1.1892071150027210667, 1.2418578120734840486, 1.2968395546510096659, 1.3542555469368927283,
-    1.4142135623730950488, 1.4768261459394993114, 1.5422108254079408236, 1.6104903319492543082,
-    1.6817928305074290861, 1.7562521603732994831, 1.8340080864093424635, 1.9152065613971472939};
 
 __device__ __forceinline__ double wave_sum64(double x) {
 #pragma unroll
@@ -749,9 +761,8 @@ __device__ __forceinline__ int64_t draft_row(const VerifyArgs& a, int b, int t) 
 // target's, then the draft's): the pass that reads the logits.
 template <typename T>
 __global__ __launch_bounds__(256) void k_seg_sums(VerifyArgs a, int waves) {
-  __shared__ double tab[kTab];
-  if (threadIdx.x < kTab) tab[threadIdx.x] = kRoots[threadIdx.x];
-  __syncthreads();
+  __shared__ uint64_t tab[kTab];
+  load_roots(tab);
   const int w = blockIdx.x * 4 + wave_id();
   if (w >= waves) return;
   const int r = w / a.nseg, seg = w - r * a.nseg;
@@ -1133,7 +1144,7 @@ struct RestRow {
   Weights t, d;
   double it, id;  // 1 / S
   bool rest;
-  __device__ __forceinline__ RestRow(const VerifyArgs& a, int b, bool rest_, const double* tab)
+  __device__ __forceinline__ RestRow(const VerifyArgs& a, int b, bool rest_, const uint64_t* tab)
       : t((float)a.norm[4 * b], a.c, tab),
         d(rest_ ? (float)a.norm[4 * b + 2] : 0.f, a.c, tab),
         it(a.norm[4 * b + 1] > 0.0 ? 1.0 / a.norm[4 * b + 1] : 0.0),
@@ -1178,9 +1189,9 @@ __device__ __forceinline__ u32x4_t draft_at(const Row<T>& d, int e, int shift) {
 // own sums serve.
 template <typename T>
 __global__ __launch_bounds__(256) void k_rest_sums(VerifyArgs a) {
-  __shared__ double tab[kTab], part[4];
-  if (threadIdx.x < kTab) tab[threadIdx.x] = kRoots[threadIdx.x];
-  __syncthreads();
+  __shared__ uint64_t tab[kTab];
+  __shared__ double part[4];
+  load_roots(tab);
   const int b = blockIdx.x / a.nseg, seg = blockIdx.x - b * a.nseg;
   const int r = a.accepted[b];
   if (r >= drafted(a, b)) return;
