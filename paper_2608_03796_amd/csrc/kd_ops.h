@@ -12,9 +12,10 @@
 constexpr int kSegCols = 2048;
 constexpr int kGroupCols = 64;
 constexpr int kSegGroups = kSegCols / kGroupCols;
-// segments of a row of V elements of eb bytes, wherever it starts
-constexpr int64_t kd_row_segs(int64_t V, int eb) {
-  return (V + 16 / eb - 1 + kSegCols - 1) / kSegCols;
+// segments of a row of V elements of eb bytes, wherever it starts, or of rows that
+// all start on a 16-byte boundary
+constexpr int64_t kd_row_segs(int64_t V, int eb, bool aligned = false) {
+  return (V + (aligned ? 0 : 16 / eb - 1) + kSegCols - 1) / kSegCols;
 }
 
 // Cache entry: index << 12 | code. Codes 0..4094 count steps below the row's

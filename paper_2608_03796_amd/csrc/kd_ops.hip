@@ -29,10 +29,15 @@ struct Row {
         V(V_),
         shift((int)((reinterpret_cast<uintptr_t>(p) & 15u) / sizeof(T))) {}
 
-  // the vector at place e (a multiple of VPT)
+  // whether the vector at place e (a multiple of VPT) lies inside the row
+  __device__ __forceinline__ bool inside(int e) const {
+    return e >= shift && e - shift + VPT <= V;
+  }
   __device__ __forceinline__ u32x4_t at(int e) const {
+    return inside(e) ? *reinterpret_cast<const u32x4_t*>(p + (e - shift)) : edge(e);
+  }
+  __device__ __forceinline__ u32x4_t edge(int e) const {
     const int v = e - shift;
-    if (v >= 0 && v + VPT <= V) return *reinterpret_cast<const u32x4_t*>(p + v);
     uint32_t w[4];
     if constexpr (sizeof(T) == 2) {
       uint16_t h[8];
@@ -146,39 +151,39 @@ __global__ __launch_bounds__(256) void k_row_groups(const T* __restrict__ logits
 // groups of 64 columns are read again instead of the row. The bound is found in
 // the 16 leading bits of the maxima (bf16's precision, no higher than the K-th),
 // by counting them per value from the largest down: for V = 131072 and K = 100 there
-// are about 105 elements that reach it. They are sorted by (value, lowest index first), the order of the
-// result, so which thread collected which does not matter. Where more elements
-// reach the bound than fit (many equal values, or V below about 64 K), the
-// K-th largest is found exactly by counting digits over those groups.
+// are about 105 elements that reach it. They are sorted by (value, lowest index
+// first), the order of the result, so which thread collected which does not
+// matter. Where more elements reach the bound than fit (many equal values), the
+// K-th largest is found exactly by counting digits over the row. Columns of -inf
+// never are candidates: where the row has too few others, the list is filled up
+// from its first columns.
+//
+// DIRECT (rows of up to 8 vectors a thread): the only pass. The row is held in
+// registers, its groups are single vectors, and their maxima and the sum of exp
+// are formed here: one launch, and groups enough for K above V / 64.
 //
 // The pass is latency-bound (a few dependent reads and barriers per row), so what
 // counts is rows in flight, and for few rows the time of one.
 constexpr int kHistBins = 2048;
 constexpr int kBoundBins = 1024;
-constexpr int kUnroll = 4;  // reads in flight
+// keys of a thread in registers: all of a row held directly, or of 131072 columns
+constexpr int select_keys(int NT, bool direct) { return direct || NT == 256 ? 8 : 2; }
 
 __host__ __device__ constexpr int select_cap(int K) {
   int c = 1024;
   while (c < 2 * K) c *= 2;
   return c;
 }
-// bytes of LDS: the groups' keys, later the candidates or the digit counts; the
+// bytes of LDS: the counts of maxima, later the candidates or the digit counts; the
 // list of groups
-__host__ __device__ constexpr int select_lds_keys(int G, int K) {
-  const int a = 4 * G, b = 8 * select_cap(K);
-  return ((a > b ? a : b) + 15) & ~15;
-}
-__host__ __device__ constexpr int select_lds(int G, int K) {
-  return select_lds_keys(G, K) + 2 * G;
-}
+__host__ __device__ constexpr int select_lds(int G, int K) { return 8 * select_cap(K) + 2 * G; }
 
 template <int NT>
 struct SelectShared {
-  int bound[kBoundBins];  // maxima by their distance from the largest
   int scan[NT / 64];
   int found, before;
   int n, nlist;
-  float logs;
+  float logs, sum[NT / 64];
   uint32_t whi[NT / 64];
 };
 
@@ -186,7 +191,8 @@ struct SelectShared {
 // and the count of the bins before it; hist holds nb = 2048 or 1024 bins.
 template <int NT>
 __device__ __forceinline__ void find_bin(SelectShared<NT>& s, const int* hist, int nb,
-                                         bool descending, int want, int& bin, int& before) {
+                                         bool descending, int want, int& bin, int& before,
+                                         int& count) {
   const int per = nb / NT, tid = threadIdx.x;
   int sum = 0;
   for (int i = 0; i < per; ++i) {
@@ -212,6 +218,7 @@ __device__ __forceinline__ void find_bin(SelectShared<NT>& s, const int* hist, i
   __syncthreads();
   bin = s.found;
   before = s.before;
+  count = hist[bin];
   __syncthreads();
 }
 
@@ -220,27 +227,52 @@ __device__ __forceinline__ int lanes_below(uint64_t b) {
   return __builtin_amdgcn_mbcnt_hi((uint32_t)(b >> 32), __builtin_amdgcn_mbcnt_lo((uint32_t)b, 0));
 }
 
-// f(in, key, v) for the VPT elements of a vector of each listed group, by all
-// lanes; `in` tells whether there is an element
-template <typename T, int NT, typename F>
+// f(in, key, v) for the VPT elements of a vector, by all lanes; `in` tells whether
+// there is an element. Of the listed groups (of GL lanes), or of the whole row.
+template <typename T, typename F>
+__device__ __forceinline__ void vector_keys(const Row<T>& row, bool have, int e, u32x4_t x, F&& f) {
+  constexpr int VPT = Row<T>::VPT;
+  bool in[VPT];
+  uint32_t k[VPT];
+#pragma unroll
+  for (int i = 0; i < VPT; ++i) {
+    in[i] = have && (unsigned)(e + i - row.shift) < (unsigned)row.V;
+    k[i] = order_key(Row<T>::elt(x, i));
+  }
+  f(in, k, e - row.shift);
+}
+template <typename T, int NT, int GL, typename F>
 __device__ __forceinline__ void listed_vectors(const Row<T>& row, const uint16_t* list, int n,
                                                F&& f) {
-  constexpr int GL = Row<T>::GL, VPT = Row<T>::VPT, GPW = 64 / GL;
+  constexpr int VPT = Row<T>::VPT, GPW = 64 / GL;
   const int lane = threadIdx.x & 63, wave = wave_id();
   for (int l0 = wave * GPW; l0 < n; l0 += NT / 64 * GPW) {
     const int l = l0 + lane / GL;
-    const bool have = l < n;
-    const int e = have ? (int)list[l] * kGroupCols + (lane & (GL - 1)) * VPT : 0;
-    const u32x4_t x = row.at(e);
-    bool in[VPT];
-    uint32_t k[VPT];
-#pragma unroll
-    for (int i = 0; i < VPT; ++i) {
-      in[i] = have && (unsigned)(e + i - row.shift) < (unsigned)row.V;
-      k[i] = order_key(Row<T>::elt(x, i));
-    }
-    f(in, k, e - row.shift);
+    const int e = l < n ? ((int)list[l] * GL + (lane & (GL - 1))) * VPT : 0;
+    vector_keys<T>(row, l < n, e, row.at(e), f);
   }
+}
+template <typename T, int NT, typename F>
+__device__ __forceinline__ void row_vectors(const Row<T>& row, F&& f) {
+  constexpr int VPT = Row<T>::VPT, R = 2;  // vectors read together
+  const int end = row.shift + row.V;
+  for (int e0 = threadIdx.x * VPT; e0 - (int)(threadIdx.x & 63) * VPT < end; e0 += R * NT * VPT) {
+    u32x4_t x[R];
+#pragma unroll
+    for (int j = 0; j < R; ++j) x[j] = row.at(e0 + j * NT * VPT);
+#pragma unroll
+    for (int j = 0; j < R; ++j) vector_keys<T>(row, true, e0 + j * NT * VPT, x[j], f);
+  }
+}
+// counts the lanes' bins: the first one's with one addition (most elements may be
+// equal), the others' by themselves
+__device__ __forceinline__ void count_bins(int* hist, bool in, int bin) {
+  const uint64_t act = __builtin_amdgcn_ballot_w64(in);
+  if (act == 0) return;
+  const int lead = __builtin_ctzll(act), first = __builtin_amdgcn_readlane(bin, lead);
+  const uint64_t same = __builtin_amdgcn_ballot_w64(in && bin == first);
+  if ((int)(threadIdx.x & 63) == lead) atomicAdd(&hist[first], __popcll(same));
+  if (in && bin != first) atomicAdd(&hist[bin], 1);
 }
 
 struct SelectArgs {
@@ -254,40 +286,70 @@ struct SelectArgs {
   float* scale;
 };
 
-template <typename T, int NT>
+template <typename T, int NT, bool DIRECT>
 __global__ __launch_bounds__(NT) void k_row_select(SelectArgs a) {
   extern __shared__ __align__(16) char lds[];
   __shared__ SelectShared<NT> s;
-  constexpr int VPT = Row<T>::VPT;
+  constexpr int VPT = Row<T>::VPT, GL = DIRECT ? 1 : Row<T>::GL;
+  constexpr int kUnroll = select_keys(NT, DIRECT);
   const int tid = threadIdx.x, lane = tid & 63, wave = wave_id();
   const int K = a.K, G = a.G, cap = select_cap(K);
   const int64_t r = blockIdx.x;
   const Row<T> row(a.logits, r * a.ld, a.V);
-  uint32_t* keys = reinterpret_cast<uint32_t*>(lds);
   uint64_t* cand = reinterpret_cast<uint64_t*>(lds);
   int* hist = reinterpret_cast<int*>(lds);
-  uint16_t* list = reinterpret_cast<uint16_t*>(lds + select_lds_keys(G, K));
+  uint16_t* list = reinterpret_cast<uint16_t*>(lds + 8 * cap);
 
-  // group maxima, the largest of them, and log of the row's sum of exp
-  uint32_t hi = 0;
-  const float* gm = a.gmax + r * G;
-  for (int i0 = tid; i0 < G; i0 += kUnroll * NT) {
+  // The group maxima as keys, some a thread: kept in registers where that holds all
+  // of them, else read again. f(keys, first
+  // group) takes keys of groups first, first + NT, ...; 0 where there is none
+  const float* gm = DIRECT ? nullptr : a.gmax + r * G;
+  uint32_t held[kUnroll];
+  u32x4_t x[DIRECT ? kUnroll : 1];
+  auto read_keys = [&](int i0, uint32_t* k) {
     float g[kUnroll];
 #pragma unroll
-    for (int j = 0; j < kUnroll; ++j) g[j] = i0 + j * NT < G ? gm[i0 + j * NT] : -INFINITY;
+    for (int j = 0; j < kUnroll; ++j) g[j] = i0 + j * NT < G ? gm[i0 + j * NT] : 0.f;
+#pragma unroll
+    for (int j = 0; j < kUnroll; ++j) k[j] = i0 + j * NT < G ? order_key(g[j]) : 0u;
+  };
+  const bool hold = DIRECT || G <= kUnroll * NT;
+  if constexpr (DIRECT) {
+#pragma unroll
+    for (int j = 0; j < kUnroll; ++j) x[j] = row.at((tid + j * NT) * VPT);
 #pragma unroll
     for (int j = 0; j < kUnroll; ++j) {
-      const uint32_t k = order_key(g[j]);
-      if (i0 + j * NT < G) keys[i0 + j * NT] = k;
-      hi = max(hi, k);
+      float m = Row<T>::elt(x[j], 0);
+#pragma unroll
+      for (int i = 1; i < VPT; ++i) m = fmaxf(m, Row<T>::elt(x[j], i));
+      held[j] = tid + j * NT < G ? order_key(m) : 0u;
     }
+  } else if (hold) {
+    read_keys(tid, held);
   }
+  auto all_keys = [&](auto&& f) {
+    if (hold) {
+      f(held, tid);
+    } else {
+      for (int i0 = tid; i0 - lane < G; i0 += kUnroll * NT) {
+        uint32_t k[kUnroll];
+        read_keys(i0, k);
+        f(k, i0);
+      }
+    }
+  };
+  // the largest of them, and log of the row's sum of exp
+  uint32_t hi = 0;
+  all_keys([&](const uint32_t* k, int) {
+#pragma unroll
+    for (int j = 0; j < kUnroll; ++j) hi = max(hi, k[j]);
+  });
 #pragma unroll
   for (int o = 32; o >= 1; o >>= 1) hi = max(hi, (uint32_t)__shfl_xor((int)hi, o));
   if (lane == 0) s.whi[wave] = hi;
   if (tid == 0) s.n = s.nlist = 0;
-  for (int i = tid; i < kBoundBins; i += NT) s.bound[i] = 0;
-  if (a.logprobs && wave == NT / 64 - 1) {
+  for (int i = tid; i < kBoundBins; i += NT) hist[i] = 0;
+  if (!DIRECT && a.logprobs && wave == NT / 64 - 1) {
     const float *pm = a.pm + r * a.nseg, *ps = a.ps + r * a.nseg;
     float m = -INFINITY, t = 0.f;
     for (int i = lane; i < a.nseg; i += 64) m = fmaxf(m, pm[i]);
@@ -301,20 +363,35 @@ __global__ __launch_bounds__(NT) void k_row_select(SelectArgs a) {
   hi = s.whi[lane % (NT / 64)];
 #pragma unroll
   for (int o = NT / 128; o >= 1; o >>= 1) hi = max(hi, (uint32_t)__shfl_xor((int)hi, o));
-  hi = (uint32_t)__builtin_amdgcn_readfirstlane((int)hi) >> 16;
+  hi = (uint32_t)__builtin_amdgcn_readfirstlane((int)hi);
+  if constexpr (DIRECT) {
+    if (a.logprobs) {
+      const float m = key_value(hi);
+      float t = 0.f;
+      if (m != -INFINITY) {
+#pragma unroll
+        for (int j = 0; j < kUnroll; ++j)
+#pragma unroll
+          for (int i = 0; i < VPT; ++i) t += exp_below(Row<T>::elt(x[j], i), m);
+      }
+      t = wave_sum(t);
+      if (lane == 0) s.sum[wave] = t;
+    }
+  }
+  hi >>= 16;
   // the largest 16-bit prefix that K maxima reach: by counts where it lies within
   // 1022 of the largest (eight factors of two), else by halving; 0 where K groups
   // do not exist
   uint32_t t = 0;
   if (K <= G) {
-    for (int i0 = tid; i0 < G; i0 += kUnroll * NT)
+    all_keys([&](const uint32_t* k, int) {
 #pragma unroll
       for (int j = 0; j < kUnroll; ++j)
-        if (i0 + j * NT < G)
-          atomicAdd(&s.bound[min(hi - (keys[i0 + j * NT] >> 16), (uint32_t)kBoundBins - 1)], 1);
+        if (k[j] != 0) atomicAdd(&hist[min(hi - (k[j] >> 16), (uint32_t)kBoundBins - 1)], 1);
+    });
     __syncthreads();
-    int bin, before;
-    find_bin<NT>(s, s.bound, kBoundBins, false, K, bin, before);
+    int bin, before, count;
+    find_bin<NT>(s, hist, kBoundBins, false, K, bin, before, count);
     if (bin < kBoundBins - 1) {
       t = hi - bin;
     } else {
@@ -322,7 +399,10 @@ __global__ __launch_bounds__(NT) void k_row_select(SelectArgs a) {
       while (top - t > 1) {
         const uint32_t mid = (t + top) / 2;
         int c = 0;
-        for (int i = tid; i < G; i += NT) c += keys[i] >> 16 >= mid;
+        all_keys([&](const uint32_t* k, int) {
+#pragma unroll
+          for (int j = 0; j < kUnroll; ++j) c += k[j] >> 16 >= mid;
+        });
 #pragma unroll
         for (int o = 32; o >= 1; o >>= 1) c += __shfl_xor(c, o);
         if (lane == 0) s.scan[wave] = c;
@@ -336,38 +416,31 @@ __global__ __launch_bounds__(NT) void k_row_select(SelectArgs a) {
     }
     t <<= 16;
   }
-  // the groups that reach it, one reservation per wave
-  int mine = 0;
-  for (int i0 = tid; i0 - lane < G; i0 += kUnroll * NT) {
+  t = max(t, kKeyNegInf + 1);
+  // the groups that reach it (a key is never 0), one reservation per wave
+  all_keys([&](const uint32_t* k, int i0) {
+    uint64_t b[kUnroll];
+    int total = 0;
 #pragma unroll
     for (int j = 0; j < kUnroll; ++j) {
-      const int i = i0 + j * NT;
-      mine += __popcll(__builtin_amdgcn_ballot_w64(i < G && keys[min(i, G - 1)] >= t));
+      b[j] = __builtin_amdgcn_ballot_w64(k[j] != 0 && k[j] >= t);
+      total += __popcll(b[j]);
     }
-  }
-  int at = 0;
-  if (lane == 0 && mine > 0) at = atomicAdd(&s.nlist, mine);
-  at = __builtin_amdgcn_readfirstlane(at);
-  for (int i0 = tid; i0 - lane < G; i0 += kUnroll * NT) {
-    bool q[kUnroll];
+    int at = 0;
+    if (lane == 0 && total > 0) at = atomicAdd(&s.nlist, total);
+    at = __builtin_amdgcn_readfirstlane(at);
 #pragma unroll
     for (int j = 0; j < kUnroll; ++j) {
-      const int i = i0 + j * NT;
-      q[j] = i < G && keys[min(i, G - 1)] >= t;
+      if (b[j] >> lane & 1) list[at + lanes_below(b[j])] = (uint16_t)(i0 + j * NT);
+      at += __popcll(b[j]);
     }
-#pragma unroll
-    for (int j = 0; j < kUnroll; ++j) {
-      const uint64_t b = __builtin_amdgcn_ballot_w64(q[j]);
-      if (q[j]) list[at + lanes_below(b)] = (uint16_t)(i0 + j * NT);
-      at += __popcll(b);
-    }
-  }
+  });
   __syncthreads();
   const int nlist = s.nlist;
 
   // elements with key > kth, or = kth and an index up to vcut, as candidates
-  auto gather = [&](uint32_t kth, int vcut) {
-    listed_vectors<T, NT>(row, list, nlist, [&](const bool* in, const uint32_t* k, int v) {
+  auto collect = [&](uint32_t kth, int vcut) {
+    return [=](const bool* in, const uint32_t* k, int v) {
       uint64_t b[VPT];
       int total = 0;
 #pragma unroll
@@ -386,55 +459,91 @@ __global__ __launch_bounds__(NT) void k_row_select(SelectArgs a) {
           cand[o] = (uint64_t)k[i] << 32 | (0xffffffffu - (uint32_t)(v + i));
         to += __popcll(b[i]);
       }
-    });
-    __syncthreads();
+    };
   };
-  gather(t, 0x7fffffff);
+  listed_vectors<T, NT, GL>(row, list, nlist, collect(t - 1, -1));
+  __syncthreads();
   int n = s.n;
+  __syncthreads();  // (before any wave adds to it again)
   if (n > cap) {
-    // the K-th largest exactly: its key in digits of 11, 11 and 10 bits, then,
-    // where not all elements of that key are wanted, the index of the last one
+    // the K-th largest exactly: its key in digits of 11 and 5 bits, in fp32 11, 11 and
+    // 10 (keys of bf16 have 16 bits of their own)
     uint32_t kth = 0;
-    int want = K;
-    const int shifts[3] = {21, 10, 0};
+    int want = K, ties = 0;
+    constexpr int kDigits = sizeof(T) == 2 ? 2 : 3;
+    constexpr int kShift[3] = {21, sizeof(T) == 2 ? 16 : 10, 0};
+    constexpr uint32_t kMask[3] = {0u, 0xffe00000u, 0xfffffc00u};
 #pragma unroll
-    for (int d = 0; d < 3; ++d) {
-      const int sh = shifts[d], nb = d == 2 ? 1024 : kHistBins;
-      const uint32_t mask = d == 0 ? 0u : d == 1 ? 0xffe00000u : 0xfffffc00u;
+    for (int d = 0; d < kDigits; ++d) {
+      const int nb = d == 2 ? 1024 : kHistBins, sh = kShift[d];
       for (int i = tid; i < nb; i += NT) hist[i] = 0;
       __syncthreads();
-      listed_vectors<T, NT>(row, list, nlist, [&](const bool* in, const uint32_t* k, int) {
+      row_vectors<T, NT>(row, [&](const bool* in, const uint32_t* k, int) {
 #pragma unroll
         for (int i = 0; i < VPT; ++i)
-          if (in[i] && (k[i] & mask) == kth) atomicAdd(&hist[(k[i] >> sh) & (nb - 1)], 1);
+          count_bins(hist, in[i] && (k[i] & kMask[d]) == kth,
+                     (int)(k[i] >> sh & (sizeof(T) == 2 && d == 1 ? 31 : nb - 1)));
       });
       __syncthreads();
       int bin, before;
-      find_bin<NT>(s, hist, nb, true, want, bin, before);
+      find_bin<NT>(s, hist, nb, true, want, bin, before, ties);
       kth |= (uint32_t)bin << sh;
       want -= before;
     }
-    int vcut = 0;
+    if (sizeof(T) == 2 && !(kth & 0x80000000u)) kth |= 0xffffu;
+    // of more elements with that key than are wanted, those of the lowest indices:
+    // columns in their order until there are enough
+    int vcut = 0x7fffffff;
+    if (ties > want) {
+      int seen = 0;
+      for (int e0 = 0; e0 < row.shift + row.V; e0 += NT * VPT) {
+        const int e = e0 + tid * VPT;
+        int mine = 0;
+        uint32_t hits = 0;
+        vector_keys<T>(row, true, e, row.at(e), [&](const bool* in, const uint32_t* k, int) {
 #pragma unroll
-    for (int d = 0; d < 2; ++d) {
-      for (int i = tid; i < 1024; i += NT) hist[i] = 0;
-      __syncthreads();
-      const int first = vcut;
-      listed_vectors<T, NT>(row, list, nlist, [&](const bool* in, const uint32_t* k, int v) {
-#pragma unroll
-        for (int i = 0; i < VPT; ++i)
-          if (in[i] && k[i] == kth && (d == 0 || (v + i) >> 10 == first >> 10))
-            atomicAdd(&hist[d == 0 ? (v + i) >> 10 : (v + i) & 1023], 1);
-      });
-      __syncthreads();
-      int bin, before;
-      find_bin<NT>(s, hist, 1024, false, want, bin, before);
-      vcut |= d == 0 ? bin << 10 : bin;
-      want -= before;
+          for (int i = 0; i < VPT; ++i)
+            if (in[i] && k[i] == kth) {
+              ++mine;
+              hits |= 1u << i;
+            }
+        });
+        int incl = wave_incl_scan(mine);
+        if (lane == 63) s.scan[wave] = incl;
+        __syncthreads();
+        int total = 0;
+        for (int w = 0; w < NT / 64; ++w) {
+          if (w < wave) incl += s.scan[w];
+          total += s.scan[w];
+        }
+        const int need = want - seen - (incl - mine);  // of this thread's, the last wanted
+        if (need >= 1 && need <= mine) {
+          for (int i = 1; i < need; ++i) hits &= hits - 1;
+          s.found = e - row.shift + __builtin_ctz(hits);
+        }
+        seen += total;
+        __syncthreads();
+        if (seen >= want) break;
+      }
+      vcut = s.found;
     }
     if (tid == 0) s.n = 0;
     __syncthreads();
-    gather(kth, vcut);
+    row_vectors<T, NT>(row, collect(kth, vcut));
+    __syncthreads();
+    n = s.n;
+  } else if (n < K) {
+    // fewer than K above -inf: of the first K columns as many as it takes are -inf
+    for (int v0 = 0; v0 < K; v0 += NT) {
+      const int v = v0 + tid;
+      const bool q = v < K && !((float)row.p[v] > -INFINITY);
+      const uint64_t b = __builtin_amdgcn_ballot_w64(q);
+      int to = 0;
+      if (lane == 0 && b != 0) to = atomicAdd(&s.n, __popcll(b));
+      to = __builtin_amdgcn_readfirstlane(to) + lanes_below(b);
+      if (q) cand[to] = (uint64_t)kKeyNegInf << 32 | (0xffffffffu - (uint32_t)v);
+    }
+    __syncthreads();
     n = s.n;
   }
   // sorted, largest first: each candidate's rank among all of them, by as many
@@ -470,7 +579,13 @@ __global__ __launch_bounds__(NT) void k_row_select(SelectArgs a) {
   __syncthreads();
 
   const float z0 = key_value((uint32_t)(cand[0] >> 32));
-  const float logs = a.logprobs ? s.logs : 0.f;
+  float logs = 0.f;
+  if (a.logprobs && DIRECT) {
+    for (int w = 0; w < NT / 64; ++w) logs += s.sum[w];
+    logs = z0 == -INFINITY ? 0.f : logf(logs);
+  } else if (a.logprobs) {
+    logs = s.logs;
+  }
   if (a.value != nullptr) {
     for (int k = tid; k < K; k += NT) {
       const uint64_t c = cand[k];
@@ -1267,23 +1382,37 @@ constexpr int kSelectManyEntries = 512;
 
 template <typename T>
 static int launch_topk(const KdTopkArgs& a, hipStream_t s) {
+  const T* x = static_cast<const T*>(a.logits);
+  SelectArgs q{a.logits, a.ld, a.V, a.K, 0, a.nseg, a.logprobs, a.gmax, a.pm, a.ps,
+               a.idx, a.value, a.entries, a.scale};
+  const dim3 rows((unsigned)a.rows);
+  const bool wide = a.rows <= kSelectFewRows || a.K > kSelectManyEntries;
+  // vectors of a row, wherever it starts
+  constexpr int VPT = Row<T>::VPT;
+  const int vectors = (a.V + 2 * (VPT - 1)) / VPT;
+  if (vectors <= (wide ? 1024 * select_keys(1024, true) : 256 * select_keys(256, true))) {
+    q.G = vectors;
+    const size_t lds = select_lds(q.G, a.K);
+    if (wide)
+      hipLaunchKernelGGL((k_row_select<T, 1024, true>), rows, dim3(1024), lds, s, q);
+    else
+      hipLaunchKernelGGL((k_row_select<T, 256, true>), rows, dim3(256), lds, s, q);
+    return (int)hipGetLastError();
+  }
   const int64_t waves = a.rows * a.nseg;
   const dim3 grid((unsigned)((waves + 3) / 4));
-  const T* x = static_cast<const T*>(a.logits);
   if (a.logprobs)
     hipLaunchKernelGGL((k_row_groups<T, true>), grid, dim3(256), 0, s, x, a.ld, a.V, a.nseg,
                        (int)waves, a.gmax, a.pm, a.ps);
   else
     hipLaunchKernelGGL((k_row_groups<T, false>), grid, dim3(256), 0, s, x, a.ld, a.V, a.nseg,
                        (int)waves, a.gmax, (float*)nullptr, (float*)nullptr);
-  const int G = a.nseg * kSegGroups;
-  const SelectArgs q{a.logits, a.ld, a.V, a.K, G, a.nseg, a.logprobs, a.gmax, a.pm, a.ps,
-                     a.idx, a.value, a.entries, a.scale};
-  const size_t lds = select_lds(G, a.K);
-  if (a.rows <= kSelectFewRows || a.K > kSelectManyEntries)
-    hipLaunchKernelGGL((k_row_select<T, 1024>), dim3((unsigned)a.rows), dim3(1024), lds, s, q);
+  q.G = a.nseg * kSegGroups;
+  const size_t lds = select_lds(q.G, a.K);
+  if (wide)
+    hipLaunchKernelGGL((k_row_select<T, 1024, false>), rows, dim3(1024), lds, s, q);
   else
-    hipLaunchKernelGGL((k_row_select<T, 256>), dim3((unsigned)a.rows), dim3(256), lds, s, q);
+    hipLaunchKernelGGL((k_row_select<T, 256, false>), rows, dim3(256), lds, s, q);
   return (int)hipGetLastError();
 }
 

@@ -69,7 +69,7 @@ kd_status topk(const kd_rows* p, const void* logits, int32_t* idx, float* value,
   a.dtype = p->dtype;
   a.V = (int)p->V;
   a.K = p->K;
-  a.nseg = (int)t.nseg;
+  a.nseg = (int)kd_row_segs(p->V, eb, aligned(logits, 16) && p->ld * eb % 16 == 0);
   a.logprobs = (p->flags & KD_FLAG_TEACHER_LOGPROBS) ? 1 : 0;
   a.gmax = reinterpret_cast<float*>(ws);
   a.pm = reinterpret_cast<float*>(ws + t.off_pm);
@@ -235,7 +235,10 @@ kd_status kd_verify_draft(const kd_draft* p, const void* target_logits,
   a.T = (int)p->T;
   a.V = (int)p->V;
   a.K = p->K;
-  a.nseg = (int)t.nseg;
+  // (places count from the target's boundaries in the draft's rows too)
+  a.nseg = (int)kd_row_segs(p->V, eb, aligned(target_logits, 16) && p->ld_target * eb % 16 == 0 &&
+                                          (!dense || (aligned(draft_logits, 16) &&
+                                                      p->ld_draft * eb % 16 == 0)));
   a.tokens = draft_tokens;
   a.didx = draft_idx;
   a.dlogit = draft_logit;

@@ -30,7 +30,7 @@ def _logits(N, V, dtype, seed, ld=None, offset=0, std=5.0):
 
 
 SPECIALS = ("plain", "ties", "constant", "masked", "lowest", "nan", "inf", "ascending", "wide",
-            "logprobs")
+            "logprobs", "two", "halves")
 
 
 def _special(x, kind):
@@ -63,6 +63,13 @@ def _special(x, kind):
         x.copy_(x.sign() * torch.exp2(e))
     elif kind == "logprobs":         # one column near 0, the others far below
         x.copy_(torch.log_softmax(x.float() * 3, 1) - 1e-5)
+    elif kind == "two":              # more equal ones than wanted below a few larger
+        big = x > 6
+        x.fill_(-2.0)
+        x[big] = 3.0
+    elif kind == "halves":           # the same at the end of the row only, -inf before
+        x[:, V // 2:] = 1.25
+        x[:, :V // 2] = float("-inf")
     elif kind == "ascending":
         x.copy_(torch.arange(V, device=x.device).to(x.dtype) * 0.5)
     return x
@@ -92,7 +99,9 @@ def _check_topk(kd, x, K):
 @pytest.mark.parametrize("dtype", ["bf16", "f32"])
 @pytest.mark.parametrize("N,V,K,ld,offset", [
     (3, 1, 1, None, 0), (4, 7, 7, 9, 1), (5, 64, 3, None, 3), (3, 300, 300, 301, 5),
-    (2, 2049, 100, 2051, 7), (3, 6500, 100, None, 0), (2, 32003, 257, 32005, 2)])
+    (2, 2049, 100, 2051, 7), (3, 6500, 100, None, 0), (2, 32003, 257, 32005, 2),
+    (2, 70001, 300, 70003, 1), (3, 132000, 100, None, 0), (520, 20000, 64, None, 0),
+    (515, 3000, 200, 3001, 0)])
 def test_topk_entries(gpu_lib, N, V, K, ld, offset, dtype, kind):
     print(f"[topk] {N} {V} {K} ld={ld} +{offset} {dtype} {kind}", flush=True)
     x = _logits(N, V, dtype, 11, ld, offset)
