@@ -97,6 +97,45 @@ __device__ __forceinline__ float exp_below(float z, float m) {
 }
 
 // ------------------------------------------------------------- top-K rows ----
+// Largest values of the 32 groups of the wave's segment: group i of the segment in
+// lane `lane` with group_of(lane) = i, for the lanes that hold one. `top`: the lane's
+// largest (of its groups).
+template <typename T>
+__device__ __forceinline__ float group_maxima(const u32x4_t* x, float& top) {
+  constexpr int U = Row<T>::U, VPT = Row<T>::VPT, GL = Row<T>::GL;
+  static_assert(U <= GL, "a lane of each group keeps each vector's maximum");
+  const int lane = threadIdx.x & 63;
+  float mine = -INFINITY;
+  top = -INFINITY;
+#pragma unroll
+  for (int u = 0; u < U; ++u) {
+    float m = Row<T>::elt(x[u], 0);
+#pragma unroll
+    for (int i = 1; i < VPT; ++i) m = fmaxf(m, Row<T>::elt(x[u], i));
+#pragma unroll
+    for (int c = 0; c < (GL == 8 ? 3 : 4); ++c) m = fmaxf(m, dpp_f(m, c));
+    if ((lane & (GL - 1)) == u) mine = m;
+    top = fmaxf(top, m);
+  }
+  return mine;
+}
+template <typename T>
+__device__ __forceinline__ int group_of(int lane) {  // -1: none
+  constexpr int U = Row<T>::U, GL = Row<T>::GL;
+  const int u = lane & (GL - 1);
+  return u < U ? u * (64 / GL) + lane / GL : -1;
+}
+// sum of exp below m > -inf over the lane's elements
+template <typename T>
+__device__ __forceinline__ float exp_sum(const u32x4_t* x, float m) {
+  float s = 0.f;
+#pragma unroll
+  for (int u = 0; u < Row<T>::U; ++u)
+#pragma unroll
+    for (int i = 0; i < Row<T>::VPT; ++i) s += exp_below(Row<T>::elt(x[u], i), m);
+  return s;
+}
+
 // First pass, the one that reads the logits: the largest value of each group of
 // 64 columns, and with LSE the segment's maximum and sum of exp below it. A wave
 // per segment, no LDS and no barrier: bound by the read (the exponentials and
@@ -110,34 +149,15 @@ __global__ __launch_bounds__(256) void k_row_groups(const T* __restrict__ logits
   if (w >= waves) return;
   const int r = w / nseg, seg = w - r * nseg;
   const Row<T> row(logits, (int64_t)r * ld, V);
-  constexpr int U = Row<T>::U, VPT = Row<T>::VPT, GL = Row<T>::GL;
-  u32x4_t x[U];
+  u32x4_t x[Row<T>::U];
   row.segment(seg, x);
-  const int lane = threadIdx.x & 63;
-  float mine = -INFINITY, top = -INFINITY;
-#pragma unroll
-  for (int u = 0; u < U; ++u) {
-    float m = Row<T>::elt(x[u], 0);
-#pragma unroll
-    for (int i = 1; i < VPT; ++i) m = fmaxf(m, Row<T>::elt(x[u], i));
-#pragma unroll
-    for (int c = 0; c < (GL == 8 ? 3 : 4); ++c) m = fmaxf(m, dpp_f(m, c));
-    if ((lane & (GL - 1)) == u) mine = m;  // (U <= GL)
-    top = fmaxf(top, m);
-  }
-  static_assert(U <= GL, "a lane of each group keeps each vector's maximum");
-  if ((lane & (GL - 1)) < U)
-    gmax[(int64_t)w * kSegGroups + (lane & (GL - 1)) * (64 / GL) + lane / GL] = mine;
+  const int lane = threadIdx.x & 63, g = group_of<T>(lane);
+  float top;
+  const float mine = group_maxima<T>(x, top);
+  if (g >= 0) gmax[(int64_t)w * kSegGroups + g] = mine;
   if constexpr (LSE) {
     top = wave_max(top);
-    float s = 0.f;
-    if (top != -INFINITY) {
-#pragma unroll
-      for (int u = 0; u < U; ++u)
-#pragma unroll
-        for (int i = 0; i < VPT; ++i) s += exp_below(Row<T>::elt(x[u], i), top);
-    }
-    s = wave_sum(s);
+    const float s = wave_sum(top != -INFINITY ? exp_sum<T>(x, top) : 0.f);
     if (lane == 0) {
       pm[w] = top;
       ps[w] = s;
@@ -158,9 +178,13 @@ __global__ __launch_bounds__(256) void k_row_groups(const T* __restrict__ logits
 // never are candidates: where the row has too few others, the list is filled up
 // from its first columns.
 //
-// DIRECT (rows of up to 8 vectors a thread): the only pass. The row is held in
+// kDirect (rows of up to 8 vectors a thread): the only pass. The row is held in
 // registers, its groups are single vectors, and their maxima and the sum of exp
 // are formed here: one launch, and groups enough for K above V / 64.
+//
+// kStream (rows of up to 2048 groups, many of them): the only pass too, the first
+// pass's work done by the row's workgroup. While some workgroups wait for their
+// scattered reads, others stream.
 //
 // The pass is latency-bound (a few dependent reads and barriers per row), so what
 // counts is rows in flight, and for few rows the time of one.
@@ -183,7 +207,7 @@ struct SelectShared {
   int scan[NT / 64];
   int found, before;
   int n, nlist;
-  float logs, sum[NT / 64];
+  float logs, sum[NT / 64], top[NT / 64];
   uint32_t whi[NT / 64];
 };
 
@@ -286,8 +310,10 @@ struct SelectArgs {
   float* scale;
 };
 
-template <typename T, int NT, bool DIRECT>
+enum SelectMode { kFromMaxima, kDirect, kStream };
+template <typename T, int NT, SelectMode MODE>
 __global__ __launch_bounds__(NT) void k_row_select(SelectArgs a) {
+  constexpr bool DIRECT = MODE == kDirect, STREAM = MODE == kStream;
   extern __shared__ __align__(16) char lds[];
   __shared__ SelectShared<NT> s;
   constexpr int VPT = Row<T>::VPT, GL = DIRECT ? 1 : Row<T>::GL;
@@ -303,7 +329,7 @@ __global__ __launch_bounds__(NT) void k_row_select(SelectArgs a) {
   // The group maxima as keys, some a thread: kept in registers where that holds all
   // of them, else read again. f(keys, first
   // group) takes keys of groups first, first + NT, ...; 0 where there is none
-  const float* gm = DIRECT ? nullptr : a.gmax + r * G;
+  const float* gm = MODE == kFromMaxima ? a.gmax + r * G : nullptr;
   uint32_t held[kUnroll];
   u32x4_t x[DIRECT ? kUnroll : 1];
   auto read_keys = [&](int i0, uint32_t* k) {
@@ -313,7 +339,7 @@ __global__ __launch_bounds__(NT) void k_row_select(SelectArgs a) {
 #pragma unroll
     for (int j = 0; j < kUnroll; ++j) k[j] = i0 + j * NT < G ? order_key(g[j]) : 0u;
   };
-  const bool hold = DIRECT || G <= kUnroll * NT;
+  const bool hold = MODE != kFromMaxima || G <= kUnroll * NT;
   if constexpr (DIRECT) {
 #pragma unroll
     for (int j = 0; j < kUnroll; ++j) x[j] = row.at((tid + j * NT) * VPT);
@@ -324,6 +350,37 @@ __global__ __launch_bounds__(NT) void k_row_select(SelectArgs a) {
       for (int i = 1; i < VPT; ++i) m = fmaxf(m, Row<T>::elt(x[j], i));
       held[j] = tid + j * NT < G ? order_key(m) : 0u;
     }
+  } else if constexpr (STREAM) {
+    uint32_t* keys = reinterpret_cast<uint32_t*>(lds);
+    const int g = group_of<T>(lane);
+    u32x4_t y[Row<T>::U];
+    float m = -INFINITY, t = 0.f;  // the wave's largest, the lane's sum of exp below it
+    if (wave < a.nseg) row.segment(wave, y);
+    for (int seg = wave; seg < a.nseg; seg += NT / 64) {
+      u32x4_t next[Row<T>::U];
+      if (seg + NT / 64 < a.nseg) row.segment(seg + NT / 64, next);
+      float top;
+      const float mine = group_maxima<T>(y, top);
+      if (g >= 0) keys[seg * kSegGroups + g] = order_key(mine);
+      if (a.logprobs) {
+        top = fmaxf(wave_max(top), m);
+        if (top != -INFINITY) t = t * exp_below(m, top) + exp_sum<T>(y, top);
+        m = top;
+      }
+#pragma unroll
+      for (int u = 0; u < Row<T>::U; ++u) y[u] = next[u];
+    }
+    if (a.logprobs) {
+      t = wave_sum(t);
+      if (lane == 0) {
+        s.sum[wave] = t;
+        s.top[wave] = m;
+      }
+    }
+    __syncthreads();
+#pragma unroll
+    for (int j = 0; j < kUnroll; ++j) held[j] = tid + j * NT < G ? keys[tid + j * NT] : 0u;
+    __syncthreads();
   } else if (hold) {
     read_keys(tid, held);
   }
@@ -349,7 +406,7 @@ __global__ __launch_bounds__(NT) void k_row_select(SelectArgs a) {
   if (lane == 0) s.whi[wave] = hi;
   if (tid == 0) s.n = s.nlist = 0;
   for (int i = tid; i < kBoundBins; i += NT) hist[i] = 0;
-  if (!DIRECT && a.logprobs && wave == NT / 64 - 1) {
+  if (MODE == kFromMaxima && a.logprobs && wave == NT / 64 - 1) {
     const float *pm = a.pm + r * a.nseg, *ps = a.ps + r * a.nseg;
     float m = -INFINITY, t = 0.f;
     for (int i = lane; i < a.nseg; i += 64) m = fmaxf(m, pm[i]);
@@ -580,8 +637,8 @@ __global__ __launch_bounds__(NT) void k_row_select(SelectArgs a) {
 
   const float z0 = key_value((uint32_t)(cand[0] >> 32));
   float logs = 0.f;
-  if (a.logprobs && DIRECT) {
-    for (int w = 0; w < NT / 64; ++w) logs += s.sum[w];
+  if (a.logprobs && MODE != kFromMaxima) {
+    for (int w = 0; w < NT / 64; ++w) logs += STREAM ? s.sum[w] * exp_below(s.top[w], z0) : s.sum[w];
     logs = z0 == -INFINITY ? 0.f : logf(logs);
   } else if (a.logprobs) {
     logs = s.logs;
@@ -1377,7 +1434,7 @@ __global__ __launch_bounds__(kVerThreads) void k_pick(VerifyArgs a) {
 // ================================================================ launchers ==
 using namespace kd;
 
-constexpr int64_t kSelectFewRows = 512;
+constexpr int64_t kSelectFewRows = 512, kSelectStreamRows = 1024;
 constexpr int kSelectManyEntries = 512;
 
 template <typename T>
@@ -1394,9 +1451,15 @@ static int launch_topk(const KdTopkArgs& a, hipStream_t s) {
     q.G = vectors;
     const size_t lds = select_lds(q.G, a.K);
     if (wide)
-      hipLaunchKernelGGL((k_row_select<T, 1024, true>), rows, dim3(1024), lds, s, q);
+      hipLaunchKernelGGL((k_row_select<T, 1024, kDirect>), rows, dim3(1024), lds, s, q);
     else
-      hipLaunchKernelGGL((k_row_select<T, 256, true>), rows, dim3(256), lds, s, q);
+      hipLaunchKernelGGL((k_row_select<T, 256, kDirect>), rows, dim3(256), lds, s, q);
+    return (int)hipGetLastError();
+  }
+  q.G = a.nseg * kSegGroups;
+  const size_t lds = select_lds(q.G, a.K);
+  if (!wide && a.rows >= kSelectStreamRows && q.G <= 256 * select_keys(256, true)) {
+    hipLaunchKernelGGL((k_row_select<T, 256, kStream>), rows, dim3(256), lds, s, q);
     return (int)hipGetLastError();
   }
   const int64_t waves = a.rows * a.nseg;
@@ -1407,12 +1470,10 @@ static int launch_topk(const KdTopkArgs& a, hipStream_t s) {
   else
     hipLaunchKernelGGL((k_row_groups<T, false>), grid, dim3(256), 0, s, x, a.ld, a.V, a.nseg,
                        (int)waves, a.gmax, (float*)nullptr, (float*)nullptr);
-  q.G = a.nseg * kSegGroups;
-  const size_t lds = select_lds(q.G, a.K);
   if (wide)
-    hipLaunchKernelGGL((k_row_select<T, 1024, false>), rows, dim3(1024), lds, s, q);
+    hipLaunchKernelGGL((k_row_select<T, 1024, kFromMaxima>), rows, dim3(1024), lds, s, q);
   else
-    hipLaunchKernelGGL((k_row_select<T, 256, false>), rows, dim3(256), lds, s, q);
+    hipLaunchKernelGGL((k_row_select<T, 256, kFromMaxima>), rows, dim3(256), lds, s, q);
   return (int)hipGetLastError();
 }
 
