@@ -8,6 +8,7 @@ PyTorch fallback: if the library is missing, the calls raise.
 from __future__ import annotations
 
 import ctypes
+import functools
 import os
 from typing import Optional
 
@@ -205,8 +206,7 @@ def _check_inputs(hidden, W, teacher_idx, teacher_logit, ignore, checkpoint=Fals
 
 def _check_tensor(name, t, shape, dtype, device):
     """A caller-provided output or extra input: exact shape, dtype, device, layout."""
-    if tuple(t.shape) != tuple(shape) or t.dtype != dtype or t.device != device \
-            or not t.is_contiguous():
+    if t.shape != shape or t.dtype != dtype or t.device != device or not t.is_contiguous():
         raise ValueError(f"{name} must be a contiguous {dtype} tensor of shape {tuple(shape)} "
                          f"on {device} (got {t.dtype} {tuple(t.shape)} on {t.device})")
 
@@ -622,6 +622,24 @@ def check_indices(teacher_idx, V, chunk=4096, D=64, tau=1.0, dtype=KD_BF16, work
     return True
 
 
+def _call(name, device, *args):
+    """One call of the library on device's current stream (the last argument); tensors
+    are passed as they are, None as NULL. The small operators' calls take a few
+    microseconds on the GPU, so the host's part counts: the device is switched to
+    only where it is not the current one."""
+    import torch
+    fn = getattr(_lib, name)
+    args = [a.data_ptr() if isinstance(a, torch.Tensor) else a for a in args]
+    stream = torch.cuda.current_stream(device).cuda_stream
+    if torch.cuda.current_device() == device.index:
+        rc = fn(*args, stream)
+    else:
+        with torch.cuda.device(device):
+            rc = fn(*args, stream)
+    if rc != 0:
+        raise KdError(rc, name)
+
+
 def _logits_rows(name, logits, dim):
     """dtype code and element stride of the rows of logits[..., V]: the last
     dimension contiguous, the rows evenly spaced."""
@@ -651,30 +669,26 @@ def _logits_rows(name, logits, dim):
 def _topk_rows(logits, K, logprobs, workspace):
     """The problem and workspace of a selection, with its checks."""
     import torch
-    lib = load_library()
+    load_library()
     code, ld = _logits_rows("logits", logits, 2)
     N, V = logits.shape
-    pr = KdRows(N, V, ld, int(K), code, KD_FLAG_TEACHER_LOGPROBS if logprobs else 0)
     if workspace is None:
-        n = ctypes.c_size_t(0)
-        rc = lib.kd_topk_entries_workspace_size(ctypes.byref(pr), ctypes.byref(n))
-        if rc != 0:
-            raise KdError(rc, "kd_topk_entries_workspace_size")
-        workspace = torch.empty(n.value, dtype=torch.uint8, device=logits.device)
+        workspace = torch.empty(topk_workspace_size(N, V, int(K), code), dtype=torch.uint8,
+                                device=logits.device)
     _check_workspace(workspace, logits.device)
-    return lib, pr, workspace
+    return KdRows(N, V, ld, int(K), code, KD_FLAG_TEACHER_LOGPROBS if logprobs else 0), workspace
 
 
 def _out_tensors(out, want, device):
     """The outputs of `want` (name -> (shape, dtype)): from `out`, checked, or new."""
     import torch
-    out = dict(out or {})
     res = {}
     for name, (shape, dtype) in want.items():
-        t = out.get(name)
+        t = out.get(name) if out else None
         if t is None:
             t = torch.empty(shape, dtype=dtype, device=device)
-        _check_tensor(name, t, shape, dtype, device)
+        else:
+            _check_tensor(name, t, shape, dtype, device)
         res[name] = t
     return res
 
@@ -687,19 +701,16 @@ def topk_entries(logits, K, logprobs: bool = False, out=None, workspace=None):
     whole vocabulary with logprobs (for teacher_logprobs=True). `out` may carry
     the outputs, `workspace` a uint8 tensor of topk_workspace_size bytes."""
     import torch
-    lib, pr, workspace = _topk_rows(logits, K, logprobs, workspace)
+    pr, workspace = _topk_rows(logits, K, logprobs, workspace)
     dev = logits.device
     res = _out_tensors(out, {"teacher_idx": ((pr.N, pr.K), torch.int32),
                              "teacher_logit": ((pr.N, pr.K), torch.float32)}, dev)
-    with torch.cuda.device(dev):
-        rc = lib.kd_topk_entries(ctypes.byref(pr), _ptr(logits), _ptr(res["teacher_idx"]),
-                                 _ptr(res["teacher_logit"]), _ptr(workspace),
-                                 ctypes.c_size_t(workspace.numel()), _stream_handle(dev))
-    if rc != 0:
-        raise KdError(rc, "kd_topk_entries")
+    _call("kd_topk_entries", dev, pr, logits, res["teacher_idx"], res["teacher_logit"], workspace,
+          workspace.numel())
     return res
 
 
+@functools.lru_cache(maxsize=256)
 def topk_workspace_size(N, V, K, dtype=KD_BF16) -> int:
     """Bytes of workspace of topk_entries and teacher_cache_write."""
     n = ctypes.c_size_t(0)
@@ -716,16 +727,12 @@ def teacher_cache_write(logits, K, logprobs: bool = False, out=None, workspace=N
     int32 (index << 12 | code), 'scale' [N, 2] fp32 (top, step)}; `out` may
     carry them, e.g. as rows of a larger cache."""
     import torch
-    lib, pr, workspace = _topk_rows(logits, K, logprobs, workspace)
+    pr, workspace = _topk_rows(logits, K, logprobs, workspace)
     dev = logits.device
     res = _out_tensors(out, {"entries": ((pr.N, pr.K), torch.int32),
                              "scale": ((pr.N, 2), torch.float32)}, dev)
-    with torch.cuda.device(dev):
-        rc = lib.kd_teacher_cache_write(ctypes.byref(pr), _ptr(logits), _ptr(res["entries"]),
-                                        _ptr(res["scale"]), _ptr(workspace),
-                                        ctypes.c_size_t(workspace.numel()), _stream_handle(dev))
-    if rc != 0:
-        raise KdError(rc, "kd_teacher_cache_write")
+    _call("kd_teacher_cache_write", dev, pr, logits, res["entries"], res["scale"], workspace,
+          workspace.numel())
     return res
 
 
@@ -735,7 +742,7 @@ def teacher_cache_read(entries, scale, rows=None, out=None):
     {'teacher_idx' [M, K], 'teacher_logit' [M, K], 'ignore' [M] uint8}; ignore is
     1 for a token without a target."""
     import torch
-    lib = load_library()
+    load_library()
     if entries.device.type != "cuda":
         raise ValueError("tensors must be on a GPU")
     if entries.dim() != 2:
@@ -753,12 +760,8 @@ def teacher_cache_read(entries, scale, rows=None, out=None):
     res = _out_tensors(out, {"teacher_idx": ((M, K), torch.int32),
                              "teacher_logit": ((M, K), torch.float32),
                              "ignore": ((M,), torch.uint8)}, dev)
-    with torch.cuda.device(dev):
-        rc = lib.kd_teacher_cache_read(N, K, _ptr(entries), _ptr(scale), _ptr(rows), M,
-                                       _ptr(res["teacher_idx"]), _ptr(res["teacher_logit"]),
-                                       _ptr(res["ignore"]), _stream_handle(dev))
-    if rc != 0:
-        raise KdError(rc, "kd_teacher_cache_read")
+    _call("kd_teacher_cache_read", dev, N, K, entries, scale, rows, M, res["teacher_idx"],
+          res["teacher_logit"], res["ignore"])
     return res
 
 
@@ -767,7 +770,7 @@ def checkpoint_write(hidden, out=None):
     D a multiple of 32) in 8 bits, {'codes' [N, D] uint8 (e4m3), 'scales'
     [N, D / 32] uint8 (power of two, biased by 127)}."""
     import torch
-    lib = load_library()
+    load_library()
     if hidden.device.type != "cuda":
         raise ValueError("tensors must be on a GPU")
     if hidden.dim() != 2 or not hidden.is_contiguous():
@@ -776,11 +779,7 @@ def checkpoint_write(hidden, out=None):
     N, D = hidden.shape
     res = _out_tensors(out, {"codes": ((N, D), torch.uint8),
                              "scales": ((N, D // 32), torch.uint8)}, dev)
-    with torch.cuda.device(dev):
-        rc = lib.kd_checkpoint_write(N, D, code, _ptr(hidden), _ptr(res["codes"]),
-                                     _ptr(res["scales"]), _stream_handle(dev))
-    if rc != 0:
-        raise KdError(rc, "kd_checkpoint_write")
+    _call("kd_checkpoint_write", dev, N, D, code, hidden, res["codes"], res["scales"])
     return res
 
 
@@ -800,16 +799,13 @@ def checkpoint_read(codes, scales, dtype, out=None):
     """kd_checkpoint_read on the current stream: the hidden states [N, D] that a
     checkpoint holds, in dtype (torch.bfloat16 or torch.float32)."""
     import torch
-    lib = load_library()
+    load_library()
     N, D, dev = _check_checkpoint(codes, scales)
     code = _dtype_code(dtype)
     hidden = torch.empty(N, D, dtype=dtype, device=dev) if out is None else out
-    _check_tensor("out", hidden, (N, D), dtype, dev)
-    with torch.cuda.device(dev):
-        rc = lib.kd_checkpoint_read(N, D, code, _ptr(codes), _ptr(scales), _ptr(hidden),
-                                    _stream_handle(dev))
-    if rc != 0:
-        raise KdError(rc, "kd_checkpoint_read")
+    if out is not None:
+        _check_tensor("out", hidden, (N, D), dtype, dev)
+    _call("kd_checkpoint_read", dev, N, D, code, codes, scales, hidden)
     return hidden
 
 
@@ -868,7 +864,7 @@ def verify_draft(target_logits, draft_tokens, uniform, draft_idx=None, draft_log
     {'tokens' [B, T + 1] int32 (kept, next, then -1), 'accepted' [B] int32} and,
     when requested, 'accept_prob' [B, T] fp32."""
     import torch
-    lib = load_library()
+    load_library()
     code, ld = _logits_rows("target_logits", target_logits, 3)
     dev = target_logits.device
     B, T, V = target_logits.shape[0], target_logits.shape[1] - 1, target_logits.shape[2]
@@ -899,21 +895,24 @@ def verify_draft(target_logits, draft_tokens, uniform, draft_idx=None, draft_log
     res = _out_tensors(out, want, dev)
     pr = KdDraft(B, T, V, ld, ld_draft, K, code, float(tau), 0)
     if workspace is None:
-        n = ctypes.c_size_t(0)
-        rc = lib.kd_verify_draft_workspace_size(ctypes.byref(pr), ctypes.byref(n))
-        if rc != 0:
-            raise KdError(rc, "kd_verify_draft_workspace_size")
-        workspace = torch.empty(n.value, dtype=torch.uint8, device=dev)
+        workspace = torch.empty(verify_workspace_size(B, T, V, K, code), dtype=torch.uint8,
+                                device=dev)
     _check_workspace(workspace, dev)
-    with torch.cuda.device(dev):
-        rc = lib.kd_verify_draft(
-            ctypes.byref(pr), _ptr(target_logits), _ptr(draft_tokens), _ptr(draft_idx),
-            _ptr(draft_logit), _ptr(draft_logits), _ptr(uniform), _ptr(lengths),
-            _ptr(res["tokens"]), _ptr(res["accepted"]), _ptr(res.get("accept_prob")),
-            _ptr(workspace), ctypes.c_size_t(workspace.numel()), _stream_handle(dev))
-    if rc != 0:
-        raise KdError(rc, "kd_verify_draft")
+    _call("kd_verify_draft", dev, pr, target_logits, draft_tokens, draft_idx, draft_logit,
+          draft_logits, uniform, lengths, res["tokens"], res["accepted"], res.get("accept_prob"),
+          workspace, workspace.numel())
     return res
+
+
+@functools.lru_cache(maxsize=256)
+def verify_workspace_size(B, T, V, K, dtype=KD_BF16) -> int:
+    """Bytes of workspace of verify_draft (K = 0: a dense draft)."""
+    n = ctypes.c_size_t(0)
+    pr = KdDraft(int(B), int(T), int(V), int(V), int(V), int(K), int(dtype), 1.0, 0)
+    rc = load_library().kd_verify_draft_workspace_size(ctypes.byref(pr), ctypes.byref(n))
+    if rc != 0:
+        raise KdError(rc, "kd_verify_draft_workspace_size")
+    return int(n.value)
 
 
 def profile_enable(on: bool = True, contractions_only: bool = False):
