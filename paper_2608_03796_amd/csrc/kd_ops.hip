@@ -111,7 +111,7 @@ __device__ __forceinline__ float group_maxima(const u32x4_t* x, float& top) {
   for (int u = 0; u < U; ++u) {
     float m = Row<T>::elt(x[u], 0);
 #pragma unroll
-    for (int i = 1; i < VPT; ++i) m = fmaxf(m, Row<T>::elt(x[u], i));
+    for (int i = 1; i < VPT; ++i) m = fmaxf(m, Row<T>::raw(x[u], i));
 #pragma unroll
     for (int c = 0; c < (GL == 8 ? 3 : 4); ++c) m = fmaxf(m, dpp_f(m, c));
     if ((lane & (GL - 1)) == u) mine = m;
@@ -952,7 +952,7 @@ __global__ __launch_bounds__(256) void k_seg_sums(VerifyArgs a, int waves) {
 #pragma unroll
   for (int u = 0; u < U; ++u)
 #pragma unroll
-    for (int i = 0; i < VPT; ++i) m = fmaxf(m, Row<T>::elt(x[u], i));
+    for (int i = 0; i < VPT; ++i) m = fmaxf(m, Row<T>::raw(x[u], i));
   m = wave_max(m);
   double s = 0.0;
   if (m != -INFINITY) {
