@@ -835,15 +835,18 @@ __device__ __forceinline__ double weight(float z, float m, double c) {
   return exp2_64(((double)z - (double)m) * c);
 }
 // Weights below one m, for passes over whole rows: 2^(y / 256) with y = 256 c (z - m)
-// by a table of 2^(i / 256) in LDS and the series of degree 3 for the rest of up to
-// half a step (the next term is below 2^-42 of the result). 9 fp64 operations and 6
-// others where exp2_64 with its difference, comparisons and sum takes 23 and 4. z is
+// by a table of 2^(i / 256) in LDS and, for the rest of a step, the series of degree
+// 3 about its middle (the next term is below 2^-42 of the result). y is held 2^18
+// higher, so that it is positive and its whole part and rest are an operation each.
+// 8 fp64 operations and 6 others where exp2_64 with its difference, comparisons and sum
+// takes 23 and 4. z is
 // held above m - 990 / c, where weights no longer count (2^-990; -inf and what is not
 // a number end there too), which fp32 can tell from m where `fast`; elsewhere
 // (infinities, extreme tau) weight() serves.
 constexpr int kTabBits = 8, kTab = 1 << kTabBits;
-// 2^(i / 256) less i << 12 in its high word: adding n << 12 for n = i + 256 j gives
-// 2^(n / 256)
+// 2^(i / 256) less i << 12 in its high word, and less 2^18 << 12: adding n << 12 for
+// n = 2^18 + i + 256 j gives 2^(j + i / 256)
+constexpr int kTabLift = 1 << 18;
 struct Roots {
   uint64_t v[kTab];
   constexpr Roots() : v() {
@@ -851,7 +854,7 @@ struct Roots {
       const double x = i * (0.69314718055994530942 / kTab);
       double s = 1.0;
       for (int k = 24; k >= 1; --k) s = 1.0 + s * x / k;
-      v[i] = __builtin_bit_cast(uint64_t, s) - ((uint64_t)i << (52 - kTabBits));
+      v[i] = __builtin_bit_cast(uint64_t, s) - ((uint64_t)(kTabLift + i) << (52 - kTabBits));
     }
   }
 };
@@ -871,17 +874,15 @@ struct Weights {
     fast = reach > big * (1.0 / 65536) && reach < 1e37 && big < 1e37;
     floor = (float)((double)m - reach);
     cs = (double)kTab * c;
-    ms = -(double)m * cs;
+    ms = kTabLift - (double)m * cs;
   }
   __device__ __forceinline__ double quick(float z) const {
     const double y = fma((double)fmaxf(z, floor), cs, ms);
-    const double t = y + 0x1.8p52;  // the nearest whole number in the low bits
-    const double g = y - (t - 0x1.8p52);
-    const uint32_t n = (uint32_t)__builtin_bit_cast(uint64_t, t);
-    // (ln 2 / 256)^k / k!
-    double p = fma(g, 3.30830268054137110e-9, 3.66556559691010608e-6);
-    p = fma(p, g, 2.70760617406228633e-3);
-    p = fma(p, g, 1.0);
+    const double g = __builtin_amdgcn_fract(y);
+    const uint32_t n = (uint32_t)(int)y;
+    double p = fma(g, 3.31278450399181539888e-9, 3.66556223478407997130e-6);
+    p = fma(p, g, 2.70760617518312146377e-3);
+    p = fma(p, g, 9.99999999999859886130e-1);
     const uint64_t e = tab[n & (kTab - 1)];
     const uint32_t high = (uint32_t)(e >> 32) + (n << (20 - kTabBits));
     return p * __builtin_bit_cast(double, (uint64_t)high << 32 | (uint32_t)e);
