@@ -841,8 +841,8 @@ __device__ __forceinline__ double weight(float z, float m, double c) {
 // 8 fp64 operations and 6 others where exp2_64 with its difference, comparisons and sum
 // takes 23 and 4. z is
 // held above m - 990 / c, where weights no longer count (2^-990; -inf and what is not
-// a number end there too), which fp32 can tell from m where `fast`; elsewhere
-// (infinities, extreme tau) weight() serves.
+// a number end there too), and below m + 900 / c. fp32 can tell these from m where
+// `fast`; elsewhere (infinities, extreme tau) weight() serves.
 constexpr int kTabBits = 8, kTab = 1 << kTabBits;
 // 2^(i / 256) less i << 12 in its high word, and less 2^18 << 12: adding n << 12 for
 // n = 2^18 + i + 256 j gives 2^(j + i / 256)
@@ -865,7 +865,7 @@ __device__ __forceinline__ void load_roots(uint64_t* tab) {
 }
 struct Weights {
   double c, cs, ms;
-  float m, floor;
+  float m, floor, ceil;
   bool fast;
   const uint64_t* tab;
   __device__ __forceinline__ Weights(float m_, double c_, const uint64_t* t)
@@ -873,11 +873,12 @@ struct Weights {
     const double reach = 990.0 / c, big = fabs((double)m);
     fast = reach > big * (1.0 / 65536) && reach < 1e37 && big < 1e37;
     floor = (float)((double)m - reach);
+    ceil = (float)((double)m + reach * (900.0 / 990.0));
     cs = (double)kTab * c;
     ms = kTabLift - (double)m * cs;
   }
   __device__ __forceinline__ double quick(float z) const {
-    const double y = fma((double)fmaxf(z, floor), cs, ms);
+    const double y = fma((double)__builtin_amdgcn_fmed3f(z, floor, ceil), cs, ms);
     const double g = __builtin_amdgcn_fract(y);
     const uint32_t n = (uint32_t)(int)y;
     double p = fma(g, 3.31278450399181539888e-9, 3.66556223478407997130e-6);
@@ -930,8 +931,12 @@ __device__ __forceinline__ int64_t draft_row(const VerifyArgs& a, int b, int t) 
   return (int64_t)b * a.T + t;
 }
 
-// Largest logit and sum of weights of each segment of the rows in question (the
-// target's, then the draft's): the pass that reads the logits.
+// Reference m and sum of 2^(c (z - m)) of each segment of the rows in question (the
+// target's, then the draft's): the pass that reads the logits, bound by its fp64
+// arithmetic (8 of about 16 operations an element). 64 bits hold the weights of
+// logits well above the reference too, so the largest of a quarter (bf16) or an
+// eighth of the segment serves, the largest of all where that is -inf; a segment
+// whose sum passes 2^899 is summed again below its largest logit.
 template <typename T>
 __global__ __launch_bounds__(256) void k_seg_sums(VerifyArgs a, int waves) {
   __shared__ uint64_t tab[kTab];
@@ -949,12 +954,16 @@ __global__ __launch_bounds__(256) void k_seg_sums(VerifyArgs a, int waves) {
   constexpr int U = Row<T>::U, VPT = Row<T>::VPT;
   u32x4_t x[U];
   row.segment(seg, x);
-  float m = -INFINITY;
+  auto largest = [&](int vectors) {
+    float m = -INFINITY;
 #pragma unroll
-  for (int u = 0; u < U; ++u)
+    for (int u = 0; u < vectors; ++u)
 #pragma unroll
-    for (int i = 0; i < VPT; ++i) m = fmaxf(m, Row<T>::raw(x[u], i));
-  m = wave_max(m);
+      for (int i = 0; i < VPT; ++i) m = fmaxf(m, Row<T>::raw(x[u], i));
+    return wave_max(m);
+  };
+  float m = largest(1);
+  if (m == -INFINITY) m = largest(U);
   double s = 0.0;
   if (m != -INFINITY) {
     const Weights q(m, a.c, tab);
@@ -968,14 +977,17 @@ __global__ __launch_bounds__(256) void k_seg_sums(VerifyArgs a, int waves) {
           h += q.quick(Row<T>::raw(x[u], i + 1));
         }
       }
-      s += h;
-    } else {
+      s = wave_sum64(s + h);
+    }
+    if (!q.fast || !(s < 0x1p899)) {
+      m = largest(U);
+      s = 0.0;
 #pragma unroll
       for (int u = 0; u < U; ++u)
-        for (int i = 0; i < VPT; ++i) s += q.exact(Row<T>::elt(x[u], i));
+        for (int i = 0; i < VPT; ++i) s += weight(Row<T>::elt(x[u], i), m, a.c);
+      s = wave_sum64(s);
     }
   }
-  s = wave_sum64(s);
   if ((threadIdx.x & 63) == 0) {
     a.segm[w] = m;
     a.segs[w] = s;

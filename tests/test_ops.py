@@ -273,8 +273,10 @@ def _check_verify(kd, target, tokens, u, draft, tau=1.0, lengths=None):
                            None if lengths is None else to64(lengths), tau)
     assert np.array_equal(to64(out["accepted"]), want[1])
     assert np.array_equal(to64(out["tokens"]), want[0])
-    # computed in 64 bits, rounded once
-    assert np.all(np.abs(to64(out["accept_prob"]) - want[2]) <= E32 * want[2] + 1e-300)
+    # computed in 64 bits, rounded once: half a step of fp32, which below 2^-126 is the
+    # half of 2^-149 (subnormal numbers), and 1e-12 of the 64-bit weights
+    assert np.all(np.abs(to64(out["accept_prob"]) - want[2])
+                  <= (E32 + 1e-12) * want[2] + 2.0 ** -150)
     return want
 
 
@@ -337,6 +339,28 @@ def test_verify_draft_edges(gpu_lib, dtype, K):
     out = gpu_lib.verify_draft(z, tokens, u, **draft)
     assert int(out["accepted"][3]) == 0
     assert 0 <= int(out["tokens"][3, 0]) < V
+
+
+@pytest.mark.parametrize("K", [0, 12])
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+def test_verify_far_logits(gpu_lib, dtype, K):
+    """Logits hundreds of powers of two apart inside a row's stretches of 2048
+    columns, stretches that begin or end in -inf, extreme tau."""
+    B, T, V = 6, 2, 9001
+    target, tokens, u, draft = _draft(B, T, V, K, dtype, 55, ld=3)
+    z = target.clone()
+    z[0, :, 2500:2600] += 700.0               # most of a stretch far below the rest of it
+    z[1, :, 4000:4010] += 3000.0
+    z[2, :, :6000] = float("-inf")
+    z[3, :, 2048:3500] = float("-inf")
+    z[3, :, 7000:] -= 900.0
+    z[4] *= 40.0
+    for s in range(0, V, 2048):
+        z[5, :, s:s + 1024] = float("-inf")
+    tokens[0] = 2550
+    tokens[1, 0] = 4003
+    for tau in (1.0, 0.05, 30.0, 1e30, 1e-20):
+        _check_verify(gpu_lib, z, tokens, u, draft, tau)
 
 
 @pytest.mark.parametrize("dtype", ["bf16", "f32"])
