@@ -183,6 +183,32 @@ def test_teacher_cache_far_rows(gpu_lib):
     assert not bool(t["ignore"].any())
 
 
+def test_large_results(gpu_lib):
+    """Results beyond the caches, which are stored another way: against the rows and
+    blocks one by one."""
+    kd = gpu_lib
+    g = _gen(25)
+    N, K = 1000, 52
+    e = torch.randint(0, 1 << 31, (N, K), generator=g, device="cuda").int()
+    sc = torch.rand(N, 2, generator=g, device="cuda")
+    sc[7, 0] = float("-inf")
+    rows = torch.randint(-2, N + 2, (300001,), generator=g, device="cuda")
+    t = kd.teacher_cache_read(e, sc, rows=rows)
+    every = kd.teacher_cache_read(e, sc, rows=torch.arange(-2, N + 2, device="cuda"))
+    for k in t:
+        assert torch.equal(t[k], every[k][rows + 2]), k
+    for dt in (torch.bfloat16, torch.float32):
+        x = (torch.randn(50001, 1184, generator=g, device="cuda") * 7).to(dt)
+        c = kd.checkpoint_write(x)
+        back = kd.checkpoint_read(c["codes"], c["scales"], dt)
+        for s0 in range(0, 50001, 10000):
+            p = kd.checkpoint_write(x[s0:s0 + 10000])
+            assert torch.equal(p["codes"], c["codes"][s0:s0 + 10000])
+            assert torch.equal(p["scales"], c["scales"][s0:s0 + 10000])
+            assert torch.equal(kd.checkpoint_read(p["codes"], p["scales"], dt),
+                               back[s0:s0 + 10000])
+
+
 # -------------------------------------------------------------- checkpoints --
 @pytest.mark.parametrize("dtype", ["bf16", "f32"])
 @pytest.mark.parametrize("N,D", [(1, 32), (3, 64), (77, 768), (5, 96)])
