@@ -182,16 +182,17 @@ __global__ __launch_bounds__(256) void k_row_groups(const T* __restrict__ logits
 // registers, its groups are single vectors, and their maxima and the sum of exp
 // are formed here: one launch, and groups enough for K above V / 64.
 //
-// kStream (rows of up to 2048 groups, many of them): the only pass too, the first
-// pass's work done by the row's workgroup. While some workgroups wait for their
-// scattered reads, others stream.
+// kStream (rows of up to 2048 groups): the only pass too, the first pass's work done
+// by the row's workgroup. The scattered reads of the second pass take 20 us and more
+// when all rows make them at once (1 GiB of logits has left the caches by then); here
+// some workgroups wait for them while others stream.
 //
 // The pass is latency-bound (a few dependent reads and barriers per row), so what
 // counts is rows in flight, and for few rows the time of one.
 constexpr int kHistBins = 2048;
 constexpr int kBoundBins = 1024;
 // keys of a thread in registers: all of a row held directly, or of 131072 columns
-constexpr int select_keys(int NT, bool direct) { return direct || NT == 256 ? 8 : 2; }
+constexpr int select_keys(int NT, bool direct) { return direct || NT <= 512 ? 8 : 2; }
 
 __host__ __device__ constexpr int select_cap(int K) {
   int c = 1024;
@@ -1466,8 +1467,20 @@ __global__ __launch_bounds__(kVerThreads) void k_pick(VerifyArgs a) {
 // ================================================================ launchers ==
 using namespace kd;
 
-constexpr int64_t kSelectFewRows = 512, kSelectStreamRows = 1024;
-constexpr int kSelectManyEntries = 512;
+// How rows are selected from (us for all of it, top 64 or 100, with the read back):
+//  * up to 256 rows, or K > 512: 1024 threads a row in the second pass. One row of
+//    131072 in fp32 11.1 (256 threads 15.7), 256 rows bf16 25.5 (30.0), 300 rows 33.9
+//    (32.7).
+//  * rows that 8 vectors a thread hold: one pass, the row in registers (8192 rows of
+//    4000 166 in two passes, 87).
+//  * more rows: each streamed by its own workgroup. Long ones (48 segments, about
+//    100000 columns) by 512 threads: 300 rows 28.8 (two passes 32.7), 777 50.1 (53.0),
+//    4096 192 (236; 256 threads 203). Shorter ones by 256 threads once there are 1536:
+//    8000 rows of 50257 169 (208; 512 threads 198), 777 rows 38.4 (36.0), 1100 rows
+//    of 50257 in fp32 with log-probabilities 61.4 (56.3).
+//  * else two passes, 256 threads a row in the second.
+constexpr int64_t kSelectFewRows = 256, kSelectStreamRows = 1536;
+constexpr int kSelectManyEntries = 512, kSelectLongSegs = 48;
 
 template <typename T>
 static int launch_topk(const KdTopkArgs& a, hipStream_t s) {
@@ -1490,7 +1503,12 @@ static int launch_topk(const KdTopkArgs& a, hipStream_t s) {
   }
   q.G = a.nseg * kSegGroups;
   const size_t lds = select_lds(q.G, a.K);
-  if (!wide && a.rows >= kSelectStreamRows && q.G <= 256 * select_keys(256, true)) {
+  // (the keys of a streamed row stand where its candidates will)
+  if (!wide && 4 * q.G <= 8 * select_cap(a.K) && a.nseg >= kSelectLongSegs) {
+    hipLaunchKernelGGL((k_row_select<T, 512, kStream>), rows, dim3(512), lds, s, q);
+    return (int)hipGetLastError();
+  }
+  if (!wide && 4 * q.G <= 8 * select_cap(a.K) && a.rows >= kSelectStreamRows) {
     hipLaunchKernelGGL((k_row_select<T, 256, kStream>), rows, dim3(256), lds, s, q);
     return (int)hipGetLastError();
   }

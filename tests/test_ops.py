@@ -118,6 +118,33 @@ def test_topk_entries_large(gpu_lib, dtype, N, V, K):
     _check_topk(gpu_lib, _logits(N, V, dtype, 12), K)
 
 
+@pytest.mark.parametrize("kind", ["plain", "masked", "two", "nan"])
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+@pytest.mark.parametrize("N,V,K,ld,offset", [(300, 101000, 60, 101001, 3), (1540, 17000, 20, None, 0),
+                                             (260, 131072, 512, None, 0)])
+def test_topk_entries_streamed(gpu_lib, N, V, K, ld, offset, dtype, kind):
+    """Rows that their own workgroups stream: the selection of the whole against
+    the oracle's on some rows, and every row against a call for it alone."""
+    kd = gpu_lib
+    x = _special(_logits(N, V, dtype, 14, ld, offset), kind)
+    for logprobs in (False, True):
+        got = kd.topk_entries(x, K, logprobs=logprobs)
+        for r0 in range(0, N, 200):   # few rows take another way
+            part = kd.topk_entries(x[r0:r0 + 200], K, logprobs=logprobs)
+            assert torch.equal(got["teacher_idx"][r0:r0 + 200], part["teacher_idx"])
+            a, b = to64(got["teacher_logit"][r0:r0 + 200]), to64(part["teacher_logit"])
+            f = np.isfinite(a)
+            assert np.array_equal(f, np.isfinite(b))
+            # (each within 64 E32 of the sum's logarithm, see _check_topk)
+            tol = 128 * E32 + 6 * E32 * np.abs(b[f]) if logprobs else 0.0
+            assert np.all(np.abs(a[f] - b[f]) <= tol)
+    some = torch.tensor([0, 1, N // 2, N - 1], device="cuda")
+    idx, val = oo.topk_entries(x[some].float().cpu().numpy(), K)
+    got = kd.topk_entries(x, K)
+    assert np.array_equal(to64(got["teacher_idx"][some]), idx)
+    assert np.array_equal(to64(got["teacher_logit"][some]), val)
+
+
 def test_topk_many_rows_in_batches(gpu_lib):
     """More rows than the workspace holds at a time."""
     kd, N, V, K = gpu_lib, 500000, 9, 2
