@@ -1177,6 +1177,28 @@ __global__ __launch_bounds__(kVerThreads) void k_accept(VerifyArgs a) {
     for (int t = n + tid; t < a.T; t += kVerThreads) a.prob[draft_row(a, b, t)] = 0.f;
   for (int t = wave; t <= n; t += kVerWaves) {
     const int64_t rt = target_row(a, b, t), rd = draft_row(a, b, t);
+    // what the place needs is read first: these reads and the segments' are cold and
+    // each takes microseconds
+    constexpr int R = 2;  // entries of a lane in registers (K up to 128)
+    int d = -1, iv[R] = {-1, -1};
+    float zt = -INFINITY, zd = -INFINITY, lv[R] = {-INFINITY, -INFINITY};
+    const float* l = a.dlogit + rd * a.K;
+    const int32_t* ix = a.didx + rd * a.K;
+    if (t < n) {
+      d = a.tokens[rd];
+      if constexpr (!DENSE) {
+#pragma unroll
+        for (int j = 0; j < R; ++j)
+          if (lane + 64 * j < a.K) {
+            lv[j] = l[lane + 64 * j];
+            iv[j] = ix[lane + 64 * j];
+          }
+      }
+      if ((unsigned)d < (unsigned)a.V) {
+        zt = Row<T>(a.target, rt * a.ld_t, a.V).one(d);
+        if constexpr (DENSE) zd = Row<T>(a.draft, rd * a.ld_d, a.V).one(d);
+      }
+    }
     float M;
     double S;
     merge_row(a, rt, M, S);
@@ -1185,27 +1207,28 @@ __global__ __launch_bounds__(kVerThreads) void k_accept(VerifyArgs a) {
       rowS[t] = S;
     }
     if (t == n) break;
-    const int d = a.tokens[rd];
     const bool known = (unsigned)d < (unsigned)a.V;
-    const Row<T> row(a.target, rt * a.ld_t, a.V);
-    const double p = known && S > 0.0 ? weight(row.one(d), M, a.c) / S : 0.0;
+    const double p = known && S > 0.0 ? weight(zt, M, a.c) / S : 0.0;
     double q = 0.0;
     if constexpr (DENSE) {
       merge_row(a, (int64_t)a.B * (a.T + 1) + rd, M, S);
-      const Row<T> dr(a.draft, rd * a.ld_d, a.V);
-      q = known && S > 0.0 ? weight(dr.one(d), M, a.c) / S : 0.0;
+      q = known && S > 0.0 ? weight(zd, M, a.c) / S : 0.0;
     } else {
-      const float* l = a.dlogit + rd * a.K;
-      const int32_t* ix = a.didx + rd * a.K;
       float m = -INFINITY;
-      for (int k = lane; k < a.K; k += 64) m = fmaxf(m, l[k]);
+#pragma unroll
+      for (int j = 0; j < R; ++j) m = fmaxf(m, lv[j]);
+      for (int k = lane + 64 * R; k < a.K; k += 64) m = fmaxf(m, l[k]);
       m = wave_max(m);
       double s = 0.0, w = 0.0;
-      for (int k = lane; k < a.K; k += 64) {
-        const double e = weight(fmaxf(l[k], -INFINITY), m, a.c);
+      auto entry = [&](float lk, int v) {
+        const double e = weight(fmaxf(lk, -INFINITY), m, a.c);
         s += e;
-        if (ix[k] == d) w += e;
-      }
+        if (v == d) w += e;
+      };
+#pragma unroll
+      for (int j = 0; j < R; ++j)
+        if (lane + 64 * j < a.K) entry(lv[j], iv[j]);
+      for (int k = lane + 64 * R; k < a.K; k += 64) entry(l[k], ix[k]);
       s = wave_sum64(s);
       w = wave_sum64(w);
       q = known && s > 0.0 ? w / s : 0.0;
