@@ -17,6 +17,8 @@ namespace kd {
 // between the boundary at or before the row and the row. Vectors that reach
 // past either end of the row are read element by element; what is not of the
 // row reads as -inf.
+// z, or -inf where it is not a number
+__device__ __forceinline__ float number(float z) { return z > -INFINITY ? z : -INFINITY; }
 template <typename T>
 struct Row {
   static constexpr int VPT = 16 / (int)sizeof(T);      // elements of a vector
@@ -66,18 +68,21 @@ struct Row {
       for (int u = 0; u < U; ++u) x[u] = at(e0 + (64 * u + lane) * VPT);
     }
   }
-  // element i of a vector
+  // element i of a vector, as it is: maxima and med3 may return a signalling NaN or
+  // drop what they had for it
   static __device__ __forceinline__ float raw(u32x4_t x, int i) {
     uint32_t b;
     if constexpr (sizeof(T) == 2) b = i & 1 ? x[i / 2] & 0xffff0000u : x[i / 2] << 16;
     else b = x[i];
     return __builtin_bit_cast(float, b);
   }
-  // the same; what is not a number counts as -inf
-  static __device__ __forceinline__ float elt(u32x4_t x, int i) { return fmaxf(raw(x, i), -INFINITY); }
-  __device__ __forceinline__ float one(int v) const {
-    return fmaxf((float)p[v], -INFINITY);
+  // the same with any NaN quiet, which a maximum passes over
+  static __device__ __forceinline__ float quiet(u32x4_t x, int i) {
+    return __builtin_canonicalizef(raw(x, i));
   }
+  // the same with any NaN as -inf
+  static __device__ __forceinline__ float elt(u32x4_t x, int i) { return number(raw(x, i)); }
+  __device__ __forceinline__ float one(int v) const { return number((float)p[v]); }
 };
 
 // values as unsigned numbers of the same order (-0 as +0)
@@ -111,7 +116,7 @@ __device__ __forceinline__ float group_maxima(const u32x4_t* x, float& top) {
   for (int u = 0; u < U; ++u) {
     float m = Row<T>::elt(x[u], 0);
 #pragma unroll
-    for (int i = 1; i < VPT; ++i) m = fmaxf(m, Row<T>::raw(x[u], i));
+    for (int i = 1; i < VPT; ++i) m = fmaxf(m, Row<T>::quiet(x[u], i));
 #pragma unroll
     for (int c = 0; c < (GL == 8 ? 3 : 4); ++c) m = fmaxf(m, dpp_f(m, c));
     if ((lane & (GL - 1)) == u) mine = m;
@@ -348,7 +353,7 @@ __global__ __launch_bounds__(NT) void k_row_select(SelectArgs a) {
     for (int j = 0; j < kUnroll; ++j) {
       float m = Row<T>::elt(x[j], 0);
 #pragma unroll
-      for (int i = 1; i < VPT; ++i) m = fmaxf(m, Row<T>::elt(x[j], i));
+      for (int i = 1; i < VPT; ++i) m = fmaxf(m, Row<T>::quiet(x[j], i));
       held[j] = tid + j * NT < G ? order_key(m) : 0u;
     }
   } else if constexpr (STREAM) {
@@ -594,7 +599,7 @@ __global__ __launch_bounds__(NT) void k_row_select(SelectArgs a) {
     // fewer than K above -inf: of the first K columns as many as it takes are -inf
     for (int v0 = 0; v0 < K; v0 += NT) {
       const int v = v0 + tid;
-      const bool q = v < K && !((float)row.p[v] > -INFINITY);
+      const bool q = v < K && row.one(v) == -INFINITY;
       const uint64_t b = __builtin_amdgcn_ballot_w64(q);
       int to = 0;
       if (lane == 0 && b != 0) to = atomicAdd(&s.n, __popcll(b));
@@ -979,7 +984,7 @@ __global__ __launch_bounds__(256) void k_seg_sums(VerifyArgs a, int waves) {
 #pragma unroll
     for (int u = 0; u < vectors; ++u)
 #pragma unroll
-      for (int i = 0; i < VPT; ++i) m = fmaxf(m, Row<T>::raw(x[u], i));
+      for (int i = 0; i < VPT; ++i) m = fmaxf(m, Row<T>::quiet(x[u], i));
     return wave_max(m);
   };
   float m = largest(1);
@@ -999,6 +1004,7 @@ __global__ __launch_bounds__(256) void k_seg_sums(VerifyArgs a, int waves) {
       }
       s = wave_sum64(s + h);
     }
+    // (a signalling NaN that med3 let through makes the sum none either)
     if (!q.fast || !(s < 0x1p899)) {
       m = largest(U);
       s = 0.0;
@@ -1190,7 +1196,7 @@ __global__ __launch_bounds__(kVerThreads) void k_accept(VerifyArgs a) {
 #pragma unroll
         for (int j = 0; j < R; ++j)
           if (lane + 64 * j < a.K) {
-            lv[j] = l[lane + 64 * j];
+            lv[j] = number(l[lane + 64 * j]);
             iv[j] = ix[lane + 64 * j];
           }
       }
@@ -1217,18 +1223,18 @@ __global__ __launch_bounds__(kVerThreads) void k_accept(VerifyArgs a) {
       float m = -INFINITY;
 #pragma unroll
       for (int j = 0; j < R; ++j) m = fmaxf(m, lv[j]);
-      for (int k = lane + 64 * R; k < a.K; k += 64) m = fmaxf(m, l[k]);
+      for (int k = lane + 64 * R; k < a.K; k += 64) m = fmaxf(m, number(l[k]));
       m = wave_max(m);
       double s = 0.0, w = 0.0;
       auto entry = [&](float lk, int v) {
-        const double e = weight(fmaxf(lk, -INFINITY), m, a.c);
+        const double e = weight(lk, m, a.c);
         s += e;
         if (v == d) w += e;
       };
 #pragma unroll
       for (int j = 0; j < R; ++j)
         if (lane + 64 * j < a.K) entry(lv[j], iv[j]);
-      for (int k = lane + 64 * R; k < a.K; k += 64) entry(l[k], ix[k]);
+      for (int k = lane + 64 * R; k < a.K; k += 64) entry(number(l[k]), ix[k]);
       s = wave_sum64(s);
       w = wave_sum64(w);
       q = known && s > 0.0 ? w / s : 0.0;
@@ -1279,14 +1285,14 @@ __global__ __launch_bounds__(kVerThreads) void k_accept(VerifyArgs a) {
     const float* l = a.dlogit + draft_row(a, b, r) * a.K;
     const int32_t* ix = a.didx + draft_row(a, b, r) * a.K;
     float m = -INFINITY;
-    for (int k = lane; k < a.K; k += 64) m = fmaxf(m, l[k]);  // (each wave for itself)
+    for (int k = lane; k < a.K; k += 64) m = fmaxf(m, number(l[k]));  // (each wave for itself)
     m = wave_max(m);
     double s = 0.0;
-    for (int k = lane; k < a.K; k += 64) s += weight(fmaxf(l[k], -INFINITY), m, a.c);
+    for (int k = lane; k < a.K; k += 64) s += weight(number(l[k]), m, a.c);
     s = wave_sum64(s);
     for (int k = tid; k < Kp; k += kVerThreads) {
       const bool entry = k < a.K;
-      em[k] = entry && s > 0.0 ? weight(fmaxf(l[k], -INFINITY), m, a.c) / s : 0.0;
+      em[k] = entry && s > 0.0 ? weight(number(l[k]), m, a.c) / s : 0.0;
       const int v = entry ? ix[k] : -1;
       ei[k] = (unsigned)v < (unsigned)a.V ? v : -1;
       eq[k] = 0.0;
@@ -1433,7 +1439,7 @@ __global__ __launch_bounds__(256) void k_rest_sums(VerifyArgs a) {
     const u32x4_t y = draft_at<T>(dr, seg * kSegCols + e, row.shift);
     if (m.fast()) {
 #pragma unroll
-      for (int i = 0; i < VPT; ++i) s += m.quick(Row<T>::raw(x, i), Row<T>::raw(y, i));
+      for (int i = 0; i < VPT; ++i) s += m.quick(Row<T>::elt(x, i), Row<T>::elt(y, i));
     } else {
       for (int i = 0; i < VPT; ++i) s += m.exact(Row<T>::elt(x, i), Row<T>::elt(y, i));
     }
@@ -1491,9 +1497,8 @@ __global__ __launch_bounds__(kVerThreads) void k_pick(VerifyArgs a) {
 using namespace kd;
 
 // How rows are selected from (us for all of it, top 64 or 100, with the read back):
-//  * up to 256 rows, or K > 512: 1024 threads a row in the second pass. One row of
-//    131072 in fp32 11.1 (256 threads 15.7), 256 rows bf16 25.5 (30.0), 300 rows 33.9
-//    (32.7).
+//  * up to 256 rows: 1024 threads a row in the second pass. One row of 131072 in fp32
+//    11.1 (256 threads 15.7), 256 rows bf16 25.5 (30.0), 300 rows 33.9 (32.7).
 //  * rows that 8 vectors a thread hold: one pass, the row in registers (8192 rows of
 //    4000 166 in two passes, 87).
 //  * more rows: each streamed by its own workgroup. Long ones (48 segments, about
@@ -1503,7 +1508,7 @@ using namespace kd;
 //    of 50257 in fp32 with log-probabilities 61.4 (56.3).
 //  * else two passes, 256 threads a row in the second.
 constexpr int64_t kSelectFewRows = 256, kSelectStreamRows = 1536;
-constexpr int kSelectManyEntries = 512, kSelectLongSegs = 48;
+constexpr int kSelectLongSegs = 48;
 
 template <typename T>
 static int launch_topk(const KdTopkArgs& a, hipStream_t s) {
@@ -1511,7 +1516,7 @@ static int launch_topk(const KdTopkArgs& a, hipStream_t s) {
   SelectArgs q{a.logits, a.ld, a.V, a.K, 0, a.nseg, a.logprobs, a.gmax, a.pm, a.ps,
                a.idx, a.value, a.entries, a.scale};
   const dim3 rows((unsigned)a.rows);
-  const bool wide = a.rows <= kSelectFewRows || a.K > kSelectManyEntries;
+  const bool wide = a.rows <= kSelectFewRows;
   // vectors of a row, wherever it starts
   constexpr int VPT = Row<T>::VPT;
   const int vectors = (a.V + 2 * (VPT - 1)) / VPT;
@@ -1526,12 +1531,15 @@ static int launch_topk(const KdTopkArgs& a, hipStream_t s) {
   }
   q.G = a.nseg * kSegGroups;
   const size_t lds = select_lds(q.G, a.K);
-  // (the keys of a streamed row stand where its candidates will)
-  if (!wide && 4 * q.G <= 8 * select_cap(a.K) && a.nseg >= kSelectLongSegs) {
+  // (the keys of a streamed row stand where its candidates will, then in registers)
+  auto streams = [&](int threads) {
+    return !wide && 4 * q.G <= 8 * select_cap(a.K) && q.G <= threads * select_keys(threads, true);
+  };
+  if (streams(512) && a.nseg >= kSelectLongSegs) {
     hipLaunchKernelGGL((k_row_select<T, 512, kStream>), rows, dim3(512), lds, s, q);
     return (int)hipGetLastError();
   }
-  if (!wide && 4 * q.G <= 8 * select_cap(a.K) && a.rows >= kSelectStreamRows) {
+  if (streams(256) && a.rows >= kSelectStreamRows) {
     hipLaunchKernelGGL((k_row_select<T, 256, kStream>), rows, dim3(256), lds, s, q);
     return (int)hipGetLastError();
   }

@@ -449,6 +449,29 @@ def test_verify_draft_follows_the_target(gpu_lib):
         assert bool(((n - B * p).abs() <= 6 * (B * p * (1 - p)).sqrt()).all())
 
 
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+@pytest.mark.parametrize("N", [2, 300])
+def test_every_kind_of_nan(gpu_lib, N, dtype):
+    """Quiet and signalling, of either sign, first in a vector or not: all count as -inf."""
+    kd, V, K = gpu_lib, 101000, 40
+    x = _logits(N, V, dtype, 15)
+    bits = x.view(torch.int16 if dtype == "bf16" else torch.int32)
+    kinds = (0x7f81, -0x7f, 0x7fc0, -1) if dtype == "bf16" else (0x7f800001, -0x7fffff, 0x7fc00000, -1)
+    for i, b in enumerate(kinds):
+        bits[:, i::5] = b
+    _check_topk(kd, x[:2], K)
+    got = kd.topk_entries(x, K, logprobs=True)
+    want = kd.topk_entries(x[:200], K, logprobs=True)   # (few rows take another way)
+    assert torch.equal(got["teacher_idx"][:200], want["teacher_idx"])
+    assert bool(torch.isfinite(got["teacher_logit"]).all())
+    target, tokens, u, draft = _draft(2, 2, 9001, 0, dtype, 16)
+    for t in (target, draft["draft_logits"]):
+        b = t.view(torch.int16 if dtype == "bf16" else torch.int32)
+        for i, k in enumerate(kinds):
+            b[:, :, i::7] = k
+    _check_verify(kd, target, tokens, u, draft)
+
+
 # ------------------------------------------------------- streams and graphs --
 def test_graph_replays_and_streams(gpu_lib):
     """Captured calls replay to the eager results between eager work, and a call on
