@@ -206,6 +206,36 @@ def test_captured_step(gpu_lib, masked):
             assert torch.equal(got[k], eager[k]), (rep, k)
 
 
+def test_captured_autograd_step(gpu_lib):
+    """Loss and gradients through autograd, captured on leaves of their own."""
+    kd = gpu_lib
+    h, W, idx, tl, ign = _problem(300, 128, 2000, 16, "bf16", 0.2, 650)
+    ws = kd.alloc_workspace(300, 128, 2000, 16, 128, 1.0, kd.KD_BF16, "cuda")
+
+    def step(x, w):
+        loss = kd.topk_kl_loss(x, w, idx, tl, ignore=ign, chunk=128, schedule="recompute",
+                               checkpoint=True, workspace=ws)
+        return (loss.detach(),) + torch.autograd.grad(loss, (x, w))
+    s = torch.cuda.Stream()
+    with torch.cuda.stream(s):      # (autograd's first call on the capturing stream)
+        eager = step(h.clone().requires_grad_(), W.clone().requires_grad_())
+    s.synchronize()
+    x, w = h.clone().requires_grad_(), W.clone().requires_grad_()
+    torch.cuda.synchronize()
+    g = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(g, stream=s):
+        got = step(x, w)
+    for rep in range(3):
+        for t in got:
+            t.zero_()
+        kd.fwd_bwd(h, W, idx, tl, ignore=ign, chunk=64)
+        torch.cuda.synchronize()
+        g.replay()
+        torch.cuda.synchronize()
+        for a, b in zip(got, eager):
+            assert torch.equal(a, b), rep
+
+
 def test_distillation_run(gpu_lib):
     """The operators together: teacher logits to the cache, a shuffled batch read
     from it, a training step with 8-bit hidden states, and the student's drafts

@@ -559,3 +559,45 @@ def test_bindings_refuse(gpu_lib):
         kd.topk_entries(x, 101)
     with pytest.raises(kd.KdError):
         kd.verify_draft(target, tokens, u, tau=0.0, **draft)
+
+
+def test_calls_on_two_streams_at_once(gpu_lib):
+    """Calls in flight together on two streams, each with its own workspace, and two
+    captured graphs that share one workspace replayed one after the other."""
+    kd, B, T, V, K = gpu_lib, 40, 3, 50001, 60
+    cases = [_draft(B, T, V, K, "bf16", seed) for seed in (101, 102)]
+    rows = [c[0][:, 0].contiguous() for c in cases]
+    wants = [(kd.topk_entries(r, K, logprobs=True), kd.verify_draft(*c[:3], accept_prob=True, **c[3]))
+             for r, c in zip(rows, cases)]
+    torch.cuda.synchronize()
+    streams = [torch.cuda.Stream(), torch.cuda.Stream()]
+    got = [[], []]
+    for _ in range(5):
+        for i, s in enumerate(streams):
+            with torch.cuda.stream(s):
+                got[i].append((kd.topk_entries(rows[i], K, logprobs=True),
+                               kd.verify_draft(*cases[i][:3], accept_prob=True, **cases[i][3])))
+    torch.cuda.synchronize()
+    for i in range(2):
+        for pair in got[i]:
+            for a, b in zip(pair, wants[i]):
+                assert all(torch.equal(a[k], b[k]) for k in b)
+    ws = torch.empty(max(kd.topk_workspace_size(B, V, K), kd.verify_workspace_size(B, T, V, K)),
+                     dtype=torch.uint8, device="cuda")
+    graphs = []
+    for i in range(2):
+        g = torch.cuda.CUDAGraph()
+        with torch.cuda.graph(g):
+            out = (kd.topk_entries(rows[i], K, logprobs=True, workspace=ws),
+                   kd.verify_draft(*cases[i][:3], accept_prob=True, workspace=ws, **cases[i][3]))
+        graphs.append((g, out))
+    for _ in range(3):
+        for i, (g, out) in enumerate(graphs):
+            for o in out:
+                for t in o.values():
+                    t.zero_()
+            g.replay()
+        torch.cuda.synchronize()
+        for (_, out), want in zip(graphs, wants):
+            for a, b in zip(out, want):
+                assert all(torch.equal(a[k], b[k]) for k in b)
