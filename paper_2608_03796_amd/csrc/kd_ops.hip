@@ -130,14 +130,26 @@ __device__ __forceinline__ int group_of(int lane) {  // -1: none
   const int u = lane & (GL - 1);
   return u < U ? u * (64 / GL) + lane / GL : -1;
 }
-// sum of exp below m > -inf over the lane's elements
-template <typename T>
+// sum of exp below m > -inf over the N vectors' elements of the lane
+template <typename T, int N>
 __device__ __forceinline__ float exp_sum(const u32x4_t* x, float m) {
   float s = 0.f;
+  if (m == INFINITY) {
 #pragma unroll
-  for (int u = 0; u < Row<T>::U; ++u)
+    for (int u = 0; u < N; ++u)
 #pragma unroll
-    for (int i = 0; i < Row<T>::VPT; ++i) s += exp_below(Row<T>::elt(x[u], i), m);
+      for (int i = 0; i < Row<T>::VPT; ++i) s += Row<T>::raw(x[u], i) == m ? 1.f : 0.f;
+    return s;
+  }
+#pragma unroll
+  for (int u = 0; u < N; ++u) {
+    // (a difference that is none, and what is far below, ends at 2^-200: 0 in fp32)
+#pragma unroll
+    for (int i = 0; i < Row<T>::VPT; ++i)
+      s += fast_exp2(fmaxf((Row<T>::raw(x[u], i) - m) * kLog2e, -200.f));
+    // one vector after the other: all at once the scheduler takes 100 registers
+    __builtin_amdgcn_sched_barrier(0);
+  }
   return s;
 }
 
@@ -162,7 +174,7 @@ __global__ __launch_bounds__(256) void k_row_groups(const T* __restrict__ logits
   if (g >= 0) gmax[(int64_t)w * kSegGroups + g] = mine;
   if constexpr (LSE) {
     top = wave_max(top);
-    const float s = wave_sum(top != -INFINITY ? exp_sum<T>(x, top) : 0.f);
+    const float s = wave_sum(top != -INFINITY ? exp_sum<T, Row<T>::U>(x, top) : 0.f);
     if (lane == 0) {
       pm[w] = top;
       ps[w] = s;
@@ -370,7 +382,7 @@ __global__ __launch_bounds__(NT) void k_row_select(SelectArgs a) {
       if (g >= 0) keys[seg * kSegGroups + g] = order_key(mine);
       if (a.logprobs) {
         top = fmaxf(wave_max(top), m);
-        if (top != -INFINITY) t = t * exp_below(m, top) + exp_sum<T>(y, top);
+        if (top != -INFINITY) t = t * exp_below(m, top) + exp_sum<T, Row<T>::U>(y, top);
         m = top;
       }
 #pragma unroll
@@ -431,12 +443,7 @@ __global__ __launch_bounds__(NT) void k_row_select(SelectArgs a) {
     if (a.logprobs) {
       const float m = key_value(hi);
       float t = 0.f;
-      if (m != -INFINITY) {
-#pragma unroll
-        for (int j = 0; j < kUnroll; ++j)
-#pragma unroll
-          for (int i = 0; i < VPT; ++i) t += exp_below(Row<T>::elt(x[j], i), m);
-      }
+      if (m != -INFINITY) t = exp_sum<T, kUnroll>(x, m);
       t = wave_sum(t);
       if (lane == 0) s.sum[wave] = t;
     }
