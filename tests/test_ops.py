@@ -449,6 +449,7 @@ def test_verify_draft_follows_the_target(gpu_lib):
         assert bool(((n - B * p).abs() <= 6 * (B * p * (1 - p)).sqrt()).all())
 
 
+@pytest.mark.filterwarnings("ignore:invalid value encountered in cast")
 @pytest.mark.parametrize("dtype", ["bf16", "f32"])
 @pytest.mark.parametrize("N", [2, 300])
 def test_every_kind_of_nan(gpu_lib, N, dtype):
