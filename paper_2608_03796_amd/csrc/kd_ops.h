@@ -63,7 +63,7 @@ struct KdVerifyArgs {
   int32_t* accepted;        // [B]
   float* prob;              // [B, T] or null
   // workspace
-  float* segm;              // [rows, nseg] largest logit of each segment; rows = the
+  float* segm;              // [rows, nseg] a reference of each segment; rows = the
   double* segs;             // target's, then the draft's. segs: sums of 2^(c (z - segm))
   double* segr;             // [B, nseg] dense draft: sums of the remaining mass
   double* norm;             // [B, 4] dense draft: M, S of the target's and the draft's row

@@ -869,8 +869,8 @@ __device__ __forceinline__ double weight(float z, float m, double c) {
   return exp2_64(((double)z - (double)m) * c);
 }
 // Weights relative to one m, for passes over whole rows: 2^(y / 256) with y = 256 c
-// (z - m) by a table of 2^(i / 256) in LDS and, for the rest of a step, the series of
-// degree 3 about its middle (the next term is below 2^-42 of the result). y is held
+// (z - m) by a table of 2^(i / 256) in LDS and, for the rest of a step, the cubic that
+// is 2^(x / 256) at x = 0, 1/4, 3/4 and 1 (off by at most 2^-44 of it between). y is held
 // 2^18 higher, so that it is positive and its whole part and rest are an operation
 // each: 8 fp64 operations and 6 others where exp2_64 with its difference, comparisons
 // and sum takes 23 and 4 (segment sums of 256 x 6 rows 134 and 72 us). z is held above
@@ -915,9 +915,9 @@ struct Weights {
     const double y = fma((double)__builtin_amdgcn_fmed3f(z, floor, ceil), cs, ms);
     const double g = __builtin_amdgcn_fract(y);
     const uint32_t n = (uint32_t)(int)y;
-    double p = fma(g, 3.31278450399181539888e-9, 3.66556223478407997130e-6);
-    p = fma(p, g, 2.70760617518312146377e-3);
-    p = fma(p, g, 9.99999999999859886130e-1);
+    double p = fma(g, 3.31278488346773615534e-9, 3.66556293497395606907e-6);
+    p = fma(p, g, 2.70760617448262800694e-3);
+    p = fma(p, g, 1.0);
     const uint64_t e = tab[n & (kTab - 1)];
     const uint32_t high = (uint32_t)(e >> 32) + (n << (20 - kTabBits));
     return p * __builtin_bit_cast(double, (uint64_t)high << 32 | (uint32_t)e);
@@ -1260,7 +1260,7 @@ __global__ __launch_bounds__(kVerThreads) void k_accept(VerifyArgs a) {
   __syncthreads();
   const int64_t rt = target_row(a, b, r);
   const float M = rowM[r];
-  const double S = rowS[r];
+  double S = rowS[r];
   if constexpr (DENSE) {
     if (wave == 0 && r < n) {
       float Md;
@@ -1281,7 +1281,7 @@ __global__ __launch_bounds__(kVerThreads) void k_accept(VerifyArgs a) {
   const Row<T> row(a.target, rt * a.ld_t, a.V);
   const float* pm = a.segm + rt * a.nseg;
   const double* ps = a.segs + rt * a.nseg;
-  // entries of the draft at the rejected place: their q, and min(p, q) times S at
+  // entries of the draft at the rejected place: q (eq) and the target's weight (em) at
   // the first of each index (one that repeats counts once, with the sum), else 0
   const bool rest = r < n && S > 0.0;
   // lanes of each of `count` sums, over a workgroup: powers of two up to a wave
@@ -1331,8 +1331,11 @@ __global__ __launch_bounds__(kVerThreads) void k_accept(VerifyArgs a) {
         q += __shfl_xor(q, o);
         again |= __shfl_xor(again, o);
       }
-      if (v >= 0 && sub == 0 && again == 0) eq[k] = fmin(q * S, weight(row.one(v), M, a.c));
+      if (v >= 0 && sub == 0 && again == 0) eq[k] = q;
     }
+    __syncthreads();
+    for (int k = tid; k < Kp; k += kVerThreads)
+      em[k] = eq[k] > 0.0 ? weight(row.one(ei[k]), M, a.c) : 0.0;
     __syncthreads();
   }
   {
@@ -1349,7 +1352,7 @@ __global__ __launch_bounds__(kVerThreads) void k_accept(VerifyArgs a) {
           const s32x4_t w = *reinterpret_cast<const s32x4_t*>(ei + k);
 #pragma unroll
           for (int x = 0; x < 4; ++x)
-            if (w[x] >= v0 && w[x] < v1) take += eq[k + x];
+            if (w[x] >= v0 && w[x] < v1) take += fmin(eq[k + x] * S, em[k + x]);
         }
       }
       for (int o = each / 2; o >= 1; o >>= 1) take += __shfl_xor(take, o);
@@ -1359,16 +1362,58 @@ __global__ __launch_bounds__(kVerThreads) void k_accept(VerifyArgs a) {
   }
   __syncthreads();
   const double u = a.uniform[target_row(a, b, a.T)];
-  int place = pick_place(sh, a.nseg, u, [&](int seg) {
+  // the masses of a segment's places, in sh.x
+  auto fill = [&](int seg) {
     fill_target<T>(sh, row, seg, M, a.c);
     __syncthreads();
     if (rest)
       for (int k = tid; k < a.K; k += kVerThreads) {
         const int e = ei[k] + row.shift - seg * kSegCols;
-        if (eq[k] > 0.0 && (unsigned)e < (unsigned)kSegCols) sh.x[e] -= eq[k];
+        if (eq[k] > 0.0 && (unsigned)e < (unsigned)kSegCols) sh.x[e] -= fmin(eq[k] * S, em[k]);
       }
     __syncthreads();
-  });
+  };
+  // the sum of sh.x, to every thread
+  auto sum_places = [&]() {
+    double t = 0.0;
+    for (int j = tid; j < kSegCols; j += kVerThreads) t += sh.x[j];
+    t = wave_sum64(t);
+    if (lane == 0) sh.scan[wave] = t;
+    __syncthreads();
+    t = 0.0;
+    for (int w = 0; w < kVerWaves; ++w) t += sh.scan[w];
+    __syncthreads();
+    return t;
+  };
+  if (rest) {
+    // Where little is left (a draft rejected with a probability below 2^-10), what is
+    // taken out of the sums leaves their rounding: then the masses place by place,
+    // with the row's sum from the same weights.
+    if (wave == 0) {
+      double t = 0.0;
+      for (int i = lane; i < a.nseg; i += 64) t += sh.seg[i];
+      t = wave_sum64(t);
+      if (lane == 0) sh.goal = t;
+    }
+    __syncthreads();
+    const bool little = sh.goal < S * 0x1p-10;
+    __syncthreads();
+    if (little) {
+      S = 0.0;
+      for (int seg = 0; seg < a.nseg; ++seg) {
+        fill_target<T>(sh, row, seg, M, a.c);
+        __syncthreads();
+        S += sum_places();
+      }
+      for (int seg = 0; seg < a.nseg; ++seg) {
+        fill(seg);
+        const double t = sum_places();
+        if (tid == 0) sh.seg[seg] = t;
+      }
+      __syncthreads();
+    }
+  }
+  int place = pick_place(sh, a.nseg, u, fill);
   if (place < 0 && rest) {
     // p does not exceed q anywhere: from p
     for (int i = tid; i < a.nseg; i += kVerThreads) sh.seg[i] = ps[i] * weight(pm[i], M, a.c);

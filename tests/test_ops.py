@@ -417,6 +417,27 @@ def test_verify_far_logits(gpu_lib, dtype, K):
 
 
 @pytest.mark.parametrize("dtype", ["bf16", "f32"])
+def test_verify_little_left(gpu_lib, dtype):
+    """A draft that is the target but for a mass far below the rounding of 1, rejected
+    for a token that neither of them has: the next one comes from that mass."""
+    B, V = 16, 70001
+    z = _logits(B * 2, V, dtype, 57, V + 1, std=1.0).unflatten(0, (B, 2))
+    z -= 60.0
+    z[:, 0, 25] = float("-inf")
+    z[:, 0, 64] = 3.0
+    z[:, 0, [3000, 65000]] = -45.0
+    draft = dict(draft_idx=torch.full((B, 1, 1), 64, dtype=torch.int32, device="cuda"),
+                 draft_logit=torch.zeros(B, 1, 1, device="cuda"))
+    tokens = torch.full((B, 1), 25, dtype=torch.int32, device="cuda")
+    u = torch.rand(B, 2, generator=_gen(58), device="cuda")
+    _, accepted, _ = _check_verify(gpu_lib, z, tokens, u, draft)
+    assert not accepted.any()
+    # and with a mass of 2^-12, near where the way changes
+    z[:, 0, 40000] = 3.0 - 12 * np.log(2.0)
+    _check_verify(gpu_lib, z, tokens, u, draft)
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
 def test_verify_without_draft(gpu_lib, dtype):
     """T = 0: a draw from the target alone; and B = 0."""
     target, tokens, u, _ = _draft(6, 0, 4099, 0, dtype, 61, ld=1)
@@ -602,3 +623,29 @@ def test_calls_on_two_streams_at_once(gpu_lib):
         for (_, out), want in zip(graphs, wants):
             for a, b in zip(out, want):
                 assert all(torch.equal(a[k], b[k]) for k in b)
+
+
+@pytest.mark.parametrize("seed", range(12))
+def test_sweep(gpu_lib, seed):
+    """Seeded problems of any size: selections and verifications against the oracle."""
+    import random
+    kd, rng = gpu_lib, random.Random(seed)
+    for _ in range(4):
+        V = int(round(2 ** rng.uniform(0, 16.2)))
+        N = rng.choice([1, 2, 5, 270]) if V < 3000 else rng.choice([1, 3])
+        K = rng.randint(1, min(V, rng.choice([3, 40, 700])))
+        dtype, pad, offset = rng.choice(["bf16", "f32"]), rng.randint(0, 9), rng.randint(0, 7)
+        kind = rng.choice(SPECIALS if V >= 3 else ("plain",))
+        print(f"[sweep] topk {N} {V} {K} +{pad} +{offset} {dtype} {kind}", flush=True)
+        _check_topk(kd, _special(_logits(N, V, dtype, seed, V + pad, offset), kind)
+                    if kind != "plain" else _logits(N, V, dtype, seed, V + pad, offset), K)
+    for _ in range(4):
+        V = int(round(2 ** rng.uniform(1, 15)))
+        B, T = rng.randint(1, 9), rng.randint(1, 6)
+        K = rng.choice([0, rng.randint(1, min(V, rng.choice([1, 30, 600])))])
+        dtype, ld = rng.choice(["bf16", "f32"]), rng.randint(0, 9)
+        tau, masked = rng.choice([0.3, 0.9, 1.0, 2.5]), rng.choice([0.0, 0.4, 0.95])
+        print(f"[sweep] verify {B} {T} {V} {K} +{ld} {dtype} {tau} {masked}", flush=True)
+        target, tokens, u, draft = _draft(B, T, V, K, dtype, seed + 200, ld, masked)
+        n = torch.randint(0, T + 1, (B,), generator=_gen(seed), device="cuda", dtype=torch.int32)
+        _check_verify(kd, target, tokens, u, draft, tau, rng.choice([None, n]))
