@@ -359,7 +359,8 @@ kd_status kd_scale_grads(const float* grad_loss,
  * buffers, checks before anything is enqueued, one stream, the same bits from
  * the same inputs). They allocate nothing and never synchronise, so they may be
  * captured into a HIP graph; calls that overlap in time need workspaces of their
- * own. kd_profile_enable times the loss's kernels only.
+ * own. An output or the workspace overlaps no other buffer of the call.
+ * kd_profile_enable times the loss's kernels only.
  *
  * Logits rows are [N, ld] with V <= ld columns used (the rest is never read),
  * and may start at any element boundary. A logit that is not a number counts

@@ -145,6 +145,23 @@ def test_topk_entries_streamed(gpu_lib, N, V, K, ld, offset, dtype, kind):
     assert np.array_equal(to64(got["teacher_logit"][some]), val)
 
 
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+def test_topk_entries_largest(gpu_lib, dtype):
+    """More rows than have a workgroup of 1024 threads each, at the largest V and K."""
+    kd, N, V, K = gpu_lib, 260, 1 << 20, 4096
+    x = _logits(N, V, dtype, 15)
+    for logprobs in (False, True):
+        got = kd.topk_entries(x, K, logprobs=logprobs)
+        for r in (0, N - 4):
+            part = kd.topk_entries(x[r:r + 4], K, logprobs=logprobs)
+            assert torch.equal(got["teacher_idx"][r:r + 4], part["teacher_idx"])
+            assert torch.equal(got["teacher_logit"][r:r + 4], part["teacher_logit"])
+    idx, val = oo.topk_entries(x[N - 1:].float().cpu().numpy(), K)
+    got = kd.topk_entries(x, K)
+    assert np.array_equal(to64(got["teacher_idx"][N - 1:]), idx)
+    assert np.array_equal(to64(got["teacher_logit"][N - 1:]), val)
+
+
 def test_topk_many_rows_in_batches(gpu_lib):
     """More rows than the workspace holds at a time."""
     kd, N, V, K = gpu_lib, 500000, 9, 2
@@ -450,6 +467,20 @@ def test_verify_draft_large_vocabulary(gpu_lib):
     for K in (0, 100):
         target, tokens, u, draft = _draft(2, 2, 1 << 20, K, "bf16", 71)
         _check_verify(gpu_lib, target, tokens, u, draft)
+
+
+@pytest.mark.parametrize("V,K", [(5000, 4096), (1 << 20, 4096), (300, 0)])
+def test_verify_longest_draft(gpu_lib, V, K):
+    """T = 1024 places, the most entries: any, all, half of them, all but the last kept."""
+    B, T = 1, 1024 if V < 1 << 20 else 20
+    target, tokens, u, draft = _draft(B, T, V, K, "bf16", 72, err=0.1)
+    _check_verify(gpu_lib, target, tokens, u, draft)
+    u[:, :T] = 0.0   # kept wherever the target has the token
+    for lengths in (None, torch.tensor([T // 2], dtype=torch.int32, device="cuda")):
+        want = _check_verify(gpu_lib, target, tokens, u, draft, lengths=lengths)
+        assert want[1][0] == (T if lengths is None else T // 2)
+    tokens[0, T - 1] = -1
+    assert _check_verify(gpu_lib, target, tokens, u, draft)[1][0] == T - 1
 
 
 def test_verify_draft_follows_the_target(gpu_lib):
