@@ -875,12 +875,15 @@ __device__ __forceinline__ double weight(float z, float m, double c) {
 // each: 8 fp64 operations and 6 others where exp2_64 with its difference, comparisons
 // and sum takes 23 and 4 (segment sums of 256 x 6 rows 134 and 72 us). z is held above
 // m - 990 / c, where weights no longer count (2^-990; -inf and a quiet NaN end there
-// too), and below m + 900 / c. fp32 can tell these from m where `fast`; elsewhere
-// (infinities, extreme tau) weight() serves.
+// too), and below m + 900 / c. fp32 can tell these from m where `fast`: its rounding of
+// them, at most 2^-24 (|m| + 990 / c) with |m| below 65536 * 990 / c, moves their weights
+// by up to 2^3.9, so one that is held back stays above kHeld. Elsewhere (infinities,
+// extreme tau) weight() serves.
 constexpr int kTabBits = 8, kTab = 1 << kTabBits;
 // 2^(i / 256) less i << 12 in its high word, and less 2^18 << 12: adding n << 12 for
 // n = 2^18 + i + 256 j gives 2^(j + i / 256)
 constexpr int kTabLift = 1 << 18;
+constexpr double kHeld = 0x1p890;
 struct Roots {
   uint64_t v[kTab];
   constexpr Roots() : v() {
@@ -971,7 +974,8 @@ __device__ __forceinline__ int64_t draft_row(const VerifyArgs& a, int b, int t) 
 // 131072 in bf16, 0.24 GB read, 72 us; the same read without the weights 44. 64 bits
 // hold the weights of logits well above the reference too, so the largest of a
 // quarter (bf16) or an eighth of the segment serves, the largest of all where that is
-// -inf; a segment whose sum passes 2^899 is summed again below its largest logit.
+// -inf; a segment whose sum reaches kHeld, as it does where a logit was held back, is
+// summed again below its largest logit.
 template <typename T>
 __global__ __launch_bounds__(256) void k_seg_sums(VerifyArgs a, int waves) {
   __shared__ uint64_t tab[kTab];
@@ -1015,7 +1019,7 @@ __global__ __launch_bounds__(256) void k_seg_sums(VerifyArgs a, int waves) {
       s = wave_sum64(s + h);
     }
     // (a signalling NaN that med3 let through makes the sum none either)
-    if (!q.fast || !(s < 0x1p899)) {
+    if (!q.fast || !(s < kHeld)) {
       m = largest(U);
       s = 0.0;
 #pragma unroll
