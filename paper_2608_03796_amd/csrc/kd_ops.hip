@@ -17,8 +17,9 @@ namespace kd {
 // between the boundary at or before the row and the row. Vectors that reach
 // past either end of the row are read element by element; what is not of the
 // row reads as -inf.
-// z, or -inf where it is not a number
-__device__ __forceinline__ float number(float z) { return z > -INFINITY ? z : -INFINITY; }
+// z, or -inf where it is not a number. (The comparison has to be with z itself: of
+// z > -inf the compiler makes a maximum, which is a NaN where z is a signalling one.)
+__device__ __forceinline__ float number(float z) { return __builtin_isnan(z) ? -INFINITY : z; }
 template <typename T>
 struct Row {
   static constexpr int VPT = 16 / (int)sizeof(T);      // elements of a vector
