@@ -1154,6 +1154,47 @@ __device__ __forceinline__ int pick_place(VerifyShared& sh, int nseg, double u, 
   return -1;
 }
 
+// What the draft leaves of p at a token, 0 up to the rounding of the two: weights hundreds
+// of powers of two from their references are off by up to 2^-42, and a draft that has the
+// target's probabilities leaves nothing.
+__device__ __forceinline__ double excess(double p, double q) {
+  return p - q > p * 0x1p-40 ? p - q : 0.0;
+}
+
+// the sum of the threads' x, to every thread
+__device__ __forceinline__ double block_sum(VerifyShared& sh, double x) {
+  x = wave_sum64(x);
+  if ((threadIdx.x & 63) == 0) sh.scan[threadIdx.x >> 6] = x;
+  __syncthreads();
+  x = 0.0;
+  for (int w = 0; w < kVerWaves; ++w) x += sh.scan[w];
+  __syncthreads();
+  return x;
+}
+// the sum of sh.x
+__device__ __forceinline__ double sum_places(VerifyShared& sh) {
+  double t = 0.0;
+  for (int j = threadIdx.x; j < kSegCols; j += kVerThreads) t += sh.x[j];
+  return block_sum(sh, t);
+}
+
+// Where little is left (a draft rejected with a probability below 2^-10), the segments'
+// sums of it are mostly the rounding of what is taken out of them: then the masses are
+// formed again place by place, with the rows' sums from the same weights. The question is
+// answered by wave 0's sum of sh.seg, which all threads have written.
+__device__ __forceinline__ bool little_left(VerifyShared& sh, int nseg, double all) {
+  if (threadIdx.x < 64) {
+    double t = 0.0;
+    for (int i = threadIdx.x; i < nseg; i += 64) t += sh.seg[i];
+    t = wave_sum64(t);
+    if (threadIdx.x == 0) sh.goal = t;
+  }
+  __syncthreads();
+  const bool little = sh.goal < all * 0x1p-10;
+  __syncthreads();
+  return little;
+}
+
 // place -> token, and the tokens behind it
 __device__ __forceinline__ void write_tokens(const VerifyArgs& a, int b, int r, int next) {
   int32_t* out = a.out_tokens + (int64_t)b * (a.T + 1);
@@ -1374,49 +1415,23 @@ __global__ __launch_bounds__(kVerThreads) void k_accept(VerifyArgs a) {
     if (rest)
       for (int k = tid; k < a.K; k += kVerThreads) {
         const int e = ei[k] + row.shift - seg * kSegCols;
-        if (eq[k] > 0.0 && (unsigned)e < (unsigned)kSegCols) sh.x[e] -= fmin(eq[k] * S, em[k]);
+        if (eq[k] > 0.0 && (unsigned)e < (unsigned)kSegCols) sh.x[e] = excess(em[k], eq[k] * S);
       }
     __syncthreads();
   };
-  // the sum of sh.x, to every thread
-  auto sum_places = [&]() {
-    double t = 0.0;
-    for (int j = tid; j < kSegCols; j += kVerThreads) t += sh.x[j];
-    t = wave_sum64(t);
-    if (lane == 0) sh.scan[wave] = t;
-    __syncthreads();
-    t = 0.0;
-    for (int w = 0; w < kVerWaves; ++w) t += sh.scan[w];
-    __syncthreads();
-    return t;
-  };
-  if (rest) {
-    // Where little is left (a draft rejected with a probability below 2^-10), what is
-    // taken out of the sums leaves their rounding: then the masses place by place,
-    // with the row's sum from the same weights.
-    if (wave == 0) {
-      double t = 0.0;
-      for (int i = lane; i < a.nseg; i += 64) t += sh.seg[i];
-      t = wave_sum64(t);
-      if (lane == 0) sh.goal = t;
-    }
-    __syncthreads();
-    const bool little = sh.goal < S * 0x1p-10;
-    __syncthreads();
-    if (little) {
-      S = 0.0;
-      for (int seg = 0; seg < a.nseg; ++seg) {
-        fill_target<T>(sh, row, seg, M, a.c);
-        __syncthreads();
-        S += sum_places();
-      }
-      for (int seg = 0; seg < a.nseg; ++seg) {
-        fill(seg);
-        const double t = sum_places();
-        if (tid == 0) sh.seg[seg] = t;
-      }
+  if (rest && little_left(sh, a.nseg, S)) {
+    S = 0.0;
+    for (int seg = 0; seg < a.nseg; ++seg) {
+      fill_target<T>(sh, row, seg, M, a.c);
       __syncthreads();
+      S += sum_places(sh);
     }
+    for (int seg = 0; seg < a.nseg; ++seg) {
+      fill(seg);
+      const double t = sum_places(sh);
+      if (tid == 0) sh.seg[seg] = t;
+    }
+    __syncthreads();
   }
   int place = pick_place(sh, a.nseg, u, fill);
   if (place < 0 && rest) {
@@ -1449,7 +1464,7 @@ struct RestRow {
   }
   __device__ __forceinline__ double exact(float zt, float zd) const {
     const double p = t.exact(zt) * it;
-    return rest ? fmax(p - d.exact(zd) * id, 0.0) : p;
+    return rest ? excess(p, d.exact(zd) * id) : p;
   }
 };
 // vector of the draft's row at the target's place e (its own boundary may differ)
@@ -1518,7 +1533,7 @@ __global__ __launch_bounds__(kVerThreads) void k_pick(VerifyArgs a) {
   const int64_t rt = target_row(a, b, r);
   const Row<T> row(a.target, rt * a.ld_t, a.V);
   const Row<T> dr(a.draft, draft_row(a, b, rest ? r : 0) * a.ld_d, a.V);
-  const RestRow m(a, b, rest, nullptr);
+  RestRow m(a, b, rest, nullptr);
   const float* pm = a.segm + rt * a.nseg;
   const double* ps = a.segs + rt * a.nseg;
   for (int i = tid; i < a.nseg; i += kVerThreads)
@@ -1528,7 +1543,7 @@ __global__ __launch_bounds__(kVerThreads) void k_pick(VerifyArgs a) {
   __syncthreads();
   const double u = a.uniform[target_row(a, b, a.T)];
   constexpr int VPT = Row<T>::VPT;
-  int place = pick_place(sh, a.nseg, u, [&](int seg) {
+  auto fill = [&](int seg) {
     for (int j = tid; j < kSegCols / VPT; j += kVerThreads) {
       const int e = seg * kSegCols + j * VPT;
       const u32x4_t x = row.at(e);
@@ -1538,7 +1553,28 @@ __global__ __launch_bounds__(kVerThreads) void k_pick(VerifyArgs a) {
         sh.x[j * VPT + i] = m.exact(Row<T>::elt(x, i), Row<T>::elt(y, i));
     }
     __syncthreads();
-  });
+  };
+  if (rest && m.it > 0.0 && little_left(sh, a.nseg, 1.0)) {
+    double st = 0.0, sd = 0.0;
+    for (int e = tid * VPT; e < a.nseg * kSegCols; e += kVerThreads * VPT) {
+      const u32x4_t x = row.at(e), y = draft_at<T>(dr, e, row.shift);
+      for (int i = 0; i < VPT; ++i) {
+        st += m.t.exact(Row<T>::elt(x, i));
+        sd += m.d.exact(Row<T>::elt(y, i));
+      }
+    }
+    st = block_sum(sh, st);
+    sd = block_sum(sh, sd);
+    m.it = 1.0 / st;
+    m.id = sd > 0.0 ? 1.0 / sd : 0.0;
+    for (int seg = 0; seg < a.nseg; ++seg) {
+      fill(seg);
+      const double t = sum_places(sh);
+      if (tid == 0) sh.seg[seg] = t;
+    }
+    __syncthreads();
+  }
+  int place = pick_place(sh, a.nseg, u, fill);
   if (place < 0 && rest && m.it > 0.0) {
     for (int i = tid; i < a.nseg; i += kVerThreads) sh.seg[i] = ps[i] * m.t.exact(pm[i]);
     __syncthreads();

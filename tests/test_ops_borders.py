@@ -115,3 +115,55 @@ def test_verify_every_kind_of_nan(gpu_lib, dtype, K, tau):
         for i, b in enumerate(kinds):
             bits[torch.rand(t.shape, generator=_gen(30 + 4 * j + i), device="cuda") < 0.2] = b
     _check_verify(gpu_lib, target, tokens, u, draft, tau)
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+def test_verify_little_left_of_a_dense_draft(gpu_lib, dtype):
+    """The draft's whole distribution on one token that has all of the target's mass but
+    far less than the rounding of 1: rejected, the next token comes from that rest."""
+    B, V = 48, 70001
+    z = _logits(B * 2, V, dtype, 57, V + 1, std=1.0).unflatten(0, (B, 2))
+    z -= 60.0
+    z[:, 0, 25] = float("-inf")
+    big = 3.0 + 4.0 * torch.rand(B, generator=_gen(59), device="cuda").to(DT[dtype])
+    z[:, 0, 1500] = big
+    z[:, 0, [3000, 65000]] = -45.0
+    d = torch.full((B, 1, V), float("-inf"), dtype=DT[dtype], device="cuda")
+    d[:, 0, 1500] = big * 0.7
+    tokens = torch.full((B, 1), 25, dtype=torch.int32, device="cuda")
+    u = torch.rand(B, 2, generator=_gen(58), device="cuda")
+    _, accepted, _ = _check_verify(gpu_lib, z, tokens, u, dict(draft_logits=d))
+    assert not accepted.any()
+    # with a small share of the draft elsewhere (twice what the target has there), and
+    # with a rest of about 2^-12 and 2^-9
+    d[:, 0, 3001] = big * 0.7 + z[:, 0, 3001] - z[:, 0, 1500] + np.log(2.0)
+    _check_verify(gpu_lib, z, tokens, u, dict(draft_logits=d))
+    for e in (12, 9):
+        z[:, 0, 40000] = big - e * np.log(2.0)
+        _check_verify(gpu_lib, z, tokens, u, dict(draft_logits=d))
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+@pytest.mark.parametrize("V,ld,dense", [(30011, 0, True), (30011, 5, True), (4096, 3, False),
+                                        (50, 0, False), (50, 1, True)])
+def test_verify_draft_equal_to_the_target(gpu_lib, V, ld, dense, dtype):
+    """The draft has the target's probabilities, and a token that neither has (or that
+    does not exist) is rejected: nothing is left of p - q, so the next token comes from
+    p, whatever the rows' strides."""
+    print(f"[equal] {V} +{ld} {dtype} dense={dense}", flush=True)
+    B, T = 24, 2
+    z = _logits(B * (T + 1), V, dtype, 61, V + ld, std=3.0).unflatten(0, (B, T + 1))
+    z[:, :, 7] = float("-inf")
+    d = z[:, :T].clone(memory_format=torch.contiguous_format)
+    tokens = torch.full((B, T), 7, dtype=torch.int32, device="cuda")
+    tokens[::3, 0] = V
+    tokens[1::3, 0] = d[1::3, 0].float().argmax(1).int()
+    u = torch.rand(B, T + 1, generator=_gen(62), device="cuda")
+    draft = dict(draft_logits=d)
+    if not dense:
+        idx = torch.arange(V, dtype=torch.int32, device="cuda").expand(B, T, V).contiguous()
+        draft = dict(draft_idx=idx, draft_logit=d.float())
+    _, accepted, _ = _check_verify(gpu_lib, z, tokens, u, draft)
+    assert set(accepted.tolist()) == {0, 1}
