@@ -1402,8 +1402,12 @@ __global__ __launch_bounds__(kVerThreads) void k_accept(VerifyArgs a) {
         }
       }
       for (int o = each / 2; o >= 1; o >>= 1) take += __shfl_xor(take, o);
-      if (sub == 0 && i < a.nseg)
-        sh.seg[i] = M == -INFINITY ? 0.0 : fmax(ps[i] * weight(pm[i], M, a.c) - take, 0.0);
+      if (sub == 0 && i < a.nseg) {
+        // (where the rounding leaves nothing of a sum that was taken from, its places
+        // may still hold a little, which a random number of 0 asks for)
+        const double left = M == -INFINITY ? 0.0 : ps[i] * weight(pm[i], M, a.c) - take;
+        sh.seg[i] = left > 0.0 ? left : take > 0.0 ? 0x1p-1000 : 0.0;
+      }
     }
   }
   __syncthreads();

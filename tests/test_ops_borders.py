@@ -167,3 +167,23 @@ def test_verify_draft_equal_to_the_target(gpu_lib, V, ld, dense, dtype):
         draft = dict(draft_idx=idx, draft_logit=d.float())
     _, accepted, _ = _check_verify(gpu_lib, z, tokens, u, draft)
     assert set(accepted.tolist()) == {0, 1}
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+def test_verify_first_of_a_small_rest(gpu_lib, dtype):
+    """A random number of 0 draws the first token of which anything is left, also where
+    the draft has taken all of its stretch of the row but far less than its rounding."""
+    B, V = 64, 9001
+    z = _logits(B * 2, V, dtype, 71, V + 2, std=1.0).unflatten(0, (B, 2))
+    z[:, 0, :4500] -= 46.0
+    z[:, 0, :10] = float("-inf")
+    z[:, 0, 1000] = 8.5 + 0.5 * torch.rand(B, generator=_gen(72), device="cuda")
+    z[:, 0, 3000] = 8.5
+    k = torch.tensor([1000, 3000], dtype=torch.int32, device="cuda").expand(B, 1, 2).contiguous()
+    l = torch.zeros(B, 1, 2, device="cuda")
+    l[:, :, 1] = -0.2
+    tokens = torch.full((B, 1), 5, dtype=torch.int32, device="cuda")
+    u = torch.zeros(B, 2, device="cuda")
+    out, accepted, _ = _check_verify(gpu_lib, z, tokens, u, dict(draft_idx=k, draft_logit=l))
+    assert not accepted.any() and (out[:, 0] == 10).all()
