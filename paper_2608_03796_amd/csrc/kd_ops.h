@@ -23,7 +23,7 @@ constexpr int64_t kd_row_segs(int64_t V, int eb, bool aligned = false) {
 constexpr int kCacheCodeBits = 12;
 constexpr int kCacheCodeMax = 4094;
 constexpr int kCacheNone = 4095;
-constexpr float kCacheReach = 1024.f;
+constexpr double kCacheReach = 1024.0;
 
 struct KdTopkArgs {
   const void* logits;       // [rows, ld]

@@ -678,7 +678,9 @@ __global__ __launch_bounds__(NT) void k_row_select(SelectArgs a) {
     for (int k0 = 0; k0 < K; k0 += 64) {
       const int k = k0 + lane;
       const float z = fminf(key_value((uint32_t)(cand[k < K ? k : 0] >> 32)), 3.402823466e38f);
-      kept += __popcll(__builtin_amdgcn_ballot_w64(!empty && k < K && z >= top - kCacheReach));
+      // (in fp32 top - 1024 is rounded to 2^-14, or 2^-13, and entries there misjudged)
+      const bool near = (double)z >= (double)top - kCacheReach;
+      kept += __popcll(__builtin_amdgcn_ballot_w64(!empty && k < K && near));
     }
     if (lane == 0) s.n = kept;
   }

@@ -187,3 +187,25 @@ def test_verify_first_of_a_small_rest(gpu_lib, dtype):
     u = torch.zeros(B, 2, device="cuda")
     out, accepted, _ = _check_verify(gpu_lib, z, tokens, u, dict(draft_idx=k, draft_logit=l))
     assert not accepted.any() and (out[:, 0] == 10).all()
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+def test_teacher_cache_next_to_the_reach(gpu_lib, dtype):
+    """Entries 1024 below the row's largest are kept, those any further are not: the
+    difference is compared, not a rounded bound."""
+    tops = torch.tensor([2.0 ** -15, 1.0, 0.1, 0.3, 3.0 ** -9, 100.7, -0.7, 5e-7], device="cuda")
+    tops = tops.to(DT[dtype])
+    x = torch.full((len(tops), 300), -5.0, dtype=DT[dtype], device="cuda")
+    x[:, 17] = tops
+    # the numbers around the bound, in steps of fp32 (bf16: of its own)
+    at = tops.float() - 1024.0
+    bits = at.to(DT[dtype]).view(torch.int32 if dtype == "f32" else torch.int16)
+    for j in range(-4, 5):
+        x[:, 100 + 7 * j] = (bits + j).view(DT[dtype])
+    x[:, 200] = -1024.0
+    K = 300
+    c = gpu_lib.teacher_cache_write(x, K)
+    e, top, step = oo.cache_write(to64(x), K)
+    assert np.array_equal(to64(c["entries"]).astype(np.int64) & 0xffffffff, e)
+    assert np.array_equal(to64(c["scale"]), np.stack([top, step], 1))
