@@ -876,7 +876,9 @@ __device__ __forceinline__ double weight(float z, float m, double c) {
 // is 2^(x / 256) at x = 0, 1/4, 3/4 and 1 (off by at most 2^-44 of it between). y is held
 // 2^18 higher, so that it is positive and its whole part and rest are an operation
 // each: 8 fp64 operations and 6 others where exp2_64 with its difference, comparisons
-// and sum takes 23 and 4 (segment sums of 256 x 6 rows 134 and 72 us). z is held above
+// and sum takes 23 and 4 (segment sums of 256 x 6 rows 134 and 72 us). The rounding of y
+// at 2^18 is 2^-43 of the weight; that of 256 c m, which is all weights' and grows with it,
+// is kept as a factor for their sum (`fix`: without it 3e-9 at m / tau = 3e7). z is held above
 // m - 990 / c, where weights no longer count (2^-990; -inf and a quiet NaN end there
 // too), and below m + 900 / c. fp32 can tell these from m where `fast`: its rounding of
 // them, at most 2^-24 (|m| + 990 / c) with |m| below 65536 * 990 / c, moves their weights
@@ -904,7 +906,7 @@ __device__ __forceinline__ void load_roots(uint64_t* tab) {
   __syncthreads();
 }
 struct Weights {
-  double c, cs, ms;
+  double c, cs, ms, fix;
   float m, floor, ceil;
   bool fast;
   const uint64_t* tab;
@@ -915,8 +917,16 @@ struct Weights {
     floor = (float)((double)m - reach);
     ceil = (float)((double)m + reach * (900.0 / 990.0));
     cs = (double)kTab * c;
-    ms = kTabLift - (double)m * cs;
+    {
+#pragma clang fp contract(off)
+      // m cs = p + e exactly, and 2^18 - p = ms + d exactly
+      const double p = (double)m * cs, e = __builtin_fma((double)m, cs, -p);
+      ms = kTabLift - p;
+      const double r = ms - kTabLift, d = (kTabLift - (ms - r)) - (p + r);
+      fix = 1.0 + (d - e) * (0.69314718055994530942 / kTab);
+    }
   }
+  // the weight of z over `fix`
   __device__ __forceinline__ double quick(float z) const {
     const double y = fma((double)__builtin_amdgcn_fmed3f(z, floor, ceil), cs, ms);
     const double g = __builtin_amdgcn_fract(y);
@@ -1019,7 +1029,7 @@ __global__ __launch_bounds__(256) void k_seg_sums(VerifyArgs a, int waves) {
           h += q.quick(Row<T>::raw(x[u], i + 1));
         }
       }
-      s = wave_sum64(s + h);
+      s = wave_sum64(s + h) * q.fix;
     }
     // (a signalling NaN that med3 let through makes the sum none either)
     if (!q.fast || !(s < kHeld)) {
@@ -1466,7 +1476,7 @@ struct RestRow {
         rest(rest_) {}
   __device__ __forceinline__ bool fast() const { return t.fast && d.fast; }
   __device__ __forceinline__ double quick(float zt, float zd) const {
-    return fmax(t.quick(zt) * it - d.quick(zd) * id, 0.0);
+    return fmax(t.quick(zt) * (it * t.fix) - d.quick(zd) * (id * d.fix), 0.0);
   }
   __device__ __forceinline__ double exact(float zt, float zd) const {
     const double p = t.exact(zt) * it;

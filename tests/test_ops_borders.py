@@ -209,3 +209,35 @@ def test_teacher_cache_next_to_the_reach(gpu_lib, dtype):
     e, top, step = oo.cache_write(to64(x), K)
     assert np.array_equal(to64(c["entries"]).astype(np.int64) & 0xffffffff, e)
     assert np.array_equal(to64(c["scale"]), np.stack([top, step], 1))
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("tau,scale", [(1e-6, 1.0), (4e-5, 32.0)])
+def test_verify_draw_next_to_a_border(gpu_lib, tau, scale):
+    """Logits of many times tau, a step of fp32 or a few of them apart, so that c z is
+    about 2^25 and rounded by far more than the weights may be. A row has equal logits in
+    its first stretch of 2048 columns and equal ones, some steps above, in its second;
+    the random number is next to the border between them, 3e-11 to 3e-10 of the row away
+    (64 bits are off by less than 1e-12)."""
+    B, V, step = 64, 4096, 2.0 ** -19
+    rng = np.random.default_rng(3)
+    z = np.full((B, 1, V), -np.inf, dtype=np.float32)
+    u = np.zeros((B, 1), dtype=np.float32)
+    n = np.arange(1, 2049, dtype=np.float64)
+    sides = []
+    for k in (1, 2, 3):
+        # counts of the two whose border c is that near a number of fp32
+        w = np.exp(k * step * scale / tau)
+        c = n[:, None] / (n[:, None] + n[None, :] * w)
+        off = (c.astype(np.float32).astype(np.float64) - c) / c
+        near = np.argwhere((np.abs(off) > 3e-11) & (np.abs(off) < 3e-10))
+        for b in range(k - 1, B, 3):
+            i, j = near[rng.integers(len(near))]
+            base = (16.0 + step * rng.integers(0, 1 << 22)) * scale
+            z[b, 0, :i + 1] = base
+            z[b, 0, 2048:2048 + j + 1] = base + k * step * scale
+            u[b, 0] = c[i, j]
+            sides.append(off[i, j] > 0)
+    assert 10 < sum(sides) < B - 10
+    tokens = torch.empty(B, 0, dtype=torch.int32, device="cuda")
+    _check_verify(gpu_lib, torch.from_numpy(z).cuda(), tokens, torch.from_numpy(u).cuda(), {}, tau)
