@@ -206,7 +206,8 @@ def _check_inputs(hidden, W, teacher_idx, teacher_logit, ignore, checkpoint=Fals
 
 def _check_tensor(name, t, shape, dtype, device):
     """A caller-provided output or extra input: exact shape, dtype, device, layout."""
-    if t.shape != shape or t.dtype != dtype or t.device != device or not t.is_contiguous():
+    if t.shape != tuple(shape) or t.dtype != dtype or t.device != device \
+            or not t.is_contiguous():
         raise ValueError(f"{name} must be a contiguous {dtype} tensor of shape {tuple(shape)} "
                          f"on {device} (got {t.dtype} {tuple(t.shape)} on {t.device})")
 

@@ -5,6 +5,7 @@ import numpy as np
 import pytest
 import torch
 
+import paper_2608_03796_amd as pkg
 from oracle import ops_oracle as oo
 from tests.helpers import to64
 from tests.test_ops import DT, E32, _check_topk, _check_verify, _draft, _gen, _logits
@@ -241,3 +242,12 @@ def test_verify_draw_next_to_a_border(gpu_lib, tau, scale):
     assert 10 < sum(sides) < B - 10
     tokens = torch.empty(B, 0, dtype=torch.int32, device="cuda")
     _check_verify(gpu_lib, torch.from_numpy(z).cuda(), tokens, torch.from_numpy(u).cuda(), {}, tau)
+
+
+def test_check_tensor_takes_any_sequence_as_shape():
+    t = torch.zeros(2, 3)
+    for shape in ((2, 3), [2, 3], t.shape):
+        pkg._check_tensor("t", t, shape, torch.float32, t.device)
+    for shape in ((3, 2), [2], (2, 3, 1)):
+        with pytest.raises(ValueError):
+            pkg._check_tensor("t", t, shape, torch.float32, t.device)
