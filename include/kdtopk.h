@@ -397,7 +397,9 @@ kd_status kd_topk_entries_workspace_size(const kd_rows* p, size_t* bytes);
  *                          16-byte aligned
  *
  * A row with fewer than K logits above -inf has its list filled with -inf at
- * the lowest indices of such columns. Errors: KD_ERR_NULL_PTR, KD_ERR_BAD_SHAPE,
+ * the lowest indices of such columns. The loss is not a number for a row whose
+ * entries are all -inf (value[n, 0] = -inf: it has no target and has to be ignored
+ * there, as kd_teacher_cache_read marks it) or hold +inf. Errors: KD_ERR_NULL_PTR, KD_ERR_BAD_SHAPE,
  * KD_ERR_BAD_ARG (flags), KD_ERR_UNSUPPORTED (dtype, a pointer that is not
  * aligned to its elements, workspace not to 16 bytes),
  * KD_ERR_WORKSPACE_TOO_SMALL, KD_ERR_DEVICE.
@@ -410,7 +412,8 @@ kd_status kd_topk_entries(const kd_rows* p, const void* logits, int32_t* idx, fl
  * index << 12 | code, and a row has a scale (top, step):
  *   value of an entry = top - code * step, code 0..4094; code 4095 = no entry.
  * step = (largest - least kept logit) / 4094 in fp32, so a kept value is off by
- * at most step / 2. Entries that are -inf or more than 1024 below the row's
+ * at most step / 2 before it is rounded to fp32 (where the kept logits lie within
+ * 2^-125, whose step fp32 cannot hold, by at most that range). Entries that are -inf or more than 1024 below the row's
  * largest (whose probability is 0 at every temperature up to 9) are not
  * kept: their code is 4095. top is the largest logit, or its log-probability
  * with KD_FLAG_TEACHER_LOGPROBS; -inf marks a row that keeps nothing. Infinite

@@ -577,7 +577,10 @@ def topk_kl_loss(hidden, W, teacher_idx, teacher_logit, tau: float = 1.0, ignore
     forward to backward in 8 bits (checkpoint_write: 1.03 bytes an element
     instead of 2 or 4; the caller's own tensor may be freed), and the gradients
     are those of the loss at the values held (bwd_checkpoint). The loss itself is
-    computed from the exact ones.
+    computed from the exact ones. The backward is the fused schedule's, which forms
+    log Z with the gradient: in bf16 grad_W's contraction has the hidden rows times
+    their tokens' factors, rounded to bf16 (2.9e-3 off in the 2-norm, final rounding
+    included), where schedule="recompute" alone has the rows as they are.
     workspace: a uint8 device tensor of at least workspace_size(...) bytes to
     reuse across calls (allocated per call when None)."""
     import torch
@@ -595,8 +598,9 @@ def topk_kl_loss(hidden, W, teacher_idx, teacher_logit, tau: float = 1.0, ignore
                        teacher_logprobs=teacher_logprobs, workspace=workspace)["loss"]
     if _TOPK_KL is None:
         _TOPK_KL = _autograd_functions()
-    return _TOPK_KL["checkpoint" if checkpoint else schedule].apply(hidden, W, teacher_idx, teacher_logit, float(tau), ignore,
-                                    int(chunk), bool(teacher_logprobs), workspace)
+    return _TOPK_KL["checkpoint" if checkpoint else schedule].apply(
+        hidden, W, teacher_idx, teacher_logit, float(tau), ignore, int(chunk),
+        bool(teacher_logprobs), workspace)
 
 
 def check_indices(teacher_idx, V, chunk=4096, D=64, tau=1.0, dtype=KD_BF16, workspace=None):
@@ -700,8 +704,10 @@ def topk_entries(logits, K, logprobs: bool = False, out=None, workspace=None):
     of logits [N, V] (bf16 or fp32, rows evenly spaced), as the loss takes them.
     Returns {'teacher_idx' [N, K] int32, 'teacher_logit' [N, K] fp32}, largest
     first, of equal ones the lowest index first; log-probabilities over the
-    whole vocabulary with logprobs (for teacher_logprobs=True). `out` may carry
-    the outputs, `workspace` a uint8 tensor of topk_workspace_size bytes."""
+    whole vocabulary with logprobs (for teacher_logprobs=True). No gradient flows
+    to logits. A row whose first value is -inf holds no target, and one with +inf
+    no finite loss: pass such rows to the loss as ignored. `out` may carry the
+    outputs, `workspace` a uint8 tensor of topk_workspace_size bytes."""
     import torch
     pr, workspace = _topk_rows(logits, K, logprobs, workspace)
     dev = logits.device

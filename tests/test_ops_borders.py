@@ -6,8 +6,9 @@ import pytest
 import torch
 
 import paper_2608_03796_amd as pkg
+from oracle import kd_topk_kl
 from oracle import ops_oracle as oo
-from tests.helpers import to64
+from tests.helpers import rel_max, to64
 from tests.test_ops import DT, E32, _check_topk, _check_verify, _draft, _gen, _logits
 
 
@@ -251,3 +252,29 @@ def test_check_tensor_takes_any_sequence_as_shape():
     for shape in ((3, 2), [2], (2, 3, 1)):
         with pytest.raises(ValueError):
             pkg._check_tensor("t", t, shape, torch.float32, t.device)
+
+
+@pytest.mark.gpu
+def test_online_target_of_a_masked_row(gpu_lib):
+    """The teacher beside the student: a row of -inf throughout has no target and is
+    ignored by the flag that its first entry gives, as the cache's reader does it."""
+    kd, N, D, V, K = gpu_lib, 24, 64, 500, 8
+    z = _logits(N, V, "f32", 81)
+    z[[3, 20]] = float("-inf")
+    t = kd.topk_entries(z, K)
+    ignore = t["teacher_logit"][:, 0].isneginf().to(torch.uint8)
+    c = kd.teacher_cache_write(z, K)
+    assert torch.equal(ignore, kd.teacher_cache_read(c["entries"], c["scale"])["ignore"])
+    assert int(ignore.sum()) == 2
+    g = _gen(82)
+    h = torch.randn(N, D, generator=g, device="cuda").requires_grad_(True)
+    W = (torch.randn(V, D, generator=g, device="cuda") * 0.1).requires_grad_(True)
+    keep = to64(ignore) == 0
+    ref = kd_topk_kl(to64(h)[keep], to64(W), to64(t["teacher_idx"])[keep],
+                     to64(t["teacher_logit"])[keep])
+    loss = kd.topk_kl_loss(h, W, **t, ignore=ignore)
+    loss.backward()
+    assert abs(float(loss.detach()) - ref["loss"]) <= 1e-5 * abs(ref["loss"])
+    assert rel_max(to64(h.grad)[keep], ref["grad_hidden"]) <= 1e-5
+    assert rel_max(to64(W.grad), ref["grad_W"]) <= 1e-5
+    assert not bool(h.grad[[3, 20]].any())
