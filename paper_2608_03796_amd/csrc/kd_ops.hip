@@ -201,8 +201,9 @@ __global__ __launch_bounds__(256) void k_row_groups(const T* __restrict__ logits
 // registers, its groups are single vectors, and their maxima and the sum of exp
 // are formed here: one launch, and groups enough for K above V / 64.
 //
-// kStream (rows of up to 2048 groups): the only pass too, the first pass's work done
-// by the row's workgroup. The scattered reads of the second pass take 20 us and more
+// kStream (rows of up to 2048 groups, with K > 512 up to 4096: their keys stand where
+// the candidates will): the only pass too, the first pass's work done by the row's
+// workgroup. The scattered reads of the second pass take 20 us and more
 // when all rows make them at once (1 GiB of logits has left the caches by then); here
 // some workgroups wait for them while others stream.
 //

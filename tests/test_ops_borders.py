@@ -9,7 +9,7 @@ import paper_2608_03796_amd as pkg
 from oracle import kd_topk_kl
 from oracle import ops_oracle as oo
 from tests.helpers import rel_max, to64
-from tests.test_ops import DT, E32, _check_topk, _check_verify, _draft, _gen, _logits
+from tests.test_ops import DT, E32, _check_topk, _check_verify, _draft, _gen, _logits, _special
 
 
 @pytest.mark.gpu
@@ -278,3 +278,91 @@ def test_online_target_of_a_masked_row(gpu_lib):
     assert rel_max(to64(h.grad)[keep], ref["grad_hidden"]) <= 1e-5
     assert rel_max(to64(W.grad), ref["grad_W"]) <= 1e-5
     assert not bool(h.grad[[3, 20]].any())
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("kind", ["plain", "masked", "two"])
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+@pytest.mark.parametrize("N,V,K,ld", [(260, 131072, 1000, None), (258, 200003, 600, 200005),
+                                      (257, 262144, 513, None)])
+def test_topk_entries_streamed_long(gpu_lib, N, V, K, ld, dtype, kind):
+    """Streamed rows of more than 64 stretches (K > 512): some rows against the oracle,
+    all against calls of few rows, which are selected in two passes."""
+    print(f"[streamed] {N} {V} {K} {dtype} {kind}", flush=True)
+    kd = gpu_lib
+    x = _special(_logits(N, V, dtype, 14, ld), kind)
+    for logprobs in (False, True):
+        got = kd.topk_entries(x, K, logprobs=logprobs)
+        for r0 in (0, 200):
+            part = kd.topk_entries(x[r0:r0 + 200], K, logprobs=logprobs)
+            assert torch.equal(got["teacher_idx"][r0:r0 + 200], part["teacher_idx"])
+            a, b = to64(got["teacher_logit"][r0:r0 + 200]), to64(part["teacher_logit"])
+            f = np.isfinite(b)
+            assert np.array_equal(a[~f], b[~f])
+            # (each within 64 E32 of the sum's logarithm, see _check_topk)
+            tol = 128 * E32 + 6 * E32 * np.abs(b[f]) if logprobs else 0.0
+            assert np.all(np.abs(a[f] - b[f]) <= tol)
+        some = torch.tensor([0, N // 2, N - 1], device="cuda")
+        idx, val = oo.topk_entries(x[some].float().cpu().numpy(), K, logprobs)
+        assert np.array_equal(to64(got["teacher_idx"][some]), idx)
+        g, f = to64(got["teacher_logit"][some]), np.isfinite(val)
+        assert np.array_equal(g[~f], val[~f])
+        tol = 64 * E32 + 3 * E32 * np.abs(val[f]) if logprobs else 0.0
+        assert np.all(np.abs(g[f] - val[f]) <= tol)
+
+
+@pytest.mark.gpu
+def test_rows_behind_2_to_31_elements(gpu_lib):
+    """Rows whose offsets pass 32 bits: selected, and verified with a dense draft and
+    with K entries, as the same rows side by side (bitwise, at the same alignment)."""
+    kd, V, K, ld = gpu_lib, 5000, 20, (1 << 30) + 8
+    flat = torch.empty(5 * ld + V, dtype=torch.bfloat16, device="cuda")   # 10.7 GB
+    far = flat.as_strided((6, V), (ld, 1))
+    near = _logits(6, V, "bf16", 91)
+    far.copy_(near)
+    a, b = kd.topk_entries(far, K, logprobs=True), kd.topk_entries(near, K, logprobs=True)
+    assert all(torch.equal(a[k], b[k]) for k in a)
+    tokens = near.view(2, 3, V)[:, :2].argmax(2).int()
+    u = torch.rand(2, 3, generator=_gen(92), device="cuda")
+    e = kd.topk_entries(near.view(2, 3, V)[:, :2].reshape(4, V) * 0.7, K)
+    draft = dict(draft_idx=e["teacher_idx"].view(2, 2, K), draft_logit=e["teacher_logit"].view(2, 2, K))
+    for kw_a, kw_b in ((draft, draft), (dict(draft_logits=flat.as_strided((2, 2, V), (2 * ld, ld, 1), ld)),
+                                        dict(draft_logits=near[1:5].view(2, 2, V)))):
+        a = kd.verify_draft(flat.as_strided((2, 3, V), (3 * ld, ld, 1)), tokens, u, accept_prob=True, **kw_a)
+        b = kd.verify_draft(near.view(2, 3, V), tokens, u, accept_prob=True, **kw_b)
+        assert all(torch.equal(a[k], b[k]) for k in a)
+
+
+@pytest.mark.gpu
+def test_calls_from_two_threads(gpu_lib):
+    """Two host threads, each with its own stream: the results of calls one by one."""
+    import threading
+    kd, B, T, V, K = gpu_lib, 8, 3, 20011, 30
+    cases = [_draft(B, T, V, K, "bf16", seed) for seed in (101, 102)]
+    rows = [c[0][:, 0].contiguous() for c in cases]
+
+    def calls(i):
+        t = kd.topk_entries(rows[i], K, logprobs=True)
+        c = kd.teacher_cache_write(rows[i], K)
+        r = kd.teacher_cache_read(c["entries"], c["scale"])
+        v = kd.verify_draft(*cases[i][:3], accept_prob=True, **cases[i][3])
+        return list(t.values()) + list(c.values()) + list(r.values()) + list(v.values())
+    want = [calls(i) for i in range(2)]
+    torch.cuda.synchronize()
+    got = [[], []]
+
+    def work(i):
+        s = torch.cuda.Stream()
+        with torch.cuda.stream(s):
+            for _ in range(20):
+                got[i].append(calls(i))
+        s.synchronize()
+    threads = [threading.Thread(target=work, args=(i,)) for i in range(2)]
+    for t in threads:
+        t.start()
+    for t in threads:
+        t.join()
+    for i in range(2):
+        assert len(got[i]) == 20
+        for one in got[i]:
+            assert all(torch.equal(a, b) for a, b in zip(one, want[i]))
