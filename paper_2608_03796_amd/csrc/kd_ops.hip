@@ -847,10 +847,11 @@ __global__ __launch_bounds__(256) void k_ckpt_read(const uint8_t* __restrict__ c
 // side by side, so weights, sums and comparisons are in 64 bits (fp64 runs at
 // the rate of unpacked fp32 here).
 
-// 2^y for y <= 0: 2^n times the exponential series of ln(2) f, |f| <= 1/2 (to
-// degree 11: the next term is below 2^-47 of the result)
-__device__ __forceinline__ double exp2_64(double y) {
-  y = fmax(y, -1100.0);
+// s 2^y: 2^n times the exponential series of ln(2) f, |f| <= 1/2 (to degree 11: the next
+// term is below 2^-47 of the result). s is 2^-1000 to 2^910, and what is below 2^-1074 is 0
+// in the result only
+__device__ __forceinline__ double exp2_64(double y, double s = 1.0) {
+  y = fmax(y, -2200.0);
   const double n = __builtin_rint(y), g = (y - n) * 0.69314718055994530942;
   double p = 1.0 / 39916800;
   p = fma(p, g, 1.0 / 3628800);
@@ -864,13 +865,20 @@ __device__ __forceinline__ double exp2_64(double y) {
   p = fma(p, g, 0.5);
   p = fma(p, g, 1.0);
   p = fma(p, g, 1.0);
-  return __builtin_amdgcn_ldexp(p, (int)n);
+  return __builtin_amdgcn_ldexp(p * s, (int)n);
 }
 // weight of z relative to m: 2^(c (z - m)); with m = +inf, 1 for z = m; 0 where
 // m = -inf (nothing is left)
 __device__ __forceinline__ double weight(float z, float m, double c) {
   if (z == m) return m == -INFINITY ? 0.0 : 1.0;
   return exp2_64(((double)z - (double)m) * c);
+}
+// a sum s of weights relative to z as one of weights relative to m. (The weight of z may be
+// too small for 64 bits where the sum is not: a segment's reference may be 2^890 below its
+// largest logit.)
+__device__ __forceinline__ double mass(double s, float z, float m, double c) {
+  if (z == m) return m == -INFINITY ? 0.0 : s;
+  return s > 0.0 ? exp2_64(((double)z - (double)m) * c, s) : 0.0;
 }
 // Weights relative to one m, for passes over whole rows: 2^(y / 256) with y = 256 c
 // (z - m) by a table of 2^(i / 256) in LDS and, for the rest of a step, the cubic that
@@ -1069,7 +1077,7 @@ __device__ __forceinline__ void merge_row(const VerifyArgs& a, int64_t r, float&
   M = wave_max(m);
   double s = 0.0;
   if (M != -INFINITY)
-    for (int i = lane; i < a.nseg; i += 64) s += ps[i] * weight(pm[i], M, a.c);
+    for (int i = lane; i < a.nseg; i += 64) s += mass(ps[i], pm[i], M, a.c);
   S = wave_sum64(s);
 }
 
@@ -1418,7 +1426,7 @@ __global__ __launch_bounds__(kVerThreads) void k_accept(VerifyArgs a) {
       if (sub == 0 && i < a.nseg) {
         // (where the rounding leaves nothing of a sum that was taken from, its places
         // may still hold a little, which a random number of 0 asks for)
-        const double left = M == -INFINITY ? 0.0 : ps[i] * weight(pm[i], M, a.c) - take;
+        const double left = mass(ps[i], pm[i], M, a.c) - take;
         sh.seg[i] = left > 0.0 ? left : take > 0.0 ? 0x1p-1000 : 0.0;
       }
     }
@@ -1453,7 +1461,7 @@ __global__ __launch_bounds__(kVerThreads) void k_accept(VerifyArgs a) {
   int place = pick_place(sh, a.nseg, u, fill);
   if (place < 0 && rest) {
     // p does not exceed q anywhere: from p
-    for (int i = tid; i < a.nseg; i += kVerThreads) sh.seg[i] = ps[i] * weight(pm[i], M, a.c);
+    for (int i = tid; i < a.nseg; i += kVerThreads) sh.seg[i] = mass(ps[i], pm[i], M, a.c);
     __syncthreads();
     place = pick_place(sh, a.nseg, u, [&](int seg) {
       fill_target<T>(sh, row, seg, M, a.c);
@@ -1555,7 +1563,7 @@ __global__ __launch_bounds__(kVerThreads) void k_pick(VerifyArgs a) {
   const double* ps = a.segs + rt * a.nseg;
   for (int i = tid; i < a.nseg; i += kVerThreads)
     sh.seg[i] = rest        ? a.segr[(int64_t)b * a.nseg + i]
-                : m.it > 0.0 ? ps[i] * m.t.exact(pm[i]) * m.it
+                : m.it > 0.0 ? mass(ps[i] * m.it, pm[i], m.t.m, a.c)
                              : 0.0;
   __syncthreads();
   const double u = a.uniform[target_row(a, b, a.T)];
@@ -1593,7 +1601,7 @@ __global__ __launch_bounds__(kVerThreads) void k_pick(VerifyArgs a) {
   }
   int place = pick_place(sh, a.nseg, u, fill);
   if (place < 0 && rest && m.it > 0.0) {
-    for (int i = tid; i < a.nseg; i += kVerThreads) sh.seg[i] = ps[i] * m.t.exact(pm[i]);
+    for (int i = tid; i < a.nseg; i += kVerThreads) sh.seg[i] = mass(ps[i], pm[i], m.t.m, a.c);
     __syncthreads();
     place = pick_place(sh, a.nseg, u, [&](int seg) {
       fill_target<T>(sh, row, seg, m.t.m, a.c);

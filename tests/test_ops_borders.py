@@ -366,3 +366,22 @@ def test_calls_from_two_threads(gpu_lib):
         assert len(got[i]) == 20
         for one in got[i]:
             assert all(torch.equal(a, b) for a, b in zip(one, want[i]))
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+@pytest.mark.parametrize("T", [0, 1])
+def test_verify_small_mass_of_a_stretch(gpu_lib, T, dtype):
+    """A stretch that begins 2^-1154 below the row's largest and goes up to 2^-433: a
+    random number of 0 draws its first token whose probability 64 bits can hold."""
+    B, V = 8, 6000
+    z = torch.full((B, T + 1, V), float("-inf"), device="cuda")
+    z[:, :, :600] = -800.0
+    at = torch.randint(700, 2000, (B,), generator=_gen(3), device="cuda")
+    z[torch.arange(B), T, at] = -300.0
+    z[:, :, 5000] = 0.0
+    z = z.to(DT[dtype])
+    draft = dict(draft_logits=z[:, :T].clone()) if T else {}
+    tokens = torch.full((B, T), 5000, dtype=torch.int32, device="cuda")
+    out, _, _ = _check_verify(gpu_lib, z, tokens, torch.zeros(B, T + 1, device="cuda"), draft)
+    assert np.array_equal(out[:, T], to64(at))
