@@ -1224,15 +1224,22 @@ __device__ __forceinline__ void write_tokens(const VerifyArgs& a, int b, int r, 
   if (threadIdx.x == 0) a.accepted[b] = r;
 }
 
-// the segment's masses of the target's row: p times S, places outside 0
+// The power of two that brings S to 1 or above, below 2: weights and sums times it are
+// probabilities but for a factor below 2, and 0 where 64 bits cannot hold those. (M may be
+// 2^890 below the row's largest logit, and weights relative to it go as much further.)
+__device__ __forceinline__ double unit(double S) {
+  return S > 0.0 ? __builtin_amdgcn_ldexp(1.0, 1 - __builtin_amdgcn_frexp_exp(S)) : 1.0;
+}
+
+// the segment's masses of the target's row: weights times f, places outside 0
 template <typename T>
 __device__ __forceinline__ void fill_target(VerifyShared& sh, const Row<T>& row, int seg, float M,
-                                            double c) {
+                                            double c, double f) {
   constexpr int VPT = Row<T>::VPT;
   for (int j = threadIdx.x; j < kSegCols / VPT; j += kVerThreads) {
     const u32x4_t x = row.at(seg * kSegCols + j * VPT);
 #pragma unroll
-    for (int i = 0; i < VPT; ++i) sh.x[j * VPT + i] = weight(Row<T>::elt(x, i), M, c);
+    for (int i = 0; i < VPT; ++i) sh.x[j * VPT + i] = weight(Row<T>::elt(x, i), M, c) * f;
   }
 }
 
@@ -1327,7 +1334,8 @@ __global__ __launch_bounds__(kVerThreads) void k_accept(VerifyArgs a) {
   __syncthreads();
   const int64_t rt = target_row(a, b, r);
   const float M = rowM[r];
-  double S = rowS[r];
+  const double f = unit(rowS[r]);
+  double S = rowS[r] * f;
   if constexpr (DENSE) {
     if (wave == 0 && r < n) {
       float Md;
@@ -1340,7 +1348,7 @@ __global__ __launch_bounds__(kVerThreads) void k_accept(VerifyArgs a) {
     }
     if (tid == 0) {
       a.norm[4 * b] = M;
-      a.norm[4 * b + 1] = S;
+      a.norm[4 * b + 1] = rowS[r];
       a.accepted[b] = r;
     }
     return;
@@ -1402,7 +1410,7 @@ __global__ __launch_bounds__(kVerThreads) void k_accept(VerifyArgs a) {
     }
     __syncthreads();
     for (int k = tid; k < Kp; k += kVerThreads)
-      em[k] = eq[k] > 0.0 ? weight(row.one(ei[k]), M, a.c) : 0.0;
+      em[k] = eq[k] > 0.0 ? weight(row.one(ei[k]), M, a.c) * f : 0.0;
     __syncthreads();
   }
   {
@@ -1426,7 +1434,7 @@ __global__ __launch_bounds__(kVerThreads) void k_accept(VerifyArgs a) {
       if (sub == 0 && i < a.nseg) {
         // (where the rounding leaves nothing of a sum that was taken from, its places
         // may still hold a little, which a random number of 0 asks for)
-        const double left = mass(ps[i], pm[i], M, a.c) - take;
+        const double left = mass(ps[i] * f, pm[i], M, a.c) - take;
         sh.seg[i] = left > 0.0 ? left : take > 0.0 ? 0x1p-1000 : 0.0;
       }
     }
@@ -1435,7 +1443,7 @@ __global__ __launch_bounds__(kVerThreads) void k_accept(VerifyArgs a) {
   const double u = a.uniform[target_row(a, b, a.T)];
   // the masses of a segment's places, in sh.x
   auto fill = [&](int seg) {
-    fill_target<T>(sh, row, seg, M, a.c);
+    fill_target<T>(sh, row, seg, M, a.c, f);
     __syncthreads();
     if (rest)
       for (int k = tid; k < a.K; k += kVerThreads) {
@@ -1447,7 +1455,7 @@ __global__ __launch_bounds__(kVerThreads) void k_accept(VerifyArgs a) {
   if (rest && little_left(sh, a.nseg, S)) {
     S = 0.0;
     for (int seg = 0; seg < a.nseg; ++seg) {
-      fill_target<T>(sh, row, seg, M, a.c);
+      fill_target<T>(sh, row, seg, M, a.c, f);
       __syncthreads();
       S += sum_places(sh);
     }
@@ -1461,10 +1469,10 @@ __global__ __launch_bounds__(kVerThreads) void k_accept(VerifyArgs a) {
   int place = pick_place(sh, a.nseg, u, fill);
   if (place < 0 && rest) {
     // p does not exceed q anywhere: from p
-    for (int i = tid; i < a.nseg; i += kVerThreads) sh.seg[i] = mass(ps[i], pm[i], M, a.c);
+    for (int i = tid; i < a.nseg; i += kVerThreads) sh.seg[i] = mass(ps[i] * f, pm[i], M, a.c);
     __syncthreads();
     place = pick_place(sh, a.nseg, u, [&](int seg) {
-      fill_target<T>(sh, row, seg, M, a.c);
+      fill_target<T>(sh, row, seg, M, a.c, f);
       __syncthreads();
     });
   }
@@ -1601,10 +1609,10 @@ __global__ __launch_bounds__(kVerThreads) void k_pick(VerifyArgs a) {
   }
   int place = pick_place(sh, a.nseg, u, fill);
   if (place < 0 && rest && m.it > 0.0) {
-    for (int i = tid; i < a.nseg; i += kVerThreads) sh.seg[i] = mass(ps[i], pm[i], m.t.m, a.c);
+    for (int i = tid; i < a.nseg; i += kVerThreads) sh.seg[i] = mass(ps[i] * m.it, pm[i], m.t.m, a.c);
     __syncthreads();
     place = pick_place(sh, a.nseg, u, [&](int seg) {
-      fill_target<T>(sh, row, seg, m.t.m, a.c);
+      fill_target<T>(sh, row, seg, m.t.m, a.c, m.it);
       __syncthreads();
     });
   }

@@ -385,3 +385,27 @@ def test_verify_small_mass_of_a_stretch(gpu_lib, T, dtype):
     tokens = torch.full((B, T), 5000, dtype=torch.int32, device="cuda")
     out, _, _ = _check_verify(gpu_lib, z, tokens, torch.zeros(B, T + 1, device="cuda"), draft)
     assert np.array_equal(out[:, T], to64(at))
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+@pytest.mark.parametrize("T,K", [(0, 0), (1, 1), (1, 0)])
+def test_verify_probabilities_below_64_bits(gpu_lib, T, K, dtype):
+    """A token at e^-900 of the largest has a probability of 0 in 64 bits and is not drawn,
+    also where the stretches' references are far below the largest."""
+    B, V = 4, 6000
+    z = torch.full((B, T + 1, V), float("-inf"), device="cuda")
+    z[:, :, 20] = -900.0
+    z[:, :, 2100:2700] = -500.0
+    z[:, :, 3500] = 0.0
+    z = z.to(DT[dtype])
+    d = torch.zeros(B, T, 1, device="cuda")
+    draft = {}
+    if K:
+        draft = dict(draft_idx=torch.full((B, T, 1), 3500, dtype=torch.int32, device="cuda"),
+                     draft_logit=d)
+    elif T:
+        draft = dict(draft_logits=z[:, :T].clone())
+    tokens = torch.full((B, T), 3500, dtype=torch.int32, device="cuda")
+    out, _, _ = _check_verify(gpu_lib, z, tokens, torch.zeros(B, T + 1, device="cuda"), draft)
+    assert (out[:, T] == 2100).all()
