@@ -532,7 +532,7 @@ kd_status kd_verify_draft_workspace_size(const kd_draft* p, size_t* bytes);
  * while u_t q_t(d_t) < p_t(d_t); the next token behind the r kept ones is the
  * first v at which the running sum of x passes u_T sum(x), where x = max(p_r -
  * q_r, 0) if d_r was rejected and p_r if all were kept (x = p_r too where
- * p_r - q_r is nowhere above 0; a difference within 2^-40 of p_r, the rounding of
+ * p_r - q_r is nowhere above 0; a difference within 2^-46 of p_r, the rounding of
  * the two, is none). All of it is held and compared in 64 bits; each 2^(z / tau) is
  * off by at most 2^-42 of itself.
  *

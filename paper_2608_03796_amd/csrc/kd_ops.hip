@@ -847,13 +847,15 @@ __global__ __launch_bounds__(256) void k_ckpt_read(const uint8_t* __restrict__ c
 // side by side, so weights, sums and comparisons are in 64 bits (fp64 runs at
 // the rate of unpacked fp32 here).
 
-// s 2^y: 2^n times the exponential series of ln(2) f, |f| <= 1/2 (to degree 11: the next
-// term is below 2^-47 of the result). s is 2^-1000 to 2^910, and what is below 2^-1074 is 0
+// s 2^y: 2^n times the exponential series of ln(2) f, |f| <= 1/2 (to degree 13: the next
+// term is below 2^-57 of the result). s is 2^-1000 to 2^910, and what is below 2^-1074 is 0
 // in the result only
 __device__ __forceinline__ double exp2_64(double y, double s = 1.0) {
   y = fmax(y, -2200.0);
   const double n = __builtin_rint(y), g = (y - n) * 0.69314718055994530942;
-  double p = 1.0 / 39916800;
+  double p = 1.0 / 6227020800;
+  p = fma(p, g, 1.0 / 479001600);
+  p = fma(p, g, 1.0 / 39916800);
   p = fma(p, g, 1.0 / 3628800);
   p = fma(p, g, 1.0 / 362880);
   p = fma(p, g, 1.0 / 40320);
@@ -1175,11 +1177,14 @@ __device__ __forceinline__ int pick_place(VerifyShared& sh, int nseg, double u, 
   return -1;
 }
 
-// What the draft leaves of p at a token, 0 up to the rounding of the two: weights hundreds
-// of powers of two from their references are off by up to 2^-42, and a draft that has the
-// target's probabilities leaves nothing.
-__device__ __forceinline__ double excess(double p, double q) {
-  return p - q > p * 0x1p-40 ? p - q : 0.0;
+// What the draft leaves of p at a token, 0 up to the rounding of the two, so that a draft
+// that has the target's probabilities leaves nothing. Weights far from their reference and
+// the sums of fast ones are off by up to 2^-42 (kNear). Relative to the rows' largest logits,
+// with sums of the same weights, probabilities are off by 2^-49 or so, and equal logits have
+// equal weights (kClose).
+constexpr double kNear = 0x1p-40, kClose = 0x1p-46;
+__device__ __forceinline__ double excess(double p, double q, double eps) {
+  return p - q > p * eps ? p - q : 0.0;
 }
 
 // the sum of the threads' x, to every thread
@@ -1192,6 +1197,15 @@ __device__ __forceinline__ double block_sum(VerifyShared& sh, double x) {
   __syncthreads();
   return x;
 }
+// the largest of the threads' x, to every thread
+__device__ __forceinline__ float block_max(VerifyShared& sh, float x) {
+  x = wave_max(x);
+  if ((threadIdx.x & 63) == 0) sh.scan[threadIdx.x >> 6] = x;
+  __syncthreads();
+  for (int w = 0; w < kVerWaves; ++w) x = fmaxf(x, (float)sh.scan[w]);
+  __syncthreads();
+  return x;
+}
 // the sum of sh.x
 __device__ __forceinline__ double sum_places(VerifyShared& sh) {
   double t = 0.0;
@@ -1201,8 +1215,9 @@ __device__ __forceinline__ double sum_places(VerifyShared& sh) {
 
 // Where little is left (a draft rejected with a probability below 2^-10), the segments'
 // sums of it are mostly the rounding of what is taken out of them: then the masses are
-// formed again place by place, with the rows' sums from the same weights. The question is
-// answered by wave 0's sum of sh.seg, which all threads have written.
+// formed again place by place, relative to the rows' largest logits and with their sums
+// from the same weights. The question is answered by wave 0's sum of sh.seg, which all
+// threads have written.
 __device__ __forceinline__ bool little_left(VerifyShared& sh, int nseg, double all) {
   if (threadIdx.x < 64) {
     double t = 0.0;
@@ -1333,9 +1348,8 @@ __global__ __launch_bounds__(kVerThreads) void k_accept(VerifyArgs a) {
   const int r = sh.first;
   __syncthreads();
   const int64_t rt = target_row(a, b, r);
-  const float M = rowM[r];
-  const double f = unit(rowS[r]);
-  double S = rowS[r] * f;
+  float M = rowM[r];
+  double f = unit(rowS[r]), S = rowS[r] * f, eps = kNear;
   if constexpr (DENSE) {
     if (wave == 0 && r < n) {
       float Md;
@@ -1448,17 +1462,30 @@ __global__ __launch_bounds__(kVerThreads) void k_accept(VerifyArgs a) {
     if (rest)
       for (int k = tid; k < a.K; k += kVerThreads) {
         const int e = ei[k] + row.shift - seg * kSegCols;
-        if (eq[k] > 0.0 && (unsigned)e < (unsigned)kSegCols) sh.x[e] = excess(em[k], eq[k] * S);
+        if (eq[k] > 0.0 && (unsigned)e < (unsigned)kSegCols) sh.x[e] = excess(em[k], eq[k] * S, eps);
       }
     __syncthreads();
   };
   if (rest && little_left(sh, a.nseg, S)) {
-    S = 0.0;
-    for (int seg = 0; seg < a.nseg; ++seg) {
-      fill_target<T>(sh, row, seg, M, a.c, f);
-      __syncthreads();
-      S += sum_places(sh);
+    constexpr int VPT = Row<T>::VPT;
+    const int end = a.nseg * kSegCols;
+    float m = -INFINITY;
+    for (int e = tid * VPT; e < end; e += kVerThreads * VPT) {
+      const u32x4_t x = row.at(e);
+      for (int i = 0; i < VPT; ++i) m = fmaxf(m, Row<T>::elt(x, i));
     }
+    M = block_max(sh, m);
+    double t = 0.0;
+    for (int e = tid * VPT; e < end; e += kVerThreads * VPT) {
+      const u32x4_t x = row.at(e);
+      for (int i = 0; i < VPT; ++i) t += weight(Row<T>::elt(x, i), M, a.c);
+    }
+    S = block_sum(sh, t);
+    f = 1.0;
+    eps = kClose;
+    for (int k = tid; k < Kp; k += kVerThreads)
+      em[k] = eq[k] > 0.0 ? weight(row.one(ei[k]), M, a.c) : 0.0;
+    __syncthreads();
     for (int seg = 0; seg < a.nseg; ++seg) {
       fill(seg);
       const double t = sum_places(sh);
@@ -1484,6 +1511,7 @@ __global__ __launch_bounds__(kVerThreads) void k_accept(VerifyArgs a) {
 struct RestRow {
   Weights t, d;
   double it, id;  // 1 / S
+  double eps = kNear;
   bool rest;
   __device__ __forceinline__ RestRow(const VerifyArgs& a, int b, bool rest_, const uint64_t* tab)
       : t((float)a.norm[4 * b], a.c, tab),
@@ -1497,7 +1525,7 @@ struct RestRow {
   }
   __device__ __forceinline__ double exact(float zt, float zd) const {
     const double p = t.exact(zt) * it;
-    return rest ? excess(p, d.exact(zd) * id) : p;
+    return rest ? excess(p, d.exact(zd) * id, eps) : p;
   }
 };
 // vector of the draft's row at the target's place e (its own boundary may differ)
@@ -1588,8 +1616,20 @@ __global__ __launch_bounds__(kVerThreads) void k_pick(VerifyArgs a) {
     __syncthreads();
   };
   if (rest && m.it > 0.0 && little_left(sh, a.nseg, 1.0)) {
+    const int end = a.nseg * kSegCols;
+    float mt = -INFINITY, md = -INFINITY;
+    for (int e = tid * VPT; e < end; e += kVerThreads * VPT) {
+      const u32x4_t x = row.at(e), y = draft_at<T>(dr, e, row.shift);
+      for (int i = 0; i < VPT; ++i) {
+        mt = fmaxf(mt, Row<T>::elt(x, i));
+        md = fmaxf(md, Row<T>::elt(y, i));
+      }
+    }
+    m.t.m = block_max(sh, mt);
+    m.d.m = block_max(sh, md);
+    m.eps = kClose;
     double st = 0.0, sd = 0.0;
-    for (int e = tid * VPT; e < a.nseg * kSegCols; e += kVerThreads * VPT) {
+    for (int e = tid * VPT; e < end; e += kVerThreads * VPT) {
       const u32x4_t x = row.at(e), y = draft_at<T>(dr, e, row.shift);
       for (int i = 0; i < VPT; ++i) {
         st += m.t.exact(Row<T>::elt(x, i));

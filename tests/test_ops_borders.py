@@ -409,3 +409,29 @@ def test_verify_probabilities_below_64_bits(gpu_lib, T, K, dtype):
     tokens = torch.full((B, T), 3500, dtype=torch.int32, device="cuda")
     out, _, _ = _check_verify(gpu_lib, z, tokens, torch.zeros(B, T + 1, device="cuda"), draft)
     assert (out[:, T] == 2100).all()
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("K", [0, 2])
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+@pytest.mark.parametrize("left", [6e-14, 2e-13, 7e-13])
+def test_verify_rest_of_one_token(gpu_lib, left, dtype, K):
+    """The draft leaves 1e-13 or so of the token that has nearly all of the target's mass,
+    which 64 bits tell from 1, and all of others that are far less likely still."""
+    B, V = 8, 9001
+    z = _logits(B * 2, V, dtype, 75, V + 3, std=1.0).unflatten(0, (B, 2))
+    z -= 70.0
+    z[:, 0, 5] = float("-inf")
+    z[:, 0, 7000] = 10.0
+    tokens = torch.full((B, 1), 5, dtype=torch.int32, device="cuda")
+    e = torch.tensor([0.0, float(np.log(left))], device="cuda")
+    d = torch.full((B, 1, V), float("-inf"), device="cuda")
+    d[:, :, [7000, 5]] = e
+    draft = dict(draft_logits=d.to(DT[dtype]))
+    if K:
+        idx = torch.tensor([7000, -1], dtype=torch.int32, device="cuda")
+        draft = dict(draft_idx=idx.expand(B, 1, 2).contiguous(),
+                     draft_logit=e.expand(B, 1, 2).contiguous())
+    u = torch.rand(B, 2, generator=_gen(76), device="cuda")
+    out, accepted, _ = _check_verify(gpu_lib, z, tokens, u, draft)
+    assert not accepted.any() and (out[:, 0] == 7000).all()
