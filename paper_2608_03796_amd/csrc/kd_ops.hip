@@ -887,7 +887,7 @@ __device__ __forceinline__ double mass(double s, float z, float m, double c) {
 // is 2^(x / 256) at x = 0, 1/4, 3/4 and 1 (off by at most 2^-44 of it between). y is held
 // 2^18 higher, so that it is positive and its whole part and rest are an operation
 // each: 8 fp64 operations and 6 others where exp2_64 with its difference, comparisons
-// and sum takes 23 and 4 (segment sums of 256 x 6 rows 134 and 72 us). The rounding of y
+// and sum takes 25 and 4 (segment sums of 256 x 6 rows 134 and 72 us). The rounding of y
 // at 2^18 is 2^-43 of the weight; that of 256 c m, which is all weights' and grows with it,
 // is kept as a factor for their sum (`fix`: without it 3e-9 at m / tau = 3e7). z is held above
 // m - 990 / c, where weights no longer count (2^-990; -inf and a quiet NaN end there
@@ -1217,7 +1217,8 @@ __device__ __forceinline__ double sum_places(VerifyShared& sh) {
 // sums of it are mostly the rounding of what is taken out of them: then the masses are
 // formed again place by place, relative to the rows' largest logits and with their sums
 // from the same weights. The question is answered by wave 0's sum of sh.seg, which all
-// threads have written.
+// threads have written. One workgroup reads the row three times then: 176 us for K entries
+// and 270 for a dense draft at V = 131072.
 __device__ __forceinline__ bool little_left(VerifyShared& sh, int nseg, double all) {
   if (threadIdx.x < 64) {
     double t = 0.0;
@@ -1672,8 +1673,9 @@ using namespace kd;
 //  * more rows: each streamed by its own workgroup. Long ones (48 segments, about
 //    100000 columns) by 512 threads: 300 rows 28.8 (two passes 32.7), 777 50.1 (53.0),
 //    4096 192 (236; 256 threads 203). Shorter ones by 256 threads once there are 1536:
-//    8000 rows of 50257 169 (208; 512 threads 198), 777 rows 38.4 (36.0), 1100 rows
-//    of 50257 in fp32 with log-probabilities 61.4 (56.3).
+//    8000 rows of 50257 169 (208; 512 threads 198). In fp32 with log-probabilities the
+//    two cross there: 1300 rows of 50257 61.7 (56.0), 1800 80.0 (79.6), 2200 91.9 (99.4);
+//    in bf16 streaming is between 4% slower and 9% faster from 600 rows to 1800.
 //  * else two passes, 256 threads a row in the second.
 constexpr int64_t kSelectFewRows = 256, kSelectStreamRows = 1536;
 constexpr int kSelectLongSegs = 48;

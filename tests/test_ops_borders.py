@@ -435,3 +435,51 @@ def test_verify_rest_of_one_token(gpu_lib, left, dtype, K):
     u = torch.rand(B, 2, generator=_gen(76), device="cuda")
     out, accepted, _ = _check_verify(gpu_lib, z, tokens, u, draft)
     assert not accepted.any() and (out[:, 0] == 7000).all()
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("seed", range(8))
+def test_verify_sweep(gpu_lib, seed):
+    """Seeded verifications over the range: temperatures from 1e-4 to 1e4, finite masks,
+    masks by row or by column, far logits, NaN and infinities, entries without a token or
+    with the same one, any strides."""
+    import random
+    rng, g = random.Random(seed + 900), _gen(seed + 900)
+
+    def rand(*shape):
+        return torch.rand(*shape, generator=g, device="cuda")
+    for _ in range(12):
+        V, B, T = int(round(2 ** rng.uniform(1, 14.5))), rng.randint(1, 8), rng.randint(0, 6)
+        K = rng.choice([0, rng.randint(1, min(V, rng.choice([1, 5, 60, 900])))]) if T else 0
+        dtype, tau = rng.choice(["bf16", "f32"]), rng.choice([1e-4, 0.01, 0.1, 0.5, 1.0, 2.0, 30.0, 1e4])
+        std, kind = rng.choice([0.01, 1, 5, 30]), rng.choice(["plain", "columns", "rows", "far", "nan", "inf"])
+        print(f"[verify sweep] {B} {T} {V} {K} {dtype} {tau} {std} {kind}", flush=True)
+        z = _logits(B * (T + 1), V, dtype, seed, V + rng.randint(0, 9), rng.randint(0, 7), std)
+        z = z.unflatten(0, (B, T + 1))
+        mask = rng.choice([-1e4, -65504.0, -1e6, -1e9, float("-inf")])
+        if kind == "columns":
+            z[:, :, rand(V) < rng.choice([0.5, 0.999])] = mask
+        elif kind == "rows":
+            z[rand(*z.shape) < rng.choice([0.5, 0.999])] = mask
+        elif kind == "far":
+            z[rand(*z.shape) < 3 / V] += rng.choice([10, 100, 1000, 1e5])
+        elif kind == "nan":
+            z[rand(*z.shape) < 0.3] = float("nan")
+        elif kind == "inf":
+            z[rand(*z.shape) < 1 / V] = float("inf")
+        d = z[:, :T].float().nan_to_num(nan=-float("inf"), posinf=float("inf"), neginf=-float("inf"))
+        d = (d + rng.choice([0.3, 2.0]) * tau * torch.randn(d.shape, generator=g, device="cuda")).to(DT[dtype])
+        tokens = (d.float() / tau - torch.log(-torch.log(rand(B, T, V).clamp(1e-9, 1 - 1e-7)))).argmax(2) \
+            if T else torch.empty(B, 0, device="cuda")
+        other = torch.randint(-1, V + 1, (B, T), generator=g, device="cuda")
+        tokens = torch.where(rand(B, T) < 0.15, other, tokens).int()
+        draft = dict(draft_logits=d) if T else {}
+        if K:
+            e = d.float().topk(K, dim=2)
+            idx = e.indices.int().contiguous()
+            if rng.random() < 0.5:
+                idx[rand(*idx.shape) < 0.1] = -1
+                idx[:, :, K // 2] = idx[:, :, 0]
+            draft = dict(draft_idx=idx, draft_logit=e.values.contiguous())
+        n = torch.randint(-1, T + 2, (B,), generator=g, device="cuda", dtype=torch.int32)
+        _check_verify(gpu_lib, z, tokens, rand(B, T + 1), draft, tau, rng.choice([None, n]))
