@@ -1623,7 +1623,8 @@ __device__ __forceinline__ void transpose_rows(int bt, int bd, const T* __restri
     T e[VPT];
     __builtin_memcpy(e, &v, 16);
     // a per-token factor of the gradient rows is applied to the hidden rows
-    // here, so that dW = sum_t (factor_t H_t)^T dZ''_t
+    // here, so that dW = sum_t (factor_t H_t)^T dZ''_t (in bf16 the product is rounded once
+    // more, as much as dZ'' was: known only with log Z, the factor can go nowhere before)
     const float f = (rowscale != nullptr && t0 + row < tokens) ? rowscale[t0 + row] : 1.f;
 #pragma unroll
     for (int x = 0; x < VPT; ++x) tile[row][c + x] = rowscale ? (T)((float)e[x] * f) : e[x];

@@ -995,7 +995,7 @@ __device__ __forceinline__ int64_t draft_row(const VerifyArgs& a, int b, int t) 
 // Reference m and sum of 2^(c (z - m)) of each segment of the rows in question (the
 // target's, then the draft's): the pass that reads the logits, bound by its fp64
 // arithmetic (8 of about 16 operations an element): 256 sequences of up to 6 rows of
-// 131072 in bf16, 0.24 GB read, 72 us; the same read without the weights 44. 64 bits
+// 131072 in bf16, 0.24 GB read, 73 us; the same read without the weights 44. 64 bits
 // hold the weights of logits well above the reference too, so the largest of a
 // quarter (bf16) or an eighth of the segment serves, the largest of all where that is
 // -inf; a segment whose sum reaches kHeld, as it does where a logit was held back, is
@@ -1262,8 +1262,8 @@ __device__ __forceinline__ void fill_target(VerifyShared& sh, const Row<T>& row,
 // A workgroup per sequence: the places' probabilities of their tokens (a wave per
 // place), the first rejected place, and with a draft of K entries the draw. The
 // draft's K entries take their part of a segment's mass out of its sum: no pass
-// over the vocabulary but the one segment's. Latency-bound: 8.7 us for one sequence,
-// 16 for 256.
+// over the vocabulary but the one segment's. Latency-bound: 9 us for one sequence,
+// 17 for 256.
 template <typename T, bool DENSE>
 __global__ __launch_bounds__(kVerThreads) void k_accept(VerifyArgs a) {
   extern __shared__ __align__(16) char lds[];
