@@ -42,7 +42,7 @@
 extern "C" {
 #endif
 
-#define KDTOPK_ABI_VERSION 4
+#define KDTOPK_ABI_VERSION 5
 
 typedef enum kd_status {
   KD_OK = 0,
@@ -60,7 +60,9 @@ typedef enum kd_dtype {
                                     operand as the exact sum of three bf16 terms,
                                     bf16 MFMA, fp32 accumulate) and fp32 elsewhere.
                                     Operands below 1e-33 keep fewer than 24 bits */
-  KD_BF16 = 1                    /* bf16 inputs, bf16 MFMA, fp32 accumulate */
+  KD_BF16 = 1,                   /* bf16 inputs, bf16 MFMA, fp32 accumulate */
+  KD_MX4 = 2                     /* hidden rows of kd_mx4_logits only: kd_mx4_write's
+                                    codes and scales */
 } kd_dtype;
 
 /* Problem description (Algorithm 1's inputs: h, W, the support and C_s). */
@@ -570,6 +572,72 @@ kd_status kd_verify_draft(const kd_draft* p, const void* target_logits,
                           const float* uniform, const int32_t* lengths, int32_t* tokens,
                           int32_t* accepted, float* accept_prob, void* workspace,
                           size_t workspace_bytes, void* hip_stream);
+
+/*
+ * Matrices in 4 bits (microscaled floating point): a student's head after training,
+ * or hidden states, at 17/32 of a byte an element. Each block of 32 consecutive
+ * columns has one byte s as scale 2^(s - 127) and its elements as e2m1 codes,
+ * rounded to nearest even: the codes 0 to 7 stand for 0, 0.5, 1, 1.5, 2, 3, 4 and
+ * 6 scales, 8 to 15 for their negatives. The scale is the least power of two, at
+ * least 2^-127, that leaves the block's largest magnitude at 6 or below: an element
+ * is off by at most a fifth of itself, or by a quarter of the scale where it is below
+ * the scale. (At the scale 2^126 an element of 3.5 of it and more, which would round to
+ * 2^128, is held as 3.)
+ * A block with an element that is infinite or not a number has s = 255 and reads
+ * back as not a number.
+ *
+ *   x        [N, D] dtype; D a multiple of 32, 32 <= D <= 65536
+ *   codes    [N, D / 2] uint8; the even column in the low half of its byte
+ *   scales   [N, D / 32] uint8
+ *
+ * kd_mx4_read gives the values back in either dtype (exact in both). x and codes
+ * 16-byte aligned. Errors: KD_ERR_NULL_PTR, KD_ERR_BAD_SHAPE, KD_ERR_UNSUPPORTED
+ * (dtype, D % 32, alignment), KD_ERR_DEVICE.
+ */
+kd_status kd_mx4_write(int64_t N, int64_t D, int32_t dtype, const void* x, uint8_t* codes,
+                       uint8_t* scales, void* hip_stream);
+kd_status kd_mx4_read(int64_t N, int64_t D, int32_t dtype, const uint8_t* codes,
+                      const uint8_t* scales, void* x, void* hip_stream);
+
+/* Logits of hidden rows with a head held in 4 bits. */
+typedef struct kd_mx4_head {
+  int64_t N;           /* hidden rows; 0 <= N < 2^31                         */
+  int64_t D;           /* hidden size; 32 <= D <= 65536, D % 32 == 0         */
+  int64_t V;           /* rows of the head; 1 <= V <= 1048576                */
+  int64_t ld_hidden;   /* elements between hidden rows (bf16 and fp32); D <=
+                          ld_hidden <= 2^31, a multiple of 16 bytes          */
+  int64_t ld_out;      /* elements between output rows; V <= ld_out <= 2^31  */
+  int32_t dtype;       /* of the hidden rows: KD_BF16, KD_F32 or KD_MX4      */
+  int32_t out_dtype;   /* of the logits: KD_BF16 or KD_F32                   */
+  int32_t flags;       /* 0                                                  */
+} kd_mx4_head;
+
+/* Bytes of device workspace kd_mx4_logits needs. Pure host function. */
+kd_status kd_mx4_logits_workspace_size(const kd_mx4_head* p, size_t* bytes);
+
+/*
+ * out = hidden W^T with the values W that the head's codes and scales stand for:
+ * what a drafting student runs before kd_topk_entries and kd_verify_draft, or a
+ * teacher before kd_teacher_cache_write. bf16 and fp32 hidden rows are used as they
+ * are (products exact in fp32: fp32 elements as the exact sum of three bf16 terms,
+ * of which those below 2^-126 may count as 0), 4-bit ones as the values they stand
+ * for; sums are fp32, rounded once to out's dtype.
+ *
+ *   hidden         [N, ld_hidden] dtype, or [N, D / 2] uint8 codes (KD_MX4)
+ *   hidden_scales  [N, D / 32] uint8 (KD_MX4), else not used
+ *   codes, scales  [V, D / 2], [V, D / 32] uint8   kd_mx4_write's of the head
+ *   out            [N, ld_out] out_dtype   out: columns V and on are left as they are
+ *   workspace, workspace_bytes   at least kd_mx4_logits_workspace_size bytes, 16-byte
+ *                  aligned
+ *
+ * hidden, codes and workspace 16-byte aligned. A head's row with a block that is not
+ * a number gives logits that are not a number. Errors: KD_ERR_NULL_PTR,
+ * KD_ERR_BAD_SHAPE, KD_ERR_BAD_ARG (flags), KD_ERR_UNSUPPORTED (dtypes, D % 32,
+ * alignment), KD_ERR_WORKSPACE_TOO_SMALL, KD_ERR_DEVICE.
+ */
+kd_status kd_mx4_logits(const kd_mx4_head* p, const void* hidden, const uint8_t* hidden_scales,
+                        const uint8_t* codes, const uint8_t* scales, void* out, void* workspace,
+                        size_t workspace_bytes, void* hip_stream);
 
 /*
  * Instrumentation, not part of the method: per-kernel timing with HIP events.

@@ -17,6 +17,7 @@ LIB_PATH = os.path.join(_HERE, "libkdtopk.so")
 
 KD_F32 = 0
 KD_BF16 = 1
+KD_MX4 = 2
 KD_FLAG_TEACHER_LOGPROBS = 1
 KD_FLAG_GRAD_HIDDEN_F32 = 2
 
@@ -32,7 +33,8 @@ EXPORTED = ("kd_topk_kl_workspace_size", "kd_topk_kl_fwd_bwd", "kd_topk_kl_fwd_b
             "kd_topk_entries_workspace_size", "kd_topk_entries", "kd_teacher_cache_write",
             "kd_teacher_cache_read", "kd_checkpoint_write", "kd_checkpoint_read",
             "kd_topk_kl_bwd_checkpoint",
-            "kd_verify_draft_workspace_size", "kd_verify_draft")
+            "kd_verify_draft_workspace_size", "kd_verify_draft", "kd_mx4_write", "kd_mx4_read",
+            "kd_mx4_logits_workspace_size", "kd_mx4_logits")
 
 
 class KdError(RuntimeError):
@@ -62,6 +64,13 @@ class KdDraft(ctypes.Structure):
                 ("ld_target", ctypes.c_int64), ("ld_draft", ctypes.c_int64),
                 ("K", ctypes.c_int32), ("dtype", ctypes.c_int32),
                 ("temperature", ctypes.c_double), ("flags", ctypes.c_int32)]
+
+
+class KdMx4Head(ctypes.Structure):
+    _fields_ = [("N", ctypes.c_int64), ("D", ctypes.c_int64), ("V", ctypes.c_int64),
+                ("ld_hidden", ctypes.c_int64), ("ld_out", ctypes.c_int64),
+                ("dtype", ctypes.c_int32), ("out_dtype", ctypes.c_int32),
+                ("flags", ctypes.c_int32)]
 
 
 _lib = None
@@ -109,6 +118,7 @@ def load_library(path: Optional[str] = None) -> ctypes.CDLL:
     lib.kd_topk_kl_bwd_checkpoint.restype = ctypes.c_int
     i32 = ctypes.c_int32
     rows, draft = ctypes.POINTER(KdRows), ctypes.POINTER(KdDraft)
+    head = ctypes.POINTER(KdMx4Head)
     for name, argtypes in (
             ("kd_topk_entries_workspace_size", [rows, ctypes.POINTER(sz)]),
             ("kd_topk_entries", [rows, vp, vp, vp, vp, sz, vp]),
@@ -117,7 +127,11 @@ def load_library(path: Optional[str] = None) -> ctypes.CDLL:
             ("kd_checkpoint_write", [i64, i64, i32, vp, vp, vp, vp]),
             ("kd_checkpoint_read", [i64, i64, i32, vp, vp, vp, vp]),
             ("kd_verify_draft_workspace_size", [draft, ctypes.POINTER(sz)]),
-            ("kd_verify_draft", [draft] + [vp] * 11 + [sz, vp])):
+            ("kd_verify_draft", [draft] + [vp] * 11 + [sz, vp]),
+            ("kd_mx4_write", [i64, i64, i32, vp, vp, vp, vp]),
+            ("kd_mx4_read", [i64, i64, i32, vp, vp, vp, vp]),
+            ("kd_mx4_logits_workspace_size", [head, ctypes.POINTER(sz)]),
+            ("kd_mx4_logits", [head] + [vp] * 6 + [sz, vp])):
         getattr(lib, name).argtypes = argtypes
         getattr(lib, name).restype = ctypes.c_int
     if path is None:
@@ -920,6 +934,128 @@ def verify_workspace_size(B, T, V, K, dtype=KD_BF16) -> int:
     rc = load_library().kd_verify_draft_workspace_size(ctypes.byref(pr), ctypes.byref(n))
     if rc != 0:
         raise KdError(rc, "kd_verify_draft_workspace_size")
+    return int(n.value)
+
+
+def mx4_write(x, out=None):
+    """kd_mx4_write on the current stream: x [N, D] (bf16 or fp32, D a multiple of
+    32) in 4 bits, {'codes' [N, D / 2] uint8 (two e2m1 codes a byte, the even column
+    low), 'scales' [N, D / 32] uint8 (power of two, biased by 127)}. No gradient
+    flows (mx4_round has one)."""
+    import torch
+    load_library()
+    if x.device.type != "cuda":
+        raise ValueError("tensors must be on a GPU")
+    if x.dim() != 2 or not x.is_contiguous():
+        raise ValueError("x must be a contiguous [N, D]")
+    dev, code = x.device, _dtype_code(x.dtype)
+    N, D = x.shape
+    res = _out_tensors(out, {"codes": ((N, D // 2), torch.uint8),
+                             "scales": ((N, D // 32), torch.uint8)}, dev)
+    _call("kd_mx4_write", dev, N, D, code, x, res["codes"], res["scales"])
+    return res
+
+
+def _check_mx4(name, codes, scales, device=None):
+    """Rows and columns of a matrix in 4 bits."""
+    import torch
+    if codes.device.type != "cuda":
+        raise ValueError("tensors must be on a GPU")
+    if codes.dim() != 2:
+        raise ValueError(f"{name} must be [rows, D / 2]")
+    dev = codes.device if device is None else device
+    N, D = codes.shape[0], 2 * codes.shape[1]
+    _check_tensor(name, codes, (N, D // 2), torch.uint8, dev)
+    _check_tensor(f"scales of {name}", scales, (N, D // 32), torch.uint8, dev)
+    return N, D, dev
+
+
+def mx4_read(codes, scales, dtype, out=None):
+    """kd_mx4_read on the current stream: the matrix [N, D] that codes and scales
+    stand for, in dtype (torch.bfloat16 or torch.float32; exact in both)."""
+    import torch
+    load_library()
+    N, D, dev = _check_mx4("codes", codes, scales)
+    code = _dtype_code(dtype)
+    x = torch.empty(N, D, dtype=dtype, device=dev) if out is None else out
+    if out is not None:
+        _check_tensor("out", x, (N, D), dtype, dev)
+    _call("kd_mx4_read", dev, N, D, code, codes, scales, x)
+    return x
+
+
+_MX4_ROUND = None
+
+
+def mx4_round(W):
+    """The values that W [V, D] has in 4 bits (mx4_write, mx4_read), in W's dtype, for
+    training a head that will be held so: the loss takes them, and the gradient goes to
+    W as it is (straight through)."""
+    import torch
+    global _MX4_ROUND
+    if _MX4_ROUND is None:
+        class Mx4Round(torch.autograd.Function):
+            @staticmethod
+            def forward(ctx, W):
+                q = mx4_write(W)
+                return mx4_read(q["codes"], q["scales"], W.dtype)
+
+            @staticmethod
+            def backward(ctx, grad_out):
+                return grad_out
+
+        _MX4_ROUND = Mx4Round
+    return _MX4_ROUND.apply(W)
+
+
+def mx4_logits(hidden, codes, scales, hidden_scales=None, dtype=None, out=None, workspace=None):
+    """kd_mx4_logits on the current stream: the logits [N, V] of hidden rows with a
+    head in 4 bits (mx4_write's codes [V, D / 2] and scales).
+
+    hidden [N, D] in bf16 or fp32 (rows evenly spaced, 16-byte aligned), used as it
+    is, or 4-bit hidden rows: codes [N, D / 2] with hidden_scales [N, D / 32]. dtype of
+    the logits: torch.bfloat16 or torch.float32; hidden's by default (bf16 for 4-bit
+    rows). `out` may carry them (rows evenly spaced), `workspace` a uint8 tensor of
+    mx4_workspace_size bytes. No gradient flows."""
+    import torch
+    load_library()
+    V, D, dev = _check_mx4("codes", codes, scales)
+    if hidden_scales is not None:
+        N, Dh, _ = _check_mx4("hidden", hidden, hidden_scales, dev)
+        code, ld = KD_MX4, Dh
+    else:
+        code, ld = _logits_rows("hidden", hidden, 2)
+        N, Dh = hidden.shape
+        if hidden.device != dev:
+            raise ValueError("inputs must be on one device")
+    if Dh != D:
+        raise ValueError(f"hidden has {Dh} columns, the head {D}")
+    if out is not None:
+        dtype = out.dtype if dtype is None else dtype
+        ocode, ldo = _logits_rows("out", out, 2)
+        if out.shape != (N, V) or out.device != dev or out.dtype != dtype:
+            raise ValueError(f"out must be a {dtype} tensor of shape {(N, V)} on {dev}")
+    else:
+        if dtype is None:
+            dtype = torch.bfloat16 if code == KD_MX4 else hidden.dtype
+        ocode, ldo = _dtype_code(dtype), V
+        out = torch.empty(N, V, dtype=dtype, device=dev)
+    if workspace is None:
+        workspace = torch.empty(mx4_workspace_size(N, D, V, code), dtype=torch.uint8, device=dev)
+    _check_workspace(workspace, dev)
+    _call("kd_mx4_logits", dev, KdMx4Head(N, D, V, ld, ldo, code, ocode, 0), hidden, hidden_scales,
+          codes, scales, out, workspace, workspace.numel())
+    return out
+
+
+@functools.lru_cache(maxsize=256)
+def mx4_workspace_size(N, D, V, dtype=KD_BF16) -> int:
+    """Bytes of workspace of mx4_logits (dtype of the hidden rows; KD_MX4: 4 bits)."""
+    n = ctypes.c_size_t(0)
+    pr = KdMx4Head(int(N), int(D), int(V), int(D), int(V), int(dtype), KD_F32, 0)
+    rc = load_library().kd_mx4_logits_workspace_size(ctypes.byref(pr), ctypes.byref(n))
+    if rc != 0:
+        raise KdError(rc, "kd_mx4_logits_workspace_size")
     return int(n.value)
 
 

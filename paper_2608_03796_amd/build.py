@@ -10,7 +10,7 @@ import sys
 HERE = os.path.dirname(os.path.abspath(__file__))
 CSRC = os.path.join(HERE, "csrc")
 LIB = os.path.join(HERE, "libkdtopk.so")
-SOURCES = ["kd_kernels.hip", "kd_api.cpp", "kd_ops.hip", "kd_ops_api.cpp"]
+SOURCES = ["kd_kernels.hip", "kd_api.cpp", "kd_ops.hip", "kd_mx4.hip", "kd_ops_api.cpp"]
 
 HIPCC_FLAGS = [
     "--offload-arch=gfx950", "-O3", "-std=c++17", "-fPIC", "-shared",

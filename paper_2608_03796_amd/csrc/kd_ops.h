@@ -69,7 +69,26 @@ struct KdVerifyArgs {
   double* norm;             // [B, 4] dense draft: M, S of the target's and the draft's row
 };
 
+// Bytes of workspace of a product of N hidden rows with a head of V rows
+constexpr size_t kd_mx4_workspace(int64_t, int64_t, int64_t, int) { return 256; }
+
+struct KdMx4Args {
+  const void* hidden;       // [N, ld_hidden], or [N, D / 2] codes
+  const uint8_t* hscales;   // [N, D / 32] (4-bit hidden rows) or null
+  const uint8_t* codes;     // [V, D / 2]
+  const uint8_t* scales;    // [V, D / 32]
+  void* out;                // [N, ld_out]
+  char* ws;                 // kd_mx4_workspace bytes
+  int64_t N, D, V, ld_hidden, ld_out;
+  int dtype, out_dtype;     // of the hidden rows (2 = 4 bits) and the output
+};
+
 extern "C" {
+int kd_launch_mx4_write(const void* x, int dtype, int64_t n, uint8_t* codes, uint8_t* scales,
+                        void* stream);
+int kd_launch_mx4_read(const uint8_t* codes, const uint8_t* scales, int dtype, int64_t n, void* x,
+                       void* stream);
+int kd_launch_mx4_logits(const KdMx4Args* a, void* stream);
 int kd_launch_topk(const KdTopkArgs* a, void* stream);
 int kd_launch_cache_read(const KdCacheReadArgs* a, void* stream);
 int kd_launch_ckpt_write(const void* hidden, int dtype, int64_t n, uint8_t* codes, uint8_t* scales,

@@ -1,6 +1,7 @@
 // C ABI of the operators around the loss (top-K entries, the teacher cache,
-// 8-bit checkpoints, draft verification): argument checks and workspace plans.
-// Plain C++: every device operation goes through the launchers of kd_ops.hip.
+// 8-bit checkpoints, draft verification, 4-bit matrices and their products): argument
+// checks and workspace plans. Plain C++: every device operation goes through the
+// launchers of kd_ops.hip and kd_mx4.hip.
 #include <math.h>
 #include <stdint.h>
 
@@ -94,6 +95,31 @@ kd_status check_checkpoint(int64_t N, int64_t D, int32_t dtype, const void* hidd
   if (N > 0 && (hidden == nullptr || codes == nullptr || scales == nullptr))
     return KD_ERR_NULL_PTR;
   if (!aligned(hidden, 16) || !aligned(codes, 16)) return KD_ERR_UNSUPPORTED;
+  return KD_OK;
+}
+
+kd_status check_mx4(int64_t N, int64_t D, int32_t dtype, const void* x, const void* codes,
+                    const void* scales) {
+  if (dtype != KD_F32 && dtype != KD_BF16) return KD_ERR_UNSUPPORTED;
+  if (N < 0 || N >= kMaxN || D < 32 || D > kMaxD) return KD_ERR_BAD_SHAPE;
+  if (D % 32 != 0) return KD_ERR_UNSUPPORTED;
+  if (N > 0 && (x == nullptr || codes == nullptr || scales == nullptr)) return KD_ERR_NULL_PTR;
+  if (!aligned(x, 16) || !aligned(codes, 16)) return KD_ERR_UNSUPPORTED;
+  return KD_OK;
+}
+
+kd_status check_head(const kd_mx4_head* p) {
+  if (p == nullptr) return KD_ERR_NULL_PTR;
+  if (p->flags != 0) return KD_ERR_BAD_ARG;
+  if (p->dtype != KD_F32 && p->dtype != KD_BF16 && p->dtype != KD_MX4) return KD_ERR_UNSUPPORTED;
+  if (p->out_dtype != KD_F32 && p->out_dtype != KD_BF16) return KD_ERR_UNSUPPORTED;
+  if (p->N < 0 || p->N >= kMaxN || p->D < 32 || p->D > kMaxD) return KD_ERR_BAD_SHAPE;
+  if (p->V < 1 || p->V > kMaxV || p->ld_out < p->V || p->ld_out > kMaxLd) return KD_ERR_BAD_SHAPE;
+  if (p->D % 32 != 0) return KD_ERR_UNSUPPORTED;
+  if (p->dtype != KD_MX4) {
+    if (p->ld_hidden < p->D || p->ld_hidden > kMaxLd) return KD_ERR_BAD_SHAPE;
+    if (p->ld_hidden * elem_bytes(p->dtype) % 16 != 0) return KD_ERR_UNSUPPORTED;
+  }
   return KD_OK;
 }
 
@@ -253,6 +279,63 @@ kd_status kd_verify_draft(const kd_draft* p, const void* target_logits,
   a.segr = reinterpret_cast<double*>(ws + t.off_segr);
   a.norm = reinterpret_cast<double*>(ws + t.off_norm);
   return kd_launch_verify(&a, hip_stream) == 0 ? KD_OK : KD_ERR_DEVICE;
+}
+
+kd_status kd_mx4_write(int64_t N, int64_t D, int32_t dtype, const void* x, uint8_t* codes,
+                       uint8_t* scales, void* hip_stream) {
+  const kd_status st = check_mx4(N, D, dtype, x, codes, scales);
+  if (st != KD_OK || N == 0) return st;
+  return kd_launch_mx4_write(x, dtype, N * D, codes, scales, hip_stream) == 0 ? KD_OK
+                                                                              : KD_ERR_DEVICE;
+}
+
+kd_status kd_mx4_read(int64_t N, int64_t D, int32_t dtype, const uint8_t* codes,
+                      const uint8_t* scales, void* x, void* hip_stream) {
+  const kd_status st = check_mx4(N, D, dtype, x, codes, scales);
+  if (st != KD_OK || N == 0) return st;
+  return kd_launch_mx4_read(codes, scales, dtype, N * D, x, hip_stream) == 0 ? KD_OK
+                                                                             : KD_ERR_DEVICE;
+}
+
+kd_status kd_mx4_logits_workspace_size(const kd_mx4_head* p, size_t* bytes) {
+  if (p == nullptr || bytes == nullptr) return KD_ERR_NULL_PTR;
+  const kd_status st = check_head(p);
+  if (st != KD_OK) return st;
+  *bytes = kd_mx4_workspace(p->N, p->D, p->V, p->dtype);
+  return KD_OK;
+}
+
+kd_status kd_mx4_logits(const kd_mx4_head* p, const void* hidden, const uint8_t* hidden_scales,
+                        const uint8_t* codes, const uint8_t* scales, void* out, void* workspace,
+                        size_t workspace_bytes, void* hip_stream) {
+  const kd_status st = check_head(p);
+  if (st != KD_OK) return st;
+  const bool mx4 = p->dtype == KD_MX4;
+  if (workspace == nullptr) return KD_ERR_NULL_PTR;
+  if (p->N > 0 && (hidden == nullptr || (mx4 && hidden_scales == nullptr) || codes == nullptr ||
+                   scales == nullptr || out == nullptr))
+    return KD_ERR_NULL_PTR;
+  if (!aligned(hidden, 16) || !aligned(codes, 16) || !aligned(workspace, 16) ||
+      !aligned(out, elem_bytes(p->out_dtype)))
+    return KD_ERR_UNSUPPORTED;
+  if (workspace_bytes < kd_mx4_workspace(p->N, p->D, p->V, p->dtype))
+    return KD_ERR_WORKSPACE_TOO_SMALL;
+  if (p->N == 0) return KD_OK;
+  KdMx4Args a{};
+  a.hidden = hidden;
+  a.hscales = mx4 ? hidden_scales : nullptr;
+  a.codes = codes;
+  a.scales = scales;
+  a.out = out;
+  a.ws = static_cast<char*>(workspace);
+  a.N = p->N;
+  a.D = p->D;
+  a.V = p->V;
+  a.ld_hidden = p->ld_hidden;
+  a.ld_out = p->ld_out;
+  a.dtype = p->dtype;
+  a.out_dtype = p->out_dtype;
+  return kd_launch_mx4_logits(&a, hip_stream) == 0 ? KD_OK : KD_ERR_DEVICE;
 }
 
 }  // extern "C"
