@@ -356,6 +356,51 @@ kd_status kd_scale_grads(const float* grad_loss,
                          void* hip_stream);
 
 /*
+ * Cross entropy against labels, the other half of a distillation run's objective:
+ * the same projection, chunks and gradients for a target of one entry a token.
+ *
+ *     l_t = ln Z_t - z_t[label_t] + z_loss (ln Z_t)^2
+ *
+ * (the last term, the "z-loss", keeps the normaliser near 1; z_loss = 0 leaves it
+ * out), the loss their mean over the tokens whose label is in [0, V); tokens with
+ * another label (-100, say) are ignored as the loss above ignores them. Gradients:
+ * dL/dz_tv = g_t ((1 + 2 z_loss ln Z_t) q_tv - [v = label_t]), grad_hidden = G W,
+ * grad_W (+)= G^T h. (The weight 1 + 2 z_loss ln Z_t is held 2^-24 away from 0.)
+ */
+typedef struct kd_label_problem {
+  int64_t N, D, V, chunk;  /* as in kd_problem                                 */
+  int32_t dtype;           /* kd_dtype of hidden, W and grad_hidden             */
+  float z_loss;            /* finite and >= 0                                   */
+  int32_t flags;           /* 0 or KD_FLAG_GRAD_HIDDEN_F32                      */
+} kd_label_problem;
+
+/* Workspace of the three calls below: kd_topk_kl_workspace_size's for K = 1, and 9
+ * bytes a token. */
+kd_status kd_cross_entropy_workspace_size(const kd_label_problem* p, size_t* bytes);
+
+/*
+ * kd_topk_kl_fwd_bwd, kd_topk_kl_fwd and kd_topk_kl_bwd for labels: loss and
+ * gradients with one projection a chunk; the loss with the log-normaliser; the
+ * gradients from it. labels [N] int64 (8-byte aligned) take the place of the
+ * teacher's arrays and the mask; the other arguments, their results on ignored tokens,
+ * and the errors are those calls' (KD_ERR_BAD_ARG also for z_loss). KD_DEBUG_CHECK
+ * has nothing to check here.
+ */
+kd_status kd_cross_entropy_fwd_bwd(const kd_label_problem* p, const void* hidden, const void* W,
+                                   const int64_t* labels, float* loss, float* loss_per_token,
+                                   void* grad_hidden, float* grad_W, int accumulate_grad_W,
+                                   void* workspace, size_t workspace_bytes, void* hip_stream);
+kd_status kd_cross_entropy_fwd(const kd_label_problem* p, const void* hidden, const void* W,
+                               const int64_t* labels, float* loss, float* loss_per_token,
+                               float* saved_logz, void* workspace, size_t workspace_bytes,
+                               void* hip_stream);
+kd_status kd_cross_entropy_bwd(const kd_label_problem* p, const void* hidden, const void* W,
+                               const int64_t* labels, const float* saved_logz,
+                               const float* grad_loss, const float* grad_loss_per_token,
+                               void* grad_hidden, float* grad_W, int accumulate_grad_W,
+                               void* workspace, size_t workspace_bytes, void* hip_stream);
+
+/*
  * ---- Operators around the loss ------------------------------------------
  * The conventions above hold for them too (device pointers, the caller's
  * buffers, checks before anything is enqueued, one stream, the same bits from

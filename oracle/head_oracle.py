@@ -65,7 +65,8 @@ def mx4_logits(hidden, codes, scales):
 def cross_entropy(hidden, W, labels, z_loss=0.0, g=1.0, g_token=None):
     """Mean over the tokens whose label is in [0, V) of ln Z - z[label] + z_loss
     (ln Z)^2 (0 if there are none), and the gradients of g times it (or of sum_t
-    g_token[t] l_t)."""
+    g_token[t] l_t). size: the larger magnitude of ln Z and z[label], whose difference
+    the loss is; q_label: the label's probability; weight: of each token."""
     h, W = np.asarray(hidden, dtype=np.float64), np.asarray(W, dtype=np.float64)
     labels = np.asarray(labels)
     N, V = h.shape[0], W.shape[0]
@@ -85,4 +86,7 @@ def cross_entropy(hidden, W, labels, z_loss=0.0, g=1.0, g_token=None):
     G[rows, at] -= 1.0
     G *= weight[:, None]
     return dict(loss=lpt.sum() / n if n else 0.0, loss_per_token=lpt,
-                logz=np.where(valid, logz, 0.0), grad_hidden=G @ W, grad_W=G.T @ h)
+                logz=np.where(valid, logz, 0.0),
+                size=np.where(valid, np.maximum(np.abs(logz), np.abs(z[rows, at])), 0.0),
+                q_label=np.where(valid, e[rows, at] / total[:, 0], 0.0), weight=weight,
+                grad_hidden=G @ W, grad_W=G.T @ h)

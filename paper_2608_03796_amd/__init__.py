@@ -34,7 +34,9 @@ EXPORTED = ("kd_topk_kl_workspace_size", "kd_topk_kl_fwd_bwd", "kd_topk_kl_fwd_b
             "kd_teacher_cache_read", "kd_checkpoint_write", "kd_checkpoint_read",
             "kd_topk_kl_bwd_checkpoint",
             "kd_verify_draft_workspace_size", "kd_verify_draft", "kd_mx4_write", "kd_mx4_read",
-            "kd_mx4_logits_workspace_size", "kd_mx4_logits")
+            "kd_mx4_logits_workspace_size", "kd_mx4_logits",
+            "kd_cross_entropy_workspace_size", "kd_cross_entropy_fwd_bwd", "kd_cross_entropy_fwd",
+            "kd_cross_entropy_bwd")
 
 
 class KdError(RuntimeError):
@@ -64,6 +66,12 @@ class KdDraft(ctypes.Structure):
                 ("ld_target", ctypes.c_int64), ("ld_draft", ctypes.c_int64),
                 ("K", ctypes.c_int32), ("dtype", ctypes.c_int32),
                 ("temperature", ctypes.c_double), ("flags", ctypes.c_int32)]
+
+
+class KdLabelProblem(ctypes.Structure):
+    _fields_ = [("N", ctypes.c_int64), ("D", ctypes.c_int64), ("V", ctypes.c_int64),
+                ("chunk", ctypes.c_int64), ("dtype", ctypes.c_int32), ("z_loss", ctypes.c_float),
+                ("flags", ctypes.c_int32)]
 
 
 class KdMx4Head(ctypes.Structure):
@@ -118,7 +126,7 @@ def load_library(path: Optional[str] = None) -> ctypes.CDLL:
     lib.kd_topk_kl_bwd_checkpoint.restype = ctypes.c_int
     i32 = ctypes.c_int32
     rows, draft = ctypes.POINTER(KdRows), ctypes.POINTER(KdDraft)
-    head = ctypes.POINTER(KdMx4Head)
+    head, labels = ctypes.POINTER(KdMx4Head), ctypes.POINTER(KdLabelProblem)
     for name, argtypes in (
             ("kd_topk_entries_workspace_size", [rows, ctypes.POINTER(sz)]),
             ("kd_topk_entries", [rows, vp, vp, vp, vp, sz, vp]),
@@ -131,7 +139,11 @@ def load_library(path: Optional[str] = None) -> ctypes.CDLL:
             ("kd_mx4_write", [i64, i64, i32, vp, vp, vp, vp]),
             ("kd_mx4_read", [i64, i64, i32, vp, vp, vp, vp]),
             ("kd_mx4_logits_workspace_size", [head, ctypes.POINTER(sz)]),
-            ("kd_mx4_logits", [head] + [vp] * 6 + [sz, vp])):
+            ("kd_mx4_logits", [head] + [vp] * 6 + [sz, vp]),
+            ("kd_cross_entropy_workspace_size", [labels, ctypes.POINTER(sz)]),
+            ("kd_cross_entropy_fwd_bwd", [labels] + [vp] * 7 + [ctypes.c_int, vp, sz, vp]),
+            ("kd_cross_entropy_fwd", [labels] + [vp] * 7 + [sz, vp]),
+            ("kd_cross_entropy_bwd", [labels] + [vp] * 8 + [ctypes.c_int, vp, sz, vp])):
         getattr(lib, name).argtypes = argtypes
         getattr(lib, name).restype = ctypes.c_int
     if path is None:
@@ -706,7 +718,7 @@ def _out_tensors(out, want, device):
     for name, (shape, dtype) in want.items():
         t = out.get(name) if out else None
         if t is None:
-            t = torch.empty(*shape, dtype=dtype, device=device)
+            t = torch.empty(shape, dtype=dtype, device=device)
         else:
             _check_tensor(name, t, shape, dtype, device)
         res[name] = t
@@ -935,6 +947,194 @@ def verify_workspace_size(B, T, V, K, dtype=KD_BF16) -> int:
     if rc != 0:
         raise KdError(rc, "kd_verify_draft_workspace_size")
     return int(n.value)
+
+
+def _label_problem(hidden, W, labels, z_loss, chunk, workspace, grad_hidden_f32=False):
+    """The problem and workspace of a cross entropy, with its checks."""
+    import torch
+    load_library()
+    if hidden.device.type != "cuda":
+        raise ValueError("tensors must be on a GPU")
+    if hidden.dim() != 2 or W.dim() != 2:
+        raise ValueError("hidden must be [N, D] and W [V, D]")
+    dev, code = hidden.device, _dtype_code(hidden.dtype)
+    if W.dtype != hidden.dtype:
+        raise TypeError("hidden and W must share a dtype")
+    if labels.dtype != torch.int64:
+        raise TypeError("labels must be torch.int64")
+    N, D = hidden.shape
+    _check_tensor("hidden", hidden, (N, D), hidden.dtype, dev)
+    _check_tensor("W", W, (W.shape[0], D), W.dtype, dev)
+    _check_tensor("labels", labels, (N,), torch.int64, dev)
+    pr = KdLabelProblem(N, D, W.shape[0], int(chunk), code, float(z_loss),
+                        _flags(grad_hidden_f32=grad_hidden_f32))
+    if workspace is None:
+        workspace = torch.empty(ce_workspace_size(N, D, W.shape[0], int(chunk), code),
+                                dtype=torch.uint8, device=dev)
+    _check_workspace(workspace, dev)
+    return pr, workspace, dev
+
+
+@functools.lru_cache(maxsize=256)
+def ce_workspace_size(N, D, V, chunk=4096, dtype=KD_BF16) -> int:
+    """Bytes of workspace of cross_entropy, ce_fwd_bwd, ce_fwd and ce_bwd."""
+    n = ctypes.c_size_t(0)
+    pr = KdLabelProblem(int(N), int(D), int(V), int(chunk), int(dtype), 0.0, 0)
+    rc = load_library().kd_cross_entropy_workspace_size(ctypes.byref(pr), ctypes.byref(n))
+    if rc != 0:
+        raise KdError(rc, "kd_cross_entropy_workspace_size")
+    return int(n.value)
+
+
+def ce_fwd_bwd(hidden, W, labels, z_loss: float = 0.0, chunk: int = 4096,
+               grad_hidden: bool = True, grad_W: bool = True, loss_per_token: bool = False,
+               grad_W_out=None, accumulate_grad_W: bool = False, workspace=None, out=None,
+               grad_hidden_f32: bool = False):
+    """kd_cross_entropy_fwd_bwd on the current stream: the mean cross entropy of
+    hidden W^T [N, V] against labels [N] int64 (a label outside [0, V) is ignored),
+    plus z_loss (ln Z)^2 a token, and its gradients. hidden [N, D] and W [V, D] in
+    bf16 or fp32. Returns and `out` as for fwd_bwd."""
+    import torch
+    pr, workspace, dev = _label_problem(hidden, W, labels, z_loss, chunk, workspace,
+                                        grad_hidden_f32)
+    want = {"loss": ((), torch.float32)}
+    if loss_per_token:
+        want["loss_per_token"] = ((pr.N,), torch.float32)
+    if grad_hidden:
+        want["grad_hidden"] = ((pr.N, pr.D), torch.float32 if grad_hidden_f32 else hidden.dtype)
+    if grad_W:
+        want["grad_W"] = ((pr.V, pr.D), torch.float32)
+        if grad_W_out is not None:
+            out = {**(out or {}), "grad_W": grad_W_out}
+    res = _out_tensors(out, want, dev)
+    _call("kd_cross_entropy_fwd_bwd", dev, pr, hidden, W, labels, res["loss"],
+          res.get("loss_per_token"), res.get("grad_hidden"), res.get("grad_W"),
+          int(bool(accumulate_grad_W)), workspace, workspace.numel())
+    return res
+
+
+def ce_fwd(hidden, W, labels, z_loss: float = 0.0, chunk: int = 4096,
+           loss_per_token: bool = False, workspace=None):
+    """kd_cross_entropy_fwd: the loss without gradient work. Returns a dict with
+    'loss' (0-d), 'saved_logz' [N] (ln Z, for ce_bwd) and, when requested,
+    'loss_per_token' [N]."""
+    import torch
+    pr, workspace, dev = _label_problem(hidden, W, labels, z_loss, chunk, workspace)
+    want = {"loss": ((), torch.float32), "saved_logz": ((pr.N,), torch.float32)}
+    if loss_per_token:
+        want["loss_per_token"] = ((pr.N,), torch.float32)
+    res = _out_tensors(None, want, dev)
+    _call("kd_cross_entropy_fwd", dev, pr, hidden, W, labels, res["loss"],
+          res.get("loss_per_token"), res["saved_logz"], workspace, workspace.numel())
+    return res
+
+
+def ce_bwd(hidden, W, labels, saved_logz, z_loss: float = 0.0, chunk: int = 4096, grad_loss=None,
+           grad_loss_per_token=None, grad_hidden: bool = True, grad_W: bool = True,
+           grad_W_out=None, accumulate_grad_W: bool = False, workspace=None,
+           grad_hidden_f32: bool = False):
+    """kd_cross_entropy_bwd: gradients from ce_fwd's log-normaliser; grad_loss and
+    grad_loss_per_token as for bwd. Returns a dict with 'grad_hidden' and 'grad_W' as
+    requested."""
+    import torch
+    pr, workspace, dev = _label_problem(hidden, W, labels, z_loss, chunk, workspace,
+                                        grad_hidden_f32)
+    _check_tensor("saved_logz", saved_logz, (pr.N,), torch.float32, dev)
+    if grad_loss is not None:
+        if grad_loss.numel() != 1:
+            raise ValueError("grad_loss must hold one value (the upstream gradient of the mean)")
+        _check_tensor("grad_loss", grad_loss, grad_loss.shape, torch.float32, dev)
+    if grad_loss_per_token is not None:
+        _check_tensor("grad_loss_per_token", grad_loss_per_token, (pr.N,), torch.float32, dev)
+    want = {}
+    if grad_hidden:
+        want["grad_hidden"] = ((pr.N, pr.D), torch.float32 if grad_hidden_f32 else hidden.dtype)
+    if grad_W:
+        want["grad_W"] = ((pr.V, pr.D), torch.float32)
+    res = _out_tensors(None if grad_W_out is None else {"grad_W": grad_W_out}, want, dev)
+    _call("kd_cross_entropy_bwd", dev, pr, hidden, W, labels, saved_logz, grad_loss,
+          grad_loss_per_token, res.get("grad_hidden"), res.get("grad_W"),
+          int(bool(accumulate_grad_W)), workspace, workspace.numel())
+    return res
+
+
+def _ce_functions():
+    import torch
+
+    class CrossEntropy(torch.autograd.Function):
+        """Mean cross entropy; forward saves ln Z, backward forms the logits again."""
+
+        @staticmethod
+        def forward(ctx, hidden, W, labels, z_loss, chunk, workspace):
+            res = ce_fwd(hidden, W, labels, z_loss=z_loss, chunk=chunk, workspace=workspace)
+            ctx.save_for_backward(hidden, W, labels, res["saved_logz"])
+            ctx.cfg = (z_loss, chunk, workspace)
+            return res["loss"]
+
+        @staticmethod
+        def backward(ctx, grad_out):
+            hidden, W, labels, logz = ctx.saved_tensors
+            z_loss, chunk, workspace = ctx.cfg
+            res = ce_bwd(hidden, W, labels, logz, z_loss=z_loss, chunk=chunk,
+                         grad_loss=grad_out.detach().to(torch.float32).contiguous(),
+                         grad_hidden=ctx.needs_input_grad[0], grad_W=ctx.needs_input_grad[1],
+                         workspace=workspace)
+            gW = res.get("grad_W")
+            return (res.get("grad_hidden"), None if gW is None else gW.to(W.dtype), None, None,
+                    None, None)
+
+    class CrossEntropyFused(torch.autograd.Function):
+        """Mean cross entropy; forward forms both gradients of the mean in fp32 with one
+        projection, backward scales them and rounds each once (kd_scale_grads). One
+        backward per graph."""
+
+        @staticmethod
+        def forward(ctx, hidden, W, labels, z_loss, chunk, workspace):
+            need_h, need_W = ctx.needs_input_grad[0], ctx.needs_input_grad[1]
+            out = ce_fwd_bwd(hidden, W, labels, z_loss=z_loss, chunk=chunk, grad_hidden=need_h,
+                             grad_W=need_W, workspace=workspace, grad_hidden_f32=True)
+            ctx.grads = (out.get("grad_hidden"), out.get("grad_W"))
+            ctx.dtype = hidden.dtype
+            return out["loss"]
+
+        @staticmethod
+        def backward(ctx, grad_out):
+            if ctx.grads is None:
+                raise RuntimeError("cross_entropy(schedule='fused') supports one backward per "
+                                   "graph; use schedule='recompute' to run backward again")
+            grads, ctx.grads = ctx.grads, None
+            outs = [None if g is None else g if ctx.dtype == torch.float32
+                    else torch.empty_like(g, dtype=ctx.dtype) for g in grads]
+            scale_grads(grad_out.detach().to(torch.float32).contiguous(), grad_hidden=grads[0],
+                        grad_hidden_out=outs[0], grad_W=grads[1], grad_W_out=outs[1])
+            return outs[0], outs[1], None, None, None, None
+
+    return {"recompute": CrossEntropy, "fused": CrossEntropyFused}
+
+
+_CE = None
+
+
+def cross_entropy(hidden, W, labels, z_loss: float = 0.0, chunk: int = 4096,
+                  schedule: str = "fused", workspace=None):
+    """Differentiable mean cross entropy of the logits hidden W^T against labels [N]
+    int64, without the logits [N, V] ever being held: the mean over the tokens whose
+    label is in [0, V) of ln Z - z[label] + z_loss (ln Z)^2 (0 if there are none).
+    hidden [N, D] and W [V, D] in bf16 or fp32.
+
+    schedule and workspace (ce_workspace_size bytes) as for topk_kl_loss: "fused" forms
+    both gradients in the forward with one projection and allows one backward;
+    "recompute" saves ln Z only. Without a gradient wanted, the loss alone is computed."""
+    import torch
+    global _CE
+    if schedule not in ("fused", "recompute"):
+        raise ValueError("schedule must be 'fused' or 'recompute'")
+    if not torch.is_grad_enabled() or not (hidden.requires_grad or W.requires_grad):
+        return ce_fwd_bwd(hidden, W, labels, z_loss=z_loss, chunk=chunk, grad_hidden=False,
+                          grad_W=False, workspace=workspace)["loss"]
+    if _CE is None:
+        _CE = _ce_functions()
+    return _CE[schedule].apply(hidden, W, labels, float(z_loss), int(chunk), workspace)
 
 
 def mx4_write(x, out=None):

@@ -394,6 +394,8 @@ struct Call {
   void* stream;
   // the hidden rows as 8-bit checkpoints instead (hidden null)
   const uint8_t *codes, *scales;
+  // labels: the weight of (ln Z)^2 in a token's loss
+  float z_loss;
 };
 
 // Common checks: problem, pointers every mode needs, alignment, workspace
@@ -455,6 +457,7 @@ kd_status enqueue(const kd_problem* p, const Plan& pl, const Call& c) {
     a.stages = stages;
     a.one_projection = scaled ? 1 : 0;
     a.teacher_logprobs = (p->flags & KD_FLAG_TEACHER_LOGPROBS) ? 1 : 0;
+    a.z_loss = c.z_loss;
     a.gscale = c.gscale;
     a.gtok = c.gtok;
     a.logz_in = c.logz_in;
@@ -797,6 +800,108 @@ kd_status kd_topk_kl_fwd_bwd_noalloc(const kd_problem* p, const void* hidden, co
   st = enqueue(p, pl, c);
   kd_launch_suppress_profiling(0);
   return st;
+}
+
+// Cross entropy against labels: the loss above for a teacher of one entry a token,
+// whose arrays stand behind the plan's workspace.
+static kd_problem label_problem(const kd_label_problem* p) {
+  return kd_problem{p->N, p->D, p->V, p->chunk, 1, p->dtype, 1.0f, p->flags};
+}
+static kd_status check_labels(const kd_label_problem* p) {
+  if (p == nullptr) return KD_ERR_NULL_PTR;
+  if ((p->flags & ~KD_FLAG_GRAD_HIDDEN_F32) != 0) return KD_ERR_BAD_ARG;
+  const kd_problem q = label_problem(p);
+  const kd_status st = check_problem(&q);
+  if (st != KD_OK) return st;
+  return isfinite(p->z_loss) && p->z_loss >= 0.0f ? KD_OK : KD_ERR_BAD_ARG;
+}
+struct LabelPlan {
+  Plan pl;
+  size_t off_idx, off_logit, off_ignore;
+};
+static LabelPlan label_plan(const kd_problem* p) {
+  LabelPlan l;
+  l.pl = make_plan(p);
+  l.off_idx = l.pl.total;
+  l.off_logit = align256(l.off_idx + (size_t)p->N * 4);
+  l.off_ignore = align256(l.off_logit + (size_t)p->N * 4);
+  l.pl.total = align256(l.off_ignore + (size_t)p->N);
+  return l;
+}
+// Checks and enqueues one call; c lacks the teacher's arrays.
+static kd_status enqueue_labels(const kd_label_problem* p, const int64_t* labels, Call c) {
+  const kd_problem q = label_problem(p);
+  const LabelPlan l = label_plan(&q);
+  c.z_loss = p->z_loss;
+  if (p->N > 0 && labels == nullptr) return KD_ERR_NULL_PTR;
+  if (c.ws == nullptr) return KD_ERR_NULL_PTR;
+  KdLabelArgs a{};
+  if (p->N > 0) {
+    char* ws = static_cast<char*>(c.ws);
+    a.labels = labels;
+    a.N = p->N;
+    a.V = p->V;
+    a.idx = reinterpret_cast<int32_t*>(ws + l.off_idx);
+    a.logit = reinterpret_cast<float*>(ws + l.off_logit);
+    a.ignore = reinterpret_cast<uint8_t*>(ws + l.off_ignore);
+    c.idx = a.idx;
+    c.tlogit = a.logit;
+    c.ignore = a.ignore;
+  }
+  const kd_status st = validate(&q, c, l.pl);
+  if (st != KD_OK) return st;
+  if (((uintptr_t)labels & 7u) != 0) return KD_ERR_UNSUPPORTED;
+  if (p->N > 0 && kd_launch_labels(&a, c.stream) != 0) return KD_ERR_DEVICE;
+  return enqueue(&q, l.pl, c);
+}
+
+kd_status kd_cross_entropy_workspace_size(const kd_label_problem* p, size_t* bytes) {
+  if (p == nullptr || bytes == nullptr) return KD_ERR_NULL_PTR;
+  const kd_status st = check_labels(p);
+  if (st != KD_OK) return st;
+  const kd_problem q = label_problem(p);
+  *bytes = label_plan(&q).pl.total;
+  return KD_OK;
+}
+
+kd_status kd_cross_entropy_fwd_bwd(const kd_label_problem* p, const void* hidden, const void* W,
+                                   const int64_t* labels, float* loss, float* loss_per_token,
+                                   void* grad_hidden, float* grad_W, int accumulate_grad_W,
+                                   void* workspace, size_t workspace_bytes, void* hip_stream) {
+  const kd_status st = check_labels(p);
+  if (st != KD_OK) return st;
+  if (loss == nullptr) return KD_ERR_NULL_PTR;
+  return enqueue_labels(p, labels,
+                        Call{KD_MODE_FWD_BWD, hidden, W, nullptr, nullptr, nullptr, loss,
+                             loss_per_token, nullptr, nullptr, nullptr, nullptr, grad_hidden,
+                             grad_W, accumulate_grad_W, workspace, workspace_bytes, hip_stream});
+}
+
+kd_status kd_cross_entropy_fwd(const kd_label_problem* p, const void* hidden, const void* W,
+                               const int64_t* labels, float* loss, float* loss_per_token,
+                               float* saved_logz, void* workspace, size_t workspace_bytes,
+                               void* hip_stream) {
+  const kd_status st = check_labels(p);
+  if (st != KD_OK) return st;
+  if (loss == nullptr || (p->N > 0 && saved_logz == nullptr)) return KD_ERR_NULL_PTR;
+  return enqueue_labels(p, labels,
+                        Call{KD_MODE_FWD, hidden, W, nullptr, nullptr, nullptr, loss,
+                             loss_per_token, saved_logz, nullptr, nullptr, nullptr, nullptr,
+                             nullptr, 0, workspace, workspace_bytes, hip_stream});
+}
+
+kd_status kd_cross_entropy_bwd(const kd_label_problem* p, const void* hidden, const void* W,
+                               const int64_t* labels, const float* saved_logz,
+                               const float* grad_loss, const float* grad_loss_per_token,
+                               void* grad_hidden, float* grad_W, int accumulate_grad_W,
+                               void* workspace, size_t workspace_bytes, void* hip_stream) {
+  const kd_status st = check_labels(p);
+  if (st != KD_OK) return st;
+  if (p->N > 0 && saved_logz == nullptr) return KD_ERR_NULL_PTR;
+  return enqueue_labels(p, labels,
+                        Call{KD_MODE_BWD, hidden, W, nullptr, nullptr, nullptr, nullptr, nullptr,
+                             nullptr, saved_logz, grad_loss, grad_loss_per_token, grad_hidden,
+                             grad_W, accumulate_grad_W, workspace, workspace_bytes, hip_stream});
 }
 
 }  // extern "C"

@@ -102,6 +102,16 @@ constexpr float kRefShift = 24.f;
 
 constexpr int prologue_lds(int K) { return 4 * prologue_hash_slots(K) + 8 * K; }
 
+// A token's weight of q in its gradient, coef M, with the z-loss's part: the loss
+// lambda (ln Z)^2 adds 2 lambda ln Z coef q (z2 = 2 lambda). Kept 2^-24 of coef away
+// from 0, the rounding of the sum itself, since the one-projection schedule divides
+// by it.
+__device__ __forceinline__ float with_z_loss(float coef_m, float coef, float z2, float lnz) {
+  const float m = coef_m + coef * (z2 * lnz);
+  const float least = fabsf(coef) * 0x1p-24f;
+  return fabsf(m) < least ? copysignf(least, m) : m;
+}
+
 struct PrologueArgs {
   const int32_t* tidx;
   int32_t* tidx_out;
@@ -112,6 +122,7 @@ struct PrologueArgs {
   int rows, K, V, D;
   float inv_tau;
   int logprobs;
+  float z2;                 // twice the z-loss's weight
   const float* inv_nvalid;  // device 1/N_valid, or null: inv_n
   float inv_n;
   const float *gscale, *gtok, *logz_in;
@@ -283,7 +294,9 @@ __device__ __forceinline__ void prologue_row(const PrologueArgs& a, int r, char*
     a.rowM[r] = m;
     a.rowH[r] = h;
     a.rowCoef[r] = coef;
-    a.rowCoefM[r] = coef * m;
+    a.rowCoefM[r] = a.z2 != 0.f && a.logz_in != nullptr
+                        ? with_z_loss(coef * m, coef, a.z2, a.logz_in[t])
+                        : coef * m;
     if (a.logz_in != nullptr) a.rowL2[r] = a.logz_in[t] * kLog2e;
   }
   if (a.rowR == nullptr) return;
@@ -1216,13 +1229,13 @@ __global__ __launch_bounds__(Geo<TS>::kThreads, TS == 256 ? 1 : 2) void k_logits
   }
 }
 
-// l_t = H_t - C_t / tau + M_t log Z_t (Eq. 2) with C_t = sum_k p_k z_{t, idx_k},
+// l_t = H_t - C_t / tau + M_t log Z_t (Eq. 2; with labels also z_loss (log Z_t)^2) with C_t = sum_k p_k z_{t, idx_k},
 // 0 on ignored rows; one wave per row and a partial sum per block of
 // kLossRows rows in a fixed order, for the deterministic mean.
 __global__ void k_row_loss(const float* zhit, const float* p, int K, const float* rowL2,
                            const float* rowM, const float* rowH, const uint8_t* ignore,
                            int64_t row0, const int* __restrict__ rowmap, int rows, float inv_tau,
-                           float* loss_per_token, float* logz_out, float* block_partial) {
+                           float z_loss, float* loss_per_token, float* logz_out, float* block_partial) {
   __shared__ float red[kLossRows];
   const int lane = threadIdx.x & 63, wave = wave_id();
   const int r = blockIdx.x * kLossRows + wave;
@@ -1241,6 +1254,7 @@ __global__ void k_row_loss(const float* zhit, const float* p, int K, const float
     c = wave_sum(c);
     const bool valid = rowmap != nullptr || ignore == nullptr || ignore[row0 + r] == 0;
     l = valid ? rowH[r] - c * inv_tau + rowM[r] * rowL2[r] * kLn2 : 0.f;
+    if (z_loss != 0.f && valid) l += z_loss * (rowL2[r] * kLn2) * (rowL2[r] * kLn2);
     if (lane == 0) {
       if (loss_per_token) loss_per_token[rowmap != nullptr ? (int64_t)tok : r] = l;
       if (logz_out) logz_out[rowmap != nullptr ? (int64_t)tok : r] = rowL2[r] * kLn2;
@@ -1259,8 +1273,8 @@ __global__ void k_row_loss(const float* zhit, const float* p, int K, const float
 // max); for a row with such a tile, every run brought to mx; the teacher
 // cells (g/tau)(M q - p) (Eq. 3) in the row's stored scale (0 where the
 // factor is 0, i.e. on ignored rows); and the token's loss (Eq. 2) with a
-// partial per block of kLossRows rows as k_row_loss forms it. With a rowmap,
-// row r is token rowmap[r] (loss_per_token is then indexed by token), and a
+// partial per block of kLossRows rows as k_row_loss forms it. With a z-loss, M is
+// M + 2 z_loss log Z in the factor and the cells. With a rowmap, row r is token rowmap[r] (loss_per_token is then indexed by token), and a
 // row without a token (-1) only gets a row factor of 0 and a loss of 0.
 template <typename T>
 __global__ __launch_bounds__(256) void k_row_finish(
@@ -1270,7 +1284,8 @@ __global__ __launch_bounds__(256) void k_row_finish(
     const float* __restrict__ rowM, const float* __restrict__ rowH,
     const float* __restrict__ rowCoef, const float* __restrict__ rowCoefM,
     const uint8_t* __restrict__ ignore, int64_t row0, const int* __restrict__ rowmap, int rows,
-    float inv_tau, float* rowL2, float* rowFactor, float* loss_per_token, float* block_partial) {
+    float inv_tau, float z_loss, float* rowL2, float* rowFactor, float* loss_per_token,
+    float* block_partial) {
   __shared__ float red[kLossRows];
   const int lane = threadIdx.x & 63, wave = wave_id();
   const int r = blockIdx.x * kLossRows + wave;
@@ -1298,7 +1313,8 @@ __global__ __launch_bounds__(256) void k_row_finish(
         psv[i] = j < nVT ? ps[j] : 0.f;
       }
     }
-    const float cm = rowCoefM[r], cf = rowCoef[r];
+    float cm = rowCoefM[r];
+    const float cf = rowCoef[r];
     float mx = -INFINITY;
     if (in_regs) {
 #pragma unroll
@@ -1320,6 +1336,7 @@ __global__ __launch_bounds__(256) void k_row_finish(
     }
     s = wave_sum(s);
     const float L2 = mx + log2f(s);
+    if (z_loss != 0.f) cm = with_z_loss(cm, cf, 2.f * z_loss, L2 * kLn2);
     const float f = cm * fast_exp2(mx - L2);
     if (lane == 0) {
       rowL2[r] = L2;
@@ -1367,6 +1384,7 @@ __global__ __launch_bounds__(256) void k_row_finish(
     c = wave_sum(c);
     const bool valid = rowmap != nullptr || ignore == nullptr || ignore[row0 + r] == 0;
     l = valid ? rowH[r] - c * inv_tau + rowM[r] * L2 * kLn2 : 0.f;
+    if (z_loss != 0.f && valid) l += z_loss * (L2 * kLn2) * (L2 * kLn2);
     if (lane == 0 && loss_per_token) loss_per_token[rowmap != nullptr ? (int64_t)tok : r] = l;
   }
   if (lane == 0) red[wave] = l;
@@ -1918,6 +1936,21 @@ __global__ __launch_bounds__(kScanThreads) void k_compact_scan(const uint8_t* __
   }
 }
 
+// ----------------------------------------------------------------- labels --
+__global__ __launch_bounds__(256) void k_labels(const int64_t* __restrict__ labels, int64_t N,
+                                                int64_t V, int32_t* __restrict__ idx,
+                                                float* __restrict__ logit,
+                                                uint8_t* __restrict__ ignore) {
+  const int64_t stride = (int64_t)gridDim.x * 256;
+  for (int64_t t = (int64_t)blockIdx.x * 256 + threadIdx.x; t < N; t += stride) {
+    const int64_t v = labels[t];
+    const bool in = v >= 0 && v < V;
+    idx[t] = in ? (int32_t)v : 0;
+    logit[t] = 0.f;
+    ignore[t] = in ? 0 : 1;
+  }
+}
+
 // ------------------------------------------------------------ index check --
 // flag |= 1 if an index is outside [0, V); |= 2 if a row repeats an index.
 __global__ void k_check_indices(const int32_t* idx, int64_t N, int K, int64_t V, int* flag) {
@@ -2150,6 +2183,7 @@ static int launch_chunk_impl(const KdChunkArgs& a, hipStream_t s) {
       p.D = (int)a.D;
       p.inv_tau = a.inv_tau;
       p.logprobs = a.teacher_logprobs;
+      p.z2 = 2.f * a.z_loss;
       p.inv_nvalid = a.inv_nvalid;
       p.inv_n = a.inv_n;
       p.gscale = a.gscale;
@@ -2210,7 +2244,7 @@ static int launch_chunk_impl(const KdChunkArgs& a, hipStream_t s) {
                        a.part_m, a.part_s, a.nP, a.nP == a.nVT ? 8 : 7, a.rowFlag,
                        static_cast<T*>(a.dZ), a.ldz, a.tidx, a.p, a.zhit, a.K, (int)a.V, k2,
                        a.rowM, a.rowH, a.rowCoef, a.rowCoefM, a.ignore, a.row0, a.rowmap, a.rows,
-                       a.inv_tau, a.rowL2, a.rowFactor, a.loss_per_token, a.block_partial);
+                       a.inv_tau, a.z_loss, a.rowL2, a.rowFactor, a.loss_per_token, a.block_partial);
   } else if (fwd) {
     {
       ProfScope ps_(P_MERGE, 0.0, s);
@@ -2221,7 +2255,7 @@ static int launch_chunk_impl(const KdChunkArgs& a, hipStream_t s) {
       ProfScope ps_(P_ROW_LOSS, 0.0, s);
       hipLaunchKernelGGL(k_row_loss, dim3(cdiv(a.rows, kLossRows)), dim3(64 * kLossRows), 0, s,
                          a.zhit, a.p, a.K, a.rowL2, a.rowM, a.rowH, a.ignore, a.row0, a.rowmap,
-                         a.rows, a.inv_tau, a.loss_per_token, a.logz_out, a.block_partial);
+                         a.rows, a.inv_tau, a.z_loss, a.loss_per_token, a.logz_out, a.block_partial);
     }
   }
   return (int)hipGetLastError();
@@ -2369,6 +2403,14 @@ extern "C" int kd_launch_compact(const KdCompactArgs* a, void* stream) {
     hipLaunchKernelGGL(k_compact_scan, dim3(1), dim3(kScanThreads), 0, s, a->ignore, a->N, a->row0,
                        a->rows, a->rowmap, a->nrow, a->inv_nvalid);
   }
+  return (int)hipGetLastError();
+}
+
+extern "C" int kd_launch_labels(const KdLabelArgs* a, void* stream) {
+  hipStream_t s = static_cast<hipStream_t>(stream);
+  const int64_t blocks = std::min<int64_t>((a->N + 255) / 256, 4096);
+  hipLaunchKernelGGL(k_labels, dim3((unsigned)blocks), dim3(256), 0, s, a->labels, a->N, a->V,
+                     a->idx, a->logit, a->ignore);
   return (int)hipGetLastError();
 }
 

@@ -36,6 +36,7 @@ struct KdChunkArgs {
   const float* logz_in;     // full [N] saved log Z (backward only) or null
   float* logz_out;          // this chunk's rows of the saved log Z (forward; full [N]
                             // with a rowmap) or null
+  float z_loss;             // weight of (ln Z)^2 in a token's loss (labels; 0: none)
   int64_t D, V;
   int K;
   int64_t row0;             // first token of the chunk (of the prepared rows)
@@ -252,6 +253,16 @@ struct KdCompactArgs {
   float* inv_nvalid;        // or null
 };
 
+// Labels as a teacher of one entry: idx[t] = label (0 where it is outside [0, V)),
+// logit[t] = 0, ignore[t] = 1 for a label outside [0, V)
+struct KdLabelArgs {
+  const int64_t* labels;    // [N]
+  int64_t N, V;
+  int32_t* idx;
+  float* logit;
+  uint8_t* ignore;
+};
+
 // out = g x for one gradient: x fp32, out fp32 or bf16, n elements (0: nothing)
 struct KdScaleArg {
   const float* x;
@@ -266,6 +277,7 @@ int kd_launch_chunk(const KdChunkArgs* a, void* stream);
 int kd_launch_dh(const KdDhArgs* a, void* stream);
 int kd_launch_dw(const KdDwArgs* a, void* stream);
 int kd_launch_compact(const KdCompactArgs* a, void* stream);
+int kd_launch_labels(const KdLabelArgs* a, void* stream);
 int kd_launch_tail(const KdTailArgs* a, void* stream);
 int kd_launch_scale(const KdScaleArg* a, const KdScaleArg* b, const float* g, void* stream);
 // the current device's scratch address (hipGetSymbolAddress on first use)
