@@ -394,7 +394,9 @@ struct Call {
   void* stream;
   // the hidden rows as 8-bit checkpoints instead (hidden null)
   const uint8_t *codes, *scales;
-  // labels: the weight of (ln Z)^2 in a token's loss
+  // labels instead of a teacher (idx, tlogit and ignore are then the workspace's,
+  // written from them), and the weight of (ln Z)^2 in a token's loss
+  const int64_t* labels;
   float z_loss;
 };
 
@@ -517,6 +519,12 @@ kd_status enqueue(const kd_problem* p, const Plan& pl, const Call& c) {
       k.rowmap = rowmap;
       k.nrow = gnrow;
       k.inv_nvalid = ci == 0 ? inv_nvalid : nullptr;
+      if (c.labels != nullptr && ci == 0) {
+        k.labels = c.labels;
+        k.V = pl.V;
+        k.idx = const_cast<int32_t*>(c.idx);
+        k.logit = const_cast<float*>(c.tlogit);
+      }
       if (kd_launch_compact(&k, c.stream) != 0) return KD_ERR_DEVICE;
     }
     if (pl.prep_per_group && slot == 0) {
@@ -835,23 +843,16 @@ static kd_status enqueue_labels(const kd_label_problem* p, const int64_t* labels
   c.z_loss = p->z_loss;
   if (p->N > 0 && labels == nullptr) return KD_ERR_NULL_PTR;
   if (c.ws == nullptr) return KD_ERR_NULL_PTR;
-  KdLabelArgs a{};
   if (p->N > 0) {
     char* ws = static_cast<char*>(c.ws);
-    a.labels = labels;
-    a.N = p->N;
-    a.V = p->V;
-    a.idx = reinterpret_cast<int32_t*>(ws + l.off_idx);
-    a.logit = reinterpret_cast<float*>(ws + l.off_logit);
-    a.ignore = reinterpret_cast<uint8_t*>(ws + l.off_ignore);
-    c.idx = a.idx;
-    c.tlogit = a.logit;
-    c.ignore = a.ignore;
+    c.labels = labels;
+    c.idx = reinterpret_cast<int32_t*>(ws + l.off_idx);
+    c.tlogit = reinterpret_cast<float*>(ws + l.off_logit);
+    c.ignore = reinterpret_cast<uint8_t*>(ws + l.off_ignore);
   }
   const kd_status st = validate(&q, c, l.pl);
   if (st != KD_OK) return st;
   if (((uintptr_t)labels & 7u) != 0) return KD_ERR_UNSUPPORTED;
-  if (p->N > 0 && kd_launch_labels(&a, c.stream) != 0) return KD_ERR_DEVICE;
   return enqueue(&q, l.pl, c);
 }
 

@@ -1892,7 +1892,30 @@ __device__ __forceinline__ int count_zero(const uint8_t* m, int64_t b, int64_t e
   while (b < e) c += m[b++] == 0 ? 1 : 0;
   return c;
 }
-__global__ __launch_bounds__(kScanThreads) void k_compact_scan(const uint8_t* __restrict__ ignore,
+// Labels as a teacher of one entry (see KdCompactArgs): by a launch of its own, or,
+// for up to kLabelsInScan tokens, by the scan's workgroup before it scans.
+constexpr int64_t kLabelsInScan = 8192;
+struct LabelArgs {
+  const int64_t* labels;  // or null
+  int64_t N, V;
+  int32_t* idx;
+  float* logit;
+  uint8_t* ignore;
+};
+__device__ __forceinline__ void put_labels(const LabelArgs& a, int64_t first, int64_t stride) {
+  for (int64_t t = first; t < a.N; t += stride) {
+    const int64_t v = a.labels[t];
+    const bool in = v >= 0 && v < a.V;
+    a.idx[t] = in ? (int32_t)v : 0;
+    a.logit[t] = 0.f;
+    a.ignore[t] = in ? 0 : 1;
+  }
+}
+__global__ __launch_bounds__(256) void k_labels(LabelArgs a) {
+  put_labels(a, (int64_t)blockIdx.x * 256 + threadIdx.x, (int64_t)gridDim.x * 256);
+}
+__global__ __launch_bounds__(kScanThreads) void k_compact_scan(LabelArgs labels,
+                                                               const uint8_t* ignore,
                                                                int64_t N, int64_t row0, int rows,
                                                                int* __restrict__ rowmap,
                                                                int* __restrict__ nrow,
@@ -1900,6 +1923,10 @@ __global__ __launch_bounds__(kScanThreads) void k_compact_scan(const uint8_t* __
   constexpr int NWV = kScanThreads / 64;
   __shared__ int sc[NWV], all[NWV];
   const int tid = threadIdx.x, lane = tid & 63, wave = wave_id();
+  if (labels.labels != nullptr) {
+    put_labels(labels, tid, kScanThreads);
+    __syncthreads();
+  }
   // long runs are a multiple of 16 tokens: aligned when the mask is
   int per = (rows + kScanThreads - 1) / kScanThreads;
   if (per > 8) per = (per + 15) & ~15;
@@ -1933,21 +1960,6 @@ __global__ __launch_bounds__(kScanThreads) void k_compact_scan(const uint8_t* __
       for (int w = 0; w < (count ? NWV : 0); ++w) n += all[w];
       inv_nvalid[0] = n > 0 ? 1.0f / (float)n : 0.0f;
     }
-  }
-}
-
-// ----------------------------------------------------------------- labels --
-__global__ __launch_bounds__(256) void k_labels(const int64_t* __restrict__ labels, int64_t N,
-                                                int64_t V, int32_t* __restrict__ idx,
-                                                float* __restrict__ logit,
-                                                uint8_t* __restrict__ ignore) {
-  const int64_t stride = (int64_t)gridDim.x * 256;
-  for (int64_t t = (int64_t)blockIdx.x * 256 + threadIdx.x; t < N; t += stride) {
-    const int64_t v = labels[t];
-    const bool in = v >= 0 && v < V;
-    idx[t] = in ? (int32_t)v : 0;
-    logit[t] = 0.f;
-    ignore[t] = in ? 0 : 1;
   }
 }
 
@@ -2400,17 +2412,15 @@ extern "C" int kd_launch_compact(const KdCompactArgs* a, void* stream) {
   if (a->rows <= 0) return 0;
   {
     ProfScope ps_(P_COMPACT, 0.0, s);
-    hipLaunchKernelGGL(k_compact_scan, dim3(1), dim3(kScanThreads), 0, s, a->ignore, a->N, a->row0,
+    LabelArgs l{a->labels, a->N, a->V, a->idx, a->logit, const_cast<uint8_t*>(a->ignore)};
+    if (a->labels != nullptr && a->N > kLabelsInScan) {
+      hipLaunchKernelGGL(k_labels, dim3((unsigned)std::min<int64_t>((a->N + 255) / 256, 4096)),
+                         dim3(256), 0, s, l);
+      l.labels = nullptr;
+    }
+    hipLaunchKernelGGL(k_compact_scan, dim3(1), dim3(kScanThreads), 0, s, l, a->ignore, a->N, a->row0,
                        a->rows, a->rowmap, a->nrow, a->inv_nvalid);
   }
-  return (int)hipGetLastError();
-}
-
-extern "C" int kd_launch_labels(const KdLabelArgs* a, void* stream) {
-  hipStream_t s = static_cast<hipStream_t>(stream);
-  const int64_t blocks = std::min<int64_t>((a->N + 255) / 256, 4096);
-  hipLaunchKernelGGL(k_labels, dim3((unsigned)blocks), dim3(256), 0, s, a->labels, a->N, a->V,
-                     a->idx, a->logit, a->ignore);
   return (int)hipGetLastError();
 }
 

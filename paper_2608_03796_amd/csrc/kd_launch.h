@@ -251,16 +251,13 @@ struct KdCompactArgs {
   int* rowmap;
   int* nrow;
   float* inv_nvalid;        // or null
-};
-
-// Labels as a teacher of one entry: idx[t] = label (0 where it is outside [0, V)),
-// logit[t] = 0, ignore[t] = 1 for a label outside [0, V)
-struct KdLabelArgs {
-  const int64_t* labels;    // [N]
-  int64_t N, V;
+  // labels [N] (or null) as a teacher of one entry, before the scan: for each of the N
+  // tokens idx = label (0 where it is outside [0, V)), logit = 0, and in `ignore`'s
+  // memory 1 for a label outside [0, V)
+  const int64_t* labels;
+  int64_t V;
   int32_t* idx;
   float* logit;
-  uint8_t* ignore;
 };
 
 // out = g x for one gradient: x fp32, out fp32 or bf16, n elements (0: nothing)
@@ -277,7 +274,6 @@ int kd_launch_chunk(const KdChunkArgs* a, void* stream);
 int kd_launch_dh(const KdDhArgs* a, void* stream);
 int kd_launch_dw(const KdDwArgs* a, void* stream);
 int kd_launch_compact(const KdCompactArgs* a, void* stream);
-int kd_launch_labels(const KdLabelArgs* a, void* stream);
 int kd_launch_tail(const KdTailArgs* a, void* stream);
 int kd_launch_scale(const KdScaleArg* a, const KdScaleArg* b, const float* g, void* stream);
 // the current device's scratch address (hipGetSymbolAddress on first use)
