@@ -105,7 +105,7 @@ struct Mx4Weights {
   const uint8_t* scales;   // of the first row
   int64_t left;            // bytes from there to the scales' end
   int vrows, nb32, pitch;
-  u32x2_t sc[R];
+  u32x2_t sc[R], next[R];
   __device__ __forceinline__ void init(const Mx4Args& a, int v0) {
     vrows = max(0, min(16 * R, a.V - v0));
     nb32 = a.D / kMx4Block;
@@ -115,17 +115,14 @@ struct Mx4Weights {
     scales = a.scales + (int64_t)v0 * nb32;
     left = ((int64_t)a.V - v0) * nb32;
   }
-  // piece u, zeros from block `end` on
-  __device__ __forceinline__ void load(int u, int end, int m, int g, u32x4_t (&w)[2][R]) const {
+  // half h of piece u, zeros from block `end` on
+  __device__ __forceinline__ void load(int u, int h, int end, int m, int g, u32x4_t (&w)[R]) const {
+    const int b = 8 * u + 4 * h + g;
 #pragma unroll
-    for (int h = 0; h < 2; ++h) {
-      const int b = 8 * u + 4 * h + g;
-#pragma unroll
-      for (int r = 0; r < R; ++r) {
-        const uint32_t off = (uint32_t)(16 * r + m) * (uint32_t)pitch + (uint32_t)b * 16u;
-        w[h][r] = __builtin_bit_cast(
-            u32x4_t, __builtin_amdgcn_raw_buffer_load_b128(rw, b < end ? off : kOobOffset, 0, 0));
-      }
+    for (int r = 0; r < R; ++r) {
+      const uint32_t off = (uint32_t)(16 * r + m) * (uint32_t)pitch + (uint32_t)b * 16u;
+      w[r] = __builtin_bit_cast(
+          u32x4_t, __builtin_amdgcn_raw_buffer_load_b128(rw, b < end ? off : kOobOffset, 0, 0));
     }
   }
   // scale bytes of pieces u .. u + 3: lane (m, g) holds the 8 of piece u + g, row m. (A
@@ -136,19 +133,25 @@ struct Mx4Weights {
 #pragma unroll
     for (int r = 0; r < R; ++r) {
       const int row = 16 * r + m;
-      sc[r] = u32x2_t{0u, 0u};
+      next[r] = u32x2_t{0u, 0u};
       if (row < vrows && b < nb32) {
         const int64_t at = (int64_t)row * nb32 + b;
         if (at + 8 <= left) {
-          __builtin_memcpy(&sc[r], scales + at, 8);
+          __builtin_memcpy(&next[r], scales + at, 8);
         } else {
           uint32_t w[2] = {0u, 0u};
           for (int i = 0; i < 8; ++i)
             if (b + i < nb32) w[i >> 2] |= (uint32_t)scales[at + i] << (8 * (i & 3));
-          sc[r] = u32x2_t{w[0], w[1]};
+          next[r] = u32x2_t{w[0], w[1]};
         }
       }
     }
+  }
+  // at every fourth piece u: what was loaded for it, and the loads of the next four
+  __device__ __forceinline__ void turn(int u, int m, int g) {
+#pragma unroll
+    for (int r = 0; r < R; ++r) sc[r] = next[r];
+    load_scales(u + 4, m, g);
   }
   // of block 8 u + 4 h + g, the t-th of the four pieces held. (A block past the row's
   // end may hold the next row's byte there: 0.)
@@ -213,16 +216,19 @@ __global__ __launch_bounds__(512) void k_mx4_rows(Mx4Args a) {
 #pragma unroll
   for (int r = 0; r < R; ++r) acc[r] = f32x4_t{0.f, 0.f, 0.f, 0.f};
   u32x4_t cw[2][R];
-  if (u0 < u1) W.load(u0, nb32, m, g, cw);
+  W.load_scales(u0, m, g);
+#pragma unroll
+  for (int h = 0; h < 2; ++h) W.load(u0, h, u0 < u1 ? nb32 : 0, m, g, cw[h]);
   for (int u = u0; u < u1; ++u) {
     const int t = (u - u0) & 3;
-    if (t == 0) W.load_scales(u, m, g);
+    if (t == 0) W.turn(u, m, g);
     u32x4_t w[2][R];
 #pragma unroll
     for (int h = 0; h < 2; ++h)
 #pragma unroll
       for (int r = 0; r < R; ++r) w[h][r] = cw[h][r];
-    W.load(u + 1, u + 1 < u1 ? nb32 : 0, m, g, cw);
+#pragma unroll
+    for (int h = 0; h < 2; ++h) W.load(u + 1, h, u + 1 < u1 ? nb32 : 0, m, g, cw[h]);
 #pragma unroll
     for (int h = 0; h < 2; ++h) {
       const int b = 8 * u + 4 * h + g;
@@ -301,8 +307,8 @@ __device__ __forceinline__ bool mx4_wide(const Mx4Args& a) {
 
 // 17 hidden rows and more, 16 NB a workgroup: its 8 waves take 16 R rows of W each and
 // share the hidden rows' columns through LDS, a stage of 256 (fp32: 128) of them at a
-// time in two buffers, one barrier a stage. Codes go from memory to registers, a piece
-// ahead.
+// time in two buffers, one barrier a stage. Codes go from memory to registers, those of the
+// next piece as soon as a half's are used.
 constexpr int kMx4Stages(int H) { return H == 1 ? 2 : 1; }  // of a piece
 constexpr int mx4_token_bytes(int H) {  // of a stage in LDS: fp32 as three terms of bf16
   return H == 0 ? 512 : H == 1 ? 768 : 128;
@@ -312,7 +318,7 @@ constexpr int mx4_stage_bytes(int H, int NB) {
 }
 
 template <int H, int NB, int R>
-__global__ __launch_bounds__(512, 2) void k_mx4_wide(Mx4Args a) {
+__global__ __launch_bounds__(512, NB * R <= 8 && R <= 2 ? 4 : 2) void k_mx4_wide(Mx4Args a) {
   __shared__ __attribute__((aligned(16))) char lds[2 * mx4_stage_bytes(H, NB)];
   constexpr int TB = mx4_token_bytes(H), STAGE = mx4_stage_bytes(H, NB), NST = kMx4Stages(H);
   constexpr int HB = H == 0 ? 64 : H == 1 ? 128 : 16;   // bytes of a block in memory
@@ -380,24 +386,21 @@ __global__ __launch_bounds__(512, 2) void k_mx4_wide(Mx4Args a) {
       if (tid < 16 * NB * 8) s[16 * NB * TB + tid] = (char)hsv;
   };
 
-  u32x4_t cw[2][R];
-  W.load(0, nb32, m, g, cw);
+  u32x4_t w[2][R];
+  W.load_scales(0, m, g);
+#pragma unroll
+  for (int h = 0; h < 2; ++h) W.load(0, h, nb32, m, g, w[h]);
   fetch(0);
   put(0);
   __syncthreads();
   int buf = 0;
   for (int u = 0; u < units; ++u) {
     const int t = u & 3;
-    if (t == 0) W.load_scales(u, m, g);
-    u32x4_t w[2][R];
-#pragma unroll
-    for (int h = 0; h < 2; ++h)
-#pragma unroll
-      for (int r = 0; r < R; ++r) w[h][r] = cw[h][r];
-    W.load(u + 1, nb32, m, g, cw);
+    if (t == 0) W.turn(u, m, g);
 #pragma unroll
     for (int st = 0; st < NST; ++st) {
       const bool more = st + 1 < NST || u + 1 < units;
+      // (before the next codes: put waits for it, and not for them)
       if (more) fetch(NST * u + st + 1);
       const char* s = lds + buf * STAGE;
 #pragma unroll
@@ -438,6 +441,7 @@ __global__ __launch_bounds__(512, 2) void k_mx4_wide(Mx4Args a) {
             }
           }
         }
+        W.load(u + 1, h, nb32, m, g, w[h]);
       }
       if (more) put(buf ^ 1);
       __syncthreads();
