@@ -459,6 +459,425 @@ __global__ __launch_bounds__(512, NB * R <= 8 && R <= 2 ? 4 : 2) void k_mx4_wide
   }
 }
 
+// ------------------------------------------------------ many hidden rows --
+// Scale bytes as the tiles below take them: of each 64 rows and 128 columns (4 blocks) 256
+// bytes [g][m][b] = scale of row 16 b + m, block g, zeros past the rows and blocks that
+// exist (a block of scale 2^-127 on both sides, or of a hidden row's zeros, adds
+// nothing). A lane's dword then holds the four row blocks of a wave, which the scaled
+// instructions select from; and 256 bytes are a wave's load.
+__host__ __device__ constexpr int64_t mx4_tile_steps(int64_t D) {  // of 128 columns, even
+  return (D / kMx4Block + 7) / 8 * 2;
+}
+__host__ __device__ constexpr int64_t mx4_tile_groups(int64_t rows) { return (rows + 255) / 256 * 4; }
+
+// a thread per dword: blockIdx.x over 16 steps of a group of rows, blockIdx.y + group0
+__global__ __launch_bounds__(256) void k_mx4_scale_tiles(const uint8_t* __restrict__ scales,
+                                                         int64_t rows, int nb32, int T,
+                                                         int64_t groups, uint8_t* out) {
+  const int m = threadIdx.x & 15, g = (threadIdx.x >> 4) & 3, sub = threadIdx.x >> 6;
+  const int64_t per = (T + 3) / 4;
+  for (int64_t i = blockIdx.x; i < groups * per; i += gridDim.x) {
+    const int64_t G = i / per;
+    const int t = (int)(i - G * per) * 4 + sub;
+    if (t >= T) continue;
+    const int b = 4 * t + g;
+    uint32_t w = 0;
+#pragma unroll
+    for (int q = 0; q < 4; ++q) {
+      const int64_t row = G * 64 + 16 * q + m;
+      if (row < rows && b < nb32) w |= (uint32_t)scales[row * nb32 + b] << (8 * q);
+    }
+    *reinterpret_cast<uint32_t*>(out + (G * T + t) * 256 + g * 64 + m * 4) = w;
+  }
+}
+
+// fp32 hidden rows as three bf16 terms a 64 columns: [N][Dp / 64][lo, mid, hi][64], zeros
+// from column D to Dp
+__global__ __launch_bounds__(256) void k_mx4_terms(const char* __restrict__ hidden, int64_t hld,
+                                                   int64_t N, int D, int Dp, char* out) {
+  const int per = Dp / 8;  // pieces of 8 columns
+  const int64_t stride = (int64_t)gridDim.x * 256;
+  for (int64_t i = (int64_t)blockIdx.x * 256 + threadIdx.x; i < N * per; i += stride) {
+    const int64_t n = i / per;
+    const int p = (int)(i - n * per);
+    u32x4_t c[3] = {{0u, 0u, 0u, 0u}, {0u, 0u, 0u, 0u}, {0u, 0u, 0u, 0u}};
+    if (8 * p < D) {
+      const u32x4_t* q = reinterpret_cast<const u32x4_t*>(hidden + n * hld + (int64_t)p * 32);
+      mx4_cut(q[0], q[1], c);
+    }
+    u32x4_t* o = reinterpret_cast<u32x4_t*>(out + n * Dp * 6 + (int64_t)(p >> 3) * 384 + (p & 7) * 16);
+    o[0] = c[2];
+    o[8] = c[1];
+    o[16] = c[0];
+  }
+}
+
+struct Mx4GemmArgs {
+  Mx4Args o;               // N, V, D, codes and the output
+  const char* hidden;      // rows of bf16 (terms), or of codes
+  int64_t hld;             // bytes between them
+  int hbytes;              // bytes of one
+  const uint8_t *wst, *hst;  // scales as tiles (hst: 4-bit hidden rows)
+  int T;                   // 128-column steps of them
+  int TV, TT;              // tiles of 256 rows of W and of 32 NJ hidden rows
+  int per, splits;         // steps of a range of columns; ranges
+  float* part;             // [splits][N][Vp] sums of each, or null with one
+  int64_t Vp;
+};
+
+// One wave-wide 4-byte-per-lane LDS-DMA load (see dma_b128)
+__device__ __forceinline__ void dma_b32(i32x4_t r, uint32_t lds_addr, uint32_t voff) {
+  asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tbuffer_load_dword %1, %2, 0 offen lds"
+               :
+               : "s"(lds_addr), "v"(voff), "s"(r)
+               : "memory");
+}
+
+template <int NJ>
+__device__ __forceinline__ void mx4_tile(const Mx4GemmArgs& a, int& v0, int64_t& n0) {
+  int vt, tt;
+  tile_at(tile_order_xcd(blockIdx.x, a.TV * a.TT), a.TV, a.TT, 4, vt, tt);
+  v0 = vt * 256;
+  n0 = (int64_t)tt * 32 * NJ;
+}
+// acc[i][j] of wave (wv, wt): rows 64 wv + 16 i + 4 g .. + 3 of W, hidden row 16 NJ wt + 16 j + m
+template <int NJ>
+__device__ __forceinline__ void mx4_tile_out(const Mx4GemmArgs& a, int v0, int64_t n0, int wv,
+                                             int wt, const f32x4_t (&acc)[4][NJ]) {
+  const int lane = threadIdx.x & 63, m = lane & 15, g = lane >> 4;
+  Mx4Args o = a.o;
+  if (a.part != nullptr) {
+    o.out = a.part + (int64_t)blockIdx.y * o.N * a.Vp;
+    o.ldo = a.Vp;
+    o.out_bf16 = 0;
+  }
+  const bool wide = mx4_wide(o);
+#pragma unroll
+  for (int j = 0; j < NJ; ++j) {
+    const int64_t n = n0 + 16 * NJ * wt + 16 * j + m;
+    if (n >= o.N) continue;
+#pragma unroll
+    for (int i = 0; i < 4; ++i) mx4_put4(o, n, v0 + 64 * wv + 16 * i + 4 * g, acc[i][j], wide);
+  }
+}
+// MFMA pair q of 2 NJ: row block q / (NJ / 2) of W, two hidden blocks, back and forth
+template <int NJ>
+__device__ __forceinline__ void mx4_pair(int q, int& i, int& j0, int& j1) {
+  i = q / (NJ / 2);
+  const int jj = 2 * (q % (NJ / 2));
+  j0 = (i & 1) ? NJ - 1 - jj : jj;
+  j1 = (i & 1) ? NJ - 2 - jj : jj + 1;
+}
+
+// Tiles of 256 rows of W by 32 NJ hidden rows, bf16 hidden rows (TERMS = 1) or three
+// terms each (3): 8 waves of 64 x 16 NJ. A step is 64 columns (of one term): hidden rows
+// 128 bytes each in three stages, codes 32 bytes a row in two, scales of four steps in
+// two, all by LDS-DMA two steps ahead; one barrier a step. A wave's 4 row blocks of W are
+// decoded in registers between the MFMAs of the half step before their use: a block's
+// codes are read from LDS twice (by two waves) and take an eighth of bf16's bytes, so that
+// the LDS, which bounds the bf16 tiles of the loss, has a quarter of its time left.
+template <int TERMS, int NJ>
+__global__ __launch_bounds__(512, 1) void k_mx4_gemm(Mx4GemmArgs a) {
+  constexpr int TOK = 32 * NJ, HST = TOK * 128, CST = 256 * 32, SST = 2048;
+  constexpr int NPW = NJ / 2, NP = 2 * NJ;
+  __shared__ __attribute__((aligned(16))) char lds[3 * HST + 2 * CST + 2 * SST];
+  char* const lc = lds + 3 * HST;
+  char* const ls = lc + 2 * CST;
+  const int lane = threadIdx.x & 63, wave = wave_id();
+  const int m = lane & 15, g = lane >> 4, wv = wave >> 1, wt = wave & 1;
+  int v0;
+  int64_t n0;
+  mx4_tile<NJ>(a, v0, n0);
+  const int kb = blockIdx.y * a.per;
+  const int ke = min(kb + a.per, ((a.o.D + 63) / 64) * TERMS);
+  const int vrows = min(256, a.o.V - v0), pitch = a.o.D / 2;
+  const int nrows = (int)min((int64_t)TOK, a.o.N - n0);
+  const i32x4_t rh = rsrc_words(a.hidden + n0 * a.hld, (uint32_t)((nrows - 1) * a.hld + a.hbytes));
+  const i32x4_t rc = rsrc_words(a.o.codes + (int64_t)v0 * pitch, (uint32_t)(vrows * pitch));
+  const i32x4_t rs = rsrc_words(a.wst + (int64_t)(v0 / 64) * a.T * 256, (uint32_t)(4 * a.T * 256));
+
+  // hidden rows: instruction i of the wave has rows 8 (NPW wave + i) .. + 7
+  const int hslot = ((lane & 7) ^ (lane >> 3)) << 4;
+  uint32_t hoff[NPW];
+#pragma unroll
+  for (int i = 0; i < NPW; ++i)
+    hoff[i] = (uint32_t)((wave * NPW + i) * 8 + (lane >> 3)) * (uint32_t)a.hld + (uint32_t)hslot;
+  // codes: rows 32 wave .. + 31, the 16-byte halves exchanged for every other 8 rows (the
+  // reads of 16 rows then touch each bank once)
+  const int crow = 32 * wave + (lane >> 1);
+  const uint32_t coff = (uint32_t)crow * (uint32_t)pitch + (((lane & 1) ^ ((crow >> 3) & 1)) << 4);
+  const uint32_t soff = (uint32_t)((wave & 3) * a.T * 256 + lane * 4);
+  auto dma_h = [&](int ks, int stage, int i) {
+    const bool live = ks < ke && ks * 128 + hslot < a.hbytes;
+    dma_b128(rh, __builtin_amdgcn_readfirstlane(lds_addr(lds + stage * HST) + (wave * NPW + i) * 1024),
+             live ? hoff[i] + (uint32_t)ks * 128u : kOobOffset);
+  };
+  auto dma_c = [&](int ks) {
+    dma_b128(rc, __builtin_amdgcn_readfirstlane(lds_addr(lc + (ks & 1) * CST) + wave * 1024),
+             ks < ke ? coff + (uint32_t)(ks / TERMS) * 32u : kOobOffset);
+  };
+  // waves 0..3 the scales of two steps, 4..7 of the next two
+  auto dma_s = [&](int ks) {
+    const int w = ks / TERMS, t = (w >> 1) + (wave >> 2);
+    dma_b32(rs, __builtin_amdgcn_readfirstlane(lds_addr(ls + ((w >> 2) & 1) * SST) + wave * 256),
+            t < a.T ? soff + (uint32_t)t * 256u : kOobOffset);
+  };
+
+  f32x4_t acc[4][NJ];
+#pragma unroll
+  for (int i = 0; i < 4; ++i)
+#pragma unroll
+    for (int j = 0; j < NJ; ++j) acc[i][j] = f32x4_t{0.f, 0.f, 0.f, 0.f};
+
+  // fragment addresses within a stage
+  const int hrd = (16 * NJ * wt + m) * 128, hx = g ^ (m & 7);
+  const int crd = (64 * wv + m) * 32 + 4 * g, cx = (m >> 3) & 1;
+  const int srd = wv * 256 + m * 4;
+  u32x4_t hf[2][NJ], wf[2][4];
+  uint32_t raw[4], sc = 0;
+  auto read_h = [&](const char* st, int s, int f) {
+    return *reinterpret_cast<const u32x4_t*>(st + hrd + f * 2048 + ((hx ^ (4 * s)) << 4));
+  };
+  auto read_c = [&](const char* st, int s, int b) {
+    return *reinterpret_cast<const uint32_t*>(st + crd + b * 512 + ((s ^ cx) << 4));
+  };
+  auto read_s = [&](int ks, int s) {
+    const int w = ks / TERMS;
+    return *reinterpret_cast<const uint32_t*>(ls + ((w >> 2) & 1) * SST + ((w >> 1) & 1) * 1024 +
+                                              srd + (2 * (w & 1) + s) * 64);
+  };
+  auto unpack = [&](int b) {
+    const uint32_t e = b == 3 ? (sc >> 1) & 0x7f800000u : (sc << (23 - 8 * b)) & 0x7f800000u;
+    return mx4_unpack8(raw[b], __builtin_bit_cast(float, e));
+  };
+
+  if (kb < ke) {
+    dma_s(kb);
+#pragma unroll
+    for (int p = 0; p < 2; ++p) {
+#pragma unroll
+      for (int i = 0; i < NPW; ++i) dma_h(kb + p, p, i);
+      dma_c(kb + p);
+    }
+    KD_VMCNT(NPW + 1);
+    __syncthreads();
+#pragma unroll
+    for (int f = 0; f < NJ; ++f) hf[0][f] = read_h(lds, 0, f);
+    sc = read_s(kb, 0);
+#pragma unroll
+    for (int b = 0; b < 4; ++b) raw[b] = read_c(lc + (kb & 1) * CST, 0, b);
+#pragma unroll
+    for (int b = 0; b < 4; ++b) wf[0][b] = unpack(b);
+    // MFMAs of half x, reads of the other half y (half s of step kr) between them
+    constexpr int U0 = NP == 16 ? 8 : 4, US = NP == 16 ? 2 : 1, H0 = NP == 16 ? 4 : 2;
+    auto half = [&](int q, int x, const char* hst, int kr, int s) {
+      const int y = x ^ 1;
+      int i, j0, j1;
+      mx4_pair<NJ>(q, i, j0, j1);
+      acc[i][j0] = mfma_slot(wf[x][i], hf[x][j0], acc[i][j0], (__bf16*)nullptr);
+      acc[i][j1] = mfma_slot(wf[x][i], hf[x][j1], acc[i][j1], (__bf16*)nullptr);
+      if (q == 0) sc = read_s(kr, s);
+      if (q < 4) raw[q] = read_c(lc + (kr & 1) * CST, s, q);
+      if (q >= H0 && q < H0 + NJ) hf[y][q - H0] = read_h(hst, s, q - H0);
+      if (q >= U0 && (q - U0) % US == 0) wf[y][(q - U0) / US] = unpack((q - U0) / US);
+      __builtin_amdgcn_sched_barrier(0);
+    };
+    int ca = 0;  // stage of step j's hidden rows
+    for (int j = kb; j < ke; ++j) {
+      const int na = ca == 2 ? 0 : ca + 1, pa = ca == 0 ? 2 : ca - 1;
+      if ((j + 2) % TERMS == 0 && (((j + 2) / TERMS) & 3) == 0) dma_s(j + 2);
+#pragma unroll
+      for (int q = 0; q < NP; ++q) {
+        if (q % 4 == 3) dma_h(j + 2, pa, q / 4);
+        half(q, 0, lds + ca * HST, j, 1);
+      }
+      __builtin_amdgcn_s_waitcnt(0xc07f & ~0x0f00);  // lgkmcnt(0)
+      KD_VMCNT(NPW);  // step j + 1 landed; step j + 2's hidden rows may still fly
+      __syncthreads();
+      __builtin_amdgcn_s_setprio(1);
+#pragma unroll
+      for (int q = 0; q < NP; ++q) {
+        if (q == 0) dma_c(j + 2);
+        half(q, 1, lds + na * HST, j + 1, 0);
+      }
+      __builtin_amdgcn_s_setprio(0);
+      ca = na;
+    }
+    KD_VMCNT(0);
+    __syncthreads();
+  }
+  mx4_tile_out<NJ>(a, v0, n0, wv, wt, acc);
+}
+
+template <int OA, int OB>
+__device__ __forceinline__ f32x4_t mfma_mx4_sel(const i32x8_t& x, const i32x8_t& y, f32x4_t c, int sa,
+                                                int sb) {
+  return __builtin_amdgcn_mfma_scale_f32_16x16x128_f8f6f4(x, y, c, 4, 4, OA, sa, OB, sb);
+}
+// one 16x16x128 step with the scales in byte ia of sa and ib of sb (constants once
+// unrolled)
+__device__ __forceinline__ f32x4_t mfma_mx4_at(u32x4_t a, u32x4_t b, f32x4_t c, int ia, uint32_t sa,
+                                               int ib, uint32_t sb) {
+  const i32x8_t x = {(int)a[0], (int)a[1], (int)a[2], (int)a[3], 0, 0, 0, 0};
+  const i32x8_t y = {(int)b[0], (int)b[1], (int)b[2], (int)b[3], 0, 0, 0, 0};
+  const int p = (int)sa, r = (int)sb;
+  switch (4 * ia + ib) {
+    case 0: return mfma_mx4_sel<0, 0>(x, y, c, p, r);
+    case 1: return mfma_mx4_sel<0, 1>(x, y, c, p, r);
+    case 2: return mfma_mx4_sel<0, 2>(x, y, c, p, r);
+    case 3: return mfma_mx4_sel<0, 3>(x, y, c, p, r);
+    case 4: return mfma_mx4_sel<1, 0>(x, y, c, p, r);
+    case 5: return mfma_mx4_sel<1, 1>(x, y, c, p, r);
+    case 6: return mfma_mx4_sel<1, 2>(x, y, c, p, r);
+    case 7: return mfma_mx4_sel<1, 3>(x, y, c, p, r);
+    case 8: return mfma_mx4_sel<2, 0>(x, y, c, p, r);
+    case 9: return mfma_mx4_sel<2, 1>(x, y, c, p, r);
+    case 10: return mfma_mx4_sel<2, 2>(x, y, c, p, r);
+    case 11: return mfma_mx4_sel<2, 3>(x, y, c, p, r);
+    case 12: return mfma_mx4_sel<3, 0>(x, y, c, p, r);
+    case 13: return mfma_mx4_sel<3, 1>(x, y, c, p, r);
+    case 14: return mfma_mx4_sel<3, 2>(x, y, c, p, r);
+    default: return mfma_mx4_sel<3, 3>(x, y, c, p, r);
+  }
+}
+
+// The same tiles with 4-bit hidden rows: a step is 128 columns, 64 bytes a row of codes
+// and one scaled MFMA a block pair, in four stages by LDS-DMA: a step's loads are issued
+// four steps ahead (three before their reads), into the stage whose fragments were
+// read in the step before. Fragments are read a step ahead of their MFMAs. One barrier
+// a step.
+template <int NJ>
+__global__ __launch_bounds__(512, 1) void k_mx4_gemm4(Mx4GemmArgs a) {
+  constexpr int TOK = 32 * NJ, HST = TOK * 64, CST = 256 * 64, SST = 2048;
+  constexpr int NH = NJ / 4, NI = 2 + NH + 1, NP = 2 * NJ, NS = 4;
+  __shared__ __attribute__((aligned(16))) char lds[NS * (HST + CST + SST)];
+  char* const lc = lds + NS * HST;
+  char* const ls = lc + NS * CST;
+  const int lane = threadIdx.x & 63, wave = wave_id();
+  const int m = lane & 15, g = lane >> 4, wv = wave >> 1, wt = wave & 1;
+  int v0;
+  int64_t n0;
+  mx4_tile<NJ>(a, v0, n0);
+  const int kb = blockIdx.y * a.per;
+  const int ke = min(kb + a.per, (a.o.D + 127) / 128);
+  const int vrows = min(256, a.o.V - v0), pitch = a.o.D / 2;
+  const int nrows = (int)min((int64_t)TOK, a.o.N - n0);
+  const i32x4_t rh = rsrc_words(a.hidden + n0 * pitch, (uint32_t)(nrows * pitch));
+  const i32x4_t rc = rsrc_words(a.o.codes + (int64_t)v0 * pitch, (uint32_t)(vrows * pitch));
+  // scales: waves 0..3 a group of 64 rows of W each, 4..7 one of hidden rows
+  const bool sh_wave = wave >= 4;
+  const int sgroup = sh_wave ? (wave & 3) % (TOK / 64) : wave;
+  const i32x4_t rs =
+      rsrc_words((sh_wave ? a.hst + (n0 / 64) * a.T * 256 : a.wst + (int64_t)(v0 / 64) * a.T * 256) +
+                     (int64_t)sgroup * a.T * 256,
+                 (uint32_t)(a.T * 256));
+  // rows of 64 bytes: slots XORed with (row / 2) % 4, which leaves 8 lanes of a read
+  // (8 rows, one slot) in 8 different 16-byte columns
+  const int lrow = lane >> 2, slot = ((lane & 3) ^ ((lrow >> 1) & 3)) << 4;
+  uint32_t hoff[NH], coff[2];
+#pragma unroll
+  for (int i = 0; i < NH; ++i)
+    hoff[i] = (uint32_t)((wave * NH + i) * 16 + lrow) * (uint32_t)pitch + (uint32_t)slot;
+#pragma unroll
+  for (int i = 0; i < 2; ++i)
+    coff[i] = (uint32_t)((wave * 2 + i) * 16 + lrow) * (uint32_t)pitch + (uint32_t)slot;
+  // instruction i of step ks
+  auto dma = [&](int ks, int i) {
+    const int st = ks & (NS - 1);
+    const bool live = ks < ke;
+    if (i < 2)
+      dma_b128(rc, __builtin_amdgcn_readfirstlane(lds_addr(lc + st * CST) + (wave * 2 + i) * 1024),
+               live ? coff[i] + (uint32_t)ks * 64u : kOobOffset);
+    else if (i < 2 + NH)
+      dma_b128(rh, __builtin_amdgcn_readfirstlane(lds_addr(lds + st * HST) + (wave * NH + i - 2) * 1024),
+               live ? hoff[i - 2] + (uint32_t)ks * 64u : kOobOffset);
+    else
+      dma_b32(rs, __builtin_amdgcn_readfirstlane(lds_addr(ls + st * SST) + wave * 256),
+              live ? (uint32_t)(ks * 256 + lane * 4) : kOobOffset);
+  };
+  f32x4_t acc[4][NJ];
+#pragma unroll
+  for (int i = 0; i < 4; ++i)
+#pragma unroll
+    for (int j = 0; j < NJ; ++j) acc[i][j] = f32x4_t{0.f, 0.f, 0.f, 0.f};
+  const int fx = (g ^ ((m >> 1) & 3)) << 4;
+  const int hrd = (16 * NJ * wt + m) * 64 + fx, crd = (64 * wv + m) * 64 + fx;
+  u32x4_t hf[2][NJ], wf[2][4];
+  uint32_t sw[2], sh[2][NJ / 4];
+  // read number f of step ks into set x
+  constexpr int NR = 1 + NJ / 4 + 4 + NJ;
+  auto read = [&](int ks, int x, int f) {
+    const int st = ks & (NS - 1);
+    if (f == 0)
+      sw[x] = *reinterpret_cast<const uint32_t*>(ls + st * SST + wv * 256 + lane * 4);
+    else if (f < 1 + NJ / 4)
+      sh[x][f - 1] = *reinterpret_cast<const uint32_t*>(
+          ls + st * SST + 1024 + ((wt * NJ / 4) + f - 1) * 256 + lane * 4);
+    else if (f < 5 + NJ / 4)
+      wf[x][f - 1 - NJ / 4] =
+          *reinterpret_cast<const u32x4_t*>(lc + st * CST + crd + (f - 1 - NJ / 4) * 1024);
+    else
+      hf[x][f - 5 - NJ / 4] =
+          *reinterpret_cast<const u32x4_t*>(lds + st * HST + hrd + (f - 5 - NJ / 4) * 1024);
+  };
+  if (kb < ke) {
+#pragma unroll
+    for (int p = 0; p < NS; ++p)
+#pragma unroll
+      for (int i = 0; i < NI; ++i) dma(kb + p, i);
+    KD_VMCNT(2 * NI);
+    __syncthreads();
+#pragma unroll
+    for (int f = 0; f < NR; ++f) read(kb, 0, f);
+    __builtin_amdgcn_s_waitcnt(0xc07f & ~0x0f00);  // lgkmcnt(0)
+    __syncthreads();
+    auto step = [&](int ks, int x) {
+#pragma unroll
+      for (int q = 0; q < NP; ++q) {
+        if (q % (NP / 8) == 0 && q / (NP / 8) < NI) dma(ks + NS, q / (NP / 8));
+        int i, j0, j1;
+        mx4_pair<NJ>(q, i, j0, j1);
+        acc[i][j0] = mfma_mx4_at(wf[x][i], hf[x][j0], acc[i][j0], i, sw[x], j0 & 3, sh[x][j0 >> 2]);
+        acc[i][j1] = mfma_mx4_at(wf[x][i], hf[x][j1], acc[i][j1], i, sw[x], j1 & 3, sh[x][j1 >> 2]);
+#pragma unroll
+        for (int f = 0; f < NR; ++f)
+          if (f * NP / NR == q) read(ks + 1, x ^ 1, f);
+        __builtin_amdgcn_sched_barrier(0);
+      }
+      __builtin_amdgcn_s_waitcnt(0xc07f & ~0x0f00);  // lgkmcnt(0)
+      KD_VMCNT(2 * NI);  // step ks + 2 landed
+      __syncthreads();
+    };
+    for (int ks = kb; ks < ke; ks += 2) {
+      step(ks, 0);
+      if (ks + 1 < ke) step(ks + 1, 1);
+    }
+    KD_VMCNT(0);
+    __syncthreads();
+  }
+  mx4_tile_out<NJ>(a, v0, n0, wv, wt, acc);
+}
+
+// out = the ranges' sums, in order
+__global__ __launch_bounds__(256) void k_mx4_join(const float* __restrict__ part, int splits,
+                                                  int64_t N, int64_t V, int64_t Vp, void* out,
+                                                  int64_t ldo, int out_bf16) {
+  const int64_t per = Vp / 4, stride = (int64_t)gridDim.x * 256;
+  Mx4Args o{};
+  o.out = out;
+  o.ldo = ldo;
+  o.V = (int)V;
+  o.out_bf16 = out_bf16;
+  const bool wide = mx4_wide(o);
+  for (int64_t i = (int64_t)blockIdx.x * 256 + threadIdx.x; i < N * per; i += stride) {
+    const int64_t n = i / per;
+    f32x4_t z = {0.f, 0.f, 0.f, 0.f};
+    for (int k = 0; k < splits; ++k)
+      z += reinterpret_cast<const f32x4_t*>(part)[(int64_t)k * N * per + i];
+    mx4_put4(o, n, (int)(i - n * per) * 4, z, wide);
+  }
+}
+
 }  // namespace kd
 
 using namespace kd;
@@ -523,6 +942,60 @@ static int launch_mx4_wide(const Mx4Args& a, hipStream_t s) {
   return (int)hipGetLastError();
 }
 
+static int launch_mx4_scale_tiles(const uint8_t* scales, int64_t rows, int64_t D, uint8_t* out,
+                                  hipStream_t s) {
+  const int64_t T = mx4_tile_steps(D), groups = mx4_tile_groups(rows);
+  const int64_t blocks = groups * ((T + 3) / 4);
+  hipLaunchKernelGGL(k_mx4_scale_tiles, dim3((unsigned)(blocks < 32768 ? blocks : 32768)), dim3(256),
+                     0, s, scales, rows, (int)(D / kMx4Block), (int)T, groups, out);
+  return (int)hipGetLastError();
+}
+
+template <int H>
+static int launch_mx4_gemm(const KdMx4Args& q, const Mx4Args& o, hipStream_t s) {
+  const KdMx4Plan p = kd_mx4_plan(q.N, q.D, q.V, q.dtype);
+  Mx4GemmArgs a{};
+  a.o = o;
+  a.wst = reinterpret_cast<uint8_t*>(q.ws + p.off_wst);
+  a.T = (int)mx4_tile_steps(q.D);
+  a.TV = (int)((q.V + 255) / 256);
+  a.TT = (int)((q.N + p.tok - 1) / p.tok);
+  a.per = p.per;
+  a.splits = p.splits;
+  a.Vp = (q.V + 3) / 4 * 4;
+  a.part = p.splits > 1 ? reinterpret_cast<float*>(q.ws + p.off_part) : nullptr;
+  if (launch_mx4_scale_tiles(q.scales, q.V, q.D, const_cast<uint8_t*>(a.wst), s) != 0) return 1;
+  a.hidden = static_cast<const char*>(q.hidden);
+  a.hld = o.hld;
+  a.hbytes = (int)(H == 2 ? q.D / 2 : q.D * 2);
+  if (H == 1) {
+    const int64_t Dp = (q.D + 63) / 64 * 64;
+    char* t = q.ws + p.off_hidden;
+    hipLaunchKernelGGL(k_mx4_terms, dim3(mx4_blocks(q.N * Dp / 8)), dim3(256), 0, s, a.hidden, o.hld,
+                       q.N, (int)q.D, (int)Dp, t);
+    a.hidden = t;
+    a.hld = Dp * 6;
+    a.hbytes = (int)(Dp * 6);
+  }
+  if (H == 2) {
+    a.hst = reinterpret_cast<uint8_t*>(q.ws + p.off_hidden);
+    if (launch_mx4_scale_tiles(q.hscales, q.N, q.D, const_cast<uint8_t*>(a.hst), s) != 0) return 1;
+  }
+  const dim3 grid((unsigned)(a.TV * a.TT), (unsigned)p.splits), block(512);
+  if constexpr (H == 2) {
+    if (p.tok == 256) hipLaunchKernelGGL((k_mx4_gemm4<8>), grid, block, 0, s, a);
+    else hipLaunchKernelGGL((k_mx4_gemm4<4>), grid, block, 0, s, a);
+  } else {
+    constexpr int TERMS = H == 1 ? 3 : 1;
+    if (p.tok == 256) hipLaunchKernelGGL((k_mx4_gemm<TERMS, 8>), grid, block, 0, s, a);
+    else hipLaunchKernelGGL((k_mx4_gemm<TERMS, 4>), grid, block, 0, s, a);
+  }
+  if (p.splits > 1)
+    hipLaunchKernelGGL(k_mx4_join, dim3(mx4_blocks(q.N * a.Vp / 4)), dim3(256), 0, s, a.part, p.splits,
+                       q.N, q.V, a.Vp, q.out, q.ld_out, o.out_bf16);
+  return (int)hipGetLastError();
+}
+
 template <int H>
 static int launch_mx4_logits(const KdMx4Args& q, hipStream_t s) {
   Mx4Args a{};
@@ -537,21 +1010,22 @@ static int launch_mx4_logits(const KdMx4Args& q, hipStream_t s) {
   a.D = (int)q.D;
   a.V = (int)q.V;
   a.out_bf16 = q.out_dtype == 1;
-  if (q.N <= 16) {
+  // (tile rows reach by 32-bit offsets)
+  if (kd_mx4_tiles(q.N) && 256 * a.hld < ((int64_t)1 << 31)) return launch_mx4_gemm<H>(q, a, s);
+  if (q.N <= 16 && q.V <= (H == 1 || q.N > 4 ? 24576 : 49152)) {
     const int units = (a.D / kMx4Block + 7) / 8;
     int ks = 1;
-    while (ks < 4 && ks < units) ks *= 2;
-    if (a.V <= 16384) return launch_mx4_rows<H, 1>(a, ks, s);
+    while (ks < (a.V <= 16384 ? 8 : 4) && ks < units) ks *= 2;
+    if (a.V <= 6144) return launch_mx4_rows<H, 1>(a, ks, s);
     return launch_mx4_rows<H, 2>(a, ks, s);
   }
-  // rows of W a wave: as many as leave a workgroup for each compute unit
-  constexpr int R4 = H == 1 ? 2 : 4;
-  if (q.N <= 32) {
-    if (a.V > 32768) return launch_mx4_wide<H, 2, R4>(a, s);
-    return launch_mx4_wide<H, 2, 1>(a, s);
-  }
-  if (a.V > 65536) return launch_mx4_wide<H, 4, R4>(a, s);
-  if (a.V > 32768) return launch_mx4_wide<H, 4, 2>(a, s);
+  // rows of W a wave (16 R): as few as leave every compute unit a workgroup
+  const int R = a.V <= 49152 ? 1 : 2;
+  if (q.N <= 16) return R == 1 ? launch_mx4_wide<H, 1, 1>(a, s) : launch_mx4_wide<H, 1, 2>(a, s);
+  if (q.N <= 32) return R == 1 ? launch_mx4_wide<H, 2, 1>(a, s) : launch_mx4_wide<H, 2, 2>(a, s);
+  if (a.V > 98304) return launch_mx4_wide<H, 4, 4>(a, s);
+  if constexpr (H != 2)
+    if (R == 2) return launch_mx4_wide<H, 4, 2>(a, s);
   return launch_mx4_wide<H, 4, 1>(a, s);
 }
 

@@ -69,8 +69,17 @@ struct KdVerifyArgs {
   double* norm;             // [B, 4] dense draft: M, S of the target's and the draft's row
 };
 
-// Bytes of workspace of a product of N hidden rows with a head of V rows
-constexpr size_t kd_mx4_workspace(int64_t, int64_t, int64_t, int) { return 256; }
+// Products of 65 hidden rows and more run in tiles of 256 rows of the head by `tok`
+// hidden rows, each over `per` steps of columns (64 a step, of each of three terms with
+// fp32 hidden rows; 128 with 4-bit ones); with splits > 1 the ranges' fp32 sums are
+// joined afterwards. Workspace: the head's scales, and the hidden rows' terms or scales, as
+// the tiles take them, and the ranges' sums.
+struct KdMx4Plan {
+  int tok, per, splits;
+  size_t off_wst, off_hidden, off_part, total;
+};
+inline bool kd_mx4_tiles(int64_t N) { return N > 64; }
+KdMx4Plan kd_mx4_plan(int64_t N, int64_t D, int64_t V, int dtype);
 
 struct KdMx4Args {
   const void* hidden;       // [N, ld_hidden], or [N, D / 2] codes
@@ -78,7 +87,7 @@ struct KdMx4Args {
   const uint8_t* codes;     // [V, D / 2]
   const uint8_t* scales;    // [V, D / 32]
   void* out;                // [N, ld_out]
-  char* ws;                 // kd_mx4_workspace bytes
+  char* ws;                 // kd_mx4_plan's bytes
   int64_t N, D, V, ld_hidden, ld_out;
   int dtype, out_dtype;     // of the hidden rows (2 = 4 bits) and the output
 };

@@ -157,6 +157,36 @@ DraftPlan draft_plan(const kd_draft* p) {
 
 }  // namespace
 
+KdMx4Plan kd_mx4_plan(int64_t N, int64_t D, int64_t V, int dtype) {
+  KdMx4Plan p{};
+  p.splits = 1;
+  p.total = 256;
+  if (!kd_mx4_tiles(N)) return p;
+  const int64_t tv = (V + 255) / 256;
+  // tiles of 128 hidden rows take 0.6 of the time of one of 256
+  p.tok = (N + 255) / 256 * 10 <= (N + 127) / 128 * 6 ? 256 : 128;
+  const int64_t tiles = tv * ((N + p.tok - 1) / p.tok);
+  // a range is a multiple of 4 steps (of every term), the scales' loads
+  const int64_t unit = dtype == KD_F32 ? 12 : 4;
+  const int64_t steps = dtype == KD_MX4 ? (D + 127) / 128 : (D + 63) / 64 * (unit / 4);
+  const int64_t units = (steps + unit - 1) / unit;
+  int64_t splits = 1;
+  if (tiles <= 128) splits = std::max<int64_t>(1, std::min<int64_t>(256 / tiles, units));
+  const int64_t per = (units + splits - 1) / splits;
+  p.per = (int)(per * unit);
+  p.splits = (int)((units + per - 1) / per);
+  const int64_t T = (D / 32 + 7) / 8 * 2;
+  p.off_wst = 0;
+  p.off_hidden = align256((size_t)(tv * 4 * T * 256));
+  size_t h = 0;
+  if (dtype == KD_F32) h = (size_t)N * (size_t)((D + 63) / 64 * 64) * 6;
+  if (dtype == KD_MX4) h = (size_t)((N + 255) / 256 * 4 * T) * 256;
+  p.off_part = align256(p.off_hidden + h);
+  p.total = p.off_part;
+  if (p.splits > 1) p.total += align256((size_t)p.splits * N * ((V + 3) / 4 * 4) * 4);
+  return p;
+}
+
 extern "C" {
 
 kd_status kd_topk_entries_workspace_size(const kd_rows* p, size_t* bytes) {
@@ -301,7 +331,7 @@ kd_status kd_mx4_logits_workspace_size(const kd_mx4_head* p, size_t* bytes) {
   if (p == nullptr || bytes == nullptr) return KD_ERR_NULL_PTR;
   const kd_status st = check_head(p);
   if (st != KD_OK) return st;
-  *bytes = kd_mx4_workspace(p->N, p->D, p->V, p->dtype);
+  *bytes = kd_mx4_plan(p->N, p->D, p->V, p->dtype).total;
   return KD_OK;
 }
 
@@ -318,7 +348,7 @@ kd_status kd_mx4_logits(const kd_mx4_head* p, const void* hidden, const uint8_t*
   if (!aligned(hidden, 16) || !aligned(codes, 16) || !aligned(workspace, 16) ||
       !aligned(out, elem_bytes(p->out_dtype)))
     return KD_ERR_UNSUPPORTED;
-  if (workspace_bytes < kd_mx4_workspace(p->N, p->D, p->V, p->dtype))
+  if (workspace_bytes < kd_mx4_plan(p->N, p->D, p->V, p->dtype).total)
     return KD_ERR_WORKSPACE_TOO_SMALL;
   if (p->N == 0) return KD_OK;
   KdMx4Args a{};
