@@ -470,24 +470,41 @@ __host__ __device__ constexpr int64_t mx4_tile_steps(int64_t D) {  // of 128 col
 }
 __host__ __device__ constexpr int64_t mx4_tile_groups(int64_t rows) { return (rows + 255) / 256 * 4; }
 
-// a thread per dword: blockIdx.x over 16 steps of a group of rows, blockIdx.y + group0
+// A workgroup per 64 rows and 32 steps, which pass through LDS: reads of 128 bytes of
+// each row, writes of 256 (dword by dword, 16 bytes of a row at a time, 131072 x 128 took 38
+// us).
+constexpr int kMx4TileSteps = 32;
 __global__ __launch_bounds__(256) void k_mx4_scale_tiles(const uint8_t* __restrict__ scales,
                                                          int64_t rows, int nb32, int T,
-                                                         int64_t groups, uint8_t* out) {
-  const int m = threadIdx.x & 15, g = (threadIdx.x >> 4) & 3, sub = threadIdx.x >> 6;
-  const int64_t per = (T + 3) / 4;
-  for (int64_t i = blockIdx.x; i < groups * per; i += gridDim.x) {
-    const int64_t G = i / per;
-    const int t = (int)(i - G * per) * 4 + sub;
-    if (t >= T) continue;
-    const int b = 4 * t + g;
+                                                         uint8_t* __restrict__ out) {
+  constexpr int LD = 4 * kMx4TileSteps + 4;  // bytes of a row in LDS
+  __shared__ __attribute__((aligned(4))) uint8_t lds[64 * LD];
+  const int per = (T + kMx4TileSteps - 1) / kMx4TileSteps;
+  const int64_t G = blockIdx.x / per;
+  const int t0 = (int)(blockIdx.x - G * per) * kMx4TileSteps, b0 = 4 * t0;
+  // 4 bytes a thread: 32 threads a row
+  const int c = (threadIdx.x & 31) * 4;
+  for (int r = threadIdx.x >> 5; r < 64; r += 8) {
+    const int64_t row = G * 64 + r;
+    uint32_t w = 0;
+    if (row < rows) {
+      const uint8_t* p = scales + row * nb32 + b0 + c;
+      if (b0 + c + 4 <= nb32) {
+        __builtin_memcpy(&w, p, 4);
+      } else {
+        for (int i = 0; i < 4; ++i)
+          if (b0 + c + i < nb32) w |= (uint32_t)p[i] << (8 * i);
+      }
+    }
+    *reinterpret_cast<uint32_t*>(lds + r * LD + c) = w;
+  }
+  __syncthreads();
+  const int m = threadIdx.x & 15, g = (threadIdx.x >> 4) & 3;
+  for (int t = threadIdx.x >> 6; t < kMx4TileSteps && t0 + t < T; t += 4) {
     uint32_t w = 0;
 #pragma unroll
-    for (int q = 0; q < 4; ++q) {
-      const int64_t row = G * 64 + 16 * q + m;
-      if (row < rows && b < nb32) w |= (uint32_t)scales[row * nb32 + b] << (8 * q);
-    }
-    *reinterpret_cast<uint32_t*>(out + (G * T + t) * 256 + g * 64 + m * 4) = w;
+    for (int q = 0; q < 4; ++q) w |= (uint32_t)lds[(16 * q + m) * LD + 4 * t + g] << (8 * q);
+    *reinterpret_cast<uint32_t*>(out + (G * T + t0 + t) * 256 + g * 64 + m * 4) = w;
   }
 }
 
@@ -540,25 +557,74 @@ __device__ __forceinline__ void mx4_tile(const Mx4GemmArgs& a, int& v0, int64_t&
   v0 = vt * 256;
   n0 = (int64_t)tt * 32 * NJ;
 }
-// acc[i][j] of wave (wv, wt): rows 64 wv + 16 i + 4 g .. + 3 of W, hidden row 16 NJ wt + 16 j + m
+// acc[i][j] of wave (wv, wt): rows 64 wv + 16 i + 4 g .. + 3 of W, hidden row 16 NJ wt + 16 j + m.
+// By way of LDS (8 KiB a wave, after the main loop's last barrier): a pass turns 64 (bf16)
+// or 32 (fp32) hidden rows of 64 logits into whole 128-byte lines. Stored from the
+// accumulators, 32 or 64 bytes of a row at a time, the tiles' stores took 0.34 (bf16 hidden
+// rows) and 0.50 ms of 4096 x 4096 x 131072.
+__device__ __forceinline__ void mx4_wave_sync() {
+  __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
+  __builtin_amdgcn_wave_barrier();
+}
+template <int NJ, bool BF16>
+__device__ __forceinline__ void mx4_lines(const Mx4Args& o, int v, int64_t n0, char* st,
+                                          const f32x4_t (&acc)[4][NJ]) {
+  constexpr int JP = BF16 ? 4 : 2, RB = BF16 ? 128 : 256;   // blocks of a pass, bytes of a row
+  constexpr int SL = RB / 16, EB = BF16 ? 2 : 4, EV = 16 / EB;
+  const int lane = threadIdx.x & 63, m = lane & 15, g = lane >> 4;
+  const bool wide = ((reinterpret_cast<uintptr_t>(o.out) | ((uintptr_t)o.ldo * EB)) & 15) == 0;
+#pragma unroll
+  for (int p = 0; p < NJ / JP; ++p) {
+#pragma unroll
+    for (int j = 0; j < JP; ++j) {
+      const int t = 16 * j + m;
+#pragma unroll
+      for (int i = 0; i < 4; ++i) {
+        const f32x4_t z = acc[i][p * JP + j];
+        if constexpr (BF16)
+          *reinterpret_cast<u32x2_t*>(st + t * RB + (((2 * i + (g >> 1)) ^ (t & 7)) << 4) + 8 * (g & 1)) =
+              u32x2_t{pack_bf16x2(z[0], z[1]), pack_bf16x2(z[2], z[3])};
+        else
+          *reinterpret_cast<f32x4_t*>(st + t * RB + (((4 * i + g) ^ (t & 15)) << 4)) = z;
+      }
+    }
+    mx4_wave_sync();
+#pragma unroll
+    for (int q = 0; q < 8; ++q) {
+      const int t = q * (64 / SL) + lane / SL, c = lane % SL;
+      const int64_t n = n0 + 16 * JP * p + t;
+      const u32x4_t x = *reinterpret_cast<const u32x4_t*>(st + t * RB + ((c ^ (t & (SL - 1))) << 4));
+      const int vv = v + c * EV;
+      if (n >= o.N || vv >= o.V) continue;
+      char* dst = static_cast<char*>(o.out) + (n * o.ldo + vv) * EB;
+      if (wide && vv + EV <= o.V) {
+        *reinterpret_cast<u32x4_t*>(dst) = x;
+      } else {
+#pragma unroll
+        for (int e = 0; e < EV; ++e) {
+          if (vv + e >= o.V) break;
+          if constexpr (BF16)
+            reinterpret_cast<uint16_t*>(dst)[e] = (uint16_t)(x[e >> 1] >> (16 * (e & 1)));
+          else
+            reinterpret_cast<uint32_t*>(dst)[e] = x[e];
+        }
+      }
+    }
+    mx4_wave_sync();
+  }
+}
 template <int NJ>
 __device__ __forceinline__ void mx4_tile_out(const Mx4GemmArgs& a, int v0, int64_t n0, int wv,
-                                             int wt, const f32x4_t (&acc)[4][NJ]) {
-  const int lane = threadIdx.x & 63, m = lane & 15, g = lane >> 4;
+                                             int wt, char* lds, const f32x4_t (&acc)[4][NJ]) {
   Mx4Args o = a.o;
   if (a.part != nullptr) {
     o.out = a.part + (int64_t)blockIdx.y * o.N * a.Vp;
     o.ldo = a.Vp;
     o.out_bf16 = 0;
   }
-  const bool wide = mx4_wide(o);
-#pragma unroll
-  for (int j = 0; j < NJ; ++j) {
-    const int64_t n = n0 + 16 * NJ * wt + 16 * j + m;
-    if (n >= o.N) continue;
-#pragma unroll
-    for (int i = 0; i < 4; ++i) mx4_put4(o, n, v0 + 64 * wv + 16 * i + 4 * g, acc[i][j], wide);
-  }
+  char* st = lds + wave_id() * 8192;
+  if (o.out_bf16) mx4_lines<NJ, true>(o, v0 + 64 * wv, n0 + 16 * NJ * wt, st, acc);
+  else mx4_lines<NJ, false>(o, v0 + 64 * wv, n0 + 16 * NJ * wt, st, acc);
 }
 // MFMA pair q of 2 NJ: row block q / (NJ / 2) of W, two hidden blocks, back and forth
 template <int NJ>
@@ -706,7 +772,7 @@ __global__ __launch_bounds__(512, 1) void k_mx4_gemm(Mx4GemmArgs a) {
     KD_VMCNT(0);
     __syncthreads();
   }
-  mx4_tile_out<NJ>(a, v0, n0, wv, wt, acc);
+  mx4_tile_out<NJ>(a, v0, n0, wv, wt, lds, acc);
 }
 
 template <int OA, int OB>
@@ -855,7 +921,7 @@ __global__ __launch_bounds__(512, 1) void k_mx4_gemm4(Mx4GemmArgs a) {
     KD_VMCNT(0);
     __syncthreads();
   }
-  mx4_tile_out<NJ>(a, v0, n0, wv, wt, acc);
+  mx4_tile_out<NJ>(a, v0, n0, wv, wt, lds, acc);
 }
 
 // out = the ranges' sums, in order
@@ -945,9 +1011,9 @@ static int launch_mx4_wide(const Mx4Args& a, hipStream_t s) {
 static int launch_mx4_scale_tiles(const uint8_t* scales, int64_t rows, int64_t D, uint8_t* out,
                                   hipStream_t s) {
   const int64_t T = mx4_tile_steps(D), groups = mx4_tile_groups(rows);
-  const int64_t blocks = groups * ((T + 3) / 4);
-  hipLaunchKernelGGL(k_mx4_scale_tiles, dim3((unsigned)(blocks < 32768 ? blocks : 32768)), dim3(256),
-                     0, s, scales, rows, (int)(D / kMx4Block), (int)T, groups, out);
+  const int64_t blocks = groups * ((T + kMx4TileSteps - 1) / kMx4TileSteps);
+  hipLaunchKernelGGL(k_mx4_scale_tiles, dim3((unsigned)blocks), dim3(256), 0, s, scales, rows,
+                     (int)(D / kMx4Block), (int)T, out);
   return (int)hipGetLastError();
 }
 
