@@ -537,7 +537,7 @@ struct Mx4GemmArgs {
   const uint8_t *wst, *hst;  // scales as tiles (hst: 4-bit hidden rows)
   int T;                   // 128-column steps of them
   int TV, TT;              // tiles of 256 rows of W and of 32 NJ hidden rows
-  int per, splits;         // steps of a range of columns; ranges
+  int per, splits;         // 64-column steps (256 with 4-bit hidden rows) of a range; ranges
   float* part;             // [splits][N][Vp] sums of each, or null with one
   int64_t Vp;
 };
@@ -807,116 +807,119 @@ __device__ __forceinline__ f32x4_t mfma_mx4_at(u32x4_t a, u32x4_t b, f32x4_t c, 
   }
 }
 
-// The same tiles with 4-bit hidden rows: a step is 128 columns, 64 bytes a row of codes
-// and one scaled MFMA a block pair, in four stages by LDS-DMA: a step's loads are issued
-// four steps ahead (three before their reads), into the stage whose fragments were
-// read in the step before. Fragments are read a step ahead of their MFMAs. One barrier
-// a step.
+// The same tiles with 4-bit hidden rows: a step is 256 columns, 128 bytes a row of codes in
+// two stages by LDS-DMA, two scaled MFMAs a block pair. The second half of a step
+// issues the loads of the step after the next, into the stage whose last
+// fragments were read in its first half; the barrier between the halves waits for
+// those of the next step.
 template <int NJ>
 __global__ __launch_bounds__(512, 1) void k_mx4_gemm4(Mx4GemmArgs a) {
-  constexpr int TOK = 32 * NJ, HST = TOK * 64, CST = 256 * 64, SST = 2048;
-  constexpr int NH = NJ / 4, NI = 2 + NH + 1, NP = 2 * NJ, NS = 4;
-  __shared__ __attribute__((aligned(16))) char lds[NS * (HST + CST + SST)];
-  char* const lc = lds + NS * HST;
-  char* const ls = lc + NS * CST;
+  constexpr int TOK = 32 * NJ, HST = TOK * 128, CST = 256 * 128, SST = 8192;
+  constexpr int NH = NJ / 2, NC = 4, NI = NC + NH + 1, NP = 2 * NJ;
+  __shared__ __attribute__((aligned(16))) char lds[2 * (HST + CST + SST)];
+  char* const lc = lds + 2 * HST;
+  char* const ls = lc + 2 * CST;
   const int lane = threadIdx.x & 63, wave = wave_id();
   const int m = lane & 15, g = lane >> 4, wv = wave >> 1, wt = wave & 1;
   int v0;
   int64_t n0;
   mx4_tile<NJ>(a, v0, n0);
   const int kb = blockIdx.y * a.per;
-  const int ke = min(kb + a.per, (a.o.D + 127) / 128);
+  const int ke = min(kb + a.per, (a.o.D + 255) / 256);
   const int vrows = min(256, a.o.V - v0), pitch = a.o.D / 2;
   const int nrows = (int)min((int64_t)TOK, a.o.N - n0);
   const i32x4_t rh = rsrc_words(a.hidden + n0 * pitch, (uint32_t)(nrows * pitch));
   const i32x4_t rc = rsrc_words(a.o.codes + (int64_t)v0 * pitch, (uint32_t)(vrows * pitch));
-  // scales: waves 0..3 a group of 64 rows of W each, 4..7 one of hidden rows
+  // scales: waves 0..3 a group of 64 rows of W each, 4..7 one of hidden rows; 512 bytes
+  // a step by the first 32 lanes
   const bool sh_wave = wave >= 4;
   const int sgroup = sh_wave ? (wave & 3) % (TOK / 64) : wave;
   const i32x4_t rs =
       rsrc_words((sh_wave ? a.hst + (n0 / 64) * a.T * 256 : a.wst + (int64_t)(v0 / 64) * a.T * 256) +
                      (int64_t)sgroup * a.T * 256,
                  (uint32_t)(a.T * 256));
-  // rows of 64 bytes: slots XORed with (row / 2) % 4, which leaves 8 lanes of a read
-  // (8 rows, one slot) in 8 different 16-byte columns
-  const int lrow = lane >> 2, slot = ((lane & 3) ^ ((lrow >> 1) & 3)) << 4;
-  uint32_t hoff[NH], coff[2];
+  const int lrow = lane >> 3, slot = ((lane & 7) ^ lrow) << 4;
+  uint32_t hoff[NH], coff[NC];
 #pragma unroll
   for (int i = 0; i < NH; ++i)
-    hoff[i] = (uint32_t)((wave * NH + i) * 16 + lrow) * (uint32_t)pitch + (uint32_t)slot;
+    hoff[i] = (uint32_t)((wave * NH + i) * 8 + lrow) * (uint32_t)pitch + (uint32_t)slot;
 #pragma unroll
-  for (int i = 0; i < 2; ++i)
-    coff[i] = (uint32_t)((wave * 2 + i) * 16 + lrow) * (uint32_t)pitch + (uint32_t)slot;
+  for (int i = 0; i < NC; ++i)
+    coff[i] = (uint32_t)((wave * NC + i) * 8 + lrow) * (uint32_t)pitch + (uint32_t)slot;
   // instruction i of step ks
   auto dma = [&](int ks, int i) {
-    const int st = ks & (NS - 1);
+    const int st = ks & 1;
     const bool live = ks < ke;
-    if (i < 2)
-      dma_b128(rc, __builtin_amdgcn_readfirstlane(lds_addr(lc + st * CST) + (wave * 2 + i) * 1024),
-               live ? coff[i] + (uint32_t)ks * 64u : kOobOffset);
-    else if (i < 2 + NH)
-      dma_b128(rh, __builtin_amdgcn_readfirstlane(lds_addr(lds + st * HST) + (wave * NH + i - 2) * 1024),
-               live ? hoff[i - 2] + (uint32_t)ks * 64u : kOobOffset);
+    if (i == 0)
+      dma_b128(rs, __builtin_amdgcn_readfirstlane(lds_addr(ls + st * SST) + wave * 1024),
+               live && lane < 32 ? (uint32_t)(ks * 512 + lane * 16) : kOobOffset);
+    else if (i <= NC)
+      dma_b128(rc, __builtin_amdgcn_readfirstlane(lds_addr(lc + st * CST) + (wave * NC + i - 1) * 1024),
+               live ? coff[i - 1] + (uint32_t)ks * 128u : kOobOffset);
     else
-      dma_b32(rs, __builtin_amdgcn_readfirstlane(lds_addr(ls + st * SST) + wave * 256),
-              live ? (uint32_t)(ks * 256 + lane * 4) : kOobOffset);
+      dma_b128(rh, __builtin_amdgcn_readfirstlane(lds_addr(lds + st * HST) + (wave * NH + i - 1 - NC) * 1024),
+               live ? hoff[i - 1 - NC] + (uint32_t)ks * 128u : kOobOffset);
   };
   f32x4_t acc[4][NJ];
 #pragma unroll
   for (int i = 0; i < 4; ++i)
 #pragma unroll
     for (int j = 0; j < NJ; ++j) acc[i][j] = f32x4_t{0.f, 0.f, 0.f, 0.f};
-  const int fx = (g ^ ((m >> 1) & 3)) << 4;
-  const int hrd = (16 * NJ * wt + m) * 64 + fx, crd = (64 * wv + m) * 64 + fx;
+  const int hrd = (16 * NJ * wt + m) * 128, crd = (64 * wv + m) * 128, fx = g ^ (m & 7);
   u32x4_t hf[2][NJ], wf[2][4];
   uint32_t sw[2], sh[2][NJ / 4];
-  // read number f of step ks into set x
+  // read number f of half s of step ks, into set s
   constexpr int NR = 1 + NJ / 4 + 4 + NJ;
-  auto read = [&](int ks, int x, int f) {
-    const int st = ks & (NS - 1);
+  auto read = [&](int ks, int s, int f) {
+    const int st = ks & 1;
     if (f == 0)
-      sw[x] = *reinterpret_cast<const uint32_t*>(ls + st * SST + wv * 256 + lane * 4);
+      sw[s] = *reinterpret_cast<const uint32_t*>(ls + st * SST + wv * 1024 + s * 256 + lane * 4);
     else if (f < 1 + NJ / 4)
-      sh[x][f - 1] = *reinterpret_cast<const uint32_t*>(
-          ls + st * SST + 1024 + ((wt * NJ / 4) + f - 1) * 256 + lane * 4);
+      sh[s][f - 1] = *reinterpret_cast<const uint32_t*>(
+          ls + st * SST + 4096 + ((wt * NJ / 4) + f - 1) * 1024 + s * 256 + lane * 4);
     else if (f < 5 + NJ / 4)
-      wf[x][f - 1 - NJ / 4] =
-          *reinterpret_cast<const u32x4_t*>(lc + st * CST + crd + (f - 1 - NJ / 4) * 1024);
+      wf[s][f - 1 - NJ / 4] = *reinterpret_cast<const u32x4_t*>(
+          lc + st * CST + crd + (f - 1 - NJ / 4) * 2048 + ((fx ^ (4 * s)) << 4));
     else
-      hf[x][f - 5 - NJ / 4] =
-          *reinterpret_cast<const u32x4_t*>(lds + st * HST + hrd + (f - 5 - NJ / 4) * 1024);
+      hf[s][f - 5 - NJ / 4] = *reinterpret_cast<const u32x4_t*>(
+          lds + st * HST + hrd + (f - 5 - NJ / 4) * 2048 + ((fx ^ (4 * s)) << 4));
   };
   if (kb < ke) {
 #pragma unroll
-    for (int p = 0; p < NS; ++p)
+    for (int p = 0; p < 2; ++p)
 #pragma unroll
       for (int i = 0; i < NI; ++i) dma(kb + p, i);
-    KD_VMCNT(2 * NI);
+    KD_VMCNT(NI);
     __syncthreads();
 #pragma unroll
     for (int f = 0; f < NR; ++f) read(kb, 0, f);
-    __builtin_amdgcn_s_waitcnt(0xc07f & ~0x0f00);  // lgkmcnt(0)
-    __syncthreads();
-    auto step = [&](int ks, int x) {
+    // MFMAs of half x, and the reads of half x ^ 1 (of step kr) between them
+    auto half = [&](int q, int x, int kr) {
+      int i, j0, j1;
+      mx4_pair<NJ>(q, i, j0, j1);
+      acc[i][j0] = mfma_mx4_at(wf[x][i], hf[x][j0], acc[i][j0], i, sw[x], j0 & 3, sh[x][j0 >> 2]);
+      acc[i][j1] = mfma_mx4_at(wf[x][i], hf[x][j1], acc[i][j1], i, sw[x], j1 & 3, sh[x][j1 >> 2]);
+#pragma unroll
+      for (int f = 0; f < NR; ++f)
+        if (f * NP / NR == q) read(kr, x ^ 1, f);
+      __builtin_amdgcn_sched_barrier(0);
+    };
+    for (int ks = kb; ks < ke; ++ks) {
+#pragma unroll
+      for (int q = 0; q < NP; ++q) half(q, 0, ks);
+      __builtin_amdgcn_s_waitcnt(0xc07f & ~0x0f00);  // lgkmcnt(0)
+      KD_VMCNT(0);  // step ks + 1 landed
+      __syncthreads();
+      __builtin_amdgcn_s_setprio(1);
 #pragma unroll
       for (int q = 0; q < NP; ++q) {
-        if (q % (NP / 8) == 0 && q / (NP / 8) < NI) dma(ks + NS, q / (NP / 8));
-        int i, j0, j1;
-        mx4_pair<NJ>(q, i, j0, j1);
-        acc[i][j0] = mfma_mx4_at(wf[x][i], hf[x][j0], acc[i][j0], i, sw[x], j0 & 3, sh[x][j0 >> 2]);
-        acc[i][j1] = mfma_mx4_at(wf[x][i], hf[x][j1], acc[i][j1], i, sw[x], j1 & 3, sh[x][j1 >> 2]);
-#pragma unroll
-        for (int f = 0; f < NR; ++f)
-          if (f * NP / NR == q) read(ks + 1, x ^ 1, f);
-        __builtin_amdgcn_sched_barrier(0);
+        if (q < NI) dma(ks + 2, q);
+        half(q, 1, ks + 1);
       }
-      __builtin_amdgcn_s_waitcnt(0xc07f & ~0x0f00);  // lgkmcnt(0)
-      KD_VMCNT(2 * NI);  // step ks + 2 landed
-      __syncthreads();
-    };
-    for (int ks = kb; ks < ke; ks += 2) {
-      step(ks, 0);
-      if (ks + 1 < ke) step(ks + 1, 1);
+      if constexpr (NI > NP)
+#pragma unroll
+        for (int i = NP; i < NI; ++i) dma(ks + 2, i);
+      __builtin_amdgcn_s_setprio(0);
     }
     KD_VMCNT(0);
     __syncthreads();

@@ -71,7 +71,7 @@ struct KdVerifyArgs {
 
 // Products of 65 hidden rows and more run in tiles of 256 rows of the head by `tok`
 // hidden rows, each over `per` steps of columns (64 a step, of each of three terms with
-// fp32 hidden rows; 128 with 4-bit ones); with splits > 1 the ranges' fp32 sums are
+// fp32 hidden rows; 256 with 4-bit ones); with splits > 1 the ranges' fp32 sums are
 // joined afterwards. Workspace: the head's scales, and the hidden rows' terms or scales, as
 // the tiles take them, and the ranges' sums.
 struct KdMx4Plan {

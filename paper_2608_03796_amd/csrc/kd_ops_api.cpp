@@ -166,9 +166,9 @@ KdMx4Plan kd_mx4_plan(int64_t N, int64_t D, int64_t V, int dtype) {
   // tiles of 128 hidden rows take 0.6 of the time of one of 256
   p.tok = (N + 255) / 256 * 10 <= (N + 127) / 128 * 6 ? 256 : 128;
   const int64_t tiles = tv * ((N + p.tok - 1) / p.tok);
-  // a range is a multiple of 4 steps (of every term), the scales' loads
-  const int64_t unit = dtype == KD_F32 ? 12 : 4;
-  const int64_t steps = dtype == KD_MX4 ? (D + 127) / 128 : (D + 63) / 64 * (unit / 4);
+  // a range is a multiple of 256 columns (of every term), the scales' loads
+  const int64_t unit = dtype == KD_F32 ? 12 : dtype == KD_MX4 ? 1 : 4;
+  const int64_t steps = dtype == KD_MX4 ? (D + 255) / 256 : (D + 63) / 64 * (unit / 4);
   const int64_t units = (steps + unit - 1) / unit;
   int64_t splits = 1;
   if (tiles <= 128) splits = std::max<int64_t>(1, std::min<int64_t>(256 / tiles, units));
