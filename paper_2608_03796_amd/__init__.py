@@ -1102,12 +1102,16 @@ def _ce_functions():
             if ctx.grads is None:
                 raise RuntimeError("cross_entropy(schedule='fused') supports one backward per "
                                    "graph; use schedule='recompute' to run backward again")
-            grads, ctx.grads = ctx.grads, None
-            outs = [None if g is None else g if ctx.dtype == torch.float32
-                    else torch.empty_like(g, dtype=ctx.dtype) for g in grads]
-            scale_grads(grad_out.detach().to(torch.float32).contiguous(), grad_hidden=grads[0],
-                        grad_hidden_out=outs[0], grad_W=grads[1], grad_W_out=outs[1])
-            return outs[0], outs[1], None, None, None, None
+            (gh, gW), ctx.grads = ctx.grads, None
+            g = grad_out.detach()
+            if g.dtype != torch.float32:
+                g = g.to(torch.float32)
+            oh, oW = [x if x is None or ctx.dtype == torch.float32
+                      else torch.empty_like(x, dtype=ctx.dtype) for x in (gh, gW)]
+            code = _dtype_code(ctx.dtype)
+            _call("kd_scale_grads", (gW if gh is None else gh).device, g, gh, code, oh,
+                  0 if gh is None else gh.numel(), gW, code, oW, 0 if gW is None else gW.numel())
+            return oh, oW, None, None, None, None
 
     return {"recompute": CrossEntropy, "fused": CrossEntropyFused}
 
