@@ -545,81 +545,110 @@ __device__ __forceinline__ void dma_b32(i32x4_t r, uint32_t lds_addr, uint32_t v
                : "memory");
 }
 
+// Workgroups are as many as the compute units; each takes the items blockIdx.x, + gridDim.x,
+// ... of a.TV a.TT tiles, range of columns after range.
 template <int NJ>
-__device__ __forceinline__ void mx4_tile(const Mx4GemmArgs& a, int& v0, int64_t& n0) {
+__device__ __forceinline__ void mx4_item(const Mx4GemmArgs& a, int item, int& v0, int64_t& n0,
+                                         int& z) {
+  const int tiles = a.TV * a.TT;
   int vt, tt;
-  tile_at(tile_order_xcd(blockIdx.x, a.TV * a.TT), a.TV, a.TT, 4, vt, tt);
-  v0 = vt * 256;
-  n0 = (int64_t)tt * 32 * NJ;
+  z = __builtin_amdgcn_readfirstlane(item / tiles);
+  tile_at(tile_order_xcd(item - z * tiles, tiles), a.TV, a.TT, 4, vt, tt);
+  // (scalar: the divisions are the vector unit's)
+  v0 = __builtin_amdgcn_readfirstlane(vt) * 256;
+  n0 = (int64_t)__builtin_amdgcn_readfirstlane(tt) * 32 * NJ;
 }
 // acc[i][j] of wave (wv, wt): rows 64 wv + 16 i + 4 g .. + 3 of W, hidden row 16 NJ wt + 16 j + m.
-// By way of LDS (8 KiB a wave, after the main loop's last barrier): a pass turns 64 (bf16)
-// or 32 (fp32) hidden rows of 64 logits into whole 128-byte lines. Stored from the
-// accumulators, 32 or 64 bytes of a row at a time, the tiles' stores took 0.34 (bf16 hidden
-// rows) and 0.50 ms of 4096 x 4096 x 131072.
+// By way of LDS (2 KiB a wave, its own, so that no barrier is needed): 16 hidden rows at a
+// time, whole 128-byte lines (64 logits of bf16, 32 of fp32). Stored from the accumulators,
+// 32 or 64 bytes of a row at a time, the tiles' stores took 0.34 (bf16 hidden rows) and
+// 0.50 ms of 4096 x 4096 x 131072. True if every lane stored every line: then the wave
+// has issued NJ * (bf16 ? 2 : 4) store instructions.
 __device__ __forceinline__ void mx4_wave_sync() {
   __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
   __builtin_amdgcn_wave_barrier();
 }
 template <int NJ, bool BF16>
-__device__ __forceinline__ void mx4_lines(const Mx4Args& o, int v, int64_t n0, char* st,
+__device__ __forceinline__ bool mx4_lines(const Mx4Args& o, int v, int64_t n0, char* st,
                                           const f32x4_t (&acc)[4][NJ]) {
-  constexpr int JP = BF16 ? 4 : 2, RB = BF16 ? 128 : 256;   // blocks of a pass, bytes of a row
-  constexpr int SL = RB / 16, EB = BF16 ? 2 : 4, EV = 16 / EB;
-  const int lane = threadIdx.x & 63, m = lane & 15, g = lane >> 4;
+  constexpr int EB = BF16 ? 2 : 4, EV = 16 / EB, HP = BF16 ? 1 : 2;
+  int lane = threadIdx.x & 63;
+  // (opaque: what depends on it is formed here, not held through the main loop)
+  asm volatile("" : "+v"(lane));
+  const int m = lane & 15, g = lane >> 4;
   const bool wide = ((reinterpret_cast<uintptr_t>(o.out) | ((uintptr_t)o.ldo * EB)) & 15) == 0;
+  // (8 rows by 32-bit offsets)
+  const bool full = wide && v + 64 <= o.V && n0 + 16 * NJ <= o.N && o.ldo < (1 << 26);
+  const int t0 = lane >> 3, c = lane & 7;
+  const uint32_t off = (uint32_t)(t0 * (int)o.ldo + c * EV) * EB;
 #pragma unroll
-  for (int p = 0; p < NJ / JP; ++p) {
+  for (int j = 0; j < NJ; ++j)
 #pragma unroll
-    for (int j = 0; j < JP; ++j) {
-      const int t = 16 * j + m;
+    for (int p = 0; p < HP; ++p) {
+      if constexpr (BF16) {
 #pragma unroll
-      for (int i = 0; i < 4; ++i) {
-        const f32x4_t z = acc[i][p * JP + j];
-        if constexpr (BF16)
-          *reinterpret_cast<u32x2_t*>(st + t * RB + (((2 * i + (g >> 1)) ^ (t & 7)) << 4) + 8 * (g & 1)) =
-              u32x2_t{pack_bf16x2(z[0], z[1]), pack_bf16x2(z[2], z[3])};
-        else
-          *reinterpret_cast<f32x4_t*>(st + t * RB + (((4 * i + g) ^ (t & 15)) << 4)) = z;
-      }
-    }
-    mx4_wave_sync();
-#pragma unroll
-    for (int q = 0; q < 8; ++q) {
-      const int t = q * (64 / SL) + lane / SL, c = lane % SL;
-      const int64_t n = n0 + 16 * JP * p + t;
-      const u32x4_t x = *reinterpret_cast<const u32x4_t*>(st + t * RB + ((c ^ (t & (SL - 1))) << 4));
-      const int vv = v + c * EV;
-      if (n >= o.N || vv >= o.V) continue;
-      char* dst = static_cast<char*>(o.out) + (n * o.ldo + vv) * EB;
-      if (wide && vv + EV <= o.V) {
-        *reinterpret_cast<u32x4_t*>(dst) = x;
+        for (int i = 0; i < 4; ++i)
+          *reinterpret_cast<u32x2_t*>(st + m * 128 + (((2 * i + (g >> 1)) ^ (m & 7)) << 4) + 8 * (g & 1)) =
+              u32x2_t{pack_bf16x2(acc[i][j][0], acc[i][j][1]), pack_bf16x2(acc[i][j][2], acc[i][j][3])};
       } else {
 #pragma unroll
-        for (int e = 0; e < EV; ++e) {
-          if (vv + e >= o.V) break;
-          if constexpr (BF16)
-            reinterpret_cast<uint16_t*>(dst)[e] = (uint16_t)(x[e >> 1] >> (16 * (e & 1)));
-          else
-            reinterpret_cast<uint32_t*>(dst)[e] = x[e];
+        for (int i = 0; i < 2; ++i)
+          *reinterpret_cast<f32x4_t*>(st + m * 128 + (((4 * i + g) ^ (m & 7)) << 4)) = acc[2 * p + i][j];
+      }
+      mx4_wave_sync();
+#pragma unroll
+      for (int q = 0; q < 2; ++q) {
+        const int t = 8 * q + t0;
+        const u32x4_t x = *reinterpret_cast<const u32x4_t*>(st + t * 128 + ((c ^ (t & 7)) << 4));
+        if (full) {
+          char* row = static_cast<char*>(o.out) + ((n0 + 16 * j + 8 * q) * o.ldo + v + 32 * p) * EB;
+          *reinterpret_cast<u32x4_t*>(row + off) = x;
+          continue;
+        }
+        const int64_t n = n0 + 16 * j + t;
+        const int vv = v + 32 * p + c * EV;
+        if (n >= o.N) continue;
+        char* dst = static_cast<char*>(o.out) + (n * o.ldo + vv) * EB;
+        if (wide && vv + EV <= o.V) {
+          *reinterpret_cast<u32x4_t*>(dst) = x;
+        } else {
+#pragma unroll
+          for (int e = 0; e < EV; ++e) {
+            if (vv + e >= o.V) break;
+            if constexpr (BF16)
+              reinterpret_cast<uint16_t*>(dst)[e] = (uint16_t)(x[e >> 1] >> (16 * (e & 1)));
+            else
+              reinterpret_cast<uint32_t*>(dst)[e] = x[e];
+          }
         }
       }
+      mx4_wave_sync();
+      __builtin_amdgcn_sched_barrier(0);
     }
-    mx4_wave_sync();
-  }
+  return full;
 }
+// the wave's store instructions in flight: 0 if it has waited for them
 template <int NJ>
-__device__ __forceinline__ void mx4_tile_out(const Mx4GemmArgs& a, int v0, int64_t n0, int wv,
-                                             int wt, char* lds, const f32x4_t (&acc)[4][NJ]) {
+__device__ __forceinline__ int mx4_tile_out(const Mx4GemmArgs& a, int v, int64_t n, int z, char* st,
+                                            const f32x4_t (&acc)[4][NJ]) {
   Mx4Args o = a.o;
   if (a.part != nullptr) {
-    o.out = a.part + (int64_t)blockIdx.y * o.N * a.Vp;
+    o.out = a.part + (int64_t)z * o.N * a.Vp;
     o.ldo = a.Vp;
     o.out_bf16 = 0;
   }
-  char* st = lds + wave_id() * 8192;
-  if (o.out_bf16) mx4_lines<NJ, true>(o, v0 + 64 * wv, n0 + 16 * NJ * wt, st, acc);
-  else mx4_lines<NJ, false>(o, v0 + 64 * wv, n0 + 16 * NJ * wt, st, acc);
+  const bool full = o.out_bf16 ? mx4_lines<NJ, true>(o, v, n, st, acc) : mx4_lines<NJ, false>(o, v, n, st, acc);
+  if (full) return o.out_bf16 ? 2 * NJ : 4 * NJ;
+  KD_VMCNT(0);
+  return 0;
+}
+// s_waitcnt vmcnt(n + the stores in flight): what was loaded before them has landed (loads
+// and stores count in the order of their issue)
+template <int NJ, int N>
+__device__ __forceinline__ void mx4_wait(int stores) {
+  if (stores == 0) KD_VMCNT(N);
+  else if (stores == 2 * NJ) KD_VMCNT(N + 2 * NJ);
+  else KD_VMCNT(N + 4 * NJ);
 }
 // MFMA pair q of 2 NJ: row block q / (NJ / 2) of W, two hidden blocks, back and forth
 template <int NJ>
@@ -632,142 +661,186 @@ __device__ __forceinline__ void mx4_pair(int q, int& i, int& j0, int& j1) {
 
 // Tiles of 256 rows of W by 32 NJ hidden rows, bf16 hidden rows (TERMS = 1) or three
 // terms each (3): 8 waves of 64 x 16 NJ. A step is 64 columns (of one term): hidden rows
-// 128 bytes each in three stages, codes 32 bytes a row in two, scales of four steps in
-// two, all by LDS-DMA two steps ahead; one barrier a step. A wave's 4 row blocks of W are
+// 128 bytes each in three stages, codes 32 bytes a row in two, scales of up to four steps
+// in three, all by LDS-DMA two steps ahead; one barrier a step. A wave's 4 row blocks of W are
 // decoded in registers between the MFMAs of the half step before their use: a block's
 // codes are read from LDS twice (by two waves) and take an eighth of bf16's bytes, so that
 // the LDS, which bounds the bf16 tiles of the loss, has a quarter of its time left.
+// The steps of a workgroup's items form one sequence: a tile's last steps load the next
+// tile's first ones, and its logits are stored under that tile's first step.
 template <int TERMS, int NJ>
 __global__ __launch_bounds__(512, 1) void k_mx4_gemm(Mx4GemmArgs a) {
   constexpr int TOK = 32 * NJ, HST = TOK * 128, CST = 256 * 32, SST = 2048;
   constexpr int NPW = NJ / 2, NP = 2 * NJ;
-  __shared__ __attribute__((aligned(16))) char lds[3 * HST + 2 * CST + 2 * SST];
+  __shared__ __attribute__((aligned(16))) char lds[3 * HST + 2 * CST + 3 * SST + 8 * 2048];
   char* const lc = lds + 3 * HST;
   char* const ls = lc + 2 * CST;
   const int lane = threadIdx.x & 63, wave = wave_id();
+  char* const lo = ls + 3 * SST + wave * 2048;
   const int m = lane & 15, g = lane >> 4, wv = wave >> 1, wt = wave & 1;
-  int v0;
-  int64_t n0;
-  mx4_tile<NJ>(a, v0, n0);
-  const int kb = blockIdx.y * a.per;
-  const int ke = min(kb + a.per, ((a.o.D + 63) / 64) * TERMS);
-  const int vrows = min(256, a.o.V - v0), pitch = a.o.D / 2;
-  const int nrows = (int)min((int64_t)TOK, a.o.N - n0);
-  const i32x4_t rh = rsrc_words(a.hidden + n0 * a.hld, (uint32_t)((nrows - 1) * a.hld + a.hbytes));
-  const i32x4_t rc = rsrc_words(a.o.codes + (int64_t)v0 * pitch, (uint32_t)(vrows * pitch));
-  const i32x4_t rs = rsrc_words(a.wst + (int64_t)(v0 / 64) * a.T * 256, (uint32_t)(4 * a.T * 256));
+  const int items = a.TV * a.TT * a.splits, steps = (a.o.D + 63) / 64 * TERMS, pitch = a.o.D / 2;
 
   // hidden rows: instruction i of the wave has rows 8 (NPW wave + i) .. + 7
   const int hslot = ((lane & 7) ^ (lane >> 3)) << 4;
-  uint32_t hoff[NPW];
-#pragma unroll
-  for (int i = 0; i < NPW; ++i)
-    hoff[i] = (uint32_t)((wave * NPW + i) * 8 + (lane >> 3)) * (uint32_t)a.hld + (uint32_t)hslot;
+  const uint32_t hoff = (uint32_t)(lane >> 3) * (uint32_t)a.hld + (uint32_t)hslot;
   // codes: rows 32 wave .. + 31, the 16-byte halves exchanged for every other 8 rows (the
   // reads of 16 rows then touch each bank once)
   const int crow = 32 * wave + (lane >> 1);
   const uint32_t coff = (uint32_t)crow * (uint32_t)pitch + (((lane & 1) ^ ((crow >> 3) & 1)) << 4);
   const uint32_t soff = (uint32_t)((wave & 3) * a.T * 256 + lane * 4);
-  auto dma_h = [&](int ks, int stage, int i) {
-    const bool live = ks < ke && ks * 128 + hslot < a.hbytes;
+
+  // the step to load next: lk of lk_end of item li, whose scales go to stage lsc
+  i32x4_t rh, rc, rs;
+  int li = (int)blockIdx.x, lk = 0, lk_end = 0, lsc = 2;
+  auto open = [&]() {
+    lk = lk_end = 0;
+    if (li >= items) return;
+    int v0, z;
+    int64_t n0;
+    mx4_item<NJ>(a, li, v0, n0, z);
+    const int vrows = min(256, a.o.V - v0), nrows = (int)min((int64_t)TOK, a.o.N - n0);
+    rh = rsrc_words(a.hidden + n0 * a.hld, (uint32_t)((nrows - 1) * a.hld + a.hbytes));
+    rc = rsrc_words(a.o.codes + (int64_t)v0 * pitch, (uint32_t)(vrows * pitch));
+    rs = rsrc_words(a.wst + (int64_t)(v0 / 64) * a.T * 256, (uint32_t)(4 * a.T * 256));
+    lk = z * a.per;
+    lk_end = min(lk + a.per, steps);
+  };
+  auto next = [&]() {
+    if (++lk >= lk_end) {
+      li += gridDim.x;
+      open();
+    }
+  };
+  auto dma_h = [&](int stage, int i) {
+    const bool live = lk < lk_end && lk * 128 + hslot < a.hbytes;
     dma_b128(rh, __builtin_amdgcn_readfirstlane(lds_addr(lds + stage * HST) + (wave * NPW + i) * 1024),
-             live ? hoff[i] + (uint32_t)ks * 128u : kOobOffset);
+             live ? hoff + ((uint32_t)((wave * NPW + i) * 8) * (uint32_t)a.hld + (uint32_t)lk * 128u)
+                  : kOobOffset);
   };
-  auto dma_c = [&](int ks) {
-    dma_b128(rc, __builtin_amdgcn_readfirstlane(lds_addr(lc + (ks & 1) * CST) + wave * 1024),
-             ks < ke ? coff + (uint32_t)(ks / TERMS) * 32u : kOobOffset);
+  auto dma_c = [&](int stage) {
+    dma_b128(rc, __builtin_amdgcn_readfirstlane(lds_addr(lc + stage * CST) + wave * 1024),
+             lk < lk_end ? coff + (uint32_t)(lk / TERMS) * 32u : kOobOffset);
   };
-  // waves 0..3 the scales of two steps, 4..7 of the next two
-  auto dma_s = [&](int ks) {
-    const int w = ks / TERMS, t = (w >> 1) + (wave >> 2);
-    dma_b32(rs, __builtin_amdgcn_readfirstlane(lds_addr(ls + ((w >> 2) & 1) * SST) + wave * 256),
+  // at every fourth 64 columns: waves 0..3 the scales of two steps, 4..7 of the next two
+  auto dma_s = [&]() {
+    if (lk >= lk_end || lk % TERMS != 0 || (lk / TERMS & 3) != 0) return;
+    lsc = lsc == 2 ? 0 : lsc + 1;
+    const int t = (lk / TERMS >> 1) + (wave >> 2);
+    dma_b32(rs, __builtin_amdgcn_readfirstlane(lds_addr(ls + lsc * SST) + wave * 256),
             t < a.T ? soff + (uint32_t)t * 256u : kOobOffset);
   };
 
   f32x4_t acc[4][NJ];
-#pragma unroll
-  for (int i = 0; i < 4; ++i)
-#pragma unroll
-    for (int j = 0; j < NJ; ++j) acc[i][j] = f32x4_t{0.f, 0.f, 0.f, 0.f};
-
   // fragment addresses within a stage
   const int hrd = (16 * NJ * wt + m) * 128, hx = g ^ (m & 7);
   const int crd = (64 * wv + m) * 32 + 4 * g, cx = (m >> 3) & 1;
   const int srd = wv * 256 + m * 4;
   u32x4_t hf[2][NJ], wf[2][4];
   uint32_t raw[4], sc = 0;
+  // half s of 64 columns number w, whose scales are in stage cs
+  auto read_s = [&](int cs, int w, int s) {
+    return *reinterpret_cast<const uint32_t*>(ls + cs * SST + ((w >> 1) & 1) * 1024 + srd +
+                                              (2 * (w & 1) + s) * 64);
+  };
   auto read_h = [&](const char* st, int s, int f) {
     return *reinterpret_cast<const u32x4_t*>(st + hrd + f * 2048 + ((hx ^ (4 * s)) << 4));
   };
   auto read_c = [&](const char* st, int s, int b) {
     return *reinterpret_cast<const uint32_t*>(st + crd + b * 512 + ((s ^ cx) << 4));
   };
-  auto read_s = [&](int ks, int s) {
-    const int w = ks / TERMS;
-    return *reinterpret_cast<const uint32_t*>(ls + ((w >> 2) & 1) * SST + ((w >> 1) & 1) * 1024 +
-                                              srd + (2 * (w & 1) + s) * 64);
-  };
   auto unpack = [&](int b) {
     const uint32_t e = b == 3 ? (sc >> 1) & 0x7f800000u : (sc << (23 - 8 * b)) & 0x7f800000u;
     return mx4_unpack8(raw[b], __builtin_bit_cast(float, e));
   };
 
-  if (kb < ke) {
-    dma_s(kb);
+  open();
 #pragma unroll
-    for (int p = 0; p < 2; ++p) {
+  for (int p = 0; p < 2; ++p) {
+    dma_s();
 #pragma unroll
-      for (int i = 0; i < NPW; ++i) dma_h(kb + p, p, i);
-      dma_c(kb + p);
-    }
-    KD_VMCNT(NPW + 1);
-    __syncthreads();
+    for (int i = 0; i < NPW; ++i) dma_h(p, i);
+    dma_c(p);
+    next();
+  }
+  KD_VMCNT(0);
+  __syncthreads();
+  int item = (int)blockIdx.x, v0, z;
+  int64_t n0;
+  mx4_item<NJ>(a, item, v0, n0, z);
+  int k = z * a.per, ke = min(k + a.per, steps);
+  int ca = 0, cc = 0, cs = 0, stores = 0;  // stages of step k's hidden rows, codes and scales
 #pragma unroll
-    for (int f = 0; f < NJ; ++f) hf[0][f] = read_h(lds, 0, f);
-    sc = read_s(kb, 0);
+  for (int f = 0; f < NJ; ++f) hf[0][f] = read_h(lds, 0, f);
+  sc = read_s(0, k / TERMS, 0);
 #pragma unroll
-    for (int b = 0; b < 4; ++b) raw[b] = read_c(lc + (kb & 1) * CST, 0, b);
+  for (int b = 0; b < 4; ++b) raw[b] = read_c(lc, 0, b);
 #pragma unroll
-    for (int b = 0; b < 4; ++b) wf[0][b] = unpack(b);
-    // MFMAs of half x, reads of the other half y (half s of step kr) between them
-    constexpr int U0 = NP == 16 ? 8 : 4, US = NP == 16 ? 2 : 1, H0 = NP == 16 ? 4 : 2;
-    auto half = [&](int q, int x, const char* hst, int kr, int s) {
-      const int y = x ^ 1;
-      int i, j0, j1;
-      mx4_pair<NJ>(q, i, j0, j1);
-      acc[i][j0] = mfma_slot(wf[x][i], hf[x][j0], acc[i][j0], (__bf16*)nullptr);
-      acc[i][j1] = mfma_slot(wf[x][i], hf[x][j1], acc[i][j1], (__bf16*)nullptr);
-      if (q == 0) sc = read_s(kr, s);
-      if (q < 4) raw[q] = read_c(lc + (kr & 1) * CST, s, q);
-      if (q >= H0 && q < H0 + NJ) hf[y][q - H0] = read_h(hst, s, q - H0);
-      if (q >= U0 && (q - U0) % US == 0) wf[y][(q - U0) / US] = unpack((q - U0) / US);
-      __builtin_amdgcn_sched_barrier(0);
-    };
-    int ca = 0;  // stage of step j's hidden rows
-    for (int j = kb; j < ke; ++j) {
+  for (int b = 0; b < 4; ++b) wf[0][b] = unpack(b);
+  // MFMAs of half x, reads of the other half y (half s of 64 columns w) between them
+  constexpr int U0 = NP == 16 ? 8 : 4, US = NP == 16 ? 2 : 1, H0 = NP == 16 ? 4 : 2;
+  auto half = [&](int q, int x, const char* hst, const char* cst, int css, int w, int s) {
+    const int y = x ^ 1;
+    int i, j0, j1;
+    mx4_pair<NJ>(q, i, j0, j1);
+    acc[i][j0] = mfma_slot(wf[x][i], hf[x][j0], acc[i][j0], (__bf16*)nullptr);
+    acc[i][j1] = mfma_slot(wf[x][i], hf[x][j1], acc[i][j1], (__bf16*)nullptr);
+    if (q == 0) sc = read_s(css, w, s);
+    if (q < 4) raw[q] = read_c(cst, s, q);
+    if (q >= H0 && q < H0 + NJ) hf[y][q - H0] = read_h(hst, s, q - H0);
+    if (q >= U0 && (q - U0) % US == 0) wf[y][(q - U0) / US] = unpack((q - U0) / US);
+    __builtin_amdgcn_sched_barrier(0);
+  };
+#pragma unroll 1
+  while (true) {
+#pragma unroll
+    for (int i = 0; i < 4; ++i)
+#pragma unroll
+      for (int j = 0; j < NJ; ++j) acc[i][j] = f32x4_t{0.f, 0.f, 0.f, 0.f};
+    const int nitem = item + gridDim.x;
+    int nv0 = 0, nz = 0;
+    int64_t nn0 = 0;
+    if (nitem < items) mx4_item<NJ>(a, nitem, nv0, nn0, nz);
+#pragma unroll 1
+    for (;;) {
       const int na = ca == 2 ? 0 : ca + 1, pa = ca == 0 ? 2 : ca - 1;
-      if ((j + 2) % TERMS == 0 && (((j + 2) / TERMS) & 3) == 0) dma_s(j + 2);
+      // the step after this one, of the next tile behind the last (its first columns' scales
+      // start a stage)
+      const int kn = k + 1 < ke ? k + 1 : nz * a.per;
+      const bool same = k + 1 < ke && (kn % TERMS != 0 || (kn / TERMS & 3) != 0);
+      const int ncs = same ? cs : cs == 2 ? 0 : cs + 1;
+      dma_s();
 #pragma unroll
       for (int q = 0; q < NP; ++q) {
-        if (q % 4 == 3) dma_h(j + 2, pa, q / 4);
-        half(q, 0, lds + ca * HST, j, 1);
+        if (q % 4 == 3) dma_h(pa, q / 4);
+        half(q, 0, lds + ca * HST, lc + cc * CST, cs, k / TERMS, 1);
       }
       __builtin_amdgcn_s_waitcnt(0xc07f & ~0x0f00);  // lgkmcnt(0)
-      KD_VMCNT(NPW);  // step j + 1 landed; step j + 2's hidden rows may still fly
+      mx4_wait<NJ, NPW>(stores);  // the next step landed; the hidden rows behind it may still fly
+      stores = 0;
       __syncthreads();
       __builtin_amdgcn_s_setprio(1);
 #pragma unroll
       for (int q = 0; q < NP; ++q) {
-        if (q == 0) dma_c(j + 2);
-        half(q, 1, lds + na * HST, j + 1, 0);
+        if (q == 0) dma_c(cc);
+        half(q, 1, lds + na * HST, lc + (cc ^ 1) * CST, ncs, kn / TERMS, 0);
       }
       __builtin_amdgcn_s_setprio(0);
+      next();
       ca = na;
+      cc ^= 1;
+      cs = ncs;
+      if (++k >= ke) break;
     }
-    KD_VMCNT(0);
-    __syncthreads();
+    stores = mx4_tile_out<NJ>(a, v0 + 64 * wv, n0 + 16 * NJ * wt, z, lo, acc);
+    if (nitem >= items) break;
+    item = nitem;
+    v0 = nv0;
+    n0 = nn0;
+    z = nz;
+    k = z * a.per;
+    ke = min(k + a.per, steps);
   }
-  mx4_tile_out<NJ>(a, v0, n0, wv, wt, lds, acc);
+  KD_VMCNT(0);  // loads into LDS end before the workgroup does
 }
 
 template <int OA, int OB>
@@ -811,62 +884,62 @@ template <int NJ>
 __global__ __launch_bounds__(512, 1) void k_mx4_gemm4(Mx4GemmArgs a) {
   constexpr int TOK = 32 * NJ, HST = TOK * 128, CST = 256 * 128, SST = 8192;
   constexpr int NH = NJ / 2, NC = 4, NI = NC + NH + 1, NP = 2 * NJ;
-  __shared__ __attribute__((aligned(16))) char lds[2 * (HST + CST + SST)];
+  static_assert(NI <= NP, "a load a pair");
+  __shared__ __attribute__((aligned(16))) char lds[2 * (HST + CST + SST) + 8 * 2048];
   char* const lc = lds + 2 * HST;
   char* const ls = lc + 2 * CST;
   const int lane = threadIdx.x & 63, wave = wave_id();
+  char* const lo = ls + 2 * SST + wave * 2048;
   const int m = lane & 15, g = lane >> 4, wv = wave >> 1, wt = wave & 1;
-  int v0;
-  int64_t n0;
-  mx4_tile<NJ>(a, v0, n0);
-  const int kb = blockIdx.y * a.per;
-  const int ke = min(kb + a.per, (a.o.D + 255) / 256);
-  const int vrows = min(256, a.o.V - v0), pitch = a.o.D / 2;
-  const int nrows = (int)min((int64_t)TOK, a.o.N - n0);
-  const i32x4_t rh = rsrc_words(a.hidden + n0 * pitch, (uint32_t)(nrows * pitch));
-  const i32x4_t rc = rsrc_words(a.o.codes + (int64_t)v0 * pitch, (uint32_t)(vrows * pitch));
-  // scales: waves 0..3 a group of 64 rows of W each, 4..7 one of hidden rows; 512 bytes
-  // a step by the first 32 lanes
-  const bool sh_wave = wave >= 4;
-  const int sgroup = sh_wave ? (wave & 3) % (TOK / 64) : wave;
-  const i32x4_t rs =
-      rsrc_words((sh_wave ? a.hst + (n0 / 64) * a.T * 256 : a.wst + (int64_t)(v0 / 64) * a.T * 256) +
-                     (int64_t)sgroup * a.T * 256,
-                 (uint32_t)(a.T * 256));
+  const int items = a.TV * a.TT * a.splits, steps = (a.o.D + 255) / 256, pitch = a.o.D / 2;
   const int lrow = lane >> 3, slot = ((lane & 7) ^ lrow) << 4;
-  uint32_t hoff[NH], coff[NC];
-#pragma unroll
-  for (int i = 0; i < NH; ++i)
-    hoff[i] = (uint32_t)((wave * NH + i) * 8 + lrow) * (uint32_t)pitch + (uint32_t)slot;
-#pragma unroll
-  for (int i = 0; i < NC; ++i)
-    coff[i] = (uint32_t)((wave * NC + i) * 8 + lrow) * (uint32_t)pitch + (uint32_t)slot;
-  // instruction i of step ks
-  auto dma = [&](int ks, int i) {
-    const int st = ks & 1;
-    const bool live = ks < ke;
+  const uint32_t off = (uint32_t)lrow * (uint32_t)pitch + (uint32_t)slot;
+
+  // the step to load next: lk of lk_end of item li
+  i32x4_t rh, rc, rs;
+  int li = (int)blockIdx.x, lk = 0, lk_end = 0;
+  auto open = [&]() {
+    lk = lk_end = 0;
+    if (li >= items) return;
+    int v0, z;
+    int64_t n0;
+    mx4_item<NJ>(a, li, v0, n0, z);
+    const int vrows = min(256, a.o.V - v0), nrows = (int)min((int64_t)TOK, a.o.N - n0);
+    rh = rsrc_words(a.hidden + n0 * pitch, (uint32_t)(nrows * pitch));
+    rc = rsrc_words(a.o.codes + (int64_t)v0 * pitch, (uint32_t)(vrows * pitch));
+    // scales: waves 0..3 a group of 64 rows of W each, 4..7 one of hidden rows; 512 bytes
+    // a step by the first 32 lanes
+    const int64_t group = wave >= 4 ? n0 / 64 + (wave & 3) % (TOK / 64) : v0 / 64 + wave;
+    rs = rsrc_words((wave >= 4 ? a.hst : a.wst) + group * a.T * 256, (uint32_t)(a.T * 256));
+    lk = z * a.per;
+    lk_end = min(lk + a.per, steps);
+  };
+  auto next = [&]() {
+    if (++lk >= lk_end) {
+      li += gridDim.x;
+      open();
+    }
+  };
+  // instruction i of that step
+  auto dma = [&](int st, int i) {
+    const bool live = lk < lk_end;
     if (i == 0)
       dma_b128(rs, __builtin_amdgcn_readfirstlane(lds_addr(ls + st * SST) + wave * 1024),
-               live && lane < 32 ? (uint32_t)(ks * 512 + lane * 16) : kOobOffset);
+               live && lane < 32 ? (uint32_t)(lk * 512 + lane * 16) : kOobOffset);
     else if (i <= NC)
       dma_b128(rc, __builtin_amdgcn_readfirstlane(lds_addr(lc + st * CST) + (wave * NC + i - 1) * 1024),
-               live ? coff[i - 1] + (uint32_t)ks * 128u : kOobOffset);
+               live ? off + (uint32_t)((wave * NC + i - 1) * 8 * pitch + lk * 128) : kOobOffset);
     else
       dma_b128(rh, __builtin_amdgcn_readfirstlane(lds_addr(lds + st * HST) + (wave * NH + i - 1 - NC) * 1024),
-               live ? hoff[i - 1 - NC] + (uint32_t)ks * 128u : kOobOffset);
+               live ? off + (uint32_t)((wave * NH + i - 1 - NC) * 8 * pitch + lk * 128) : kOobOffset);
   };
   f32x4_t acc[4][NJ];
-#pragma unroll
-  for (int i = 0; i < 4; ++i)
-#pragma unroll
-    for (int j = 0; j < NJ; ++j) acc[i][j] = f32x4_t{0.f, 0.f, 0.f, 0.f};
   const int hrd = (16 * NJ * wt + m) * 128, crd = (64 * wv + m) * 128, fx = g ^ (m & 7);
   u32x4_t hf[2][NJ], wf[2][4];
   uint32_t sw[2], sh[2][NJ / 4];
-  // read number f of half s of step ks, into set s
+  // read number f of half s of the step in stage st, into set s
   constexpr int NR = 1 + NJ / 4 + 4 + NJ;
-  auto read = [&](int ks, int s, int f) {
-    const int st = ks & 1;
+  auto read = [&](int st, int s, int f) {
     if (f == 0)
       sw[s] = *reinterpret_cast<const uint32_t*>(ls + st * SST + wv * 1024 + s * 256 + lane * 4);
     else if (f < 1 + NJ / 4)
@@ -879,47 +952,60 @@ __global__ __launch_bounds__(512, 1) void k_mx4_gemm4(Mx4GemmArgs a) {
       hf[s][f - 5 - NJ / 4] = *reinterpret_cast<const u32x4_t*>(
           lds + st * HST + hrd + (f - 5 - NJ / 4) * 2048 + ((fx ^ (4 * s)) << 4));
   };
-  if (kb < ke) {
+  open();
 #pragma unroll
-    for (int p = 0; p < 2; ++p)
+  for (int p = 0; p < 2; ++p) {
 #pragma unroll
-      for (int i = 0; i < NI; ++i) dma(kb + p, i);
-    KD_VMCNT(NI);
-    __syncthreads();
+    for (int i = 0; i < NI; ++i) dma(p, i);
+    next();
+  }
+  KD_VMCNT(NI);
+  __syncthreads();
 #pragma unroll
-    for (int f = 0; f < NR; ++f) read(kb, 0, f);
-    // MFMAs of half x, and the reads of half x ^ 1 (of step kr) between them
-    auto half = [&](int q, int x, int kr) {
-      int i, j0, j1;
-      mx4_pair<NJ>(q, i, j0, j1);
-      acc[i][j0] = mfma_mx4_at(wf[x][i], hf[x][j0], acc[i][j0], i, sw[x], j0 & 3, sh[x][j0 >> 2]);
-      acc[i][j1] = mfma_mx4_at(wf[x][i], hf[x][j1], acc[i][j1], i, sw[x], j1 & 3, sh[x][j1 >> 2]);
+  for (int f = 0; f < NR; ++f) read(0, 0, f);
+  // MFMAs of half x, and the reads of half x ^ 1 (of the step in stage st) between them
+  auto half = [&](int q, int x, int st) {
+    int i, j0, j1;
+    mx4_pair<NJ>(q, i, j0, j1);
+    acc[i][j0] = mfma_mx4_at(wf[x][i], hf[x][j0], acc[i][j0], i, sw[x], j0 & 3, sh[x][j0 >> 2]);
+    acc[i][j1] = mfma_mx4_at(wf[x][i], hf[x][j1], acc[i][j1], i, sw[x], j1 & 3, sh[x][j1 >> 2]);
 #pragma unroll
-      for (int f = 0; f < NR; ++f)
-        if (f * NP / NR == q) read(kr, x ^ 1, f);
-      __builtin_amdgcn_sched_barrier(0);
-    };
-    for (int ks = kb; ks < ke; ++ks) {
+    for (int f = 0; f < NR; ++f)
+      if (f * NP / NR == q) read(st, x ^ 1, f);
+    __builtin_amdgcn_sched_barrier(0);
+  };
+  int st = 0, stores = 0;
+#pragma unroll 1
+  for (int item = (int)blockIdx.x; item < items; item += gridDim.x) {
+    int v0, z;
+    int64_t n0;
+    mx4_item<NJ>(a, item, v0, n0, z);
+    const int ke = min((z + 1) * a.per, steps);
 #pragma unroll
-      for (int q = 0; q < NP; ++q) half(q, 0, ks);
+    for (int i = 0; i < 4; ++i)
+#pragma unroll
+      for (int j = 0; j < NJ; ++j) acc[i][j] = f32x4_t{0.f, 0.f, 0.f, 0.f};
+#pragma unroll 1
+    for (int k = z * a.per; k < ke; ++k) {
+#pragma unroll
+      for (int q = 0; q < NP; ++q) half(q, 0, st);
       __builtin_amdgcn_s_waitcnt(0xc07f & ~0x0f00);  // lgkmcnt(0)
-      KD_VMCNT(0);  // step ks + 1 landed
+      mx4_wait<NJ, 0>(stores);  // the next step landed
+      stores = 0;
       __syncthreads();
       __builtin_amdgcn_s_setprio(1);
 #pragma unroll
       for (int q = 0; q < NP; ++q) {
-        if (q < NI) dma(ks + 2, q);
-        half(q, 1, ks + 1);
+        if (q < NI) dma(st, q);
+        half(q, 1, st ^ 1);
       }
-      if constexpr (NI > NP)
-#pragma unroll
-        for (int i = NP; i < NI; ++i) dma(ks + 2, i);
       __builtin_amdgcn_s_setprio(0);
+      next();
+      st ^= 1;
     }
-    KD_VMCNT(0);
-    __syncthreads();
+    stores = mx4_tile_out<NJ>(a, v0 + 64 * wv, n0 + 16 * NJ * wt, z, lo, acc);
   }
-  mx4_tile_out<NJ>(a, v0, n0, wv, wt, lds, acc);
+  KD_VMCNT(0);  // loads into LDS end before the workgroup does
 }
 
 // out = the ranges' sums, in order
@@ -1009,6 +1095,8 @@ static int launch_mx4_wide(const Mx4Args& a, hipStream_t s) {
   return (int)hipGetLastError();
 }
 
+constexpr int64_t kMx4Units = 256;  // compute units
+
 static int launch_mx4_scale_tiles(const uint8_t* scales, int64_t rows, int64_t D, uint8_t* out,
                                   hipStream_t s) {
   const int64_t T = mx4_tile_steps(D), groups = mx4_tile_groups(rows);
@@ -1048,7 +1136,8 @@ static int launch_mx4_gemm(const KdMx4Args& q, const Mx4Args& o, hipStream_t s) 
     a.hst = reinterpret_cast<uint8_t*>(q.ws + p.off_hidden);
     if (launch_mx4_scale_tiles(q.hscales, q.N, q.D, const_cast<uint8_t*>(a.hst), s) != 0) return 1;
   }
-  const dim3 grid((unsigned)(a.TV * a.TT), (unsigned)p.splits), block(512);
+  const int64_t items = (int64_t)a.TV * a.TT * p.splits;
+  const dim3 grid((unsigned)(items < kMx4Units ? items : kMx4Units)), block(512);
   if constexpr (H == 2) {
     if (p.tok == 256) hipLaunchKernelGGL((k_mx4_gemm4<8>), grid, block, 0, s, a);
     else hipLaunchKernelGGL((k_mx4_gemm4<4>), grid, block, 0, s, a);
