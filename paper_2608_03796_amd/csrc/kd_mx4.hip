@@ -277,15 +277,17 @@ __global__ __launch_bounds__(512) void k_mx4_rows(Mx4Args a) {
   }
 }
 
-// 4 consecutive logits of a row; `wide` where the rows allow 4 elements a store
-__device__ __forceinline__ void mx4_put4(const Mx4Args& a, int64_t n, int v, f32x4_t z, bool wide) {
+// 4 consecutive logits of a row (stored together at any element boundary, which the
+// target allows)
+__device__ __forceinline__ void mx4_put4(const Mx4Args& a, int64_t n, int v, f32x4_t z) {
   const int64_t o = n * a.ldo + v;
-  if (wide && v + 4 <= a.V) {
-    if (a.out_bf16)
-      *reinterpret_cast<u32x2_t*>(static_cast<__bf16*>(a.out) + o) =
-          u32x2_t{pack_bf16x2(z[0], z[1]), pack_bf16x2(z[2], z[3])};
-    else
-      *reinterpret_cast<f32x4_t*>(static_cast<float*>(a.out) + o) = z;
+  if (v + 4 <= a.V) {
+    if (a.out_bf16) {
+      const u32x2_t x = {pack_bf16x2(z[0], z[1]), pack_bf16x2(z[2], z[3])};
+      __builtin_memcpy(static_cast<__bf16*>(a.out) + o, &x, 8);
+    } else {
+      __builtin_memcpy(static_cast<float*>(a.out) + o, &z, 16);
+    }
     return;
   }
 #pragma unroll
@@ -294,10 +296,6 @@ __device__ __forceinline__ void mx4_put4(const Mx4Args& a, int64_t n, int v, f32
     if (a.out_bf16) static_cast<__bf16*>(a.out)[o + i] = (__bf16)z[i];
     else static_cast<float*>(a.out)[o + i] = z[i];
   }
-}
-__device__ __forceinline__ bool mx4_wide(const Mx4Args& a) {
-  const uintptr_t eb = a.out_bf16 ? 2 : 4;
-  return ((reinterpret_cast<uintptr_t>(a.out) | ((uintptr_t)a.ldo * eb)) & (4 * eb - 1)) == 0;
 }
 
 // 17 hidden rows and more, 16 NB a workgroup: its 8 waves take 16 R rows of W each and
@@ -444,13 +442,12 @@ __global__ __launch_bounds__(512, NB * R <= 8 && R <= 2 ? 4 : 2) void k_mx4_wide
     }
   }
 
-  const bool wide = mx4_wide(a);
 #pragma unroll
   for (int q = 0; q < NB; ++q) {
     const int n = 16 * q + m;
     if (n >= nrows) continue;
 #pragma unroll
-    for (int r = 0; r < R; ++r) mx4_put4(a, n0 + n, v0 + 16 * r + 4 * g, acc[r][q], wide);
+    for (int r = 0; r < R; ++r) mx4_put4(a, n0 + n, v0 + 16 * r + 4 * g, acc[r][q]);
   }
 }
 
@@ -576,9 +573,8 @@ __device__ __forceinline__ bool mx4_lines(const Mx4Args& o, int v, int64_t n0, c
   // (opaque: what depends on it is formed here, not held through the main loop)
   asm volatile("" : "+v"(lane));
   const int m = lane & 15, g = lane >> 4;
-  const bool wide = ((reinterpret_cast<uintptr_t>(o.out) | ((uintptr_t)o.ldo * EB)) & 15) == 0;
-  // (8 rows by 32-bit offsets)
-  const bool full = wide && v + 64 <= o.V && n0 + 16 * NJ <= o.N && o.ldo < (1 << 26);
+  // (8 rows by 32-bit offsets; a store of 16 bytes may lie at any element boundary)
+  const bool full = v + 64 <= o.V && n0 + 16 * NJ <= o.N && o.ldo < (1 << 26);
   const int t0 = lane >> 3, c = lane & 7;
   const uint32_t off = (uint32_t)(t0 * (int)o.ldo + c * EV) * EB;
 #pragma unroll
@@ -602,15 +598,15 @@ __device__ __forceinline__ bool mx4_lines(const Mx4Args& o, int v, int64_t n0, c
         const u32x4_t x = *reinterpret_cast<const u32x4_t*>(st + t * 128 + ((c ^ (t & 7)) << 4));
         if (full) {
           char* row = static_cast<char*>(o.out) + ((n0 + 16 * j + 8 * q) * o.ldo + v + 32 * p) * EB;
-          *reinterpret_cast<u32x4_t*>(row + off) = x;
+          __builtin_memcpy(row + off, &x, 16);
           continue;
         }
         const int64_t n = n0 + 16 * j + t;
         const int vv = v + 32 * p + c * EV;
         if (n >= o.N) continue;
         char* dst = static_cast<char*>(o.out) + (n * o.ldo + vv) * EB;
-        if (wide && vv + EV <= o.V) {
-          *reinterpret_cast<u32x4_t*>(dst) = x;
+        if (vv + EV <= o.V) {
+          __builtin_memcpy(dst, &x, 16);
         } else {
 #pragma unroll
           for (int e = 0; e < EV; ++e) {
@@ -1018,13 +1014,12 @@ __global__ __launch_bounds__(256) void k_mx4_join(const float* __restrict__ part
   o.ldo = ldo;
   o.V = (int)V;
   o.out_bf16 = out_bf16;
-  const bool wide = mx4_wide(o);
   for (int64_t i = (int64_t)blockIdx.x * 256 + threadIdx.x; i < N * per; i += stride) {
     const int64_t n = i / per;
     f32x4_t z = {0.f, 0.f, 0.f, 0.f};
     for (int k = 0; k < splits; ++k)
       z += reinterpret_cast<const f32x4_t*>(part)[(int64_t)k * N * per + i];
-    mx4_put4(o, n, (int)(i - n * per) * 4, z, wide);
+    mx4_put4(o, n, (int)(i - n * per) * 4, z);
   }
 }
 
