@@ -1245,7 +1245,8 @@ def mx4_logits(hidden, codes, scales, hidden_scales=None, dtype=None, out=None, 
         ocode, ldo = _dtype_code(dtype), V
         out = torch.empty(N, V, dtype=dtype, device=dev)
     if workspace is None:
-        workspace = torch.empty(mx4_workspace_size(N, D, V, code), dtype=torch.uint8, device=dev)
+        workspace = torch.empty(mx4_workspace_size(N, D, V, code, ld), dtype=torch.uint8,
+                                device=dev)
     _check_workspace(workspace, dev)
     _call("kd_mx4_logits", dev, KdMx4Head(N, D, V, ld, ldo, code, ocode, 0), hidden, hidden_scales,
           codes, scales, out, workspace, workspace.numel())
@@ -1253,10 +1254,11 @@ def mx4_logits(hidden, codes, scales, hidden_scales=None, dtype=None, out=None, 
 
 
 @functools.lru_cache(maxsize=256)
-def mx4_workspace_size(N, D, V, dtype=KD_BF16) -> int:
-    """Bytes of workspace of mx4_logits (dtype of the hidden rows; KD_MX4: 4 bits)."""
+def mx4_workspace_size(N, D, V, dtype=KD_BF16, ld_hidden=None) -> int:
+    """Bytes of workspace of mx4_logits (dtype of the hidden rows, KD_MX4: 4 bits; their
+    row stride in elements where it is not D)."""
     n = ctypes.c_size_t(0)
-    pr = KdMx4Head(int(N), int(D), int(V), int(D), int(V), int(dtype), KD_F32, 0)
+    pr = KdMx4Head(int(N), int(D), int(V), int(ld_hidden or D), int(V), int(dtype), KD_F32, 0)
     rc = load_library().kd_mx4_logits_workspace_size(ctypes.byref(pr), ctypes.byref(n))
     if rc != 0:
         raise KdError(rc, "kd_mx4_logits_workspace_size")

@@ -83,6 +83,11 @@ struct Mx4Args {
   int64_t ldo;             // elements between output rows
   int64_t N;
   int D, V, out_bf16;
+  // k_mx4_wide: pieces of 256 columns of a range, and with several ranges their sums
+  // [range][N][Vp], which are joined afterwards
+  int per;
+  float* part;
+  int64_t Vp;
 };
 
 // Both kernels form out[n, v] = sum_d h[n, d] W[v, d] on matrix instructions, rows v of
@@ -300,7 +305,8 @@ __device__ __forceinline__ void mx4_put4(const Mx4Args& a, int64_t n, int v, f32
 
 // 17 hidden rows and more, 16 NB a workgroup: its 8 waves take 16 R rows of W each and
 // share the hidden rows' columns through LDS, a stage of 256 (fp32: 128) of them at a
-// time in two buffers, one barrier a stage. Codes go from memory to registers, those of the
+// time in two buffers, one barrier a stage. Where workgroups are few, the columns are
+// split into ranges. Codes go from memory to registers, those of the
 // next piece as soon as a half's are used.
 constexpr int kMx4Stages(int H) { return H == 1 ? 2 : 1; }  // of a piece
 constexpr int mx4_token_bytes(int H) {  // of a stage in LDS: fp32 as three terms of bf16
@@ -326,7 +332,8 @@ __global__ __launch_bounds__(512, NB * R <= 8 && R <= 2 ? 4 : 2) void k_mx4_wide
   const int nrows = (int)min((int64_t)16 * NB, a.N - n0);
   Mx4Weights<R> W;
   W.init(a, min(v0, a.V));
-  const int nb32 = W.nb32, units = (nb32 + 7) / 8;
+  const int nb32 = W.nb32;
+  const int ub = blockIdx.z * a.per, units = min(ub + a.per, (nb32 + 7) / 8);
   f32x4_t acc[R][NB];
 #pragma unroll
   for (int r = 0; r < R; ++r)
@@ -380,15 +387,15 @@ __global__ __launch_bounds__(512, NB * R <= 8 && R <= 2 ? 4 : 2) void k_mx4_wide
   };
 
   u32x4_t w[2][R];
-  W.load_scales(0, m, g);
+  W.load_scales(ub, m, g);
 #pragma unroll
-  for (int h = 0; h < 2; ++h) W.load(0, h, nb32, m, g, w[h]);
-  fetch(0);
+  for (int h = 0; h < 2; ++h) W.load(ub, h, nb32, m, g, w[h]);
+  fetch(NST * ub);
   put(0);
   __syncthreads();
   int buf = 0;
-  for (int u = 0; u < units; ++u) {
-    const int t = u & 3;
+  for (int u = ub; u < units; ++u) {
+    const int t = (u - ub) & 3;
     if (t == 0) W.turn(u, m, g);
 #pragma unroll
     for (int st = 0; st < NST; ++st) {
@@ -442,6 +449,11 @@ __global__ __launch_bounds__(512, NB * R <= 8 && R <= 2 ? 4 : 2) void k_mx4_wide
     }
   }
 
+  if (a.part != nullptr) {
+    a.out = a.part + blockIdx.z * a.N * a.Vp;
+    a.ldo = a.Vp;
+    a.out_bf16 = 0;
+  }
 #pragma unroll
   for (int q = 0; q < NB; ++q) {
     const int n = 16 * q + m;
@@ -1072,21 +1084,26 @@ static int launch_mx4_rows(const Mx4Args& a, int ks, hipStream_t s) {
   return (int)hipGetLastError();
 }
 
+static int launch_mx4_join(const KdMx4Args& q, const KdMx4Plan& p, int64_t rows, void* out,
+                           hipStream_t s) {
+  const int64_t Vp = (q.V + 3) / 4 * 4;
+  hipLaunchKernelGGL(k_mx4_join, dim3(mx4_blocks(rows * Vp / 4)), dim3(256), 0, s,
+                     reinterpret_cast<const float*>(q.ws + p.off_part), p.splits, rows, q.V, Vp, out,
+                     q.ld_out, q.out_dtype == 1);
+  return (int)hipGetLastError();
+}
+
+// hidden rows [0, o.N) of the call, at most 65535 tiles of 16 NB
 template <int H, int NB, int R>
-static int launch_mx4_wide(const Mx4Args& a, hipStream_t s) {
-  const int64_t per = 16 * NB, ty = (a.N + per - 1) / per;
-  // (the grid's second dimension holds 65535 tiles)
-  for (int64_t t = 0; t < ty; t += 65535) {
-    Mx4Args b = a;
-    b.hidden = static_cast<const char*>(a.hidden) + t * per * a.hld;
-    if (H == 2) b.hscales = a.hscales + t * per * (a.D / kMx4Block);
-    b.out = static_cast<char*>(a.out) + t * per * a.ldo * (a.out_bf16 ? 2 : 4);
-    b.N = a.N - t * per;
-    hipLaunchKernelGGL((k_mx4_wide<H, NB, R>),
-                       dim3((a.V + 128 * R - 1) / (128 * R),
-                            (unsigned)(ty - t < 65535 ? ty - t : 65535)),
-                       dim3(512), 0, s, b);
-  }
+static int launch_mx4_wide(const KdMx4Args& q, const KdMx4Plan& p, Mx4Args o, hipStream_t s) {
+  o.per = p.per;
+  o.Vp = (q.V + 3) / 4 * 4;
+  o.part = p.splits > 1 ? reinterpret_cast<float*>(q.ws + p.off_part) : nullptr;
+  hipLaunchKernelGGL((k_mx4_wide<H, NB, R>),
+                     dim3((o.V + 128 * R - 1) / (128 * R), (unsigned)((o.N + 16 * NB - 1) / (16 * NB)),
+                          (unsigned)p.splits),
+                     dim3(512), 0, s, o);
+  if (p.splits > 1) return launch_mx4_join(q, p, o.N, o.out, s);
   return (int)hipGetLastError();
 }
 
@@ -1102,34 +1119,32 @@ static int launch_mx4_scale_tiles(const uint8_t* scales, int64_t rows, int64_t D
 }
 
 template <int H>
-static int launch_mx4_gemm(const KdMx4Args& q, const Mx4Args& o, hipStream_t s) {
-  const KdMx4Plan p = kd_mx4_plan(q.N, q.D, q.V, q.dtype);
+static int launch_mx4_gemm(const KdMx4Args& q, const KdMx4Plan& p, const Mx4Args& o, hipStream_t s) {
   Mx4GemmArgs a{};
   a.o = o;
   a.wst = reinterpret_cast<uint8_t*>(q.ws + p.off_wst);
   a.T = (int)mx4_tile_steps(q.D);
   a.TV = (int)((q.V + 255) / 256);
-  a.TT = (int)((q.N + p.tok - 1) / p.tok);
+  a.TT = (int)((o.N + p.tok - 1) / p.tok);
   a.per = p.per;
   a.splits = p.splits;
   a.Vp = (q.V + 3) / 4 * 4;
   a.part = p.splits > 1 ? reinterpret_cast<float*>(q.ws + p.off_part) : nullptr;
-  if (launch_mx4_scale_tiles(q.scales, q.V, q.D, const_cast<uint8_t*>(a.wst), s) != 0) return 1;
-  a.hidden = static_cast<const char*>(q.hidden);
+  a.hidden = static_cast<const char*>(o.hidden);
   a.hld = o.hld;
   a.hbytes = (int)(H == 2 ? q.D / 2 : q.D * 2);
   if (H == 1) {
     const int64_t Dp = (q.D + 63) / 64 * 64;
     char* t = q.ws + p.off_hidden;
-    hipLaunchKernelGGL(k_mx4_terms, dim3(mx4_blocks(q.N * Dp / 8)), dim3(256), 0, s, a.hidden, o.hld,
-                       q.N, (int)q.D, (int)Dp, t);
+    hipLaunchKernelGGL(k_mx4_terms, dim3(mx4_blocks(o.N * Dp / 8)), dim3(256), 0, s, a.hidden, o.hld,
+                       o.N, (int)q.D, (int)Dp, t);
     a.hidden = t;
     a.hld = Dp * 6;
     a.hbytes = (int)(Dp * 6);
   }
   if (H == 2) {
     a.hst = reinterpret_cast<uint8_t*>(q.ws + p.off_hidden);
-    if (launch_mx4_scale_tiles(q.hscales, q.N, q.D, const_cast<uint8_t*>(a.hst), s) != 0) return 1;
+    if (launch_mx4_scale_tiles(o.hscales, o.N, q.D, const_cast<uint8_t*>(a.hst), s) != 0) return 1;
   }
   const int64_t items = (int64_t)a.TV * a.TT * p.splits;
   const dim3 grid((unsigned)(items < kMx4Units ? items : kMx4Units)), block(512);
@@ -1141,43 +1156,49 @@ static int launch_mx4_gemm(const KdMx4Args& q, const Mx4Args& o, hipStream_t s) 
     if (p.tok == 256) hipLaunchKernelGGL((k_mx4_gemm<TERMS, 8>), grid, block, 0, s, a);
     else hipLaunchKernelGGL((k_mx4_gemm<TERMS, 4>), grid, block, 0, s, a);
   }
-  if (p.splits > 1)
-    hipLaunchKernelGGL(k_mx4_join, dim3(mx4_blocks(q.N * a.Vp / 4)), dim3(256), 0, s, a.part, p.splits,
-                       q.N, q.V, a.Vp, q.out, q.ld_out, o.out_bf16);
+  if (p.splits > 1) return launch_mx4_join(q, p, o.N, o.out, s);
   return (int)hipGetLastError();
 }
 
 template <int H>
 static int launch_mx4_logits(const KdMx4Args& q, hipStream_t s) {
+  const KdMx4Plan p = kd_mx4_plan(q.N, q.D, q.V, q.dtype, q.ld_hidden);
   Mx4Args a{};
-  a.hidden = q.hidden;
   a.hld = H == 2 ? q.D / 2 : q.ld_hidden * (H == 1 ? 4 : 2);
-  a.hscales = q.hscales;
   a.codes = q.codes;
   a.scales = q.scales;
-  a.out = q.out;
   a.ldo = q.ld_out;
-  a.N = q.N;
   a.D = (int)q.D;
   a.V = (int)q.V;
   a.out_bf16 = q.out_dtype == 1;
-  // (tile rows reach by 32-bit offsets)
-  if (kd_mx4_tiles(q.N) && 256 * a.hld < ((int64_t)1 << 31)) return launch_mx4_gemm<H>(q, a, s);
-  if (q.N <= 16 && q.V <= (H == 1 || q.N > 4 ? 24576 : 49152)) {
-    const int units = (a.D / kMx4Block + 7) / 8;
-    int ks = 1;
-    while (ks < (a.V <= 16384 ? 8 : 4) && ks < units) ks *= 2;
-    if (a.V <= 6144) return launch_mx4_rows<H, 1>(a, ks, s);
-    return launch_mx4_rows<H, 2>(a, ks, s);
+  if (p.kind == KD_MX4_TILES &&
+      launch_mx4_scale_tiles(q.scales, q.V, q.D, reinterpret_cast<uint8_t*>(q.ws + p.off_wst), s) != 0)
+    return 1;
+  for (int64_t r = 0; r < q.N; r += p.rows) {
+    a.N = q.N - r < p.rows ? q.N - r : p.rows;
+    a.hidden = static_cast<const char*>(q.hidden) + r * a.hld;
+    if (H == 2) a.hscales = q.hscales + r * (q.D / kMx4Block);
+    a.out = static_cast<char*>(q.out) + r * q.ld_out * (a.out_bf16 ? 2 : 4);
+    int rc;
+    if (p.kind == KD_MX4_TILES) {
+      rc = launch_mx4_gemm<H>(q, p, a, s);
+    } else if (p.kind == KD_MX4_ROWS) {
+      rc = p.r == 1 ? launch_mx4_rows<H, 1>(a, p.ks, s) : launch_mx4_rows<H, 2>(a, p.ks, s);
+    } else if (p.nb == 1) {
+      rc = p.r == 1 ? launch_mx4_wide<H, 1, 1>(q, p, a, s) : launch_mx4_wide<H, 1, 2>(q, p, a, s);
+    } else if (p.nb == 2) {
+      rc = p.r == 1 ? launch_mx4_wide<H, 2, 1>(q, p, a, s) : launch_mx4_wide<H, 2, 2>(q, p, a, s);
+    } else if (p.r == 4) {
+      rc = launch_mx4_wide<H, 4, 4>(q, p, a, s);
+    } else if (p.r == 1) {
+      rc = launch_mx4_wide<H, 4, 1>(q, p, a, s);
+    } else {
+      if constexpr (H == 2) rc = launch_mx4_wide<H, 4, 1>(q, p, a, s);
+      else rc = launch_mx4_wide<H, 4, 2>(q, p, a, s);
+    }
+    if (rc != 0) return rc;
   }
-  // rows of W a wave (16 R): as few as leave every compute unit a workgroup
-  const int R = a.V <= 49152 ? 1 : 2;
-  if (q.N <= 16) return R == 1 ? launch_mx4_wide<H, 1, 1>(a, s) : launch_mx4_wide<H, 1, 2>(a, s);
-  if (q.N <= 32) return R == 1 ? launch_mx4_wide<H, 2, 1>(a, s) : launch_mx4_wide<H, 2, 2>(a, s);
-  if (a.V > 98304) return launch_mx4_wide<H, 4, 4>(a, s);
-  if constexpr (H != 2)
-    if (R == 2) return launch_mx4_wide<H, 4, 2>(a, s);
-  return launch_mx4_wide<H, 4, 1>(a, s);
+  return 0;
 }
 
 extern "C" int kd_launch_mx4_logits(const KdMx4Args* a, void* stream) {

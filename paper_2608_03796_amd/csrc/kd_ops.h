@@ -69,17 +69,23 @@ struct KdVerifyArgs {
   double* norm;             // [B, 4] dense draft: M, S of the target's and the draft's row
 };
 
-// Products of 65 hidden rows and more run in tiles of 256 rows of the head by `tok`
-// hidden rows, each over `per` steps of columns (64 a step, of each of three terms with
-// fp32 hidden rows; 256 with 4-bit ones); with splits > 1 the ranges' fp32 sums are
-// joined afterwards. Workspace: the head's scales, and the hidden rows' terms or scales, as
-// the tiles take them, and the ranges' sums.
+// How a product of N hidden rows with a head of V rows runs:
+//  ROWS   up to 16 hidden rows: a workgroup per 16 r rows of the head, its ks waves
+//         sharing the columns
+//  WIDE   16 nb hidden rows by 128 r of the head a workgroup, in `splits` ranges of `per`
+//         256-column pieces
+//  TILES  `tok` hidden rows by 256 of the head, in `splits` ranges of `per` steps (64
+//         columns, of each of three terms with fp32 hidden rows; 256 with 4-bit ones)
+// `rows` hidden rows at a time. Workspace: with several ranges their fp32 sums, joined
+// afterwards; for tiles the head's scales, and the hidden rows' terms or scales, as they
+// take them.
+enum { KD_MX4_ROWS = 0, KD_MX4_WIDE = 1, KD_MX4_TILES = 2 };
 struct KdMx4Plan {
-  int tok, per, splits;
+  int kind, nb, r, ks, tok, per, splits;
+  int64_t rows;
   size_t off_wst, off_hidden, off_part, total;
 };
-inline bool kd_mx4_tiles(int64_t N) { return N > 64; }
-KdMx4Plan kd_mx4_plan(int64_t N, int64_t D, int64_t V, int dtype);
+KdMx4Plan kd_mx4_plan(int64_t N, int64_t D, int64_t V, int dtype, int64_t ld_hidden);
 
 struct KdMx4Args {
   const void* hidden;       // [N, ld_hidden], or [N, D / 2] codes

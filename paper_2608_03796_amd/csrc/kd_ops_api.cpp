@@ -157,33 +157,59 @@ DraftPlan draft_plan(const kd_draft* p) {
 
 }  // namespace
 
-KdMx4Plan kd_mx4_plan(int64_t N, int64_t D, int64_t V, int dtype) {
+KdMx4Plan kd_mx4_plan(int64_t N, int64_t D, int64_t V, int dtype, int64_t ld_hidden) {
   KdMx4Plan p{};
   p.splits = 1;
-  p.total = 256;
-  if (!kd_mx4_tiles(N)) return p;
-  const int64_t tv = (V + 255) / 256;
-  // tiles of 128 hidden rows take 0.6 of the time of one of 256
-  p.tok = (N + 255) / 256 * 10 <= (N + 127) / 128 * 6 ? 256 : 128;
-  const int64_t tiles = tv * ((N + p.tok - 1) / p.tok);
-  // a range is a multiple of 256 columns (of every term), the scales' loads
-  const int64_t unit = dtype == KD_F32 ? 12 : dtype == KD_MX4 ? 1 : 4;
-  const int64_t steps = dtype == KD_MX4 ? (D + 255) / 256 : (D + 63) / 64 * (unit / 4);
-  const int64_t units = (steps + unit - 1) / unit;
-  int64_t splits = 1;
-  if (tiles <= 128) splits = std::max<int64_t>(1, std::min<int64_t>(256 / tiles, units));
-  const int64_t per = (units + splits - 1) / splits;
-  p.per = (int)(per * unit);
-  p.splits = (int)((units + per - 1) / per);
-  const int64_t T = (D / 32 + 7) / 8 * 2;
-  p.off_wst = 0;
-  p.off_hidden = align256((size_t)(tv * 4 * T * 256));
-  size_t h = 0;
-  if (dtype == KD_F32) h = (size_t)N * (size_t)((D + 63) / 64 * 64) * 6;
-  if (dtype == KD_MX4) h = (size_t)((N + 255) / 256 * 4 * T) * 256;
-  p.off_part = align256(p.off_hidden + h);
-  p.total = p.off_part;
-  if (p.splits > 1) p.total += align256((size_t)p.splits * N * ((V + 3) / 4 * 4) * 4);
+  p.rows = N;
+  const int64_t pieces = (D + 255) / 256;
+  const int64_t hld = dtype == KD_MX4 ? D / 2 : ld_hidden * elem_bytes(dtype);
+  size_t t = 0;
+  // tiles reach their hidden rows by 32-bit offsets
+  if (N > 64 && 256 * hld < ((int64_t)1 << 31)) {
+    p.kind = KD_MX4_TILES;
+    // 256 MiB of terms, and grids that the launch takes
+    const int64_t Dp = (D + 63) / 64 * 64;
+    p.rows = (int64_t)1 << 18;
+    if (dtype == KD_F32) p.rows = std::max<int64_t>(256, (((int64_t)256 << 20) / (Dp * 6)) & ~255);
+    p.rows = std::min(p.rows, N);
+    const int64_t tv = (V + 255) / 256;
+    // tiles of 128 hidden rows take 0.6 of the time of one of 256
+    p.tok = (p.rows + 255) / 256 * 10 <= (p.rows + 127) / 128 * 6 ? 256 : 128;
+    const int64_t tiles = tv * ((p.rows + p.tok - 1) / p.tok);
+    // a range is a multiple of 256 columns (of every term), the scales' loads
+    const int64_t unit = dtype == KD_F32 ? 12 : dtype == KD_MX4 ? 1 : 4;
+    const int64_t splits = tiles <= 128 ? std::min<int64_t>(256 / tiles, pieces) : 1;
+    const int64_t per = (pieces + splits - 1) / splits;
+    p.per = (int)(per * unit);
+    p.splits = (int)((pieces + per - 1) / per);
+    const int64_t T = pieces * 2;
+    p.off_wst = 0;
+    p.off_hidden = align256((size_t)(tv * 4 * T * 256));
+    t = p.off_hidden;
+    if (dtype == KD_F32) t += (size_t)(p.rows * Dp * 6);
+    if (dtype == KD_MX4) t += (size_t)((p.rows + 255) / 256 * 4 * T) * 256;
+  } else if (N <= 16 && V <= (dtype == KD_F32 || N > 4 ? 24576 : 49152)) {
+    p.kind = KD_MX4_ROWS;
+    p.r = V <= 6144 ? 1 : 2;
+    p.ks = 1;
+    while (p.ks < (V <= 16384 ? 8 : 4) && p.ks < pieces) p.ks *= 2;
+  } else {
+    p.kind = KD_MX4_WIDE;
+    p.nb = N <= 16 ? 1 : N <= 32 ? 2 : 4;
+    p.rows = std::min<int64_t>(N, (int64_t)65535 * 16 * p.nb);
+    // rows of the head a wave: as few as leave every compute unit a workgroup
+    p.r = V <= 49152 ? 1 : V <= 98304 || p.nb < 4 ? 2 : 4;
+    if (p.nb == 4 && p.r == 2 && dtype == KD_MX4) p.r = 1;
+    const int64_t groups = (V + 128 * p.r - 1) / (128 * p.r) * ((p.rows + 16 * p.nb - 1) / (16 * p.nb));
+    int64_t splits = 1;
+    if (groups <= 128) splits = std::max<int64_t>(1, std::min<int64_t>(256 / groups, pieces / 2));
+    const int64_t per = (pieces + splits - 1) / splits;
+    p.per = (int)per;
+    p.splits = (int)((pieces + per - 1) / per);
+  }
+  p.off_part = align256(t);
+  p.total = std::max<size_t>(256, p.off_part);
+  if (p.splits > 1) p.total += align256((size_t)(p.splits * p.rows * ((V + 3) / 4 * 4)) * 4);
   return p;
 }
 
@@ -331,7 +357,7 @@ kd_status kd_mx4_logits_workspace_size(const kd_mx4_head* p, size_t* bytes) {
   if (p == nullptr || bytes == nullptr) return KD_ERR_NULL_PTR;
   const kd_status st = check_head(p);
   if (st != KD_OK) return st;
-  *bytes = kd_mx4_plan(p->N, p->D, p->V, p->dtype).total;
+  *bytes = kd_mx4_plan(p->N, p->D, p->V, p->dtype, p->ld_hidden).total;
   return KD_OK;
 }
 
@@ -348,7 +374,7 @@ kd_status kd_mx4_logits(const kd_mx4_head* p, const void* hidden, const uint8_t*
   if (!aligned(hidden, 16) || !aligned(codes, 16) || !aligned(workspace, 16) ||
       !aligned(out, elem_bytes(p->out_dtype)))
     return KD_ERR_UNSUPPORTED;
-  if (workspace_bytes < kd_mx4_plan(p->N, p->D, p->V, p->dtype).total)
+  if (workspace_bytes < kd_mx4_plan(p->N, p->D, p->V, p->dtype, p->ld_hidden).total)
     return KD_ERR_WORKSPACE_TOO_SMALL;
   if (p->N == 0) return KD_OK;
   KdMx4Args a{};
