@@ -157,59 +157,71 @@ DraftPlan draft_plan(const kd_draft* p) {
 
 }  // namespace
 
+// The bounds below are fits to 300 products (N 24 to 1000, D 512 to 4096, V 1001 to 100001),
+// each timed with every kernel: the choice takes on average 1.01 of the best one's time
+// (fp32 hidden rows 1.1). bf16, us, wide and tiles: 160 x 1024 x 10001 11.4 and 22; 160 x
+// 1024 x 30001 29 and 23.8; 96 x 4096 x 3001 14.9 and 26; 96 x 4096 x 30001 68 and 46.9.
 KdMx4Plan kd_mx4_plan(int64_t N, int64_t D, int64_t V, int dtype, int64_t ld_hidden) {
   KdMx4Plan p{};
   p.splits = 1;
   p.rows = N;
+  const bool f32 = dtype == KD_F32, mx4 = dtype == KD_MX4;
   const int64_t pieces = (D + 255) / 256;
-  const int64_t hld = dtype == KD_MX4 ? D / 2 : ld_hidden * elem_bytes(dtype);
+  const int64_t hld = mx4 ? D / 2 : ld_hidden * elem_bytes(dtype);
+  auto cdiv = [](int64_t a, int64_t b) { return (a + b - 1) / b; };
+  // pieces of the workgroups of 64 hidden rows by 128 of the head
+  const int64_t work = cdiv(V, 128) * cdiv(N, 64) * pieces;
   size_t t = 0;
-  // tiles reach their hidden rows by 32-bit offsets
-  if (N > 64 && 256 * hld < ((int64_t)1 << 31)) {
+  // (tiles reach their hidden rows by 32-bit offsets)
+  if (N > 64 && work > (f32 ? 1500 : mx4 ? 4000 : 2000) && 256 * hld < ((int64_t)1 << 31)) {
     p.kind = KD_MX4_TILES;
     // 256 MiB of terms, and grids that the launch takes
-    const int64_t Dp = (D + 63) / 64 * 64;
+    const int64_t Dp = cdiv(D, 64) * 64;
     p.rows = (int64_t)1 << 18;
-    if (dtype == KD_F32) p.rows = std::max<int64_t>(256, (((int64_t)256 << 20) / (Dp * 6)) & ~255);
+    if (f32) p.rows = std::max<int64_t>(256, (((int64_t)256 << 20) / (Dp * 6)) & ~255);
     p.rows = std::min(p.rows, N);
-    const int64_t tv = (V + 255) / 256;
     // tiles of 128 hidden rows take 0.6 of the time of one of 256
-    p.tok = (p.rows + 255) / 256 * 10 <= (p.rows + 127) / 128 * 6 ? 256 : 128;
-    const int64_t tiles = tv * ((p.rows + p.tok - 1) / p.tok);
+    const int64_t tv = cdiv(V, 256);
+    p.tok = p.rows > 128 && cdiv(tv * cdiv(p.rows, 256), 256) * 10 <=
+                                cdiv(tv * cdiv(p.rows, 128), 256) * 6
+                ? 256
+                : 128;
+    const int64_t tiles = tv * cdiv(p.rows, p.tok);
     // a range is a multiple of 256 columns (of every term), the scales' loads
-    const int64_t unit = dtype == KD_F32 ? 12 : dtype == KD_MX4 ? 1 : 4;
-    const int64_t splits = tiles <= 128 ? std::min<int64_t>(256 / tiles, pieces) : 1;
-    const int64_t per = (pieces + splits - 1) / splits;
+    const int64_t unit = f32 ? 12 : mx4 ? 1 : 4, most = mx4 ? 128 : 256;
+    const int64_t splits = tiles * 2 <= most ? std::min<int64_t>(most / tiles, pieces) : 1;
+    const int64_t per = cdiv(pieces, splits);
     p.per = (int)(per * unit);
-    p.splits = (int)((pieces + per - 1) / per);
+    p.splits = (int)cdiv(pieces, per);
     const int64_t T = pieces * 2;
     p.off_wst = 0;
     p.off_hidden = align256((size_t)(tv * 4 * T * 256));
     t = p.off_hidden;
-    if (dtype == KD_F32) t += (size_t)(p.rows * Dp * 6);
-    if (dtype == KD_MX4) t += (size_t)((p.rows + 255) / 256 * 4 * T) * 256;
-  } else if (N <= 16 && V <= (dtype == KD_F32 || N > 4 ? 24576 : 49152)) {
+    if (f32) t += (size_t)(p.rows * Dp * 6);
+    if (mx4) t += (size_t)(cdiv(p.rows, 256) * 4 * T) * 256;
+  } else if (N <= 16 && V <= (f32 || N > 4 ? 24576 : 49152)) {
     p.kind = KD_MX4_ROWS;
     p.r = V <= 6144 ? 1 : 2;
     p.ks = 1;
     while (p.ks < (V <= 16384 ? 8 : 4) && p.ks < pieces) p.ks *= 2;
   } else {
     p.kind = KD_MX4_WIDE;
-    p.nb = N <= 16 ? 1 : N <= 32 ? 2 : 4;
+    p.nb = N <= 16 ? 1 : N <= 32 || (N <= 64 && !mx4 && work < 2000) ? 2 : 4;
     p.rows = std::min<int64_t>(N, (int64_t)65535 * 16 * p.nb);
     // rows of the head a wave: as few as leave every compute unit a workgroup
-    p.r = V <= 49152 ? 1 : V <= 98304 || p.nb < 4 ? 2 : 4;
-    if (p.nb == 4 && p.r == 2 && dtype == KD_MX4) p.r = 1;
-    const int64_t groups = (V + 128 * p.r - 1) / (128 * p.r) * ((p.rows + 16 * p.nb - 1) / (16 * p.nb));
+    p.r = V <= (f32 ? 16384 : 49152) ? 1 : V <= 65536 || p.nb < 4 ? 2 : 4;
+    if (p.nb == 4 && p.r == 2 && mx4) p.r = 1;
+    const int64_t groups = cdiv(V, 128 * p.r) * cdiv(p.rows, 16 * p.nb);
     int64_t splits = 1;
-    if (groups <= 128) splits = std::max<int64_t>(1, std::min<int64_t>(256 / groups, pieces / 2));
-    const int64_t per = (pieces + splits - 1) / splits;
+    if (groups <= 128 && pieces >= (f32 ? 4 : 8))
+      splits = std::max<int64_t>(1, std::min<int64_t>(256 / groups, pieces / 2));
+    const int64_t per = cdiv(pieces, splits);
     p.per = (int)per;
-    p.splits = (int)((pieces + per - 1) / per);
+    p.splits = (int)cdiv(pieces, per);
   }
   p.off_part = align256(t);
   p.total = std::max<size_t>(256, p.off_part);
-  if (p.splits > 1) p.total += align256((size_t)(p.splits * p.rows * ((V + 3) / 4 * 4)) * 4);
+  if (p.splits > 1) p.total += align256((size_t)(p.splits * p.rows * cdiv(V, 4) * 4) * 4);
   return p;
 }
 

@@ -170,13 +170,87 @@ def test_logits_long(gpu_lib, kind, N, D, V):
     _check_logits(gpu_lib, N, D, V, kind, "f32", seed=D)
 
 
+# Products of enough work for tiles (bf16 and fp32, 4 bits): widths of one to many steps,
+# with and without a last half step; tiles of 128 and 256 hidden rows; ranges of
+# columns that are joined; fewer and more items than compute units
+TILES = [
+    (300, 768, 20011), (300, 800, 40009), (600, 1632, 20003), (2000, 64, 9001), (3000, 96, 17001),
+    (3100, 32, 16411), (700, 288, 65537), (70, 8192, 5003), (129, 16384, 5500), (257, 4096, 9003),
+    (1025, 544, 24577), (90, 2080, 30001)]
+
+
+def _tiled(kd, N, D, V, kind):
+    code = {"mx4": kd.KD_MX4, "bf16": kd.KD_BF16, "f32": kd.KD_F32}[kind]
+    return kd.mx4_workspace_size(N, D, V, code) >= (V + 255) // 256 * 4 * ((D + 255) // 256 * 512)
+
+
+@pytest.mark.parametrize("kind,out", [("bf16", "f32"), ("bf16", "bf16"), ("f32", "f32"),
+                                      ("mx4", "f32"), ("mx4", "bf16")])
+@pytest.mark.parametrize("N,D,V", TILES)
+def test_logits_tiles(gpu_lib, kind, out, N, D, V):
+    _check_logits(gpu_lib, N, D, V, kind, out, seed=N + D + V)
+
+
+def test_tiles_are_reached(gpu_lib):
+    """Each kind of hidden rows takes the tiles' workspace for most of them."""
+    for kind in ("bf16", "f32", "mx4"):
+        assert sum(_tiled(gpu_lib, N, D, V, kind) for N, D, V in TILES) >= 8, kind
+
+
+def test_logits_many_passes(gpu_lib):
+    """More fp32 hidden rows than a pass's terms hold, and more rows than a pass takes."""
+    _check_logits(gpu_lib, 600, 65536, 130, "f32", "f32", seed=3)
+    kd = gpu_lib
+    N, D, V = 2 ** 18 + 5, 64, 130
+    codes, scales = _head(V, D, 5)
+    (h, _), hv = _hidden(N, D, "bf16", 5)
+    got = kd.mx4_logits(h, codes, scales, dtype=torch.float32)
+    for rows in (slice(0, 40), slice(2 ** 18 - 40, N)):
+        ref, mag = ho.mx4_logits(hv[rows], codes.cpu().numpy(), scales.cpu().numpy())
+        assert (np.abs(to64(got[rows]) - ref) <= _tol("bf16", D, mag, ref, "f32")).all()
+
+
+@pytest.mark.parametrize("N,D,V", [(3, 96, 1003), (40, 288, 1003), (100, 768, 40001)])
+def test_logits_far_apart(gpu_lib, N, D, V):
+    """Rows of hidden states and of logits so far apart that offsets pass 32 bits."""
+    kd = gpu_lib
+    codes, scales = _head(V, D, 6)
+    ldh, ldo = 2 ** 23 + 8 * 61, 2 ** 26 + 3
+    (x, _), hv = _hidden(N, D, "bf16", 6)
+    h = torch.empty(N, ldh, dtype=torch.bfloat16, device="cuda")[:, :D]
+    h.copy_(x)
+    z = torch.empty(N, ldo, dtype=torch.bfloat16, device="cuda")[:, :V]
+    z.fill_(7.0)
+    kd.mx4_logits(h, codes, scales, out=z)
+    ref, mag = ho.mx4_logits(hv, codes.cpu().numpy(), scales.cpu().numpy())
+    assert (np.abs(to64(z) - ref) <= _tol("bf16", D, mag, ref, "bf16")).all()
+    # hidden rows close together: by tiles where there is the work
+    z.fill_(7.0)
+    kd.mx4_logits(x, codes, scales, out=z)
+    assert (np.abs(to64(z) - ref) <= _tol("bf16", D, mag, ref, "bf16")).all()
+
+
 @pytest.mark.parametrize("kind", ["bf16", "f32", "mx4"])
-@pytest.mark.parametrize("N", [1, 40, 260])
-def test_logits_strides(gpu_lib, kind, N):
+def test_logits_sweep(gpu_lib, kind):
+    """Seeded sizes over the ranges of every kernel's choice."""
+    rng = np.random.default_rng({"bf16": 1, "f32": 2, "mx4": 3}[kind])
+    for i in range(24):
+        N = int(round(2 ** rng.uniform(0, 10.5)))
+        D = 32 * int(round(2 ** rng.uniform(0, 7)))
+        V = int(round(2 ** rng.uniform(0, 16)))
+        while N * D * V > 2 ** 34:
+            V = V // 2 + 1
+        print(kind, N, D, V, flush=True)
+        _check_logits(gpu_lib, N, D, V, kind, ("bf16", "f32")[i % 2], seed=100 + i)
+
+
+@pytest.mark.parametrize("kind", ["bf16", "f32", "mx4"])
+@pytest.mark.parametrize("N,D,V", [(1, 288, 1003), (40, 288, 1003), (260, 288, 1003),
+                                   (260, 288, 60003)])
+def test_logits_strides(gpu_lib, kind, N, D, V):
     """Hidden rows out of a larger tensor, logits into a padded one at an odd element:
     what lies around them is neither read nor written."""
     kd = gpu_lib
-    D, V = 288, 1003
     codes, scales = _head(V, D, 3)
     (h, hs), hv = _hidden(N, D, kind, 3)
     if kind != "mx4":
@@ -193,11 +267,11 @@ def test_logits_strides(gpu_lib, kind, N):
         assert bool((buf[:3] == 7).all()) and bool((buf[3:].view(N, V + 6)[:, V:] == 7).all())
 
 
-@pytest.mark.parametrize("N", [1, 40, 300])
-def test_logits_special_values(gpu_lib, N):
+@pytest.mark.parametrize("N,V", [(1, 600), (40, 600), (300, 600), (300, 130003)])
+def test_logits_special_values(gpu_lib, N, V):
     """Blocks that are not numbers stay with their row; infinite and huge hidden values."""
     kd = gpu_lib
-    D, V = 160, 600
+    D = 160
     codes, scales = _head(V, D, 8)
     scales[5, 2] = 255
     scales[599, 4] = 255
@@ -240,11 +314,11 @@ def test_logits_few(gpu_lib, N):
 
 
 @pytest.mark.parametrize("kind", ["bf16", "f32", "mx4"])
-@pytest.mark.parametrize("N", [4, 300])
-def test_logits_graph_and_streams(gpu_lib, kind, N):
+@pytest.mark.parametrize("N,D,V", [(4, 512, 2500), (300, 512, 2500), (40, 4096, 1500),
+                                   (300, 512, 70001), (80, 8192, 9001)])
+def test_logits_graph_and_streams(gpu_lib, kind, N, D, V):
     """The same bits from a replayed graph, from another stream, and twice in a row."""
     kd = gpu_lib
-    D, V = 512, 2500
     codes, scales = _head(V, D, 4)
     (h, hs), _ = _hidden(N, D, kind, 4)
     want = kd.mx4_logits(h, codes, scales, hidden_scales=hs, dtype=torch.float32)
