@@ -352,22 +352,30 @@ __global__ __launch_bounds__(512, NB * R <= 8 && R <= 2 ? 4 : 2) void k_mx4_wide
       const char* q = hbase + (int64_t)tok * a.hld + (int64_t)min(b, nb32 - 1) * HB +
                       (p % PT) * (16 * PV) % HB;
 #pragma unroll
-      for (int i = 0; i < PV; ++i) {
-        hv[l][i] = reinterpret_cast<const u32x4_t*>(q)[i];
-        if (b >= nb32) hv[l][i] = u32x4_t{0u, 0u, 0u, 0u};
-      }
+      for (int i = 0; i < PV; ++i) hv[l][i] = reinterpret_cast<const u32x4_t*>(q)[i];
     }
     if constexpr (H == 2) {
       const int tok = min(tid >> 3, nrows - 1), b = SB * st + (tid & 7);
       hsv = a.hscales[(n0 + tok) * nb32 + min(b, nb32 - 1)];
-      if (b >= nb32) hsv = 0;
     }
   };
   // to LDS: rows of TB bytes, 16-byte slots XORed with the token's low bits, which
   // leaves 8 lanes of a read (8 tokens, one slot) and of a write (8 slots of a token) in
-  // 8 different ones
-  auto put = [&](int buf) {
+  // 8 different ones. Zeros past the rows' end (here: a choice behind the load would wait
+  // for it there)
+  auto put = [&](int buf, int st) {
     char* s = lds + buf * STAGE;
+    if (SB * st + SB > nb32) {
+#pragma unroll
+      for (int l = 0; l < LT; ++l) {
+        const int p = tid + 512 * l;
+        if (SB * st + (p % PT) * (16 * PV) / HB >= nb32) {
+#pragma unroll
+          for (int i = 0; i < PV; ++i) hv[l][i] = u32x4_t{0u, 0u, 0u, 0u};
+        }
+      }
+      if (H == 2 && SB * st + (tid & 7) >= nb32) hsv = 0;
+    }
 #pragma unroll
     for (int l = 0; l < LT; ++l) {
       const int p = tid + 512 * l, tok = p / PT, slot = p % PT;
@@ -391,7 +399,7 @@ __global__ __launch_bounds__(512, NB * R <= 8 && R <= 2 ? 4 : 2) void k_mx4_wide
 #pragma unroll
   for (int h = 0; h < 2; ++h) W.load(ub, h, nb32, m, g, w[h]);
   fetch(NST * ub);
-  put(0);
+  put(0, NST * ub);
   __syncthreads();
   int buf = 0;
   for (int u = ub; u < units; ++u) {
@@ -443,7 +451,7 @@ __global__ __launch_bounds__(512, NB * R <= 8 && R <= 2 ? 4 : 2) void k_mx4_wide
         }
         W.load(u + 1, h, nb32, m, g, w[h]);
       }
-      if (more) put(buf ^ 1);
+      if (more) put(buf ^ 1, NST * u + st + 1);
       __syncthreads();
       buf ^= 1;
     }
