@@ -317,7 +317,7 @@ constexpr int mx4_stage_bytes(int H, int NB) {
 }
 
 template <int H, int NB, int R>
-__global__ __launch_bounds__(512, NB * R <= 8 && R <= 2 ? 4 : 2) void k_mx4_wide(Mx4Args a) {
+__global__ __launch_bounds__(512, NB * R <= 4 ? 4 : 2) void k_mx4_wide(Mx4Args a) {
   __shared__ __attribute__((aligned(16))) char lds[2 * mx4_stage_bytes(H, NB)];
   constexpr int TB = mx4_token_bytes(H), STAGE = mx4_stage_bytes(H, NB), NST = kMx4Stages(H);
   constexpr int HB = H == 0 ? 64 : H == 1 ? 128 : 16;   // bytes of a block in memory
@@ -411,14 +411,13 @@ __global__ __launch_bounds__(512, NB * R <= 8 && R <= 2 ? 4 : 2) void k_mx4_wide
       // (before the next codes: put waits for it, and not for them)
       if (more) fetch(NST * u + st + 1);
       const char* s = lds + buf * STAGE;
+      if constexpr (H == 2) {
 #pragma unroll
-      for (int hh = 0; hh < 2 / NST; ++hh) {
-        const int h = NST == 1 ? hh : st;
-        const int sb = NST == 1 ? 4 * hh + g : g;  // block of the stage
-        uint32_t ws[R];
+        for (int h = 0; h < 2; ++h) {
+          const int sb = 4 * h + g;  // block of the stage
+          uint32_t ws[R];
 #pragma unroll
-        for (int r = 0; r < R; ++r) ws[r] = W.scale(r, u, h, t, m, g);
-        if constexpr (H == 2) {
+          for (int r = 0; r < R; ++r) ws[r] = W.scale(r, u, h, t, m, g);
 #pragma unroll
           for (int q = 0; q < NB; ++q) {
             const int tok = 16 * q + m;
@@ -428,28 +427,47 @@ __global__ __launch_bounds__(512, NB * R <= 8 && R <= 2 ? 4 : 2) void k_mx4_wide
 #pragma unroll
             for (int r = 0; r < R; ++r) acc[r][q] = mx4_block<2>(w[h][r], ws[r], x, hs, acc[r][q]);
           }
-        } else {
+          W.load(u + 1, h, nb32, m, g, w[h]);
+        }
+      } else {
+        // groups of NB R MFMAs (8 columns a lane, one term); the hidden rows and the codes
+        // of a group are read and decoded while the group before it runs
+        constexpr int TERMS = H == 1 ? 3 : 1, NG = 8 / NST * TERMS;
+        u32x4_t x[2][NB], f[2][R];
+        float sc[R];
+        auto read = [&](int e) {
+          const int sb = NST == 1 ? 4 * (e / 4 / TERMS) + g : g, i = e / TERMS % 4, k = TERMS - 1 - e % TERMS;
 #pragma unroll
-          for (int i = 0; i < 4; ++i) {
-            u32x4_t f[R];
+          for (int q = 0; q < NB; ++q) {
+            const int tok = 16 * q + m;
+            x[e & 1][q] = *reinterpret_cast<const u32x4_t*>(
+                s + tok * TB + k * 256 + (((4 * sb + i) ^ (tok & 7)) << 4));
+          }
+        };
+        auto decode = [&](int e) {
+          const int h = NST == 1 ? e / 4 / TERMS : st, i = e / TERMS % 4;
+          if (i == 0) {
 #pragma unroll
             for (int r = 0; r < R; ++r)
-              f[r] = mx4_unpack8(w[h][r][i], __builtin_bit_cast(float, ws[r] << 23));
-#pragma unroll
-            for (int q = 0; q < NB; ++q) {
-              const int tok = 16 * q + m;
-#pragma unroll
-              for (int k = H == 1 ? 2 : 0; k >= 0; --k) {
-                const u32x4_t x = *reinterpret_cast<const u32x4_t*>(
-                    s + tok * TB + k * 256 + (((4 * sb + i) ^ (tok & 7)) << 4));
-#pragma unroll
-                for (int r = 0; r < R; ++r)
-                  acc[r][q] = mfma_slot(f[r], x, acc[r][q], (__bf16*)nullptr);
-              }
-            }
+              sc[r] = __builtin_bit_cast(float, W.scale(r, u, h, t, m, g) << 23);
           }
+#pragma unroll
+          for (int r = 0; r < R; ++r) f[e / TERMS & 1][r] = mx4_unpack8(w[h][r][i], sc[r]);
+          if (i == 3) W.load(u + 1, h, nb32, m, g, w[h]);
+        };
+        read(0);
+        decode(0);
+#pragma unroll
+        for (int e = 0; e < NG; ++e) {
+          if (e + 1 < NG) read(e + 1);
+          if (e + 1 < NG && (e + 1) % TERMS == 0) decode(e + 1);
+#pragma unroll
+          for (int q = 0; q < NB; ++q)
+#pragma unroll
+            for (int r = 0; r < R; ++r)
+              acc[r][q] = mfma_slot(f[e / TERMS & 1][r], x[e & 1][q], acc[r][q], (__bf16*)nullptr);
+          __builtin_amdgcn_sched_barrier(0);
         }
-        W.load(u + 1, h, nb32, m, g, w[h]);
       }
       if (more) put(buf ^ 1, NST * u + st + 1);
       __syncthreads();

@@ -157,10 +157,12 @@ DraftPlan draft_plan(const kd_draft* p) {
 
 }  // namespace
 
-// The bounds below are fits to 300 products (N 24 to 1000, D 512 to 4096, V 1001 to 100001),
-// each timed with every kernel: the choice takes on average 1.01 of the best one's time
-// (fp32 hidden rows 1.1). bf16, us, wide and tiles: 160 x 1024 x 10001 11.4 and 22; 160 x
-// 1024 x 30001 29 and 23.8; 96 x 4096 x 3001 14.9 and 26; 96 x 4096 x 30001 68 and 46.9.
+// The bounds below are fits to 400 products (N 24 to 1000, D 512 to 4096, V 1001 to 100001),
+// each timed with every kernel: the choice takes on average 1.03 of the best one's time
+// (fp32 hidden rows 1.08). bf16, us, wide and tiles: 96 x 2048 x 30001 21.9 and 33.7; 256 x
+// 2048 x 55001 69.5 and 53.9; 96 x 4096 x 55001 60.3 and 64.2; 256 x 4096 x 55001 116 and
+// 90.2. Rows of the head a wave (1, 2, 4): 64 x 4096 x 55001 48.2, 39.7, 57.8; 64 x 4096 x
+// 100001 89.6, 73.1, 58.5.
 KdMx4Plan kd_mx4_plan(int64_t N, int64_t D, int64_t V, int dtype, int64_t ld_hidden) {
   KdMx4Plan p{};
   p.splits = 1;
@@ -173,7 +175,7 @@ KdMx4Plan kd_mx4_plan(int64_t N, int64_t D, int64_t V, int dtype, int64_t ld_hid
   const int64_t work = cdiv(V, 128) * cdiv(N, 64) * pieces;
   size_t t = 0;
   // (tiles reach their hidden rows by 32-bit offsets)
-  if (N > 64 && work > (f32 ? 1500 : mx4 ? 4000 : 2000) && 256 * hld < ((int64_t)1 << 31)) {
+  if (N > 64 && work > (f32 ? 1500 : mx4 ? 4000 : 3000) && 256 * hld < ((int64_t)1 << 31)) {
     p.kind = KD_MX4_TILES;
     // 256 MiB of terms, and grids that the launch takes
     const int64_t Dp = cdiv(D, 64) * 64;
@@ -208,10 +210,12 @@ KdMx4Plan kd_mx4_plan(int64_t N, int64_t D, int64_t V, int dtype, int64_t ld_hid
     p.kind = KD_MX4_WIDE;
     p.nb = N <= 16 ? 1 : N <= 32 || (N <= 64 && !mx4 && work < 2000) ? 2 : 4;
     p.rows = std::min<int64_t>(N, (int64_t)65535 * 16 * p.nb);
-    // rows of the head a wave: as few as leave every compute unit a workgroup
-    p.r = V <= (f32 ? 16384 : 49152) ? 1 : V <= 65536 || p.nb < 4 ? 2 : 4;
-    if (p.nb == 4 && p.r == 2 && mx4) p.r = 1;
-    const int64_t groups = cdiv(V, 128 * p.r) * cdiv(p.rows, 16 * p.nb);
+    // rows of the head a wave: as many as leave most compute units a workgroup
+    const int64_t toks = cdiv(p.rows, 16 * p.nb), least = f32 ? 64 : 180;
+    p.r = 1;
+    if (cdiv(V, 256) * toks >= least && !(p.nb == 4 && mx4)) p.r = 2;
+    if (p.nb == 4 && cdiv(V, 512) * toks >= 180) p.r = 4;
+    const int64_t groups = cdiv(V, 128 * p.r) * toks;
     int64_t splits = 1;
     if (groups <= 128 && pieces >= (f32 ? 4 : 8))
       splits = std::max<int64_t>(1, std::min<int64_t>(256 / groups, pieces / 2));
