@@ -211,13 +211,14 @@ KdMx4Plan kd_mx4_plan(int64_t N, int64_t D, int64_t V, int dtype, int64_t ld_hid
     p.nb = N <= 16 ? 1 : N <= 32 || (N <= 64 && !mx4 && work < 2000) ? 2 : 4;
     p.rows = std::min<int64_t>(N, (int64_t)65535 * 16 * p.nb);
     // rows of the head a wave: as many as leave most compute units a workgroup
-    const int64_t toks = cdiv(p.rows, 16 * p.nb), least = f32 ? 64 : 180;
+    const int64_t toks = cdiv(p.rows, 16 * p.nb), least = f32 && pieces >= 8 ? 64 : 180;
     p.r = 1;
     if (cdiv(V, 256) * toks >= least && !(p.nb == 4 && mx4)) p.r = 2;
-    if (p.nb == 4 && cdiv(V, 512) * toks >= 180) p.r = 4;
+    // (two rows of 16 run a workgroup a compute unit: four where those take a second round)
+    if (p.nb == 4 && (mx4 ? cdiv(V, 512) * toks >= 180 : cdiv(V, 256) * toks > 256)) p.r = 4;
     const int64_t groups = cdiv(V, 128 * p.r) * toks;
     int64_t splits = 1;
-    if (groups <= 128 && pieces >= (f32 ? 4 : 8))
+    if (groups <= (pieces >= 8 ? 128 : f32 && pieces >= 4 ? 64 : 0))
       splits = std::max<int64_t>(1, std::min<int64_t>(256 / groups, pieces / 2));
     const int64_t per = cdiv(pieces, splits);
     p.per = (int)per;
