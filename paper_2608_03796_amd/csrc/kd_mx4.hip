@@ -504,14 +504,24 @@ __host__ __device__ constexpr int64_t mx4_tile_groups(int64_t rows) { return (ro
 // each row, writes of 256 (dword by dword, 16 bytes of a row at a time, 131072 x 128 took 38
 // us).
 constexpr int kMx4TileSteps = 32;
-__global__ __launch_bounds__(256) void k_mx4_scale_tiles(const uint8_t* __restrict__ scales,
-                                                         int64_t rows, int nb32, int T,
-                                                         uint8_t* __restrict__ out) {
+struct Mx4Scales {
+  const uint8_t* scales;
+  int64_t rows;
+  uint8_t* out;
+  int blocks;
+};
+// two matrices of as many columns: blocks [0, a.blocks) are the first one's
+__global__ __launch_bounds__(256) void k_mx4_scale_tiles(Mx4Scales a, Mx4Scales b, int nb32, int T) {
   constexpr int LD = 4 * kMx4TileSteps + 4;  // bytes of a row in LDS
   __shared__ __attribute__((aligned(4))) uint8_t lds[64 * LD];
+  const bool second = (int)blockIdx.x >= a.blocks;
+  const uint8_t* __restrict__ scales = second ? b.scales : a.scales;
+  uint8_t* __restrict__ out = second ? b.out : a.out;
+  const int64_t rows = second ? b.rows : a.rows;
+  const int block = (int)blockIdx.x - (second ? a.blocks : 0);
   const int per = (T + kMx4TileSteps - 1) / kMx4TileSteps;
-  const int64_t G = blockIdx.x / per;
-  const int t0 = (int)(blockIdx.x - G * per) * kMx4TileSteps, b0 = 4 * t0;
+  const int64_t G = block / per;
+  const int t0 = (int)(block - G * per) * kMx4TileSteps, b0 = 4 * t0;
   // 4 bytes a thread: 32 threads a row
   const int c = (threadIdx.x & 31) * 4;
   for (int r = threadIdx.x >> 5; r < 64; r += 8) {
@@ -1135,17 +1145,21 @@ static int launch_mx4_wide(const KdMx4Args& q, const KdMx4Plan& p, Mx4Args o, hi
 
 constexpr int64_t kMx4Units = 256;  // compute units
 
-static int launch_mx4_scale_tiles(const uint8_t* scales, int64_t rows, int64_t D, uint8_t* out,
-                                  hipStream_t s) {
-  const int64_t T = mx4_tile_steps(D), groups = mx4_tile_groups(rows);
-  const int64_t blocks = groups * ((T + kMx4TileSteps - 1) / kMx4TileSteps);
-  hipLaunchKernelGGL(k_mx4_scale_tiles, dim3((unsigned)blocks), dim3(256), 0, s, scales, rows,
-                     (int)(D / kMx4Block), (int)T, out);
+static Mx4Scales mx4_scales(const uint8_t* scales, int64_t rows, int64_t D, void* out) {
+  const int64_t per = (mx4_tile_steps(D) + kMx4TileSteps - 1) / kMx4TileSteps;
+  return Mx4Scales{scales, rows, static_cast<uint8_t*>(out), (int)(mx4_tile_groups(rows) * per)};
+}
+static int launch_mx4_scale_tiles(const Mx4Scales& a, const Mx4Scales& b, int64_t D, hipStream_t s) {
+  if (a.blocks + b.blocks == 0) return 0;
+  hipLaunchKernelGGL(k_mx4_scale_tiles, dim3((unsigned)(a.blocks + b.blocks)), dim3(256), 0, s, a, b,
+                     (int)(D / kMx4Block), (int)mx4_tile_steps(D));
   return (int)hipGetLastError();
 }
 
+// hidden rows of one pass; the head's scales come with the first
 template <int H>
-static int launch_mx4_gemm(const KdMx4Args& q, const KdMx4Plan& p, const Mx4Args& o, hipStream_t s) {
+static int launch_mx4_gemm(const KdMx4Args& q, const KdMx4Plan& p, const Mx4Args& o, bool first,
+                           hipStream_t s) {
   Mx4GemmArgs a{};
   a.o = o;
   a.wst = reinterpret_cast<uint8_t*>(q.ws + p.off_wst);
@@ -1168,10 +1182,12 @@ static int launch_mx4_gemm(const KdMx4Args& q, const KdMx4Plan& p, const Mx4Args
     a.hld = Dp * 6;
     a.hbytes = (int)(Dp * 6);
   }
-  if (H == 2) {
-    a.hst = reinterpret_cast<uint8_t*>(q.ws + p.off_hidden);
-    if (launch_mx4_scale_tiles(o.hscales, o.N, q.D, const_cast<uint8_t*>(a.hst), s) != 0) return 1;
-  }
+  if (H == 2) a.hst = reinterpret_cast<uint8_t*>(q.ws + p.off_hidden);
+  const Mx4Scales none{nullptr, 0, nullptr, 0};
+  if (launch_mx4_scale_tiles(
+          first ? mx4_scales(q.scales, q.V, q.D, q.ws + p.off_wst) : none,
+          H == 2 ? mx4_scales(o.hscales, o.N, q.D, q.ws + p.off_hidden) : none, q.D, s) != 0)
+    return 1;
   const int64_t items = (int64_t)a.TV * a.TT * p.splits;
   const dim3 grid((unsigned)(items < kMx4Units ? items : kMx4Units)), block(512);
   if constexpr (H == 2) {
@@ -1197,9 +1213,6 @@ static int launch_mx4_logits(const KdMx4Args& q, hipStream_t s) {
   a.D = (int)q.D;
   a.V = (int)q.V;
   a.out_bf16 = q.out_dtype == 1;
-  if (p.kind == KD_MX4_TILES &&
-      launch_mx4_scale_tiles(q.scales, q.V, q.D, reinterpret_cast<uint8_t*>(q.ws + p.off_wst), s) != 0)
-    return 1;
   for (int64_t r = 0; r < q.N; r += p.rows) {
     a.N = q.N - r < p.rows ? q.N - r : p.rows;
     a.hidden = static_cast<const char*>(q.hidden) + r * a.hld;
@@ -1207,7 +1220,7 @@ static int launch_mx4_logits(const KdMx4Args& q, hipStream_t s) {
     a.out = static_cast<char*>(q.out) + r * q.ld_out * (a.out_bf16 ? 2 : 4);
     int rc;
     if (p.kind == KD_MX4_TILES) {
-      rc = launch_mx4_gemm<H>(q, p, a, s);
+      rc = launch_mx4_gemm<H>(q, p, a, r == 0, s);
     } else if (p.kind == KD_MX4_ROWS) {
       rc = p.r == 1 ? launch_mx4_rows<H, 1>(a, p.ks, s) : launch_mx4_rows<H, 2>(a, p.ks, s);
     } else if (p.nb == 1) {
