@@ -2453,7 +2453,12 @@ extern "C" int kd_launch_scale(const KdScaleArg* a, const KdScaleArg* b, const f
                                void* stream) {
   hipStream_t s = static_cast<hipStream_t>(stream);
   auto arg = [](const KdScaleArg* q) { return ScaleArg{q->x, q->y, q->n, q->out_bf16}; };
-  auto blocks = [](int64_t n) { return (int)std::min<int64_t>((n + 2047) / 2048, 8192); };
+  // two pieces a thread where there are many: the fewer the workgroups, the farther apart
+  // what they touch at a time
+  auto blocks = [](int64_t n) {
+    const int64_t b = (n + 2047) / 2048;
+    return (int)std::min<int64_t>(b <= 8192 ? b : std::max<int64_t>(8192, (b + 1) / 2), 1 << 22);
+  };
   const int ba = blocks(a->n), bb = blocks(b->n);
   if (ba + bb == 0) return 0;
   hipLaunchKernelGGL(k_scale, dim3(ba + bb), dim3(256), 0, s, arg(a), arg(b), ba, g);
