@@ -657,7 +657,12 @@ typedef struct kd_mx4_head {
   int32_t flags;       /* 0                                                  */
 } kd_mx4_head;
 
-/* Bytes of device workspace kd_mx4_logits needs. Pure host function. */
+/*
+ * Bytes of device workspace kd_mx4_logits needs: 256 for most products of up to 64
+ * hidden rows; for larger ones 1/32 of a byte an element of the head and of 4-bit hidden
+ * rows, or 6 an element of fp32 ones (at most 256 MiB at a time); and up to 64 MiB of
+ * sums where the columns are split into ranges. Pure host function.
+ */
 kd_status kd_mx4_logits_workspace_size(const kd_mx4_head* p, size_t* bytes);
 
 /*

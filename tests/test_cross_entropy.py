@@ -260,6 +260,55 @@ def test_graph(gpu_lib, z):
             assert torch.equal(out[k], want[k]), k
 
 
+def test_two_at_a_time(gpu_lib):
+    """Calls that overlap on streams of their own, and graphs that share a workspace."""
+    kd = gpu_lib
+    N, D, V = 500, 256, 3000
+    sets = []
+    for seed in (1, 2):
+        h, W, lab = _inputs(N, D, V, "bf16", "some", seed)
+        sets.append((h, W, lab, kd.ce_fwd_bwd(h, W, lab, z_loss=1e-3), torch.cuda.Stream()))
+    torch.cuda.synchronize()
+    got = []
+    for _ in range(3):
+        for h, W, lab, want, s in sets:
+            with torch.cuda.stream(s):
+                got.append((kd.ce_fwd_bwd(h, W, lab, z_loss=1e-3), want))
+    torch.cuda.synchronize()
+    for a, b in got:
+        assert all(torch.equal(a[k], b[k]) for k in b)
+    ws = torch.empty(kd.ce_workspace_size(N, D, V), dtype=torch.uint8, device="cuda")
+    graphs, outs = [], []
+    for h, W, lab, want, s in sets:
+        out = {k: torch.zeros_like(v) for k, v in want.items()}
+        g = torch.cuda.CUDAGraph()
+        with torch.cuda.graph(g):
+            kd.ce_fwd_bwd(h, W, lab, z_loss=1e-3, workspace=ws, out=out)
+        graphs.append(g)
+        outs.append(out)
+    for _ in range(3):
+        for g in graphs:
+            g.replay()
+        torch.cuda.synchronize()
+        for out, s in zip(outs, sets):
+            assert all(torch.equal(out[k], s[3][k]) for k in out)
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+def test_many_groups(gpu_lib, dtype):
+    """More tokens than a contraction gathers and than the scan takes labels for, most of
+    them ignored in stretches."""
+    kd = gpu_lib
+    N, D, V = 20000, 64, 257
+    h, W, lab = _inputs(N, D, V, dtype, "some", 23)
+    lab[3000:17000] = -100
+    ref = _ref(h, W, lab, z_loss=1e-3)
+    got = kd.ce_fwd_bwd(h, W, lab, z_loss=1e-3, chunk=1000, loss_per_token=True)
+    _check(got, ref, dtype, h, W, lab)
+    f = kd.ce_fwd(h, W, lab, z_loss=1e-3, chunk=1000)
+    _check(kd.ce_bwd(h, W, lab, f["saved_logz"], z_loss=1e-3, chunk=1000), ref, dtype, h, W, lab)
+
+
 def test_captured_autograd_step(gpu_lib):
     kd = gpu_lib
     h, W, lab = _inputs(200, 128, 1500, "bf16", "some", 17)
@@ -294,6 +343,8 @@ def test_refusals(gpu_lib):
                 lambda: kd.ce_bwd(h, W, lab, torch.zeros(20, device="cuda"),
                                   grad_loss=torch.ones(2, device="cuda")),
                 lambda: kd.ce_fwd_bwd(h, W, lab, grad_W_out=torch.zeros(100, 32, device="cuda")),
+                lambda: kd.ce_fwd_bwd(h, W, lab, accumulate_grad_W=True),
+                lambda: kd.ce_bwd(h, W, lab, torch.zeros(20, device="cuda"), accumulate_grad_W=True),
                 lambda: kd.ce_fwd_bwd(h, W, lab, workspace=torch.empty(9, device="cuda"))):
         with pytest.raises(ValueError):
             bad()

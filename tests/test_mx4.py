@@ -305,6 +305,73 @@ def test_logits_special_values(gpu_lib, N, V):
     assert (np.abs(np.delete(got, 3, axis=1) - ref) <= ref * 2.0 ** -22).all()
 
 
+@pytest.mark.parametrize("N,V", [(3, 600), (40, 600), (300, 130003)])
+def test_hidden_block_not_a_number(gpu_lib, N, V):
+    """A 4-bit hidden row with such a block has no number in its logits, the others do."""
+    kd = gpu_lib
+    D = 416
+    codes, scales = _head(V, D, 8)
+    (h, hs), hv = _hidden(N, D, "mx4", 9)
+    hs[N - 1, 12] = 255
+    got = kd.mx4_logits(h, codes, scales, hidden_scales=hs, dtype=torch.float32)
+    assert bool(got[N - 1].isnan().all()) and bool(got[:N - 1].isfinite().all())
+
+
+@pytest.mark.parametrize("kind", ["bf16", "f32", "mx4"])
+@pytest.mark.parametrize("N,D,V", [(40, 4096, 1500), (300, 512, 70001)])
+def test_logits_two_at_a_time(gpu_lib, kind, N, D, V):
+    """Two calls that overlap on streams of their own, and two captured graphs that
+    share a workspace one after the other."""
+    kd = gpu_lib
+    code = {"mx4": kd.KD_MX4, "bf16": kd.KD_BF16, "f32": kd.KD_F32}[kind]
+    n = kd.mx4_workspace_size(N, D, V, code)
+    sets = []
+    for seed in (1, 2):
+        codes, scales = _head(V, D, seed)
+        (h, hs), _ = _hidden(N, D, kind, seed)
+        want = kd.mx4_logits(h, codes, scales, hidden_scales=hs, dtype=torch.float32)
+        sets.append((h, hs, codes, scales, want, torch.zeros_like(want), torch.cuda.Stream()))
+    torch.cuda.synchronize()
+    for _ in range(5):
+        for h, hs, codes, scales, want, out, s in sets:
+            with torch.cuda.stream(s):
+                kd.mx4_logits(h, codes, scales, hidden_scales=hs, out=out)
+    torch.cuda.synchronize()
+    for *_, want, out, _ in sets:
+        assert torch.equal(out, want)
+    ws = torch.empty(n, dtype=torch.uint8, device="cuda")
+    graphs = []
+    for h, hs, codes, scales, want, out, s in sets:
+        g = torch.cuda.CUDAGraph()
+        with torch.cuda.graph(g):
+            kd.mx4_logits(h, codes, scales, hidden_scales=hs, out=out, workspace=ws)
+        graphs.append(g)
+    for _ in range(3):
+        for s in sets:
+            s[5].zero_()
+        for g in graphs:
+            g.replay()
+        torch.cuda.synchronize()
+        for *_, want, out, _ in sets:
+            assert torch.equal(out, want)
+
+
+def test_write_read_graph(gpu_lib):
+    kd = gpu_lib
+    x = torch.randn(100, 256, generator=_gen(1), device="cuda")
+    q = kd.mx4_write(x)
+    back = kd.mx4_read(q["codes"], q["scales"], torch.bfloat16)
+    g = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(g):
+        kd.mx4_write(x, out=q)
+        kd.mx4_read(q["codes"], q["scales"], torch.bfloat16, out=back)
+    for seed in (2, 3, 4):
+        x.copy_(torch.randn(100, 256, generator=_gen(seed), device="cuda"))
+        g.replay()
+        torch.cuda.synchronize()
+        _same(back, ho.mx4_read(*ho.mx4_write(to64(x))))
+
+
 @pytest.mark.parametrize("N", [0, 1])
 def test_logits_few(gpu_lib, N):
     kd = gpu_lib
