@@ -1135,7 +1135,8 @@ def cross_entropy(hidden, W, labels, z_loss: float = 0.0, chunk: int = 4096,
     "recompute" saves ln Z only. In bf16 the fused grad_W is 2.8e-3 off in the 2-norm
     (its contraction has the hidden rows times their tokens' factors, rounded to bf16;
     the final rounding alone is 1.7e-3), the recomputed one 2.3e-3. Without a gradient
-    wanted, the loss alone is computed."""
+    wanted, the loss alone is computed. Capture a step into a graph with no eager loss of
+    the same hidden or W alive: torch ties their gradients to the stream of the first."""
     import torch
     global _CE
     if schedule not in ("fused", "recompute"):

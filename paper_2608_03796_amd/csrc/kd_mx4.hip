@@ -1,6 +1,11 @@
 // HIP kernels (gfx950) of 4-bit microscaled numbers and their launchers:
 //   mx4_write, mx4_read    a matrix to codes and scales, and back
-//   mx4_rows               logits of few hidden rows with a head of such numbers
+//   logits of hidden rows with a head W of such numbers, by the rule of kd_mx4_plan:
+//   mx4_rows               few hidden rows, small heads
+//   mx4_wide               few hidden rows
+//   [mx4_terms,] mx4_scale_tiles, mx4_gemm     many, in bf16 (fp32 ones as three terms)
+//   mx4_scale_tiles, mx4_gemm4                 many, in 4 bits
+//   each of the last three with mx4_join where its columns are split into ranges
 #include "kd_mx4.h"
 #include "kd_ops.h"
 
@@ -16,7 +21,8 @@ __device__ __forceinline__ void mx4_store(V v, V* p) {
   else *p = v;
 }
 
-// Eight elements a thread, four threads a block of 32.
+// Eight elements a thread, four threads a block of 32. Bound by memory: 131072 x 4096 in
+// bf16 216 us, 6.3 TB/s of matrix, codes and scales; back 226 us, 6.0 TB/s.
 template <typename T>
 __global__ __launch_bounds__(256) void k_mx4_write(const T* __restrict__ x, int64_t n8,
                                                    uint32_t* __restrict__ codes,
@@ -192,7 +198,10 @@ __device__ __forceinline__ void mx4_cut(u32x4_t lo, u32x4_t hi, u32x4_t (&t)[3])
   cut8(f, t);
 }
 
-// Up to 16 hidden rows. Bound by reading W: a workgroup takes 16 R rows of it, whose
+// Up to 16 hidden rows and a small W, whose workgroups would be too few if each took more
+// of it. Bound by latency: 8000 x 4096 for one row 6.8 us (k_mx4_wide 19), 2000 x 1024 2.8
+// (5.5); from 32000 rows of W on its hidden rows' reads cost more (16 rows of 32000 x 4096
+// 26.5 us, k_mx4_wide 21). A workgroup takes 16 R rows of it, whose
 // columns its waves share, a range of pieces each, with the next piece's codes in flight;
 // nothing of W passes through LDS. Hidden rows come from the caches. The waves' sums
 // are added in LDS in order. Columns behind the last hidden row hold that row again
@@ -303,11 +312,15 @@ __device__ __forceinline__ void mx4_put4(const Mx4Args& a, int64_t n, int v, f32
   }
 }
 
-// 17 hidden rows and more, 16 NB a workgroup: its 8 waves take 16 R rows of W each and
-// share the hidden rows' columns through LDS, a stage of 256 (fp32: 128) of them at a
-// time in two buffers, one barrier a stage. Where workgroups are few, the columns are
-// split into ranges. Codes go from memory to registers, those of the
-// next piece as soon as a half's are used.
+// 16 NB hidden rows a workgroup: its 8 waves take 16 R rows of W each and share the hidden
+// rows' columns through LDS, a stage of 256 (fp32: 128) of them at a time in two
+// buffers, one barrier a stage. Where workgroups are few, the columns are split into
+// ranges. Codes go from memory to registers, those of the next piece as soon as a
+// half's are used. Bound by reading W while hidden rows are few: 131072 x 4096 for 1 row
+// 54 us (5.3 TB/s; reading alone 48 at 5.6), for 16 57, for 32 66; 64 rows 77, whose MFMAs
+// take 30 and which one workgroup a compute unit does not hide entirely (R = 4; fewer
+// rows a wave read the hidden rows from LDS more often: R = 2 106). 4-bit rows 51, 57, 66 us
+// (16, 32, 64), fp32 rows 79, 120, 165.
 constexpr int kMx4Stages(int H) { return H == 1 ? 2 : 1; }  // of a piece
 constexpr int mx4_token_bytes(int H) {  // of a stage in LDS: fp32 as three terms of bf16
   return H == 0 ? 512 : H == 1 ? 768 : 128;
@@ -708,8 +721,9 @@ __device__ __forceinline__ void mx4_pair(int q, int& i, int& j0, int& j1) {
 // 128 bytes each in three stages, codes 32 bytes a row in two, scales of up to four steps
 // in three, all by LDS-DMA two steps ahead; one barrier a step. A wave's 4 row blocks of W are
 // decoded in registers between the MFMAs of the half step before their use: a block's
-// codes are read from LDS twice (by two waves) and take an eighth of bf16's bytes, so that
-// the LDS, which bounds the bf16 tiles of the loss, has a quarter of its time left.
+// codes are read from LDS twice (by two waves) and take a quarter of bf16's bytes: the LDS,
+// which bounds the bf16 tiles of the loss, is active 30% of the time, the MFMAs 73% at the
+// clock that power leaves. 4096 x 4096 x 131072: 2.92 ms, 1.5 PFLOP/s.
 // The steps of a workgroup's items form one sequence: a tile's last steps load the next
 // tile's first ones, and its logits are stored under that tile's first step.
 template <int TERMS, int NJ>
@@ -923,7 +937,9 @@ __device__ __forceinline__ f32x4_t mfma_mx4_at(u32x4_t a, u32x4_t b, f32x4_t c, 
 // two stages by LDS-DMA, two scaled MFMAs a block pair. The second half of a step
 // issues the loads of the step after the next, into the stage whose last
 // fragments were read in its first half; the barrier between the halves waits for
-// those of the next step.
+// those of the next step. 4096 x 4096 x 131072: 1.10 ms, 4.0 PFLOP/s with the MFMAs 50% busy;
+// 0.95 without the loads, 0.82 with neither these nor the fragments' reads, 0.15 of each the
+// logits' stores.
 template <int NJ>
 __global__ __launch_bounds__(512, 1) void k_mx4_gemm4(Mx4GemmArgs a) {
   constexpr int TOK = 32 * NJ, HST = TOK * 128, CST = 256 * 128, SST = 8192;
