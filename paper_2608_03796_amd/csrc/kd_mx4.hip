@@ -133,7 +133,7 @@ struct Mx4Weights {
   }
   // scale bytes of pieces u .. u + 3: lane (m, g) holds the 8 of piece u + g, row m. (A
   // byte a piece and lane fetched each line of the scales once a piece, as many
-  // requests as the codes': one row of 131072 x 4096 81 us, now 61.)
+  // requests as the codes': one row of 131072 x 4096 81 us, this way, at that time, 61.)
   __device__ __forceinline__ void load_scales(int u, int m, int g) {
     const int b = 8 * (u + g);
 #pragma unroll
@@ -199,7 +199,7 @@ __device__ __forceinline__ void mx4_cut(u32x4_t lo, u32x4_t hi, u32x4_t (&t)[3])
 }
 
 // Up to 16 hidden rows and a small W, whose workgroups would be too few if each took more
-// of it. Bound by latency: 8000 x 4096 for one row 6.8 us (k_mx4_wide 19), 2000 x 1024 2.8
+// of it. Bound by latency: 8000 x 4096 for one row 6.8 us (k_mx4_wide 19), 2000 x 1024 2.9
 // (5.5); from 32000 rows of W on its hidden rows' reads cost more (16 rows of 32000 x 4096
 // 26.5 us, k_mx4_wide 21). A workgroup takes 16 R rows of it, whose
 // columns its waves share, a range of pieces each, with the next piece's codes in flight;
@@ -316,11 +316,11 @@ __device__ __forceinline__ void mx4_put4(const Mx4Args& a, int64_t n, int v, f32
 // rows' columns through LDS, a stage of 256 (fp32: 128) of them at a time in two
 // buffers, one barrier a stage. Where workgroups are few, the columns are split into
 // ranges. Codes go from memory to registers, those of the next piece as soon as a
-// half's are used. Bound by reading W while hidden rows are few: 131072 x 4096 for 1 row
-// 54 us (5.3 TB/s; reading alone 48 at 5.6), for 16 57, for 32 66; 64 rows 77, whose MFMAs
-// take 30 and which one workgroup a compute unit does not hide entirely (R = 4; fewer
-// rows a wave read the hidden rows from LDS more often: R = 2 106). 4-bit rows 51, 57, 66 us
-// (16, 32, 64), fp32 rows 79, 120, 165.
+// half's are used. Bound by reading W while hidden rows are few: 131072 x 4096, one launch
+// after the other, for 1 row 55 us (5.2 TB/s; reading alone 48 at 5.6), for 16 60, for 32 70;
+// 64 rows 82, whose MFMAs take 30 and which one workgroup a compute unit does not hide
+// entirely (R = 4; fewer rows of W a wave read the hidden rows from LDS more often: R = 2
+// 104). 4-bit rows 50, 56, 66 us (16, 32, 64), fp32 rows 79, 115, 164.
 constexpr int kMx4Stages(int H) { return H == 1 ? 2 : 1; }  // of a piece
 constexpr int mx4_token_bytes(int H) {  // of a stage in LDS: fp32 as three terms of bf16
   return H == 0 ? 512 : H == 1 ? 768 : 128;
@@ -374,8 +374,9 @@ __global__ __launch_bounds__(512, NB * R <= 4 ? 4 : 2) void k_mx4_wide(Mx4Args a
   };
   // to LDS: rows of TB bytes, 16-byte slots XORed with the token's low bits, which
   // leaves 8 lanes of a read (8 tokens, one slot) and of a write (8 slots of a token) in
-  // 8 different ones. Zeros past the rows' end (here: a choice behind the load would wait
-  // for it there)
+  // 8 different ones. (With 64 bf16 rows a counter still gives conflicts 9% of the time; other
+  // slots changed nothing.) Zeros past the rows' end (here: a choice behind the load would
+  // wait for it there)
   auto put = [&](int buf, int st) {
     char* s = lds + buf * STAGE;
     if (SB * st + SB > nb32) {
@@ -742,7 +743,7 @@ __global__ __launch_bounds__(512, 1) void k_mx4_gemm(Mx4GemmArgs a) {
   const int hslot = ((lane & 7) ^ (lane >> 3)) << 4;
   const uint32_t hoff = (uint32_t)(lane >> 3) * (uint32_t)a.hld + (uint32_t)hslot;
   // codes: rows 32 wave .. + 31, the 16-byte halves exchanged for every other 8 rows (the
-  // reads of 16 rows then touch each bank once)
+  // 4-byte reads still conflict two ways, a sixth of the LDS's active time)
   const int crow = 32 * wave + (lane >> 1);
   const uint32_t coff = (uint32_t)crow * (uint32_t)pitch + (((lane & 1) ^ ((crow >> 3) & 1)) << 4);
   const uint32_t soff = (uint32_t)((wave & 3) * a.T * 256 + lane * 4);
