@@ -237,6 +237,39 @@ def test_empty(gpu_lib):
     assert out["grad_hidden"].shape == (0, 64)
 
 
+@pytest.mark.parametrize("schedule", ["fused", "recompute"])
+@pytest.mark.parametrize("dtype", [torch.bfloat16, torch.float32])
+@pytest.mark.parametrize("N", [0, 3])
+def test_no_labels_autograd(gpu_lib, N, dtype, schedule):
+    """No token, and none with a label: a loss of 0 and gradients of 0."""
+    kd = gpu_lib
+    h = torch.ones(N, 64, device="cuda", dtype=dtype, requires_grad=True)
+    W = torch.ones(10, 64, device="cuda", dtype=dtype, requires_grad=True)
+    lab = torch.tensor([-100, 10, 1 << 40][:N], dtype=torch.int64, device="cuda")
+    loss = kd.cross_entropy(h, W, lab, z_loss=1e-3, schedule=schedule)
+    loss.backward()
+    assert float(loss.detach()) == 0 and h.grad.shape == h.shape
+    assert not h.grad.any() and not W.grad.any()
+
+
+def test_ignored_upstream_not_a_number(gpu_lib):
+    """An ignored token's upstream gradient, logit row and ln Z reach no result."""
+    kd = gpu_lib
+    h, W, lab = _inputs(130, 64, 700, "f32", "some", 19)
+    keep = (lab >= 0) & (lab < 700)
+    assert keep.any() and not keep.all()
+    up = torch.ones(130, device="cuda")
+    logz = kd.ce_fwd(h, W, lab)["saved_logz"]
+    want = kd.ce_bwd(h, W, lab, logz, grad_loss_per_token=up)
+    h2, up2, logz2 = h.clone(), up.clone(), logz.clone()
+    h2[~keep], up2[~keep], logz2[~keep] = float("nan"), float("nan"), float("nan")
+    got = kd.ce_bwd(h2, W, lab, logz2, grad_loss_per_token=up2)
+    for k in want:
+        assert torch.equal(got[k], want[k]), k
+    for k, v in kd.ce_fwd_bwd(h, W, lab).items():
+        assert torch.equal(v, kd.ce_fwd_bwd(h2, W, lab)[k]), k
+
+
 @pytest.mark.parametrize("z", [0.0, 1e-3])
 def test_graph(gpu_lib, z):
     """A captured step replays with new inputs, on workspaces full of anything."""
