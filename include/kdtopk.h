@@ -371,7 +371,8 @@ typedef struct kd_label_problem {
   int64_t N, D, V, chunk;  /* as in kd_problem                                 */
   int32_t dtype;           /* kd_dtype of hidden, W and grad_hidden             */
   float z_loss;            /* finite and >= 0                                   */
-  int32_t flags;           /* 0 or KD_FLAG_GRAD_HIDDEN_F32                      */
+  int32_t flags;           /* 0 or KD_FLAG_GRAD_HIDDEN_F32 (with a part for
+                              grad_W too: see kd_cross_entropy_fwd_bwd)         */
 } kd_label_problem;
 
 /* Workspace of the three calls below: kd_topk_kl_workspace_size's for K = 1, and 9
@@ -385,6 +386,13 @@ kd_status kd_cross_entropy_workspace_size(const kd_label_problem* p, size_t* byt
  * teacher's arrays and the mask; the other arguments, their results on ignored tokens,
  * and the errors are those calls' (KD_ERR_BAD_ARG also for z_loss). KD_DEBUG_CHECK
  * has nothing to check here.
+ *
+ * In bf16 the entries of dL/dz are held in bf16 on their way into the gradients, and with
+ * one projection the hidden rows are rounded to bf16 once more for grad_W. With
+ * KD_FLAG_GRAD_HIDDEN_F32, kd_cross_entropy_fwd_bwd keeps this off each token's label:
+ * its part of both gradients (of grad_W alone too, with grad_hidden NULL) is formed in
+ * fp32. Without the flag results are bitwise kd_topk_kl_fwd_bwd's for a teacher of one
+ * entry.
  */
 kd_status kd_cross_entropy_fwd_bwd(const kd_label_problem* p, const void* hidden, const void* W,
                                    const int64_t* labels, float* loss, float* loss_per_token,

@@ -437,6 +437,10 @@ kd_status enqueue(const kd_problem* p, const Plan& pl, const Call& c) {
   // the single-projection schedule stores dZ up to a factor per row, which
   // dH applies to its rows and dW to the hidden rows
   const bool scaled = fwd && bwd && (want_dh || want_dw);
+  // gradients of labels in fp32: dZ's rounding to bf16, and the scaled hidden rows', are
+  // kept off the label's entry, most of a row of dL/dz until a student is sure of it
+  const bool label_part = c.labels != nullptr && scaled && p->dtype == KD_BF16 &&
+                          (p->flags & KD_FLAG_GRAD_HIDDEN_F32) != 0;
   // With a mask, every entry point leaves the ignored tokens out (their loss
   // and gradient rows are 0): each dW group's other tokens are gathered
   // first, and the group's rows are those tokens in order, then rows without
@@ -486,6 +490,9 @@ kd_status enqueue(const kd_problem* p, const Plan& pl, const Call& c) {
     a.grad_hidden = want_dh ? c.grad_hidden : nullptr;
     a.gh_f32 = (p->flags & KD_FLAG_GRAD_HIDDEN_F32) ? 1 : 0;
     a.lpt_full = c.lpt;
+    // (the teacher's logits, 0 by the labels' conversion, are read by the rows'
+    // preparation alone, before their cells are formed)
+    a.label_w = label_part ? const_cast<float*>(c.tlogit) : nullptr;
     a.rowmap = compact ? rowmap + g : nullptr;
     a.nrow = compact ? gnrow : nullptr;
     a.nrow_base = (int)g;
@@ -617,6 +624,12 @@ kd_status enqueue(const kd_problem* p, const Plan& pl, const Call& c) {
       dw_done = true;
     }
     group_tokens = 0;
+  }
+  if (label_part) {
+    KdChunkArgs a = chunk_args(0, (int)pl.N, 0, 0, KD_STAGE_LABELS);
+    a.labels = c.labels;
+    a.grad_W = want_dw ? c.grad_W : nullptr;
+    if (kd_launch_chunk(&a, c.stream) != 0) return KD_ERR_DEVICE;
   }
   if (fwd && pl.nchunks == 0) {
     KdTailArgs tail{};

@@ -1274,8 +1274,10 @@ __global__ void k_row_loss(const float* zhit, const float* p, int K, const float
 // cells (g/tau)(M q - p) (Eq. 3) in the row's stored scale (0 where the
 // factor is 0, i.e. on ignored rows); and the token's loss (Eq. 2) with a
 // partial per block of kLossRows rows as k_row_loss forms it. With a z-loss, M is
-// M + 2 z_loss log Z in the factor and the cells. With a rowmap, row r is token rowmap[r] (loss_per_token is then indexed by token), and a
-// row without a token (-1) only gets a row factor of 0 and a loss of 0.
+// M + 2 z_loss log Z in the factor and the cells. With a rowmap, row r is token rowmap[r]
+// (loss_per_token and label_w are then indexed by token), and a row without a token (-1)
+// only gets a row factor of 0 and a loss of 0. With label_w the one cell of a row goes
+// there in fp32, for k_label_grads, and holds 0.
 template <typename T>
 __global__ __launch_bounds__(256) void k_row_finish(
     const float* __restrict__ part_m, const float* __restrict__ part_s, int nVT, int vt_shift,
@@ -1284,8 +1286,8 @@ __global__ __launch_bounds__(256) void k_row_finish(
     const float* __restrict__ rowM, const float* __restrict__ rowH,
     const float* __restrict__ rowCoef, const float* __restrict__ rowCoefM,
     const uint8_t* __restrict__ ignore, int64_t row0, const int* __restrict__ rowmap, int rows,
-    float inv_tau, float z_loss, float* rowL2, float* rowFactor, float* loss_per_token,
-    float* block_partial) {
+    float inv_tau, float z_loss, float* label_w, float* rowL2, float* rowFactor,
+    float* loss_per_token, float* block_partial) {
   __shared__ float red[kLossRows];
   const int lane = threadIdx.x & 63, wave = wave_id();
   const int r = blockIdx.x * kLossRows + wave;
@@ -1378,7 +1380,8 @@ __global__ __launch_bounds__(256) void k_row_finish(
       const int v = tidx[e];
       if ((unsigned)v < (unsigned)V) {
         const float g = cm * fast_exp2(z * k2 - L2) - cf * pk;
-        row[v] = (T)(f != 0.f ? g / f : 0.f);
+        row[v] = (T)(f != 0.f && label_w == nullptr ? g / f : 0.f);
+        if (label_w != nullptr) label_w[tok] = g;
       }
     }
     c = wave_sum(c);
@@ -1390,6 +1393,92 @@ __global__ __launch_bounds__(256) void k_row_finish(
   if (lane == 0) red[wave] = l;
   __syncthreads();
   if (threadIdx.x == 0) block_partial[blockIdx.x] = (red[0] + red[1]) + (red[2] + red[3]);
+}
+
+// The labels' part of fp32 gradients, G[t, l_t] = w_t of dL/dz:
+//   grad_hidden[t] += w_t W[l_t],   grad_W[l] += sum of w_t h_t over the tokens with l_t = l
+// in fp32, for tokens [row0, row0 + rows), at most kLabelWindow. While labels are not yet
+// likely this is nearly all of both gradients: by way of dZ it would be rounded to bf16
+// there, and for grad_W with the hidden rows times their factors (fp32 results of 4096
+// tokens, 4096 x 131072, near uniform: 1.7e-3 and 2.3e-3 off in the 2-norm, this way
+// 1.0e-5 and 1.5e-5). A workgroup per token and kLabelCols columns; the first token with
+// a label forms its row of grad_W for all of them, in their order, so there are no atomics,
+// and the same bits every time. Bound by memory (each row of both gradients read and
+// written once more): those 4096 tokens 104 us, 3.2 TB/s, 1% of the call.
+constexpr int kLabelWindow = 4096, kLabelCols = 1024;
+__global__ __launch_bounds__(256) void k_label_grads(const int64_t* __restrict__ labels,
+                                                     const float* __restrict__ w,
+                                                     const __bf16* __restrict__ hidden,
+                                                     const __bf16* __restrict__ W, int64_t row0,
+                                                     int rows, int D, int V,
+                                                     float* __restrict__ gH,
+                                                     float* __restrict__ gW) {
+  __shared__ uint64_t same[kLabelWindow / 64];
+  __shared__ uint16_t list[kLabelWindow];
+  __shared__ int count;
+  const int tid = threadIdx.x, lane = tid & 63, wave = wave_id();
+  const int t = blockIdx.x;
+  const int64_t label = labels[row0 + t];
+  if (label < 0 || label >= V) return;
+  const int c = blockIdx.y * kLabelCols + tid * 4;  // (D % 64 == 0: four columns or none)
+  const bool in = c < D;
+  auto row4 = [&](const __bf16* x, int64_t r) {
+    const u32x2_t q = *reinterpret_cast<const u32x2_t*>(x + r * D + c);
+    return f32x4_t{__builtin_bit_cast(float, q[0] << 16), __builtin_bit_cast(float, q[0] & 0xffff0000u),
+                   __builtin_bit_cast(float, q[1] << 16), __builtin_bit_cast(float, q[1] & 0xffff0000u)};
+  };
+  if (gH != nullptr && in) {
+    f32x4_t* p = reinterpret_cast<f32x4_t*>(gH + (row0 + t) * D + c);
+    *p += row4(W, label) * w[row0 + t];
+  }
+  if (gW == nullptr) return;
+  // which tokens of the window have the label, 64 a word; a wave's loads all at once
+  int64_t other[kLabelWindow / 256];
+#pragma unroll
+  for (int i = 0; i < kLabelWindow / 256; ++i)
+    other[i] = labels[row0 + min(256 * i + tid, rows - 1)];
+#pragma unroll
+  for (int i = 0; i < kLabelWindow / 256; ++i) {
+    const uint64_t m = __ballot(256 * i + tid < rows && other[i] == label);
+    if (lane == 0) same[4 * i + wave] = m;
+  }
+  __syncthreads();
+  uint64_t m = same[lane];
+  const uint64_t before = lane < t / 64 ? ~0ull : lane == t / 64 ? (1ull << (t & 63)) - 1 : 0;
+  if (__ballot((m & before) != 0) != 0) return;  // (the same in every wave)
+  if (wave == 0) {
+    const int n = __popcll(m);
+    int at = n;  // tokens up to this word, by a scan over the lanes
+#pragma unroll
+    for (int o = 1; o < 64; o <<= 1) {
+      const int v = __shfl_up(at, o);
+      if (lane >= o) at += v;
+    }
+    if (lane == 63) count = at;
+    at -= n;
+    for (; m != 0; m &= m - 1) list[at++] = (uint16_t)(lane * 64 + __ffsll((unsigned long long)m) - 1);
+  }
+  __syncthreads();
+  if (!in) return;
+  const int n = count;
+  f32x4_t* p = reinterpret_cast<f32x4_t*>(gW + label * D + c);
+  const f32x4_t old = *p;
+  f32x4_t sum = {0.f, 0.f, 0.f, 0.f};
+  constexpr int U = 8;  // rows in flight
+  for (int i = 0; i < n; i += U) {
+    f32x4_t x[U];
+    float f[U];
+#pragma unroll
+    for (int k = 0; k < U; ++k) {
+      const int64_t s = row0 + list[min(i + k, n - 1)];
+      x[k] = row4(hidden, s);
+      f[k] = w[s];
+    }
+#pragma unroll
+    for (int k = 0; k < U; ++k)
+      if (i + k < n) sum += x[k] * f[k];
+  }
+  *p = old + sum;
 }
 
 // loss = (sum of the loss partials) / N_valid, in a fixed order: thread i of
@@ -2047,11 +2136,11 @@ static inline int cdiv(int64_t a, int64_t b) { return (int)((a + b - 1) / b); }
 namespace {
 enum ProfKind {
   P_PREP, P_LOGITS, P_MERGE, P_DZ, P_ROW_LOSS, P_DH, P_DW, P_TAIL, P_FILL,
-  P_LOGITS_DZ, P_ROW_FINISH, P_DW_FIXUP, P_COMPACT, P_NKINDS
+  P_LOGITS_DZ, P_ROW_FINISH, P_DW_FIXUP, P_COMPACT, P_LABELS, P_NKINDS
 };
 const char* const kProfNames[P_NKINDS] = {
     "prep", "logits_lse", "lse_merge", "dz", "row_loss", "dh", "dw", "tail", "fill",
-    "logits_dz", "row_finish", "dw_fixup", "compact"};
+    "logits_dz", "row_finish", "dw_fixup", "compact", "label_grads"};
 struct ProfRec {
   int kind;
   hipEvent_t a, b;
@@ -2174,6 +2263,18 @@ static void launch_projection(const KdChunkArgs& a, int first, int count, hipStr
   }
 }
 
+static int launch_labels(const KdChunkArgs& a, hipStream_t s) {
+  ProfScope ps_(P_LABELS, 0.0, s);
+  for (int64_t r = 0; r < a.rows; r += kLabelWindow) {
+    const int n = (int)std::min<int64_t>(kLabelWindow, a.rows - r);
+    hipLaunchKernelGGL(k_label_grads, dim3(n, cdiv(a.D, kLabelCols)), dim3(256), 0, s, a.labels,
+                       a.label_w, static_cast<const __bf16*>(a.hidden),
+                       static_cast<const __bf16*>(a.W), r, n, (int)a.D, (int)a.V,
+                       static_cast<float*>(a.grad_hidden), a.grad_W);
+  }
+  return (int)hipGetLastError();
+}
+
 template <typename T>
 static int launch_chunk_impl(const KdChunkArgs& a, hipStream_t s) {
   const int nbt = cdiv(a.rows, kTile);  // 256-token tiles (of the buckets too)
@@ -2256,7 +2357,8 @@ static int launch_chunk_impl(const KdChunkArgs& a, hipStream_t s) {
                        a.part_m, a.part_s, a.nP, a.nP == a.nVT ? 8 : 7, a.rowFlag,
                        static_cast<T*>(a.dZ), a.ldz, a.tidx, a.p, a.zhit, a.K, (int)a.V, k2,
                        a.rowM, a.rowH, a.rowCoef, a.rowCoefM, a.ignore, a.row0, a.rowmap, a.rows,
-                       a.inv_tau, a.z_loss, a.rowL2, a.rowFactor, a.loss_per_token, a.block_partial);
+                       a.inv_tau, a.z_loss, a.label_w, a.rowL2, a.rowFactor, a.loss_per_token,
+                       a.block_partial);
   } else if (fwd) {
     {
       ProfScope ps_(P_MERGE, 0.0, s);
@@ -2275,6 +2377,7 @@ static int launch_chunk_impl(const KdChunkArgs& a, hipStream_t s) {
 
 extern "C" int kd_launch_chunk(const KdChunkArgs* a, void* stream) {
   hipStream_t s = static_cast<hipStream_t>(stream);
+  if (a->stages & KD_STAGE_LABELS) return launch_labels(*a, s);
   return a->dtype == 1 ? launch_chunk_impl<__bf16>(*a, s) : launch_chunk_impl<float>(*a, s);
 }
 

@@ -21,7 +21,9 @@ constexpr int kLossRows = 4;
 // Stages of kd_launch_chunk: preparing rows (prologue, bucketing) and the
 // chunk's projection and what follows it. The host prepares the rows of a whole dW
 // group at once when chunks align with 256-token tiles, else each chunk.
-enum { KD_STAGE_PREP = 1, KD_STAGE_CHUNK = 2 };
+// KD_STAGE_LABELS (rows = all tokens, after every contraction): the labels' part of the
+// gradients, see KdChunkArgs::label_w.
+enum { KD_STAGE_PREP = 1, KD_STAGE_CHUNK = 2, KD_STAGE_LABELS = 4 };
 
 struct KdChunkArgs {
   int dtype;
@@ -68,6 +70,14 @@ struct KdChunkArgs {
   void* grad_hidden;
   int gh_f32;
   float* lpt_full;
+  // labels whose part of fp32 gradients is formed in fp32 (one-projection schedule,
+  // bf16, with a rowmap), or null: row_finish leaves 0 in each label's cell and its
+  // gradient in label_w[token], full [N] and 0 before; KD_STAGE_LABELS then adds
+  // label_w W[label] to the token's row of grad_hidden and label_w h to the label's row
+  // of grad_W (each where it is not null)
+  const int64_t* labels;
+  float* label_w;
+  float* grad_W;
   // per-chunk workspace
   float* p;                 // [rows, K]
   float *rowM, *rowH, *rowCoef, *rowCoefM, *rowL2;   // [rows]
