@@ -1067,11 +1067,18 @@ def ce_bwd(hidden, W, labels, saved_logz, z_loss: float = 0.0, chunk: int = 4096
 def _ce_functions():
     import torch
 
+    def alone(hidden, W, labels, z_loss, chunk, workspace):
+        """The loss where no gradient is wanted."""
+        return ce_fwd_bwd(hidden, W, labels, z_loss=z_loss, chunk=chunk, grad_hidden=False,
+                          grad_W=False, workspace=workspace)["loss"]
+
     class CrossEntropy(torch.autograd.Function):
         """Mean cross entropy; forward saves ln Z, backward forms the logits again."""
 
         @staticmethod
-        def forward(ctx, hidden, W, labels, z_loss, chunk, workspace):
+        def forward(ctx, hidden, W, labels, z_loss, chunk, workspace, grad):
+            if not (grad and (ctx.needs_input_grad[0] or ctx.needs_input_grad[1])):
+                return alone(hidden, W, labels, z_loss, chunk, workspace)
             res = ce_fwd(hidden, W, labels, z_loss=z_loss, chunk=chunk, workspace=workspace)
             ctx.save_for_backward(hidden, W, labels, res["saved_logz"])
             ctx.cfg = (z_loss, chunk, workspace)
@@ -1087,7 +1094,7 @@ def _ce_functions():
                          workspace=workspace)
             gW = res.get("grad_W")
             return (res.get("grad_hidden"), None if gW is None else gW.to(W.dtype), None, None,
-                    None, None)
+                    None, None, None)
 
     class CrossEntropyFused(torch.autograd.Function):
         """Mean cross entropy; forward forms both gradients of the mean in fp32 with one
@@ -1095,8 +1102,10 @@ def _ce_functions():
         backward per graph."""
 
         @staticmethod
-        def forward(ctx, hidden, W, labels, z_loss, chunk, workspace):
+        def forward(ctx, hidden, W, labels, z_loss, chunk, workspace, grad):
             need_h, need_W = ctx.needs_input_grad[0], ctx.needs_input_grad[1]
+            if not (grad and (need_h or need_W)):
+                return alone(hidden, W, labels, z_loss, chunk, workspace)
             out = ce_fwd_bwd(hidden, W, labels, z_loss=z_loss, chunk=chunk, grad_hidden=need_h,
                              grad_W=need_W, workspace=workspace, grad_hidden_f32=True)
             ctx.grads = (out.get("grad_hidden"), out.get("grad_W"))
@@ -1117,7 +1126,7 @@ def _ce_functions():
             code = _dtype_code(ctx.dtype)
             _call("kd_scale_grads", (gW if gh is None else gh).device, g, gh, code, oh,
                   0 if gh is None else gh.numel(), gW, code, oW, 0 if gW is None else gW.numel())
-            return oh, oW, None, None, None, None
+            return oh, oW, None, None, None, None, None
 
     return {"recompute": CrossEntropy, "fused": CrossEntropyFused}
 
@@ -1137,19 +1146,20 @@ def cross_entropy(hidden, W, labels, z_loss: float = 0.0, chunk: int = 4096,
     "recompute" saves ln Z only. In bf16 the labels' part of the fused gradients is formed
     in fp32; every other entry of dL/dz is held in bf16, in the recomputed ones the labels'
     too: near a uniform distribution 1.7e-3 off in the 2-norm, the final rounding, and up
-    to 2.2e-3. Without a gradient wanted, the loss alone is computed. Capture a step into a
+    to 2.2e-3. Without a gradient wanted, the loss alone is computed. There is no
+    forward-mode rule: tensors that carry tangents are an error. Capture a step into a
     graph with no eager loss of the same hidden or W alive: torch ties their gradients to
     the stream of the first."""
     import torch
     global _CE
     if schedule not in ("fused", "recompute"):
         raise ValueError("schedule must be 'fused' or 'recompute'")
-    if not torch.is_grad_enabled() or not (hidden.requires_grad or W.requires_grad):
-        return ce_fwd_bwd(hidden, W, labels, z_loss=z_loss, chunk=chunk, grad_hidden=False,
-                          grad_W=False, workspace=workspace)["loss"]
     if _CE is None:
         _CE = _ce_functions()
-    return _CE[schedule].apply(hidden, W, labels, float(z_loss), int(chunk), workspace)
+    # (also where no gradient is wanted: a tensor may carry a tangent, which the function
+    # refuses)
+    return _CE[schedule].apply(hidden, W, labels, float(z_loss), int(chunk), workspace,
+                               torch.is_grad_enabled())
 
 
 def mx4_write(x, out=None):
