@@ -1067,6 +1067,24 @@ def ce_bwd(hidden, W, labels, saved_logz, z_loss: float = 0.0, chunk: int = 4096
 def _ce_functions():
     import torch
 
+    class Once(torch.autograd.Function):
+        """A gradient as it is, whose own derivative is an error."""
+
+        @staticmethod
+        def forward(ctx, grad):
+            return grad.view_as(grad)
+
+        @staticmethod
+        def backward(ctx, grad_out):
+            raise RuntimeError("cross_entropy has no second derivative")
+
+    def once(grad):
+        """What a backward returns: with create_graph, not a constant, whose derivative
+        would be taken for 0."""
+        if grad is None or not torch.is_grad_enabled():
+            return grad
+        return Once.apply(grad.detach().requires_grad_())
+
     def alone(hidden, W, labels, z_loss, chunk, workspace):
         """The loss where no gradient is wanted."""
         return ce_fwd_bwd(hidden, W, labels, z_loss=z_loss, chunk=chunk, grad_hidden=False,
@@ -1093,8 +1111,8 @@ def _ce_functions():
                          grad_hidden=ctx.needs_input_grad[0], grad_W=ctx.needs_input_grad[1],
                          workspace=workspace)
             gW = res.get("grad_W")
-            return (res.get("grad_hidden"), None if gW is None else gW.to(W.dtype), None, None,
-                    None, None, None)
+            return (once(res.get("grad_hidden")), once(None if gW is None else gW.to(W.dtype)),
+                    None, None, None, None, None)
 
     class CrossEntropyFused(torch.autograd.Function):
         """Mean cross entropy; forward forms both gradients of the mean in fp32 with one
@@ -1126,7 +1144,7 @@ def _ce_functions():
             code = _dtype_code(ctx.dtype)
             _call("kd_scale_grads", (gW if gh is None else gh).device, g, gh, code, oh,
                   0 if gh is None else gh.numel(), gW, code, oW, 0 if gW is None else gW.numel())
-            return oh, oW, None, None, None, None, None
+            return once(oh), once(oW), None, None, None, None, None
 
     return {"recompute": CrossEntropy, "fused": CrossEntropyFused}
 
@@ -1147,7 +1165,8 @@ def cross_entropy(hidden, W, labels, z_loss: float = 0.0, chunk: int = 4096,
     in fp32; every other entry of dL/dz is held in bf16, in the recomputed ones the labels'
     too: near a uniform distribution 1.7e-3 off in the 2-norm, the final rounding, and up
     to 2.2e-3. Without a gradient wanted, the loss alone is computed. There is no
-    forward-mode rule: tensors that carry tangents are an error. Capture a step into a
+    forward-mode rule and no second derivative: tensors that carry tangents are an error, and
+    so is a derivative of the gradients. Capture a step into a
     graph with no eager loss of the same hidden or W alive: torch ties their gradients to
     the stream of the first."""
     import torch
