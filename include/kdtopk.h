@@ -666,10 +666,12 @@ typedef struct kd_mx4_head {
 } kd_mx4_head;
 
 /*
- * Bytes of device workspace kd_mx4_logits needs: 256 for most products of up to 64
- * hidden rows; for larger ones 1/32 of a byte an element of the head and of 4-bit hidden
- * rows, or 6 an element of fp32 ones (at most 256 MiB at a time); and up to 64 MiB of
- * sums where the columns are split into ranges. Pure host function.
+ * Bytes of device workspace with which kd_mx4_logits takes N hidden rows and any fewer
+ * (the other sizes as they are): 256 for most products of up to 64 hidden rows; for
+ * larger ones 1/32 of a byte an element of the head and of 4-bit hidden rows, or 6 an
+ * element of fp32 ones (at most 256 MiB at a time); and up to 64 MiB of sums where the
+ * columns are split into ranges, which fewer rows may need and more not. Pure host
+ * function.
  */
 kd_status kd_mx4_logits_workspace_size(const kd_mx4_head* p, size_t* bytes);
 
@@ -685,8 +687,8 @@ kd_status kd_mx4_logits_workspace_size(const kd_mx4_head* p, size_t* bytes);
  *   hidden_scales  [N, D / 32] uint8 (KD_MX4), else not used
  *   codes, scales  [V, D / 2], [V, D / 32] uint8   kd_mx4_write's of the head
  *   out            [N, ld_out] out_dtype   out: columns V and on are left as they are
- *   workspace, workspace_bytes   at least kd_mx4_logits_workspace_size bytes, 16-byte
- *                  aligned
+ *   workspace, workspace_bytes   kd_mx4_logits_workspace_size bytes or more (of this N or a
+ *                  larger one), 16-byte aligned
  *
  * hidden, codes and workspace 16-byte aligned. A head's row with a block that is not
  * a number gives logits that are not a number. Errors: KD_ERR_NULL_PTR,

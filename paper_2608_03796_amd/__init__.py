@@ -1295,8 +1295,8 @@ def mx4_logits(hidden, codes, scales, hidden_scales=None, dtype=None, out=None, 
 
 @functools.lru_cache(maxsize=256)
 def mx4_workspace_size(N, D, V, dtype=KD_BF16, ld_hidden=None) -> int:
-    """Bytes of workspace of mx4_logits (dtype of the hidden rows, KD_MX4: 4 bits; their
-    row stride in elements where it is not D)."""
+    """Bytes of workspace of mx4_logits for N hidden rows and any fewer (dtype of the
+    hidden rows, KD_MX4: 4 bits; their row stride in elements where it is not D)."""
     n = ctypes.c_size_t(0)
     pr = KdMx4Head(int(N), int(D), int(V), int(ld_hidden or D), int(V), int(dtype), KD_F32, 0)
     rc = load_library().kd_mx4_logits_workspace_size(ctypes.byref(pr), ctypes.byref(n))

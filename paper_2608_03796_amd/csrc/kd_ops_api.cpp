@@ -230,6 +230,19 @@ KdMx4Plan kd_mx4_plan(int64_t N, int64_t D, int64_t V, int dtype, int64_t ld_hid
   return p;
 }
 
+// Workspace of up to N hidden rows. Only the ranges' sums make fewer rows need more than
+// N; ranges take at most 128 workgroups (V <= 65536) of at most 128 hidden rows each. The
+// plan is the same for all rows up to a multiple of 16, and from 64 on of 64 (of one tile of
+// a kernel), but for its space, which grows with them. At most 259 plans, 10 us.
+static size_t mx4_workspace(const kd_mx4_head* p) {
+  auto bytes = [&](int64_t n) { return kd_mx4_plan(n, p->D, p->V, p->dtype, p->ld_hidden).total; };
+  size_t most = bytes(p->N);
+  if (p->V > 65536) return most;
+  for (int64_t n = 16; n < p->N && n <= 128 * 128; n += n < 64 ? 16 : 64)
+    most = std::max(most, bytes(n));
+  return most;
+}
+
 extern "C" {
 
 kd_status kd_topk_entries_workspace_size(const kd_rows* p, size_t* bytes) {
@@ -374,7 +387,7 @@ kd_status kd_mx4_logits_workspace_size(const kd_mx4_head* p, size_t* bytes) {
   if (p == nullptr || bytes == nullptr) return KD_ERR_NULL_PTR;
   const kd_status st = check_head(p);
   if (st != KD_OK) return st;
-  *bytes = kd_mx4_plan(p->N, p->D, p->V, p->dtype, p->ld_hidden).total;
+  *bytes = mx4_workspace(p);
   return KD_OK;
 }
 
