@@ -8,6 +8,7 @@ import subprocess
 import pytest
 
 import paper_2608_03796_amd as kd
+from tests.mx4_shapes import VARIANTS
 
 HERE = os.path.dirname(os.path.abspath(__file__))
 CSRC = os.path.join(os.path.dirname(HERE), "paper_2608_03796_amd", "csrc")
@@ -75,3 +76,29 @@ def test_workspace_grows_with_the_rows(host):
             n = int(rng.uniform(1, N))
             assert _plan(host, n, D, V, dtype)["bytes"] <= size, (n, N, D, V, dtype)
             assert _logits(host, N, D, V, dtype, _plan(host, N, D, V, dtype)["bytes"] - 1) == 5
+
+
+NAMES = {"f32": kd.KD_F32, "bf16": kd.KD_BF16, "mx4": kd.KD_MX4}
+
+
+def _variant(host, N, D, V, dtype):
+    p = _plan(host, N, D, V, dtype)
+    if p["kind"] == 0:
+        return "rows", p["r"], p["ks"]
+    if p["kind"] == 1:
+        return "wide", p["nb"], p["r"], p["splits"] > 1
+    return "tiles", p["tok"], p["splits"] > 1
+
+
+@pytest.mark.parametrize("name", NAMES)
+def test_sizes_take_their_variant(host, name):
+    """The sizes that the values are tested at take what they are listed for, and
+    nothing that the plan returns is left out (seeded sizes)."""
+    for variant, shapes in VARIANTS[name].items():
+        for shape in shapes:
+            assert _variant(host, *shape, NAMES[name]) == variant, shape
+    rng = random.Random(3)
+    for _ in range(60000):
+        N, D, V = (int(2 ** rng.uniform(0, 13)), 32 * int(2 ** rng.uniform(0, 11)),
+                   int(2 ** rng.uniform(0, 20)))
+        assert _variant(host, N, D, V, NAMES[name]) in VARIANTS[name], (N, D, V)
