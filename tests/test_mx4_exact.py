@@ -4,7 +4,7 @@ checks that these sizes take them all)."""
 import pytest
 import torch
 
-from tests.mx4_shapes import CASES
+from tests.mx4_shapes import CASES, FAR
 
 pytestmark = pytest.mark.gpu
 
@@ -113,3 +113,15 @@ def test_many_rows(gpu_lib):
     h, hs, codes, scales, ref = _whole("bf16", 2 ** 18 + 5, 64, 130, 1)
     got = gpu_lib.mx4_logits(h, codes, scales, dtype=torch.float32)
     assert torch.equal(got.double(), ref)
+
+
+@pytest.mark.parametrize("out", ["bf16", "f32"])
+@pytest.mark.parametrize("kind,N,D,V", FAR)
+def test_far_apart(gpu_lib, kind, N, D, V, out):
+    """Rows of logits that a tile's 32-bit offsets do not reach."""
+    h, hs, codes, scales, ref = _whole(kind, N, D, V, 2)
+    z = torch.empty(N, 2 ** 26 + 3, dtype=DT[out], device="cuda")
+    z[:, V:V + 70].fill_(7.0)
+    gpu_lib.mx4_logits(h, codes, scales, hidden_scales=hs, out=z[:, :V])
+    assert torch.equal(z[:, :V], ref.float().to(DT[out]))
+    assert bool((z[:, V:V + 70] == 7).all())

@@ -8,7 +8,7 @@ import subprocess
 import pytest
 
 import paper_2608_03796_amd as kd
-from tests.mx4_shapes import VARIANTS
+from tests.mx4_shapes import FAR, VARIANTS
 
 HERE = os.path.dirname(os.path.abspath(__file__))
 CSRC = os.path.join(os.path.dirname(HERE), "paper_2608_03796_amd", "csrc")
@@ -102,3 +102,8 @@ def test_sizes_take_their_variant(host, name):
         N, D, V = (int(2 ** rng.uniform(0, 13)), 32 * int(2 ** rng.uniform(0, 11)),
                    int(2 ** rng.uniform(0, 20)))
         assert _variant(host, N, D, V, NAMES[name]) in VARIANTS[name], (N, D, V)
+
+
+def test_far_rows_take_tiles(host):
+    for name, *shape in FAR:
+        assert _variant(host, *shape, NAMES[name])[0] == "tiles", (name, shape)
