@@ -125,3 +125,16 @@ def test_far_apart(gpu_lib, kind, N, D, V, out):
     gpu_lib.mx4_logits(h, codes, scales, hidden_scales=hs, out=z[:, :V])
     assert torch.equal(z[:, :V], ref.float().to(DT[out]))
     assert bool((z[:, V:V + 70] == 7).all())
+
+
+@pytest.mark.parametrize("kind,D,V", [("bf16", 8192, 5003), ("f32", 4096, 8001), ("mx4", 8192, 5003)])
+def test_one_workspace(gpu_lib, kind, D, V):
+    """One workspace, of the size for the largest batch, serves every smaller one."""
+    kd = gpu_lib
+    code = {"f32": kd.KD_F32, "bf16": kd.KD_BF16, "mx4": kd.KD_MX4}[kind]
+    ws = torch.empty(kd.mx4_workspace_size(600, D, V, code), dtype=torch.uint8, device="cuda")
+    for N in (600, 300, 257, 128, 65, 64, 20, 1):
+        h, hs, codes, scales, ref = _whole(kind, N, D, V, N)
+        ws.fill_(255)
+        got = kd.mx4_logits(h, codes, scales, hidden_scales=hs, dtype=torch.float32, workspace=ws)
+        assert torch.equal(got.double(), ref), N
