@@ -22,7 +22,8 @@ __device__ __forceinline__ void mx4_store(V v, V* p) {
 }
 
 // Eight elements a thread, four threads a block of 32. Bound by memory: 131072 x 4096 in
-// bf16 216 us, 6.3 TB/s of matrix, codes and scales; back 226 us, 6.0 TB/s.
+// bf16 230 to 244 us (medians on two cards), 5.6 to 5.9 TB/s of matrix, codes and scales;
+// back 231 to 234 us, 5.8 TB/s. fp32 459 us, 5.3 TB/s, and 535 us, 4.5 TB/s.
 template <typename T>
 __global__ __launch_bounds__(256) void k_mx4_write(const T* __restrict__ x, int64_t n8,
                                                    uint32_t* __restrict__ codes,
@@ -317,10 +318,11 @@ __device__ __forceinline__ void mx4_put4(const Mx4Args& a, int64_t n, int v, f32
 // buffers, one barrier a stage. Where workgroups are few, the columns are split into
 // ranges. Codes go from memory to registers, those of the next piece as soon as a
 // half's are used. Bound by reading W while hidden rows are few: 131072 x 4096, one launch
-// after the other, for 1 row 55 us (5.2 TB/s; reading alone 48 at 5.6), for 16 60, for 32 70;
-// 64 rows 82, whose MFMAs take 30 and which one workgroup a compute unit does not hide
-// entirely (R = 4; fewer rows of W a wave read the hidden rows from LDS more often: R = 2
-// 104). 4-bit rows 50, 56, 66 us (16, 32, 64), fp32 rows 79, 115, 164.
+// after the other, bf16 logits (medians), for 1 row 55 us (5.2 TB/s; reading alone 48 at
+// 5.6), for 16 56, for 32 60; 64 rows 71 (77 with fp32 logits), whose MFMAs take 30 and
+// which one workgroup a compute unit does not hide entirely (R = 4; fewer rows of W a wave
+// read the hidden rows from LDS more often: R = 2 was a quarter slower). 4-bit rows 47, 49,
+// 52, 62 us (1, 16, 32, 64), fp32 rows 70, 72, 103, 177.
 constexpr int kMx4Stages(int H) { return H == 1 ? 2 : 1; }  // of a piece
 constexpr int mx4_token_bytes(int H) {  // of a stage in LDS: fp32 as three terms of bf16
   return H == 0 ? 512 : H == 1 ? 768 : 128;
@@ -724,7 +726,8 @@ __device__ __forceinline__ void mx4_pair(int q, int& i, int& j0, int& j1) {
 // decoded in registers between the MFMAs of the half step before their use: a block's
 // codes are read from LDS twice (by two waves) and take a quarter of bf16's bytes: the LDS,
 // which bounds the bf16 tiles of the loss, is active 30% of the time, the MFMAs 73% at the
-// clock that power leaves. 4096 x 4096 x 131072: 2.92 ms, 1.5 PFLOP/s.
+// clock that power leaves. 4096 x 4096 x 131072: 2.92 ms, 1.5 PFLOP/s; with three terms 8.86
+// ms, 1.5 PFLOP/s of them (k_mx4_terms 28 us).
 // The steps of a workgroup's items form one sequence: a tile's last steps load the next
 // tile's first ones, and its logits are stored under that tile's first step.
 template <int TERMS, int NJ>
@@ -938,9 +941,9 @@ __device__ __forceinline__ f32x4_t mfma_mx4_at(u32x4_t a, u32x4_t b, f32x4_t c, 
 // two stages by LDS-DMA, two scaled MFMAs a block pair. The second half of a step
 // issues the loads of the step after the next, into the stage whose last
 // fragments were read in its first half; the barrier between the halves waits for
-// those of the next step. 4096 x 4096 x 131072: 1.10 ms, 4.0 PFLOP/s with the MFMAs 50% busy;
-// 0.95 without the loads, 0.82 with neither these nor the fragments' reads, 0.15 of each the
-// logits' stores.
+// those of the next step. 4096 x 4096 x 131072: 1.10 ms, 4.0 PFLOP/s with the MFMAs 50% busy
+// (from registers alone, at the clock that power leaves, these reach 5.5); 0.95 without the
+// loads, 0.82 with neither these nor the fragments' reads, 0.15 of each the logits' stores.
 template <int NJ>
 __global__ __launch_bounds__(512, 1) void k_mx4_gemm4(Mx4GemmArgs a) {
   constexpr int TOK = 32 * NJ, HST = TOK * 128, CST = 256 * 128, SST = 8192;

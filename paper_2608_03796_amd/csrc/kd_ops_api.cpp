@@ -157,9 +157,9 @@ DraftPlan draft_plan(const kd_draft* p) {
 
 }  // namespace
 
-// The bounds below are fits to 400 products (N 24 to 1000, D 512 to 4096, V 1001 to 100001),
-// each timed with every kernel: the choice takes on average 1.03 of the best one's time
-// (fp32 hidden rows 1.08). bf16, us, wide and tiles: 96 x 2048 x 30001 21.9 and 33.7; 256 x
+// The bounds below are fits to products timed with every kernel; over 180 of them (N 24 to
+// 256, D 512 to 4096, V 3001 to 100001) the choice takes on average 1.03 of the best one's
+// time (fp32 hidden rows 1.06, 4-bit ones 1.05; at most 1.54). bf16, us, wide and tiles: 96 x 2048 x 30001 21.9 and 33.7; 256 x
 // 2048 x 55001 69.5 and 53.9; 96 x 4096 x 55001 60.3 and 64.2; 256 x 4096 x 55001 116 and
 // 90.2. Rows of the head a wave (1, 2, 4): 64 x 4096 x 55001 48.2, 39.7, 57.8; 64 x 4096 x
 // 100001 89.6, 73.1, 58.5.
